@@ -356,3 +356,104 @@ def sumloss_fwd(x):
 
 def sumloss_bwd(x_shape):
     return np.ones(x_shape, F64)
+
+
+# ---------------------------------------------------------------------- a transformer's step
+def attention_fwd(q, k, v, cu, scale):
+    """Causal attention over packed sequences.  q [tokens, heads, dim], k and v [tokens, kv_heads, dim], cu: offsets of the
+    sequences.  Returns o and lse [heads, tokens]; rows of no sequence are zero."""
+    o = np.zeros(q.shape)
+    lse = np.zeros((q.shape[1], q.shape[0]))
+    for a, b in zip(cu[:-1], cu[1:]):
+        for h in range(q.shape[1]):
+            p, ls = _attention_rows(q, k, a, b, h, scale)
+            o[a:b, h] = p @ v[a:b, _kv_head(q, k, h)]
+            lse[h, a:b] = ls
+    return o, lse
+
+
+def _kv_head(q, k, h):
+    return h // (q.shape[1] // k.shape[1])
+
+
+def _attention_rows(q, k, a, b, h, scale):
+    n = b - a
+    s = scale * (q[a:b, h] @ k[a:b, _kv_head(q, k, h)].T)
+    s[np.triu_indices(n, 1)] = -np.inf
+    m = s.max(axis=1, initial=-np.inf)
+    e = np.exp(s - m[:, None])
+    total = e.sum(axis=1)
+    return e / total[:, None], m + np.log(total)
+
+
+def attention_bwd(do, q, k, v, cu, scale):
+    """Gradients of sum(do * o): dq, dk, dv (summed over the heads that share a key / value head)."""
+    dq, dk, dv = np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape)
+    for a, b in zip(cu[:-1], cu[1:]):
+        for h in range(q.shape[1]):
+            kv = _kv_head(q, k, h)
+            p, _ = _attention_rows(q, k, a, b, h, scale)
+            dp = do[a:b, h] @ v[a:b, kv].T
+            ds = p * (dp - (p * dp).sum(axis=1, keepdims=True))
+            dq[a:b, h] = scale * (ds @ k[a:b, kv])
+            dk[a:b, kv] += scale * (ds.T @ q[a:b, h])
+            dv[a:b, kv] += p.T @ do[a:b, h]
+    return dq, dk, dv
+
+
+def linear_ce_fwd(x, w, labels):
+    """Mean over the rows with a label in 0 .. vocab - 1 of -log softmax(x w^T)[label] (0 if there are none), and lse per row."""
+    logits = x @ w.T
+    m = logits.max(axis=1)
+    lse = m + np.log(np.exp(logits - m[:, None]).sum(axis=1))
+    has = np.flatnonzero((labels >= 0) & (labels < w.shape[0]))
+    loss = (lse[has] - logits[has, labels[has]]).sum() / max(len(has), 1)
+    return loss, lse
+
+
+def linear_ce_bwd(x, w, labels):
+    """Gradients of that loss: dx, dw."""
+    logits = x @ w.T
+    _, lse = linear_ce_fwd(x, w, labels)
+    has = np.flatnonzero((labels >= 0) & (labels < w.shape[0]))
+    dl = np.zeros(logits.shape)
+    dl[has] = np.exp(logits[has] - lse[has, None])
+    dl[has, labels[has]] -= 1.0
+    dl /= max(len(has), 1)
+    return dl @ w, dl.T @ x
+
+
+ACT8_GROUP = 32
+
+
+def act8_pack(x):
+    """An activation [rows, cols] in 8 bits: (codes [rows, round_up(cols, 32)] int8, exponent bytes [rows, groups] uint8).
+    A group's scale 2^e is the smallest from 2^-126 up with max|x| / 2^e < 127.5; a code is x / 2^e rounded to nearest, ties to
+    even; byte e + 127.  A group with an infinity or a NaN: codes 0, byte 255."""
+    x = np.asarray(x, dtype=np.float64)
+    rows, cols = x.shape
+    groups = -(-cols // ACT8_GROUP)
+    p = np.zeros((rows, groups * ACT8_GROUP))
+    p[:, :cols] = x
+    p = p.reshape(rows, groups, ACT8_GROUP)
+    top = np.abs(p).max(axis=2)
+    bad = ~np.isfinite(top)
+    safe = np.where(bad, 0.0, top)
+    e = np.full(top.shape, -126)
+    big = safe > 0
+    e[big] = np.maximum(np.ceil(np.log2(safe[big] / 127.5)).astype(int) - 1, -126)
+    while True:                                   # log2 may be off by a rounding: walk to the smallest that holds
+        over = safe / np.exp2(e.astype(float)) >= 127.5
+        if not over.any():
+            break
+        e = e + over
+    code = np.where(bad[..., None], 0.0, np.rint(np.where(bad[..., None], 0.0, p) / np.exp2(e.astype(float))[..., None]))
+    byte = np.where(bad, 255, e + 127)
+    return code.astype(np.int8).reshape(rows, groups * ACT8_GROUP), byte.astype(np.uint8)
+
+
+def act8_unpack(code, byte, cols):
+    """The values that such an activation stands for."""
+    rows = code.shape[0]
+    scale = np.where(byte == 255, np.nan, np.exp2(byte.astype(float) - 127.0))
+    return (code.reshape(rows, -1, ACT8_GROUP) * scale[..., None]).reshape(rows, -1)[:, :cols]

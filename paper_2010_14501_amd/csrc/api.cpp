@@ -1171,3 +1171,57 @@ extern "C" int monet_softmaxce_rows_bwd(void *stream, const float *logits, const
                                         int accumulate) {
     return guarded([&] { softmaxce_rows_bwd((hipStream_t)stream, logits, labels, dlogits, rows, classes, accumulate != 0); });
 }
+
+// ------------------------------------------------------------------ a transformer's step
+template <class F>
+static int64_t guarded_bytes(F &&f) {
+    int64_t bytes = -1;
+    const int rc = guarded([&] { bytes = (int64_t)f(); });
+    return rc == MONET_OK ? bytes : (int64_t)rc;
+}
+extern "C" int monet_attention_fwd(void *stream, int dtype, const void *q, const void *k, const void *v, void *o, float *lse, const int32_t *cu_seqlens,
+                                   int seqs, int64_t tokens, int heads, int kv_heads, int head_dim, int64_t q_ld, int64_t k_ld, int64_t v_ld,
+                                   int64_t o_ld, float scale) {
+    return guarded([&] {
+        attention_fwd((hipStream_t)stream, dtype, q, k, v, o, lse, cu_seqlens, seqs, tokens, heads, kv_heads, head_dim, q_ld, k_ld, v_ld, o_ld, scale);
+    });
+}
+extern "C" int monet_attention_bwd(void *stream, int dtype, const void *dout, const void *q, const void *k, const void *v, const void *o, const float *lse,
+                                   void *dq, void *dk, void *dv, const int32_t *cu_seqlens, int seqs, int64_t tokens, int heads, int kv_heads,
+                                   int head_dim, int64_t q_ld, int64_t k_ld, int64_t v_ld, int64_t o_ld, float scale, int accumulate, void *ws,
+                                   size_t ws_bytes) {
+    return guarded([&] {
+        attention_bwd((hipStream_t)stream, dtype, dout, q, k, v, o, lse, dq, dk, dv, cu_seqlens, seqs, tokens, heads, kv_heads, head_dim, q_ld, k_ld,
+                      v_ld, o_ld, scale, accumulate, ws, ws_bytes);
+    });
+}
+extern "C" int64_t monet_attention_bwd_workspace_bytes(int dtype, int seqs, int64_t tokens, int heads, int kv_heads, int head_dim) {
+    return guarded_bytes([&] { return attention_bwd_workspace_bytes(dtype, seqs, tokens, heads, kv_heads, head_dim); });
+}
+extern "C" int monet_linear_ce_fwd(void *stream, int dtype, const void *x, const void *w, const int32_t *labels, float *loss, float *lse, int64_t rows,
+                                   int width, int vocab, void *ws, size_t ws_bytes) {
+    return guarded([&] { linear_ce_fwd((hipStream_t)stream, dtype, x, w, labels, loss, lse, rows, width, vocab, ws, ws_bytes); });
+}
+extern "C" int monet_linear_ce_bwd(void *stream, int dtype, const void *x, const void *w, const int32_t *labels, const float *lse, void *dx, void *dw,
+                                   int64_t rows, int width, int vocab, int accumulate, void *ws, size_t ws_bytes) {
+    return guarded([&] { linear_ce_bwd((hipStream_t)stream, dtype, x, w, labels, lse, dx, dw, rows, width, vocab, accumulate != 0, ws, ws_bytes); });
+}
+extern "C" int64_t monet_linear_ce_workspace_bytes(int grad, int dtype, int64_t rows, int width, int vocab) {
+    return guarded_bytes([&] { return linear_ce_workspace_bytes(grad != 0, dtype, rows, width, vocab); });
+}
+extern "C" int64_t monet_act8_bytes(int64_t rows, int64_t cols) {
+    return guarded_bytes([&] { return act8_bytes(rows, cols); });
+}
+extern "C" int monet_act8_pack(void *stream, int dtype, const void *x, int64_t ld, void *code, int64_t rows, int64_t cols) {
+    return guarded([&] { act8_pack((hipStream_t)stream, dtype, x, ld, code, rows, cols); });
+}
+extern "C" int monet_act8_unpack(void *stream, int dtype, const void *code, void *y, int64_t ld, int64_t rows, int64_t cols) {
+    return guarded([&] { act8_unpack((hipStream_t)stream, dtype, code, y, ld, rows, cols); });
+}
+extern "C" int monet_act8_wgrad(void *stream, int dtype, const void *code, const void *dy, float *dw, int64_t rows, int64_t cols, int64_t outs, void *ws,
+                                size_t ws_bytes) {
+    return guarded([&] { act8_wgrad((hipStream_t)stream, dtype, code, dy, dw, rows, cols, outs, ws, ws_bytes); });
+}
+extern "C" int64_t monet_act8_wgrad_workspace_bytes(int dtype, int64_t rows, int64_t cols, int64_t outs) {
+    return guarded_bytes([&] { return act8_wgrad_workspace_bytes(dtype, rows, cols, outs); });
+}

@@ -1,0 +1,570 @@
+// Causal attention over packed sequences with grouped heads.
+//
+//   s[i][j] = scale q[i] . k[j] for j <= i of the same sequence,  lse[i] = log sum_j exp s[i][j],  p = exp(s - lse),  o[i] = sum_j p[i][j] v[j]
+//   delta[i] = do[i] . o[i],  ds = p (do v^T - delta),  dq = scale ds k,  dk = scale ds^T q,  dv = p^T do  (dk, dv summed over a group's heads)
+//
+// Nothing of size length x length is kept: the forward pass leaves lse, the backward pass computes p again.
+//
+// The products are worked as their transposes, so that a lane of the matrix instruction holds 16 scores of one row: the row's maximum and
+// sum need one exchange between the wave's halves, and the scores leave the first product where the second one reads its operand (the
+// order of a reduction's indices is free as long as both operands agree).  The other operand of the second product runs across the
+// reduction and is read from LDS by ds_read_b64_tr_b16 (bf16) or by single floats.
+//
+// bf16: v_mfma_f32_32x32x16_bf16; p and ds are rounded to bf16 between the products (at most 2^-8 of a value each, which averages
+// out over the sums: the results' own rounding to bf16 costs more).  fp32: v_mfma_f32_32x32x2_f32, nothing is rounded below fp32.  Scores, maxima, sums
+// and gradients are fp32 in both.
+//
+// Backward is two kernels without atomics, so results do not depend on the order of anything: the first walks along the keys of 128
+// rows (dq, and delta on the way), the second along the rows and the group's heads of 128 keys (dk, dv).  That computes the scores
+// and do v^T twice, seven products for five.
+#include <initializer_list>
+
+#include "../../include/monet_kernels.h"
+#include "kernels.hpp"
+#include "tile_bf16.hpp"
+
+namespace monet {
+
+namespace {
+
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+constexpr int ATT_ROWS = 128;        // rows (keys in the second backward kernel) of a workgroup, 32 to a wave
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+// What a lane holds of an operand, 16 bytes, and the product of two such pieces: 16 reduction indices in bf16, 8 in fp32.
+template <class T> struct Piece;
+template <> struct Piece<unsigned short> {
+    typedef bf16x8 V;
+    static constexpr int STEPS = 2;      // pieces along 32 reduction indices
+    static __device__ __forceinline__ floatx16 mma(V a, V b, floatx16 c) { return mfma_bf16(a, b, c); }
+    // results 8 s .. 8 s + 7 of a lane as an operand
+    static __device__ __forceinline__ V from_result(const floatx16 &p, int s) {
+        const uintx4 w{pack_bf16(p[8 * s], p[8 * s + 1]), pack_bf16(p[8 * s + 2], p[8 * s + 3]), pack_bf16(p[8 * s + 4], p[8 * s + 5]),
+                       pack_bf16(p[8 * s + 6], p[8 * s + 7])};
+        return __builtin_bit_cast(V, w);
+    }
+    static __device__ __forceinline__ float dot(V a, V b) {
+        float s = 0.f;
+        const uintx4 x = __builtin_bit_cast(uintx4, a), y = __builtin_bit_cast(uintx4, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s += __uint_as_float(x[i] << 16) * __uint_as_float(y[i] << 16);
+            s += __uint_as_float(x[i] & 0xffff0000u) * __uint_as_float(y[i] & 0xffff0000u);
+        }
+        return s;
+    }
+};
+template <> struct Piece<float> {
+    typedef floatx4 V;
+    static constexpr int STEPS = 4;
+    static __device__ __forceinline__ floatx16 mma(V a, V b, floatx16 c) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+        return c;
+    }
+    static __device__ __forceinline__ V from_result(const floatx16 &p, int s) { return V{p[4 * s], p[4 * s + 1], p[4 * s + 2], p[4 * s + 3]}; }
+    static __device__ __forceinline__ float dot(V a, V b) { return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]; }
+};
+
+// A tile of R rows of D values in LDS: strips of 128 bytes, each R rows of eight 16-byte pieces turned by the row (tile_bf16.hpp).
+template <class T, int D, int R>
+struct AttTile {
+    static constexpr int STRIPS = D * (int)sizeof(T) / 128, BYTES = R * 128 * STRIPS, COPIES = BYTES / (256 * 16);
+    unsigned off[COPIES];
+    int64_t ld;
+    int used;               // bytes of a row that exist
+    __device__ __forceinline__ void init(int64_t ld_, int head_dim) {
+        ld = ld_;
+        used = head_dim * (int)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+            const unsigned piece = i * 256 + threadIdx.x, strip = piece / (R * 8), row = piece / 8 % R, c = (piece % 8) ^ wide_turn(row);
+            const unsigned col = strip * 128 + c * 16;
+            off[i] = (int)col < used ? row * (unsigned)(ld * sizeof(T)) + col : BUFFER_ABSENT;
+        }
+    }
+    // rows of which `left` exist; the others arrive as zeros
+    __device__ __forceinline__ void copy(lds_char *lds, const T *rows, int left) const {
+        const __amdgpu_buffer_rsrc_t r = buffer_of(rows, left > 0 ? (unsigned)((min(left, R) - 1) * ld * sizeof(T)) + used : 0u);
+        const int wave = threadIdx.x / 64;
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) copy_to_lds(r, lds + (i * 256 + wave * 64) * 16, off[i], 0);
+    }
+};
+// where a lane reads such tiles
+template <class T, int R>
+struct AttReader {
+    static constexpr bool BF16 = sizeof(T) == 2;
+    unsigned wide_at[4], deep_at[BF16 ? 4 : 8];
+    __device__ __forceinline__ void init() {
+        const unsigned l = threadIdx.x & 63, h = l >> 5;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) wide_at[s] = (l & 31) * 128 + (((2 * s + h) ^ wide_turn(l & 31)) << 4);
+        if (BF16) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {      // bit 0: rows + 8, bit 1: columns + 32
+                const unsigned row = 4 * h + ((l & 15) >> 2) + 8 * (p & 1), c = 4 * (p >> 1) + 2 * ((l >> 4) & 1) + ((l & 3) >> 1);
+                deep_at[p] = row * 128 + ((c ^ wide_turn(row)) << 4) + (l & 1) * 8;
+            }
+        } else {
+#pragma unroll
+            for (int p = 0; p < 8; ++p) {      // bits 0, 1: row of four, bit 2: rows + 8
+                const unsigned row = 4 * h + (p & 3) + 8 * (p >> 2);
+                deep_at[p] = row * 128 + ((((l & 31) >> 2) ^ wide_turn(row)) << 4) + (l & 3) * 4;
+            }
+        }
+    }
+    // rows 32 b + (l & 31), piece s along the row
+    __device__ __forceinline__ typename Piece<T>::V wide(const lds_char *t, int b, int s) const {
+        return *(const __attribute__((address_space(3))) typename Piece<T>::V *)(t + wide_at[s & 3] + b * 32 * 128 + (s >> 2) * R * 128);
+    }
+    // columns 32 c + (l & 31), the rows of 32 b .. that results of step s hold
+    __device__ __forceinline__ typename Piece<T>::V deep(const lds_char *t, int b, int s, int c) const {
+        if constexpr (BF16) {
+            const lds_char *p = t + (c >> 1) * R * 128 + (32 * b + 16 * s) * 128;
+            return join(read_turned(p + deep_at[2 * (c & 1)]), read_turned(p + deep_at[2 * (c & 1) + 1]));
+        } else {
+            const lds_char *p = t + c * R * 128 + (32 * b + 16 * (s >> 1)) * 128;
+            floatx4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = *(const __attribute__((address_space(3))) float *)(p + deep_at[4 * (s & 1) + j]);
+            return v;
+        }
+    }
+};
+
+// The pieces of row l & 31 of 32 rows (of which `left` exist) straight from memory
+template <class T, int D>
+struct RowPieces {
+    typename Piece<T>::V p[D * sizeof(T) / 32];
+    __device__ __forceinline__ void load(const T *rows, int64_t ld, int left, int head_dim) {
+        const int l = threadIdx.x & 63;
+        const T *row = rows + (l & 31) * ld;
+#pragma unroll
+        for (int s = 0; s < (int)(D * sizeof(T) / 32); ++s) {
+            const int col = (2 * s + (l >> 5)) * (int)(16 / sizeof(T));
+            p[s] = typename Piece<T>::V{};
+            if ((l & 31) < left && col < head_dim) p[s] = *(const typename Piece<T>::V *)(row + col);
+        }
+    }
+};
+
+struct AttShape {
+    const int32_t *cu;
+    int seqs, tokens, heads, kv_heads, head_dim, slots;
+    int64_t q_ld, k_ld, v_ld, o_ld;
+    float scale;
+};
+
+// Sequence s owns the slots from cu[s] / ATT_ROWS + s on: at least one for every ATT_ROWS rows begun, whatever the lengths, so the grid
+// needs no more than tokens / ATT_ROWS + seqs slots and a workgroup finds its sequence by a search of 64 at a time.  Offsets are held
+// to 0 .. tokens.
+__device__ __forceinline__ bool find_rows(const AttShape &a, int slot, int &start, int &len, int &row0) {
+    const int lane = threadIdx.x & 63;
+    auto at = [&](int s) { return min(max(a.cu[s], 0), a.tokens); };
+    int lo = 0, n = a.seqs;
+    while (true) {
+        const int step = (n + 63) / 64, i = lane * step;
+        const unsigned long long ok = __ballot(i < n && at(lo + min(i, n - 1)) / ATT_ROWS + lo + i <= slot);
+        if (!ok) return false;
+        const int last = 63 - __builtin_clzll(ok);
+        lo += last * step;
+        n = min(step, n - last * step);
+        if (n <= 1) break;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    start = __builtin_amdgcn_readfirstlane(at(lo));
+    len = __builtin_amdgcn_readfirstlane(at(lo + 1)) - start;
+    row0 = (slot - (start / ATT_ROWS + lo)) * ATT_ROWS;
+    return row0 < len;
+}
+// Workgroups go round the eight XCDs in turn; each gets a connected range of (head, slot), so that a group's keys and values stay in
+// one L2.
+__device__ __forceinline__ void att_place(int heads, int slots, int &head, int &slot) {
+    const int all = heads * slots, x = blockIdx.x % 8, t = x * (all / 8) + min(x, all % 8) + blockIdx.x / 8;
+    head = t / slots;
+    slot = t - head * slots;
+}
+
+__device__ __forceinline__ float exchange_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float exchange_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A lane's columns of a transposed result (32 c + result_row) to a row in memory, four neighbours at a time
+template <class T, int D>
+__device__ __forceinline__ void store_row(T *row, const floatx16 (&acc)[D / 32], float by, int head_dim, bool add) {
+    const int l = threadIdx.x & 63;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int col = 32 * c + result_row(r, l);
+            if (col >= head_dim) continue;
+            float v[4] = {acc[c][r] * by, acc[c][r + 1] * by, acc[c][r + 2] * by, acc[c][r + 3] * by};
+            if constexpr (sizeof(T) == 2) {
+                uint2 *p = (uint2 *)(row + col);
+                if (add) {
+                    const uint2 o = *p;
+                    v[0] += __uint_as_float(o.x << 16); v[1] += __uint_as_float(o.x & 0xffff0000u);
+                    v[2] += __uint_as_float(o.y << 16); v[3] += __uint_as_float(o.y & 0xffff0000u);
+                }
+                *p = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+            } else {
+                float4 *p = (float4 *)(row + col);
+                if (add) { const float4 o = *p; v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w; }
+                *p = make_float4(v[0], v[1], v[2], v[3]);
+            }
+        }
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(256, 2) void attention_fwd_kernel(AttShape a, const T *__restrict__ q, const T *__restrict__ k, const T *__restrict__ v,
+                                                               T *__restrict__ o, float *__restrict__ lse) {
+    constexpr int R = sizeof(T) == 2 ? 64 : 32, B = R / 32, PIECES = D * sizeof(T) / 32, STEPS = Piece<T>::STEPS;
+    typedef AttTile<T, D, R> Tile;
+    __shared__ __attribute__((aligned(16))) char k0[Tile::BYTES], k1[Tile::BYTES], v0[Tile::BYTES], v1[Tile::BYTES];
+    int head, slot, start, len, row0;
+    att_place(a.heads, a.slots, head, slot);
+    if (!find_rows(a, a.slots - 1 - slot, start, len, row0)) return;      // the longest rows first
+    const int kv_head = head / (a.heads / a.kv_heads), l = threadIdx.x & 63, wave = threadIdx.x / 64;
+    const int first = row0 + 32 * wave, row = first + (l & 31);
+    Tile tk, tv;
+    tk.init(a.k_ld, a.head_dim);
+    tv.init(a.v_ld, a.head_dim);
+    AttReader<T, R> rd;
+    rd.init();
+    const T *kp = k + start * a.k_ld + (int64_t)kv_head * a.head_dim, *vp = v + start * a.v_ld + (int64_t)kv_head * a.head_dim;
+    RowPieces<T, D> qr;
+    qr.load(q + (start + first) * a.q_ld + (int64_t)head * a.head_dim, a.q_ld, len - first, a.head_dim);
+    const float by = a.scale * LOG2E;
+    float top = -INFINITY, sum = 0.f;
+    floatx16 acc[D / 32];
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[c][r] = 0.f;
+    const int end = min(len, row0 + ATT_ROWS);
+    auto fetch = [&](lds_char *lk, lds_char *lv, int key0) {      // none is under way when the last tile has been used
+        if (key0 >= end) return;
+        tk.copy(lk, kp + key0 * a.k_ld, len - key0);
+        tv.copy(lv, vp + key0 * a.v_ld, len - key0);
+    };
+    auto work = [&](const lds_char *lk, const lds_char *lv, int key0) {
+        if (key0 > first + 31 || key0 >= end) return;
+        floatx16 s[B];
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) s[b] = Piece<T>::mma(rd.wide(lk, b, p), qr.p[p], s[b]);
+        }
+        if (key0 + R - 1 > first) {
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (key0 + 32 * b + result_row(r, l) > row) s[b][r] = -INFINITY;
+        }
+        float most = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) most = fmaxf(most, s[b][r]);
+        most = exchange_max(most) * by;
+        // The sums are kept relative to a maximum that may lie up to 2^8 below the true one: they are only rescaled when it falls
+        // further behind, which after the first tiles is rare.
+        if (__any(most > top + 8.f)) {
+            const float next = fmaxf(top, most), f = __builtin_amdgcn_exp2f(top - next);
+            sum *= f;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[c][r] *= f;
+            top = next;
+        }
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[b][r] = __builtin_amdgcn_exp2f(s[b][r] * by - top);
+                sum += s[b][r];
+            }
+#pragma unroll
+            for (int p = 0; p < STEPS; ++p) {
+                const typename Piece<T>::V pr = Piece<T>::from_result(s[b], p);
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) acc[c] = Piece<T>::mma(rd.deep(lv, b, p, c), pr, acc[c]);
+            }
+        }
+    };
+    lds_char *lk0 = (lds_char *)k0, *lk1 = (lds_char *)k1, *lv0 = (lds_char *)v0, *lv1 = (lds_char *)v1;
+    fetch(lk0, lv0, 0);
+    for (int key0 = 0; key0 < end; key0 += 2 * R) {
+        copies_arrived();
+        fetch(lk1, lv1, key0 + R);
+        work(lk0, lv0, key0);
+        copies_arrived();
+        fetch(lk0, lv0, key0 + 2 * R);
+        work(lk1, lv1, key0 + R);
+    }
+    if (row >= len) return;
+    sum = exchange_sum(sum);
+    store_row<T, D>(o + (int64_t)(start + row) * a.o_ld + (int64_t)head * a.head_dim, acc, 1.f / sum, a.head_dim, false);
+    if (l < 32) lse[(int64_t)head * a.tokens + start + row] = (top + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+// dq, and delta for the other kernel
+template <class T, int D>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kernel(
+    AttShape a, const T *__restrict__ go, const T *__restrict__ q, const T *__restrict__ k, const T *__restrict__ v, const T *__restrict__ o,
+    const float *__restrict__ lse, T *dq, float *__restrict__ delta, int add) {
+    constexpr int R = sizeof(T) == 2 ? 64 : 32, B = R / 32, PIECES = D * sizeof(T) / 32, STEPS = Piece<T>::STEPS;
+    typedef AttTile<T, D, R> Tile;
+    __shared__ __attribute__((aligned(16))) char k0[Tile::BYTES], k1[Tile::BYTES], v0[Tile::BYTES], v1[Tile::BYTES];
+    int head, slot, start, len, row0;
+    att_place(a.heads, a.slots, head, slot);
+    if (!find_rows(a, a.slots - 1 - slot, start, len, row0)) return;
+    const int kv_head = head / (a.heads / a.kv_heads), l = threadIdx.x & 63, wave = threadIdx.x / 64;
+    const int first = row0 + 32 * wave, row = first + (l & 31);
+    Tile tk, tv;
+    tk.init(a.k_ld, a.head_dim);
+    tv.init(a.v_ld, a.head_dim);
+    AttReader<T, R> rd;
+    rd.init();
+    const T *kp = k + start * a.k_ld + (int64_t)kv_head * a.head_dim, *vp = v + start * a.v_ld + (int64_t)kv_head * a.head_dim;
+    RowPieces<T, D> qr, gr;
+    qr.load(q + (start + first) * a.q_ld + (int64_t)head * a.head_dim, a.q_ld, len - first, a.head_dim);
+    gr.load(go + (start + first) * a.o_ld + (int64_t)head * a.head_dim, a.o_ld, len - first, a.head_dim);
+    float dot = 0.f;
+    {
+        RowPieces<T, D> orow;
+        orow.load(o + (start + first) * a.o_ld + (int64_t)head * a.head_dim, a.o_ld, len - first, a.head_dim);
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) dot += Piece<T>::dot(orow.p[p], gr.p[p]);
+        dot = exchange_sum(dot);
+    }
+    const int64_t at = (int64_t)head * a.tokens + start + row;
+    const float by = a.scale * LOG2E, ls = row < len ? lse[at] * LOG2E : 0.f;
+    if (l < 32 && row < len) delta[at] = dot;
+    floatx16 acc[D / 32];
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[c][r] = 0.f;
+    const int end = min(len, row0 + ATT_ROWS);
+    auto fetch = [&](lds_char *lk, lds_char *lv, int key0) {      // none is under way when the last tile has been used
+        if (key0 >= end) return;
+        tk.copy(lk, kp + key0 * a.k_ld, len - key0);
+        tv.copy(lv, vp + key0 * a.v_ld, len - key0);
+    };
+    auto work = [&](const lds_char *lk, const lds_char *lv, int key0) {
+        if (key0 > first + 31 || key0 >= end) return;
+        const bool edge = key0 + R - 1 > first;
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            floatx16 s, d;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = d[r] = 0.f;
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) s = Piece<T>::mma(rd.wide(lk, b, p), qr.p[p], s);
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) d = Piece<T>::mma(rd.wide(lv, b, p), gr.p[p], d);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * by - ls) * (d[r] - dot);
+            if (edge) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (key0 + 32 * b + result_row(r, l) > row) s[r] = 0.f;
+            }
+#pragma unroll
+            for (int p = 0; p < STEPS; ++p) {
+                const typename Piece<T>::V ds = Piece<T>::from_result(s, p);
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) acc[c] = Piece<T>::mma(rd.deep(lk, b, p, c), ds, acc[c]);
+            }
+        }
+    };
+    lds_char *lk0 = (lds_char *)k0, *lk1 = (lds_char *)k1, *lv0 = (lds_char *)v0, *lv1 = (lds_char *)v1;
+    fetch(lk0, lv0, 0);
+    for (int key0 = 0; key0 < end; key0 += 2 * R) {
+        copies_arrived();
+        fetch(lk1, lv1, key0 + R);
+        work(lk0, lv0, key0);
+        copies_arrived();
+        fetch(lk0, lv0, key0 + 2 * R);
+        work(lk1, lv1, key0 + R);
+    }
+    if (row < len) store_row<T, D>(dq + (int64_t)(start + row) * a.q_ld + (int64_t)head * a.head_dim, acc, a.scale, a.head_dim, add);
+}
+
+// dk and dv: a wave holds 32 keys and walks along the rows behind them, head by head of the group
+template <class T, int D>
+__global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttShape a, const T *__restrict__ go, const T *__restrict__ q, const T *__restrict__ k,
+                                                               const T *__restrict__ v, const float *__restrict__ lse, const float *__restrict__ delta,
+                                                               T *dk, T *dv, int add_k, int add_v) {
+    constexpr int R = sizeof(T) == 2 ? 64 : 32, B = R / 32, PIECES = D * sizeof(T) / 32, STEPS = Piece<T>::STEPS;
+    typedef AttTile<T, D, R> Tile;
+    __shared__ __attribute__((aligned(16))) char q0[Tile::BYTES], q1[Tile::BYTES], g0[Tile::BYTES], g1[Tile::BYTES];
+    __shared__ __attribute__((aligned(16))) float stat0[128], stat1[128];      // lse of 64 rows, delta of 64
+    int kv_head, slot, start, len, key0;
+    att_place(a.kv_heads, a.slots, kv_head, slot);
+    if (!find_rows(a, slot, start, len, key0)) return;
+    const int group = a.heads / a.kv_heads, l = threadIdx.x & 63, wave = threadIdx.x / 64;
+    const int first = key0 + 32 * wave, key = first + (l & 31);
+    Tile tq, tg;
+    tq.init(a.q_ld, a.head_dim);
+    tg.init(a.o_ld, a.head_dim);
+    AttReader<T, R> rd;
+    rd.init();
+    RowPieces<T, D> kr, vr;
+    kr.load(k + (start + first) * a.k_ld + (int64_t)kv_head * a.head_dim, a.k_ld, len - first, a.head_dim);
+    vr.load(v + (start + first) * a.v_ld + (int64_t)kv_head * a.head_dim, a.v_ld, len - first, a.head_dim);
+    const float by = a.scale * LOG2E;
+    floatx16 ak[D / 32], av[D / 32];
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) ak[c][r] = av[c][r] = 0.f;
+    const int from = key0 / R * R, tiles = (len - from + R - 1) / R, all = tiles * group;
+    auto fetch = [&](lds_char *lq, lds_char *lg, lds_char *ls, int t) {
+        if (t >= all) return;
+        const int g = t / tiles, row = from + (t - g * tiles) * R, head = kv_head * group + g;
+        tq.copy(lq, q + (start + row) * a.q_ld + (int64_t)head * a.head_dim, len - row);
+        tg.copy(lg, go + (start + row) * a.o_ld + (int64_t)head * a.head_dim, len - row);
+        if (wave < 2) {
+            const float *p = (wave ? delta : lse) + (int64_t)head * a.tokens + start + row;
+            const __amdgpu_buffer_rsrc_t r = buffer_of(p, (unsigned)min(len - row, R) * 4);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(ls + wave * 256), 4, l * 4, 0, 0, 0);
+        }
+    };
+    auto work = [&](const lds_char *lq, const lds_char *lg, const lds_char *ls, int t) {
+        const int row = from + t % tiles * R;
+        if (t >= all || row + R - 1 < first) return;
+        const bool edge = row < first + 31;
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            floatx16 s, d;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = d[r] = 0.f;
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) s = Piece<T>::mma(rd.wide(lq, b, p), kr.p[p], s);
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) d = Piece<T>::mma(rd.wide(lg, b, p), vr.p[p], d);
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const lds_char *at = ls + (32 * b + result_row(r, l)) * 4;
+                const floatx4 x = *(const __attribute__((address_space(3))) floatx4 *)at, y = *(const __attribute__((address_space(3))) floatx4 *)(at + 256);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[r + j] = __builtin_amdgcn_exp2f(s[r + j] * by - x[j] * LOG2E);
+                    if (edge && row + 32 * b + result_row(r + j, l) < key) s[r + j] = 0.f;
+                    d[r + j] = s[r + j] * (d[r + j] - y[j]);
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < STEPS; ++p) {
+                const typename Piece<T>::V pr = Piece<T>::from_result(s, p), ds = Piece<T>::from_result(d, p);
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) av[c] = Piece<T>::mma(rd.deep(lg, b, p, c), pr, av[c]);
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) ak[c] = Piece<T>::mma(rd.deep(lq, b, p, c), ds, ak[c]);
+            }
+        }
+    };
+    lds_char *lq0 = (lds_char *)q0, *lq1 = (lds_char *)q1, *lg0 = (lds_char *)g0, *lg1 = (lds_char *)g1, *ls0 = (lds_char *)stat0, *ls1 = (lds_char *)stat1;
+    fetch(lq0, lg0, ls0, 0);
+    for (int t = 0; t < all; t += 2) {
+        copies_arrived();
+        fetch(lq1, lg1, ls1, t + 1);
+        work(lq0, lg0, ls0, t);
+        copies_arrived();
+        fetch(lq0, lg0, ls0, t + 2);
+        work(lq1, lg1, ls1, t + 1);
+    }
+    if (key >= len) return;
+    store_row<T, D>(dk + (int64_t)(start + key) * a.k_ld + (int64_t)kv_head * a.head_dim, ak, a.scale, a.head_dim, add_k);
+    store_row<T, D>(dv + (int64_t)(start + key) * a.v_ld + (int64_t)kv_head * a.head_dim, av, 1.f, a.head_dim, add_v);
+}
+
+AttShape att_shape(int dtype, const int32_t *cu, int seqs, int64_t tokens, int heads, int kv_heads, int head_dim, int64_t q_ld, int64_t k_ld,
+                   int64_t v_ld, int64_t o_ld, float scale) {
+    if (dtype != MONET_F32 && dtype != MONET_BF16) throw KernelError("attention: dtype must be MONET_F32 or MONET_BF16");
+    if (seqs < 1 || tokens < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads) throw KernelError("attention: bad shape (heads must be a multiple of kv_heads)");
+    if (head_dim < 8 || head_dim > 128 || head_dim % 8) throw KernelError("attention: head_dim must be a multiple of 8 between 8 and 128");
+    if (!(scale > 0.f) || scale > 1e30f) throw KernelError("attention: scale must be positive and finite");
+    const int64_t step = dtype == MONET_BF16 ? 8 : 4;
+    for (int64_t ld : {q_ld, o_ld})
+        if (ld < (int64_t)heads * head_dim || ld % step || ld >= (1 << 23)) throw KernelError("attention: row strides must hold all heads, be a multiple of 16 bytes and below 2^23 elements");
+    for (int64_t ld : {k_ld, v_ld})
+        if (ld < (int64_t)kv_heads * head_dim || ld % step || ld >= (1 << 23)) throw KernelError("attention: row strides must hold all heads, be a multiple of 16 bytes and below 2^23 elements");
+    const int64_t slots = tokens / ATT_ROWS + seqs;
+    if (tokens > 0x7fffffff || slots * heads > 0x7fffffff) throw KernelError("attention: too many tokens");
+    if (!cu) throw KernelError("attention: null pointer");
+    return AttShape{cu, seqs, (int)tokens, heads, kv_heads, head_dim, (int)slots, q_ld, k_ld, v_ld, o_ld, scale};
+}
+void check_tensors(std::initializer_list<const void *> ptrs) {
+    for (const void *p : ptrs) {
+        if (!p) throw KernelError("attention: null pointer");
+        if ((uintptr_t)p % 16) throw KernelError("attention: tensors must be 16-byte aligned");
+    }
+}
+
+template <class T, int D>
+void fwd_launch(hipStream_t st, const AttShape &a, const void *q, const void *k, const void *v, void *o, float *lse) {
+    hipLaunchKernelGGL((attention_fwd_kernel<T, D>), dim3(a.slots * a.heads), dim3(256), 0, st, a, (const T *)q, (const T *)k, (const T *)v, (T *)o, lse);
+    hip_check(hipGetLastError(), "attention forward launch");
+}
+template <class T, int D>
+void bwd_launch(hipStream_t st, const AttShape &a, const void *go, const void *q, const void *k, const void *v, const void *o, const float *lse, void *dq,
+                void *dk, void *dv, int accumulate, float *delta) {
+    hipLaunchKernelGGL((attention_dq_kernel<T, D>), dim3(a.slots * a.heads), dim3(256), 0, st, a, (const T *)go, (const T *)q, (const T *)k,
+                       (const T *)v, (const T *)o, lse, (T *)dq, delta, accumulate & 1);
+    hip_check(hipGetLastError(), "attention query gradient launch");
+    hipLaunchKernelGGL((attention_dkv_kernel<T, D>), dim3(a.slots * a.kv_heads), dim3(256), 0, st, a, (const T *)go, (const T *)q, (const T *)k,
+                       (const T *)v, lse, delta, (T *)dk, (T *)dv, accumulate & 2, accumulate & 4);
+    hip_check(hipGetLastError(), "attention key gradient launch");
+}
+
+}  // namespace
+
+void attention_fwd(hipStream_t st, int dtype, const void *q, const void *k, const void *v, void *o, float *lse, const int32_t *cu, int seqs,
+                   int64_t tokens, int heads, int kv_heads, int head_dim, int64_t q_ld, int64_t k_ld, int64_t v_ld, int64_t o_ld, float scale) {
+    const AttShape a = att_shape(dtype, cu, seqs, tokens, heads, kv_heads, head_dim, q_ld, k_ld, v_ld, o_ld, scale);
+    if (!tokens) return;
+    check_tensors({q, k, v, o});
+    if (!lse) throw KernelError("attention: null pointer");
+    if (dtype == MONET_BF16) (head_dim <= 64 ? fwd_launch<unsigned short, 64> : fwd_launch<unsigned short, 128>)(st, a, q, k, v, o, lse);
+    else (head_dim <= 64 ? fwd_launch<float, 64> : fwd_launch<float, 128>)(st, a, q, k, v, o, lse);
+}
+
+size_t attention_bwd_workspace_bytes(int dtype, int seqs, int64_t tokens, int heads, int kv_heads, int head_dim) {
+    static const int32_t none = 0;
+    att_shape(dtype, &none, seqs, tokens, heads, kv_heads, head_dim, (int64_t)heads * head_dim, (int64_t)kv_heads * head_dim,
+              (int64_t)kv_heads * head_dim, (int64_t)heads * head_dim, 1.f);
+    return (size_t)(((int64_t)heads * tokens * 4 + 255) / 256 * 256);
+}
+
+void attention_bwd(hipStream_t st, int dtype, const void *go, const void *q, const void *k, const void *v, const void *o, const float *lse, void *dq,
+                   void *dk, void *dv, const int32_t *cu, int seqs, int64_t tokens, int heads, int kv_heads, int head_dim, int64_t q_ld, int64_t k_ld,
+                   int64_t v_ld, int64_t o_ld, float scale, int accumulate, void *ws, size_t ws_bytes) {
+    const AttShape a = att_shape(dtype, cu, seqs, tokens, heads, kv_heads, head_dim, q_ld, k_ld, v_ld, o_ld, scale);
+    if (!tokens) return;
+    check_tensors({go, q, k, v, o, dq, dk, dv});
+    if (!lse) throw KernelError("attention: null pointer");
+    if (accumulate & ~7) throw KernelError("attention: accumulate has one bit each for dq, dk and dv");
+    if (!ws || ws_bytes < attention_bwd_workspace_bytes(dtype, seqs, tokens, heads, kv_heads, head_dim))
+        throw KernelError("attention: workspace too small");
+    if ((uintptr_t)ws % 256) throw KernelError("attention: the workspace must be 256-byte aligned");
+    if (dtype == MONET_BF16)
+        (head_dim <= 64 ? bwd_launch<unsigned short, 64> : bwd_launch<unsigned short, 128>)(st, a, go, q, k, v, o, lse, dq, dk, dv, accumulate, (float *)ws);
+    else (head_dim <= 64 ? bwd_launch<float, 64> : bwd_launch<float, 128>)(st, a, go, q, k, v, o, lse, dq, dk, dv, accumulate, (float *)ws);
+}
+
+}  // namespace monet

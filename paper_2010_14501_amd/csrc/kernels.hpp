@@ -222,4 +222,23 @@ void softmaxce_rows_fwd(hipStream_t st, const float *logits, const int32_t *labe
 void softmaxce_rows_bwd(hipStream_t st, const float *logits, const int32_t *labels, float *dlogits, int64_t rows, int classes, bool accumulate);
 void sumloss_fwd(hipStream_t st, const float *x, float *loss, int64_t n, float *scratch, size_t scratch_bytes);
 
+// ---- a transformer's step (dtype: monet_dtype)
+void attention_fwd(hipStream_t st, int dtype, const void *q, const void *k, const void *v, void *o, float *lse, const int32_t *cu, int seqs,
+                   int64_t tokens, int heads, int kv_heads, int head_dim, int64_t q_ld, int64_t k_ld, int64_t v_ld, int64_t o_ld, float scale);
+size_t attention_bwd_workspace_bytes(int dtype, int seqs, int64_t tokens, int heads, int kv_heads, int head_dim);
+void attention_bwd(hipStream_t st, int dtype, const void *go, const void *q, const void *k, const void *v, const void *o, const float *lse, void *dq,
+                   void *dk, void *dv, const int32_t *cu, int seqs, int64_t tokens, int heads, int kv_heads, int head_dim, int64_t q_ld, int64_t k_ld,
+                   int64_t v_ld, int64_t o_ld, float scale, int accumulate, void *ws, size_t ws_bytes);
+size_t linear_ce_workspace_bytes(bool grad, int dtype, int64_t rows, int width, int vocab);
+void linear_ce_fwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *labels, float *loss, float *lse, int64_t rows,
+                   int width, int vocab, void *ws, size_t ws_bytes);
+void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *labels, const float *lse, void *dx, void *dw,
+                   int64_t rows, int width, int vocab, bool accumulate, void *ws, size_t ws_bytes);
+size_t act8_bytes(int64_t rows, int64_t cols);
+void act8_pack(hipStream_t st, int dtype, const void *x, int64_t ld, void *code, int64_t rows, int64_t cols);
+void act8_unpack(hipStream_t st, int dtype, const void *code, void *y, int64_t ld, int64_t rows, int64_t cols);
+size_t act8_wgrad_workspace_bytes(int dtype, int64_t rows, int64_t cols, int64_t outs);
+void act8_wgrad(hipStream_t st, int dtype, const void *code, const void *dy, float *dw, int64_t rows, int64_t cols, int64_t outs, void *ws,
+                size_t ws_bytes);
+
 }  // namespace monet

@@ -1,0 +1,429 @@
+// Softmax cross entropy of a linear layer over a large vocabulary, in pieces of the vocabulary: the logits
+//   l[t][v] = x[t] . w[v]
+// are never kept.  Forward: lse[t] = log sum_v exp l[t][v], loss = mean over the rows that have a label of lse[t] - l[t][label].
+// Backward: dl[t][v] = (exp(l[t][v] - lse[t]) - [v == label]) / count, dx = dl w, dw = dl^T x, one piece of dl at a time.
+//
+// bf16: three matrix products on the bf16 matrix cores (gemm_bf16.hpp).  The first one's epilogue keeps a maximum and a sum of
+// exponentials per row and 128 logits (forward) or writes dl, rounded to bf16 (backward: dl is the operand of two bf16 products whose
+// results are rounded to bf16 themselves; the rounding, at most 2^-8 of a value, averages out over the sums).  All sums are fp32.
+// fp32: the convolution kernels' products, a piece of logits in the workspace at a time.
+#include <initializer_list>
+#include <vector>
+
+#include "../../include/monet_kernels.h"
+#include "gemm_bf16.hpp"
+#include "kernels.hpp"
+
+namespace monet {
+
+namespace {
+
+constexpr float LOG2E = 1.44269504088896340736f;
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
+
+// Maximum and sum of a set of logits: nothing: (-inf, 0); one infinite: (FLT_MAX, inf), which stays so whatever joins it.
+struct Soft { float m, s; };
+__device__ __forceinline__ Soft soft_join(Soft a, Soft b) {
+    const float m = fmaxf(a.m, b.m);
+    if (m == -INFINITY) return {m, a.s + b.s};
+    return {m, (a.m == -INFINITY ? a.s : a.s * exp_of(a.m - m)) + (b.m == -INFINITY ? b.s : b.s * exp_of(b.m - m))};
+}
+
+// rows of the result are vocabulary entries, columns tokens: a lane has 16 * MB logits of each of its NB tokens
+struct CeStatsEpilogue {
+    const int32_t *labels;
+    float2 *part;           // [vocab / (32 MB)][rows]: a wave's rows together
+    float *hit;             // the label's logit
+    int rows, vocab;
+    template <int MB, int NB>
+    __device__ __forceinline__ void operator()(floatx16 (&acc)[MB][NB], int m0, int n0, int, int) const {
+        static_assert(MB == 4 || MB == 2, "");
+        const int l = threadIdx.x & 63;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int t = n0 + 32 * j + (l & 31);
+            const int label = t < rows ? labels[t] : -1;
+            float top = -INFINITY, mine = 0.f;
+            bool found = false;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int v = m0 + 32 * i + result_row(r, l);
+                    if (v >= vocab) acc[i][j][r] = -INFINITY;
+                    if (v == label) { mine = acc[i][j][r]; found = true; }
+                    top = fmaxf(top, acc[i][j][r]);
+                }
+            if (found && label < vocab) hit[t] = mine;
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float base = top == -INFINITY ? 0.f : fminf(top, 3.4028235e38f);
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum += exp_of(acc[i][j][r] - base);
+            sum += __shfl_xor(sum, 32);
+            if (top == INFINITY) { top = 3.4028235e38f; sum = INFINITY; }
+            if (l < 32 && t < rows && m0 < vocab) part[(int64_t)(m0 / (32 * MB)) * rows + t] = make_float2(top, sum);
+        }
+    }
+};
+
+// dl[t][v - v0]; columns behind the vocabulary are zero up to the row's end
+struct CeGradEpilogue {
+    const int32_t *labels;
+    const float *lse, *inv_count;
+    unsigned short *dl;
+    int64_t ld;
+    int rows, piece, v0, vocab;      // `piece` logits from v0 on
+    template <int MB, int NB>
+    __device__ __forceinline__ void operator()(floatx16 (&acc)[MB][NB], int m0, int n0, int, int) const {
+        const int l = threadIdx.x & 63;
+        const float inv = *inv_count;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int t = n0 + 32 * j + (l & 31);
+            if (t >= rows) continue;
+            const int label = labels[t];
+            const bool has = (unsigned)label < (unsigned)vocab;
+            const float ls = lse[t];
+            unsigned short *row = dl + t * ld + m0;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    float d[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int v = m0 + 32 * i + result_row(r + q, l);
+                        const float p = exp_of(acc[i][j][r + q] - ls);
+                        d[q] = has && v < piece ? (p - (v0 + v == label ? 1.f : 0.f)) * inv : 0.f;
+                    }
+                    if (m0 + 32 * i + result_row(r, l) < ld)
+                        *(uint2 *)(row + 32 * i + result_row(r, l)) = make_uint2(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]));
+                }
+        }
+    }
+};
+
+// out[n][m]: fp32 partial results of a range of the reduction, written or added to
+struct SumEpilogue {
+    float *out;
+    int64_t ld, range;      // elements between rows, between ranges
+    int add;
+    template <int MB, int NB>
+    __device__ __forceinline__ void operator()(floatx16 (&acc)[MB][NB], int m0, int n0, int m, int n) const {
+        const int l = threadIdx.x & 63;
+        float *o = out + blockIdx.y * range;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int c = n0 + 32 * j + (l & 31);
+            if (c >= n) continue;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const int row = m0 + 32 * i + result_row(r, l);
+                    if (row >= m) continue;
+                    float4 *p = (float4 *)(o + c * ld + row);
+                    float4 v = make_float4(acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]);
+                    if (add) { const float4 w = *p; v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w; }
+                    *p = v;
+                }
+        }
+    }
+};
+
+// out[n][m] in bf16
+struct RoundEpilogue {
+    unsigned short *out;
+    int64_t ld;
+    template <int MB, int NB>
+    __device__ __forceinline__ void operator()(floatx16 (&acc)[MB][NB], int m0, int n0, int m, int n) const {
+        const int l = threadIdx.x & 63;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int c = n0 + 32 * j + (l & 31);
+            if (c >= n) continue;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const int row = m0 + 32 * i + result_row(r, l);
+                    if (row < m) *(uint2 *)(out + c * ld + row) = make_uint2(pack_bf16(acc[i][j][r], acc[i][j][r + 1]), pack_bf16(acc[i][j][r + 2], acc[i][j][r + 3]));
+                }
+        }
+    }
+};
+
+// 64 tokens a workgroup, 16 threads to a token: lse and the row's loss from the parts of its logits
+__global__ __launch_bounds__(1024) void ce_merge_kernel(const float2 *__restrict__ part, int parts, const float *__restrict__ hit,
+                                                        const int32_t *__restrict__ labels, float *__restrict__ lse, float *__restrict__ row_loss,
+                                                        int rows, int vocab) {
+    __shared__ Soft seg[16][64];
+    const int l = threadIdx.x % 64, s = threadIdx.x / 64, t = blockIdx.x * 64 + l;
+    Soft a{-INFINITY, 0.f};
+    if (t < rows)
+        for (int b = s; b < parts; b += 16) {
+            const float2 v = part[(int64_t)b * rows + t];
+            a = soft_join(a, Soft{v.x, v.y});
+        }
+    seg[s][l] = a;
+    __syncthreads();
+    if (s || t >= rows) return;
+    for (int b = 1; b < 16; ++b) a = soft_join(a, seg[b][l]);
+    const float ls = a.m + logf(a.s);
+    lse[t] = ls;
+    row_loss[t] = (unsigned)labels[t] < (unsigned)vocab ? ls - hit[t] : 0.f;
+}
+
+// the number of rows with a label (inv: its reciprocal, 0 for none) and the mean of their losses; sums in a fixed order
+__global__ __launch_bounds__(1024) void ce_mean_kernel(const float *__restrict__ row_loss, const int32_t *__restrict__ labels, int rows, int vocab,
+                                                       float *__restrict__ loss, float *__restrict__ inv) {
+    __shared__ double sums[1024];
+    __shared__ int counts[1024];
+    double sum = 0;
+    int count = 0;
+    for (int t = threadIdx.x; t < rows; t += 1024)
+        if ((unsigned)labels[t] < (unsigned)vocab) { ++count; if (row_loss) sum += row_loss[t]; }
+    sums[threadIdx.x] = sum;
+    counts[threadIdx.x] = count;
+    for (int w = 512; w; w /= 2) {
+        __syncthreads();
+        if ((int)threadIdx.x < w) { sums[threadIdx.x] += sums[threadIdx.x + w]; counts[threadIdx.x] += counts[threadIdx.x + w]; }
+    }
+    if (threadIdx.x) return;
+    if (loss) *loss = counts[0] ? (float)(sums[0] / counts[0]) : 0.f;
+    if (inv) *inv = counts[0] ? 1.f / counts[0] : 0.f;
+}
+
+// out = sum over ranges of part (+ out), rounded to bf16; eight values a thread
+__global__ __launch_bounds__(256) void ce_round_kernel(const float *__restrict__ part, int ranges, int64_t n, unsigned short *__restrict__ out, int add) {
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (i >= n) return;
+    float v[8] = {};
+    if (add) {
+        const uint4 o = *(const uint4 *)(out + i);
+        const unsigned w[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) { v[2 * q] = __uint_as_float(w[q] << 16); v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u); }
+    }
+    for (int r = 0; r < ranges; ++r) {
+        const float4 a = *(const float4 *)(part + r * n + i), b = *(const float4 *)(part + r * n + i + 4);
+        v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+    }
+    *(uint4 *)(out + i) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+}
+
+// fp32: maximum and sum of a row's piece of logits, and the label's logit
+__global__ __launch_bounds__(256) void ce_piece_stats_kernel(const float *__restrict__ logits, int piece, int v0, const int32_t *__restrict__ labels,
+                                                             float2 *__restrict__ part, float *__restrict__ hit) {
+    __shared__ Soft seg[256];
+    const int64_t t = blockIdx.x;
+    const float *row = logits + t * piece;
+    float top = -INFINITY;
+    for (int v = threadIdx.x; v < piece; v += 256) top = fmaxf(top, row[v]);
+    const float base = top == -INFINITY ? 0.f : fminf(top, 3.4028235e38f);
+    float sum = 0.f;
+    for (int v = threadIdx.x; v < piece; v += 256) sum += exp_of(row[v] - base);
+    if (top == INFINITY) { top = 3.4028235e38f; sum = INFINITY; }
+    seg[threadIdx.x] = Soft{top, sum};
+    for (int w = 128; w; w /= 2) {
+        __syncthreads();
+        if ((int)threadIdx.x < w) seg[threadIdx.x] = soft_join(seg[threadIdx.x], seg[threadIdx.x + w]);
+    }
+    if (threadIdx.x) return;
+    part[t] = make_float2(seg[0].m, seg[0].s);
+    const int label = labels[t] - v0;
+    if (label >= 0 && label < piece) hit[t] = row[label];
+}
+// fp32: dl in the place of the logits
+__global__ __launch_bounds__(256) void ce_piece_grad_kernel(float *__restrict__ logits, int piece, int v0, const int32_t *__restrict__ labels,
+                                                            const float *__restrict__ lse, const float *__restrict__ inv_count, int vocab) {
+    const int64_t t = blockIdx.x;
+    const int v = blockIdx.y * 256 + threadIdx.x;
+    if (v >= piece) return;
+    const int label = labels[t];
+    float *at = logits + t * piece + v;
+    *at = (unsigned)label < (unsigned)vocab ? (exp_of(*at - lse[t]) - (v0 + v == label ? 1.f : 0.f)) * *inv_count : 0.f;
+}
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+int64_t cut(int64_t n, int64_t by) { return (n + by - 1) / by; }
+
+constexpr int64_t CE_PIECE_BYTES = 256ll << 20;      // a piece of logits or of their gradient
+
+// How a call goes through the vocabulary, and its workspace: forward [hit][row_loss][part][logits (fp32)], backward
+// [inv][dx parts (bf16)][dl][parts of the fp32 products].
+struct CePlan {
+    int rows, width, vocab;
+    bool bf16;
+    int unit = 0;                   // bf16 forward: logits to a part
+    int piece = 0;                  // logits of a piece
+    int ranges = 1, chunk = 0;      // bf16 backward: of the reduction over a piece in dx
+    int dgrad_splits = 1, wgrad_splits = 1;      // fp32 backward
+    int64_t fixed = 0, per_col = 0;              // bytes without the pieces, and for each logit of a piece
+
+    int64_t parts() const { return bf16 ? cut(vocab, unit) : pieces().size(); }
+    int64_t bytes() const { return fixed + per_col * piece; }
+    // where the pieces begin, and the vocabulary's end.  fp32: the products read 16 bytes at a time where the piece is a multiple of
+    // 16, so what a large vocabulary has over that is a piece of its own
+    std::vector<int> pieces() const {
+        std::vector<int> at;
+        const int tail = !bf16 && vocab > 4096 ? vocab % 16 : 0;
+        for (int v = 0; v < vocab - tail; v += piece) at.push_back(v);
+        if (tail) at.push_back(vocab - tail);
+        return at;
+    }
+};
+
+// A reduction of `red` into rows x cols results gives few tiles where both are small: as many ranges as fill the card, of 512 indices at least.
+int ce_splits(int64_t tiles, int64_t red) { return (int)std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), red / 512, 16})); }
+
+CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab) {
+    if (dtype != MONET_F32 && dtype != MONET_BF16) throw KernelError("linear_ce: dtype must be MONET_F32 or MONET_BF16");
+    if (rows < 1 || width < 1 || vocab < 1) throw KernelError("linear_ce: bad shape");
+    const bool bf16 = dtype == MONET_BF16;
+    if (bf16 && width % 8) throw KernelError("linear_ce: bf16 needs a width that is a multiple of 8");
+    if (rows > (1 << 24) || width > (1 << 20) || vocab > (1 << 28)) throw KernelError("linear_ce: shape too large");
+    CePlan p{(int)rows, width, vocab, bf16};
+    if (bf16 && !grad) {
+        p.unit = gemm_tile(vocab, rows) / 2;
+        p.fixed = 2 * up(rows * 4, 256) + up(p.parts() * rows * 8, 256);
+        return p;
+    }
+    p.per_col = up(rows * (bf16 ? 2 : 4), 256);
+    const int64_t pieces = cut(vocab, std::max<int64_t>(CE_PIECE_BYTES / p.per_col / 256 * 256, 256));
+    p.piece = (int)std::min<int64_t>(up(cut(vocab, pieces), 256), 1 << 20);
+    if (!bf16) p.piece = std::min(p.piece, vocab);
+    if (!grad) {
+        p.fixed = 2 * up(rows * 4, 256) + up(p.parts() * rows * 8, 256);
+        return p;
+    }
+    p.fixed = 256;
+    if (bf16) {
+        p.ranges = ce_splits(cut(width, 128) * cut(rows, 128), p.piece);
+        p.chunk = (int)up(cut(p.piece, p.ranges), GEMM_DEPTH);
+        p.ranges = (int)cut(std::min(p.piece, vocab), p.chunk);      // a later piece is no longer than the first
+        if (p.ranges > 1 || p.piece < vocab) p.fixed += up(p.ranges * rows * width * 4, 256);
+    } else {
+        p.dgrad_splits = ce_splits(cut(width, 128) * cut(rows, 128), p.piece);
+        p.wgrad_splits = ce_splits(cut(width, 128) * cut(p.piece, 128), rows);
+        int64_t part = 0;
+        if (p.dgrad_splits > 1) part = p.dgrad_splits * rows * width * 4;
+        if (p.wgrad_splits > 1) part = std::max(part, p.wgrad_splits * (int64_t)p.piece * width * 4);
+        p.fixed += up(part, 256);
+    }
+    return p;
+}
+
+void check_ws(const CePlan &p, const void *ws, size_t ws_bytes) {
+    if (!ws || (int64_t)ws_bytes < p.bytes()) throw KernelError("linear_ce: workspace of " + std::to_string(ws_bytes) + " bytes, " + std::to_string(p.bytes()) + " needed");
+    if ((uintptr_t)ws % 256) throw KernelError("linear_ce: the workspace must be 256-byte aligned");
+}
+void check_aligned(const CePlan &p, std::initializer_list<const void *> ptrs) {
+    for (const void *q : ptrs) {
+        if (!q) throw KernelError("linear_ce: null pointer");
+        if ((uintptr_t)q % (p.bf16 ? 16 : 4)) throw KernelError("linear_ce: bf16 tensors must be 16-byte aligned");
+    }
+}
+
+GemmShape ce_logits_shape(const CePlan &p, const void *x, const void *w, int v0, int piece) {
+    GemmShape g{};
+    g.a = (const unsigned short *)w + (int64_t)v0 * p.width;
+    g.b = (const unsigned short *)x;
+    g.lda = g.ldb = p.width;
+    g.m = piece; g.n = p.rows; g.k = p.width;
+    g.splits = 1; g.chunk = (int)up(p.width, GEMM_DEPTH);
+    return g;
+}
+ConvShape ce_conv_shape(const CePlan &p, int piece) { return ConvShape{p.rows, 1, 1, p.width, piece, 1, 1, 1, 0, 1, 1}; }
+
+}  // namespace
+
+size_t linear_ce_workspace_bytes(bool grad, int dtype, int64_t rows, int width, int vocab) {
+    return (size_t)std::max(ce_plan(grad, dtype, rows, width, vocab).bytes(), ce_plan(false, dtype, rows, width, vocab).bytes());
+}
+
+void linear_ce_fwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *labels, float *loss, float *lse, int64_t rows,
+                   int width, int vocab, void *ws, size_t ws_bytes) {
+    const CePlan p = ce_plan(false, dtype, rows, width, vocab);
+    check_ws(p, ws, ws_bytes);
+    check_aligned(p, {x, w});
+    if (!labels || !loss || !lse) throw KernelError("linear_ce: null pointer");
+    float *hit = (float *)ws, *row_loss = hit + up(rows, 64);
+    float2 *part = (float2 *)(row_loss + up(rows, 64));
+    if (p.bf16) {
+        gemm_bf16<false, false>(st, ce_logits_shape(p, x, w, 0, vocab), CeStatsEpilogue{labels, part, hit, p.rows, vocab}, "linear_ce logits launch");
+    } else {
+        float *logits = (float *)((char *)ws + p.fixed);
+        const std::vector<int> at = p.pieces();
+        for (size_t i = 0; i < at.size(); ++i) {
+            const int piece = (i + 1 < at.size() ? at[i + 1] : vocab) - at[i];
+            conv_fwd(st, (const float *)x, (const float *)w + (int64_t)at[i] * width, logits, ce_conv_shape(p, piece));
+            hipLaunchKernelGGL(ce_piece_stats_kernel, dim3(p.rows), dim3(256), 0, st, logits, piece, at[i], labels, part + i * rows, hit);
+            hip_check(hipGetLastError(), "linear_ce statistics launch");
+        }
+    }
+    hipLaunchKernelGGL(ce_merge_kernel, dim3((unsigned)cut(rows, 64)), dim3(1024), 0, st, part, (int)p.parts(), hit, labels, lse, row_loss, p.rows, vocab);
+    hip_check(hipGetLastError(), "linear_ce merge launch");
+    hipLaunchKernelGGL(ce_mean_kernel, dim3(1), dim3(1024), 0, st, row_loss, labels, p.rows, vocab, loss, (float *)nullptr);
+    hip_check(hipGetLastError(), "linear_ce mean launch");
+}
+
+void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *labels, const float *lse, void *dx, void *dw,
+                   int64_t rows, int width, int vocab, bool accumulate, void *ws, size_t ws_bytes) {
+    const CePlan p = ce_plan(true, dtype, rows, width, vocab);
+    check_ws(p, ws, ws_bytes);
+    check_aligned(p, {x, w, dx, dw});
+    if (!labels || !lse) throw KernelError("linear_ce: null pointer");
+    float *inv = (float *)ws;
+    hipLaunchKernelGGL(ce_mean_kernel, dim3(1), dim3(1024), 0, st, (const float *)nullptr, labels, p.rows, vocab, (float *)nullptr, inv);
+    hip_check(hipGetLastError(), "linear_ce count launch");
+    const std::vector<int> at = p.pieces();
+    char *dl = (char *)ws + p.fixed;
+    float *parts = (float *)((char *)ws + 256);
+    for (size_t i = 0; i < at.size(); ++i) {
+        const int v0 = at[i], piece = (i + 1 < at.size() ? at[i + 1] : vocab) - v0;
+        if (p.bf16) {
+            unsigned short *d = (unsigned short *)dl;
+            const int64_t ld = up(piece, 8);
+            gemm_bf16<false, false>(st, ce_logits_shape(p, x, w, v0, piece),
+                                    CeGradEpilogue{labels, lse, inv, d, ld, p.rows, piece, v0, vocab}, "linear_ce gradient launch");
+            GemmShape g{};
+            // dx[t][c] (+)= sum over v of w[v][c] dl[t][v]
+            g.a = (const unsigned short *)w + (int64_t)v0 * width; g.lda = width;
+            g.b = d; g.ldb = ld;
+            g.m = width; g.n = p.rows; g.k = piece;
+            g.chunk = p.chunk; g.splits = (int)cut(piece, p.chunk);
+            if (p.ranges == 1 && at.size() == 1 && !accumulate)
+                gemm_bf16<true, false>(st, g, RoundEpilogue{(unsigned short *)dx, width}, "linear_ce input gradient launch");
+            else {
+                gemm_bf16<true, false>(st, g, SumEpilogue{parts, width, rows * width, i > 0}, "linear_ce input gradient launch");
+                if (i + 1 == at.size()) {
+                    const int64_t n = rows * width;
+                    hipLaunchKernelGGL(ce_round_kernel, dim3((unsigned)cut(n, 2048)), dim3(256), 0, st, parts, p.ranges, n, (unsigned short *)dx, accumulate);
+                    hip_check(hipGetLastError(), "linear_ce round launch");
+                }
+            }
+            // dw[v][c] = sum over t of x[t][c] dl[t][v]
+            g.a = (const unsigned short *)x; g.lda = width;
+            g.m = width; g.n = piece; g.k = p.rows;
+            g.splits = 1; g.chunk = (int)up(rows, GEMM_DEPTH);
+            gemm_bf16<true, true>(st, g, RoundEpilogue{(unsigned short *)dw + (int64_t)v0 * width, width}, "linear_ce weight gradient launch");
+        } else {
+            const ConvShape cs = ce_conv_shape(p, piece);
+            const float *wp = (const float *)w + (int64_t)v0 * width;
+            float *d = (float *)dl;
+            const size_t part_bytes = (size_t)(p.fixed - 256);
+            conv_fwd(st, (const float *)x, wp, d, cs);
+            hipLaunchKernelGGL(ce_piece_grad_kernel, dim3(p.rows, (unsigned)cut(piece, 256)), dim3(256), 0, st, d, piece, v0, labels, lse, inv, vocab);
+            hip_check(hipGetLastError(), "linear_ce gradient launch");
+            conv_dgrad(st, d, wp, (float *)dx, cs, accumulate || i > 0, p.dgrad_splits, p.dgrad_splits > 1 ? parts : nullptr, p.dgrad_splits > 1 ? part_bytes : 0);
+            conv_wgrad(st, (const float *)x, d, (float *)dw + (int64_t)v0 * width, cs, p.wgrad_splits, p.wgrad_splits > 1 ? parts : nullptr,
+                       p.wgrad_splits > 1 ? part_bytes : 0);
+        }
+    }
+}
+
+}  // namespace monet

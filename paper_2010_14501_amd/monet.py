@@ -8,6 +8,8 @@ import os
 
 import numpy as np
 
+F32, BF16 = 0, 1        # monet_dtype
+
 ALLOC, FREE, RUN_FWD, RUN_RECOMPUTE, RUN_BWD, SAVE, ALIAS = range(7)
 
 EVENT_DTYPE = np.dtype([("kind", "<i4"), ("stage", "<i4"), ("node", "<i4"), ("impl", "<i4"), ("aux", "<i4"),
@@ -134,6 +136,23 @@ def load_library():
     lib.monet_column_copy.argtypes = [vp, vp, i64, vp, i64, i32, i64, i32]
     lib.monet_softmaxce_rows_fwd.argtypes = [vp, vp, vp, vp, i64, i32, vp, sz]
     lib.monet_softmaxce_rows_bwd.argtypes = [vp, vp, vp, vp, i64, i32, i32]
+    lib.monet_attention_fwd.argtypes = [vp, i32] + [vp] * 6 + [i32, i64, i32, i32, i32] + [i64] * 4 + [f]
+    lib.monet_attention_bwd.argtypes = [vp, i32] + [vp] * 10 + [i32, i64, i32, i32, i32] + [i64] * 4 + [f, i32, vp, sz]
+    lib.monet_attention_bwd_workspace_bytes.argtypes = [i32, i32, i64, i32, i32, i32]
+    lib.monet_linear_ce_fwd.argtypes = [vp, i32] + [vp] * 5 + [i64, i32, i32, vp, sz]
+    lib.monet_linear_ce_bwd.argtypes = [vp, i32] + [vp] * 6 + [i64, i32, i32, i32, vp, sz]
+    lib.monet_linear_ce_workspace_bytes.argtypes = [i32, i32, i64, i32, i32]
+    lib.monet_act8_bytes.argtypes = [i64, i64]
+    lib.monet_act8_pack.argtypes = [vp, i32, vp, i64, vp, i64, i64]
+    lib.monet_act8_unpack.argtypes = [vp, i32, vp, vp, i64, i64, i64]
+    lib.monet_act8_wgrad.argtypes = [vp, i32, vp, vp, vp, i64, i64, i64, vp, sz]
+    lib.monet_act8_wgrad_workspace_bytes.argtypes = [i32, i64, i64, i64]
+    for name in ("monet_attention_bwd_workspace_bytes", "monet_linear_ce_workspace_bytes", "monet_act8_bytes",
+                 "monet_act8_wgrad_workspace_bytes"):
+        getattr(lib, name).restype = i64
+    for name in ("monet_attention_fwd", "monet_attention_bwd", "monet_linear_ce_fwd", "monet_linear_ce_bwd", "monet_act8_pack",
+                 "monet_act8_unpack", "monet_act8_wgrad"):
+        getattr(lib, name).restype = i32
     for name in ("monet_conv_fwd", "monet_conv_dgrad", "monet_conv_wgrad", "monet_bn_stats", "monet_bn_stats_static", "monet_bn_apply", "monet_bn_bwd",
                  "monet_relu_fwd", "monet_relu_bwd", "monet_maxpool_fwd", "monet_maxpool_bwd", "monet_copy",
                  "monet_tconv_fwd", "monet_tconv_dgrad", "monet_tconv_wgrad", "monet_dwconv_fwd", "monet_dwconv_dgrad",

@@ -1,0 +1,168 @@
+"""Pins of the oracle's definitions of attention, the vocabulary loss and 8-bit activations: hand-worked values, finite
+differences, closed forms; and refusals of their entry points, which need no GPU."""
+import numpy as np
+import pytest
+
+from oracle import numerics as nm
+from paper_2010_14501_amd import monet
+
+
+def fd(f, x, i, h=1e-5):
+    a, b = x.copy(), x.copy()
+    a[i] += h
+    b[i] -= h
+    return (f(a) - f(b)) / (2 * h)
+
+
+def test_attention_by_hand():
+    # one head, two keys: softmax of (0, ln 3) is (1/4, 3/4)
+    q = np.array([[[1.0, 0.0]], [[0.0, 1.0]]])
+    k = np.array([[[5.0, 0.0]], [[7.0, np.log(3.0)]]])
+    v = np.array([[[1.0, 2.0]], [[5.0, 6.0]]])
+    o, lse = nm.attention_fwd(q, k, v, [0, 2], 1.0)
+    assert np.allclose(o[0, 0], v[0, 0]) and np.isclose(lse[0, 0], 5.0)
+    assert np.allclose(o[1, 0], [4.0, 5.0]) and np.isclose(lse[0, 1], np.log(4.0))
+
+
+def test_attention_sequences_and_groups_are_separate():
+    rng = np.random.default_rng(0)
+    q, k, v = rng.standard_normal((9, 4, 8)), rng.standard_normal((9, 2, 8)), rng.standard_normal((9, 2, 8))
+    o, lse = nm.attention_fwd(q, k, v, [0, 4, 4, 9], 0.3)
+    for h in range(4):
+        one, ls = nm.attention_fwd(q[4:, h:h + 1], k[4:, h // 2:h // 2 + 1], v[4:, h // 2:h // 2 + 1], [0, 5], 0.3)
+        assert np.allclose(o[4:, h], one[:, 0]) and np.allclose(lse[h, 4:], ls[0])
+
+
+def test_attention_gradient_is_the_difference_quotient():
+    rng = np.random.default_rng(1)
+    q, k, v = rng.standard_normal((7, 4, 3)), rng.standard_normal((7, 2, 3)), rng.standard_normal((7, 2, 3))
+    do = rng.standard_normal(q.shape)
+    cu, scale = [1, 4, 4, 7], 0.7
+    f = lambda a, b, c: (do * nm.attention_fwd(a, b, c, cu, scale)[0]).sum()   # noqa: E731
+    dq, dk, dv = nm.attention_bwd(do, q, k, v, cu, scale)
+    for i in np.ndindex(q.shape):
+        assert abs(fd(lambda t: f(t, k, v), q, i) - dq[i]) < 1e-8
+    for i in np.ndindex(k.shape):
+        assert abs(fd(lambda t: f(q, t, v), k, i) - dk[i]) < 1e-8
+        assert abs(fd(lambda t: f(q, k, t), v, i) - dv[i]) < 1e-8
+
+
+def test_linear_ce_by_hand_and_by_differences():
+    # no weight: uniform logits
+    loss, lse = nm.linear_ce_fwd(np.ones((3, 2)), np.zeros((5, 2)), np.array([1, -1, 4]))
+    assert np.isclose(loss, np.log(5.0)) and np.allclose(lse, np.log(5.0))
+    assert nm.linear_ce_fwd(np.ones((2, 2)), np.ones((5, 2)), np.array([-1, 5]))[0] == 0.0
+    rng = np.random.default_rng(2)
+    x, w, lab = rng.standard_normal((6, 4)), rng.standard_normal((9, 4)), np.array([0, 8, -1, 3, 9, 3])
+    dx, dw = nm.linear_ce_bwd(x, w, lab)
+    for i in np.ndindex(x.shape):
+        assert abs(fd(lambda t: nm.linear_ce_fwd(t, w, lab)[0], x, i) - dx[i]) < 1e-8
+    for i in np.ndindex(w.shape):
+        assert abs(fd(lambda t: nm.linear_ce_fwd(x, t, lab)[0], w, i) - dw[i]) < 1e-8
+    assert not dx[[2, 4]].any()
+    # the loss of given logits, with every row labelled
+    lab = np.array([0, 8, 1, 3, 2, 3])
+    assert np.isclose(nm.linear_ce_fwd(x, w, lab)[0], nm.softmaxce_fwd(x @ w.T, lab))
+
+
+def test_act8_by_hand():
+    x = np.zeros((1, 70))
+    x[0, :4] = [127.0, -63.5, 0.5, 1.5]           # e = 0: halves go to even
+    x[0, 32:35] = [127.5, 1.0, -3.0]              # e = 1: 63.75, 0.5, -1.5
+    x[0, 64] = 1e-45                              # below 2^-126: 0 there
+    code, byte = nm.act8_pack(x)
+    assert code.shape == (1, 96) and byte.tolist() == [[127, 128, 1]]
+    assert code[0, :4].tolist() == [127, -64, 0, 2] and code[0, 32:35].tolist() == [64, 0, -2] and code[0, 64] == 0
+    y = nm.act8_unpack(code, byte, 70)
+    assert y[0, :4].tolist() == [127.0, -64.0, 0.0, 2.0] and y[0, 32:35].tolist() == [128.0, 0.0, -4.0]
+
+
+def test_act8_bounds_and_special_values():
+    rng = np.random.default_rng(3)
+    x = rng.standard_normal((40, 75)) * np.exp2(rng.integers(-140, 120, size=(40, 75)).astype(float))
+    code, byte = nm.act8_pack(x)
+    y = nm.act8_unpack(code, byte, 75)
+    step = np.repeat(np.exp2(byte.astype(float) - 127), 32, axis=1)[:, :75]
+    assert (np.abs(y - x) <= 0.5 * step).all() and np.abs(code).max() <= 127
+    x[3, 40] = np.nan
+    x[5, 2] = np.inf
+    code, byte = nm.act8_pack(x)
+    y = nm.act8_unpack(code, byte, 75)
+    bad = np.zeros(x.shape, bool)
+    bad[3, 32:64] = bad[5, :32] = True
+    assert (np.isnan(y) == bad).all()
+
+
+# ---- refusals: arguments are checked before anything is enqueued, so that these need no GPU
+P = 1 << 20        # an aligned address that is never read
+
+
+def refused(name, args, match):
+    with pytest.raises(monet.MonetError, match=match):
+        monet.call(name, *args)
+
+
+@pytest.mark.parametrize("change,match", [
+    (dict(dtype=2), "dtype"), (dict(seqs=0), "bad shape"), (dict(tokens=-1), "bad shape"), (dict(heads=6), "multiple of kv_heads"),
+    (dict(head_dim=12), "head_dim"), (dict(head_dim=136), "head_dim"), (dict(head_dim=0), "head_dim"), (dict(q_ld=256), "strides"),
+    (dict(k_ld=260), "strides"), (dict(v_ld=128), "strides"), (dict(o_ld=1 << 23), "strides"), (dict(scale=0.0), "scale"),
+    (dict(scale=float("nan")), "scale"), (dict(scale=float("inf")), "scale"), (dict(tokens=1 << 31), "too many"), (dict(q=P + 8), "aligned"),
+    (dict(k=None), "null"), (dict(lse=None), "null"), (dict(cu=None), "null"), (dict(accumulate=8), "accumulate"), (dict(ws=None), "workspace"),
+    (dict(ws=P + 16), "workspace"), (dict(ws_bytes=8 * 100 * 4 - 1), "workspace"), (dict(go=None), "null"), (dict(dv=P + 4), "aligned"),
+])
+def test_attention_refuses(change, match):
+    a = dict(dtype=monet.BF16, go=P, q=P, k=P, v=P, o=P, lse=P, dq=P, dk=P, dv=P, cu=P, seqs=3, tokens=100, heads=8, kv_heads=4, head_dim=64,
+             q_ld=512, k_ld=256, v_ld=256, o_ld=512, scale=0.125, accumulate=0, ws=P, ws_bytes=1 << 20)
+    a.update(change)
+    shape = ["cu", "seqs", "tokens", "heads", "kv_heads", "head_dim", "q_ld", "k_ld", "v_ld", "o_ld", "scale"]
+    refused("monet_attention_bwd", [None] + [a[n] for n in ["dtype", "go", "q", "k", "v", "o", "lse", "dq", "dk", "dv"] + shape + ["accumulate", "ws", "ws_bytes"]], match)
+    if not set(change) & {"accumulate", "ws", "ws_bytes", "go", "dv"}:
+        refused("monet_attention_fwd", [None] + [a[n] for n in ["dtype", "q", "k", "v", "o", "lse"] + shape], match)
+
+
+def test_attention_of_no_tokens_is_no_call():
+    shape = (P, 1, 0, 8, 4, 64, 512, 256, 256, 512, 0.125)
+    monet.call("monet_attention_fwd", None, monet.BF16, None, None, None, None, None, *shape)
+    monet.call("monet_attention_bwd", None, monet.F32, *[None] * 9, *shape, 0, None, 0)
+    assert monet.call("monet_attention_bwd_workspace_bytes", monet.F32, 1, 0, 8, 4, 64) == 0
+
+
+@pytest.mark.parametrize("change,match", [
+    (dict(dtype=5), "dtype"), (dict(rows=0), "bad shape"), (dict(width=0), "bad shape"), (dict(vocab=-1), "bad shape"), (dict(width=100), "multiple of 8"),
+    (dict(vocab=(1 << 28) + 1), "too large"), (dict(rows=(1 << 24) + 1), "too large"), (dict(x=None), "null"), (dict(w=P + 2), "aligned"),
+    (dict(labels=None), "null"), (dict(lse=None), "null"), (dict(ws=None), "workspace"), (dict(ws_bytes=100), "workspace"), (dict(ws=P + 64), "workspace"),
+])
+def test_linear_ce_refuses(change, match):
+    a = dict(dtype=monet.BF16, x=P, w=P, labels=P, loss=P, lse=P, dx=P, dw=P, rows=50, width=64, vocab=1000, ws=P, ws_bytes=1 << 30)
+    a.update(change)
+    tail = [a[n] for n in ["rows", "width", "vocab"]]
+    refused("monet_linear_ce_fwd", [None] + [a[n] for n in ["dtype", "x", "w", "labels", "loss", "lse"]] + tail + [a["ws"], a["ws_bytes"]], match)
+    refused("monet_linear_ce_bwd", [None] + [a[n] for n in ["dtype", "x", "w", "labels", "lse", "dx", "dw"]] + tail + [0, a["ws"], a["ws_bytes"]], match)
+
+
+def test_linear_ce_workspace_is_a_piece_and_no_logits():
+    # 8192 rows of 131072 logits are 2 GiB in bf16: the backward pass holds 256 MiB of them and dx in fp32
+    need = monet.call("monet_linear_ce_workspace_bytes", 1, monet.BF16, 8192, 4096, 131072)
+    assert need <= (256 << 20) + 8192 * 4096 * 4 + 4096
+    assert monet.call("monet_linear_ce_workspace_bytes", 0, monet.BF16, 8192, 4096, 131072) <= (64 << 20) + (1 << 20)
+    for grad in (0, 1):
+        for dtype in (monet.F32, monet.BF16):
+            assert monet.call("monet_linear_ce_workspace_bytes", grad, dtype, 1, 8, 1) > 0
+
+
+@pytest.mark.parametrize("name,args,match", [
+    ("monet_act8_bytes", (0, 4), "bad shape"), ("monet_act8_bytes", (4, 0), "bad shape"), ("monet_act8_bytes", (1 << 40, 32), "bad shape"),
+    ("monet_act8_pack", (None, 3, P, 32, P, 4, 32), "dtype"), ("monet_act8_pack", (None, 1, P, 31, P, 4, 32), "stride"),
+    ("monet_act8_pack", (None, 1, P + 1, 32, P, 4, 32), "aligned"), ("monet_act8_pack", (None, 0, P, 32, P + 8, 4, 32), "aligned"),
+    ("monet_act8_pack", (None, 0, None, 32, P, 4, 32), "null"), ("monet_act8_unpack", (None, 0, None, P, 32, 4, 32), "null"),
+    ("monet_act8_unpack", (None, 0, P, P, 31, 4, 32), "stride"), ("monet_act8_unpack", (None, 9, P, P, 32, 4, 32), "dtype"),
+    ("monet_act8_wgrad", (None, 1, P, P, P, 4, 32, 0, None, 0), "bad shape"), ("monet_act8_wgrad", (None, 2, P, P, P, 4, 32, 8, None, 0), "dtype"),
+    ("monet_act8_wgrad", (None, 1, P, P + 1, P, 4, 32, 8, None, 0), "aligned"), ("monet_act8_wgrad", (None, 1, P, None, P, 4, 32, 8, None, 0), "null"),
+    ("monet_act8_wgrad", (None, 1, P, P, P, 8192, 32, 8, None, 0), "workspace"), ("monet_act8_wgrad", (None, 1, P, P, P, 8192, 32, 8, P, 64), "workspace"),
+])
+def test_act8_refuses(name, args, match):
+    refused(name, args, match)
+
+
+def test_act8_bytes():
+    assert monet.call("monet_act8_bytes", 5, 32) == 5 * 33 and monet.call("monet_act8_bytes", 5, 33) == 5 * 66
