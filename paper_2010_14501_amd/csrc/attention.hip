@@ -28,8 +28,6 @@ namespace monet {
 namespace {
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
-constexpr int ATT_ROWS = 128;        // rows (keys in the second backward kernel) of a workgroup, 32 to a wave
-
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 // What a lane holds of an operand, 16 bytes, and the product of two such pieces: 16 reduction indices in bf16, 8 in fp32.
@@ -157,16 +155,28 @@ struct AttShape {
     float scale;
 };
 
-// Sequence s owns the slots from cu[s] / ATT_ROWS + s on: at least one for every ATT_ROWS rows begun, whatever the lengths, so the grid
-// needs no more than tokens / ATT_ROWS + seqs slots and a workgroup finds its sequence by a search of 64 at a time.  Offsets are held
+// How a workgroup's four waves share a tile.  PARTS = 1: 32 rows each, every wave takes the whole tile.  PARTS = 2, 4: 64 or 32 rows in all,
+// the waves of the same rows take 32 of the tile's columns each and add up what they have at the end: two and four times as many
+// workgroups and as short a way for each, for as much more traffic from L2.
+template <class T, int D, int PARTS>
+struct AttForm {
+    static constexpr int ROWS = 128 / PARTS, BLOCKS = sizeof(T) == 2 && PARTS == 1 ? 2 : 1, TILE = 32 * BLOCKS * PARTS;
+    static constexpr int PIECES = D * (int)sizeof(T) / 32, STEPS = Piece<T>::STEPS;
+    typedef AttTile<T, D, TILE> Tile;
+    static constexpr bool TWO_GROUPS = 4 * Tile::BYTES <= 64 << 10;      // two workgroups in a CU's LDS
+};
+
+// Sequence s owns the slots from cu[s] / ROWS + s on: at least one for every ROWS rows begun, whatever the lengths, so the grid
+// needs no more than tokens / ROWS + seqs slots and a workgroup finds its sequence by a search of 64 at a time.  Offsets are held
 // to 0 .. tokens.
+template <int ROWS>
 __device__ __forceinline__ bool find_rows(const AttShape &a, int slot, int &start, int &len, int &row0) {
     const int lane = threadIdx.x & 63;
     auto at = [&](int s) { return min(max(a.cu[s], 0), a.tokens); };
     int lo = 0, n = a.seqs;
     while (true) {
         const int step = (n + 63) / 64, i = lane * step;
-        const unsigned long long ok = __ballot(i < n && at(lo + min(i, n - 1)) / ATT_ROWS + lo + i <= slot);
+        const unsigned long long ok = __ballot(i < n && at(lo + min(i, n - 1)) / ROWS + lo + i <= slot);
         if (!ok) return false;
         const int last = 63 - __builtin_clzll(ok);
         lo += last * step;
@@ -176,7 +186,7 @@ __device__ __forceinline__ bool find_rows(const AttShape &a, int slot, int &star
     lo = __builtin_amdgcn_readfirstlane(lo);
     start = __builtin_amdgcn_readfirstlane(at(lo));
     len = __builtin_amdgcn_readfirstlane(at(lo + 1)) - start;
-    row0 = (slot - (start / ATT_ROWS + lo)) * ATT_ROWS;
+    row0 = (slot - (start / ROWS + lo)) * ROWS;
     return row0 < len;
 }
 // Workgroups go round the eight XCDs in turn; each gets a connected range of (head, slot), so that a group's keys and values stay in
@@ -196,44 +206,79 @@ __device__ __forceinline__ float exchange_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// A lane's columns of a transposed result (32 c + result_row) to a row in memory, four neighbours at a time
-template <class T, int D>
-__device__ __forceinline__ void store_row(T *row, const floatx16 (&acc)[D / 32], float by, int head_dim, bool add) {
+// A lane's columns 32 c + result_row of a transposed result to a row in memory, four neighbours at a time
+template <class T>
+__device__ __forceinline__ void store_block(T *row, int c, const floatx16 &acc, float by, int head_dim, bool add) {
     const int l = threadIdx.x & 63;
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+        const int col = 32 * c + result_row(r, l);
+        if (col >= head_dim) continue;
+        float v[4] = {acc[r] * by, acc[r + 1] * by, acc[r + 2] * by, acc[r + 3] * by};
+        if constexpr (sizeof(T) == 2) {
+            uint2 *p = (uint2 *)(row + col);
+            if (add) {
+                const uint2 o = *p;
+                v[0] += __uint_as_float(o.x << 16); v[1] += __uint_as_float(o.x & 0xffff0000u);
+                v[2] += __uint_as_float(o.y << 16); v[3] += __uint_as_float(o.y & 0xffff0000u);
+            }
+            *p = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+        } else {
+            float4 *p = (float4 *)(row + col);
+            if (add) { const float4 o = *p; v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w; }
+            *p = make_float4(v[0], v[1], v[2], v[3]);
+        }
+    }
+}
+
+// The PARTS waves of the same rows add up their results (each times its own factor) and store them, D / 32 blocks of columns dealt out
+// among them.  area(w): LDS for wave w's results, free by now.
+template <class T, int D, int PARTS, class Area>
+__device__ __forceinline__ void join_and_store(Area area, const floatx16 (&acc)[D / 32], float factor, T *row, bool exists, float by, int head_dim, bool add) {
+    const int l = threadIdx.x & 63, wave = threadIdx.x / 64, part = wave % PARTS;
+    if constexpr (PARTS == 1) {
+        if (exists) {
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) store_block(row, c, acc[c], by * factor, head_dim, add);
+        }
+        return;
+    }
+    typedef __attribute__((address_space(3))) float lds_float;
+    lds_float *mine = (lds_float *)area(wave);
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const int col = 32 * c + result_row(r, l);
-            if (col >= head_dim) continue;
-            float v[4] = {acc[c][r] * by, acc[c][r + 1] * by, acc[c][r + 2] * by, acc[c][r + 3] * by};
-            if constexpr (sizeof(T) == 2) {
-                uint2 *p = (uint2 *)(row + col);
-                if (add) {
-                    const uint2 o = *p;
-                    v[0] += __uint_as_float(o.x << 16); v[1] += __uint_as_float(o.x & 0xffff0000u);
-                    v[2] += __uint_as_float(o.y << 16); v[3] += __uint_as_float(o.y & 0xffff0000u);
-                }
-                *p = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-            } else {
-                float4 *p = (float4 *)(row + col);
-                if (add) { const float4 o = *p; v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w; }
-                *p = make_float4(v[0], v[1], v[2], v[3]);
-            }
+        for (int r = 0; r < 16; ++r) mine[(c * 16 + r) * 64 + l] = acc[c][r] * factor;
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+        if (c % PARTS != part) continue;
+        floatx16 sum;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum[r] = 0.f;
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) {
+            const lds_float *p = (const lds_float *)area(wave - part + i);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum[r] += p[(c * 16 + r) * 64 + l];
         }
+        if (exists) store_block(row, c, sum, by, head_dim, add);
+    }
 }
 
-template <class T, int D>
-__global__ __launch_bounds__(256, 2) void attention_fwd_kernel(AttShape a, const T *__restrict__ q, const T *__restrict__ k, const T *__restrict__ v,
-                                                               T *__restrict__ o, float *__restrict__ lse) {
-    constexpr int R = sizeof(T) == 2 ? 64 : 32, B = R / 32, PIECES = D * sizeof(T) / 32, STEPS = Piece<T>::STEPS;
-    typedef AttTile<T, D, R> Tile;
+template <class T, int D, int PARTS>
+__global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS ? 2 : 1)) void attention_fwd_kernel(
+    AttShape a, const T *__restrict__ q, const T *__restrict__ k, const T *__restrict__ v, T *__restrict__ o, float *__restrict__ lse) {
+    typedef AttForm<T, D, PARTS> F;
+    typedef typename F::Tile Tile;
+    constexpr int R = F::TILE, B = F::BLOCKS, PIECES = F::PIECES, STEPS = F::STEPS;
+    __shared__ float stats[2][4][64];
     __shared__ __attribute__((aligned(16))) char k0[Tile::BYTES], k1[Tile::BYTES], v0[Tile::BYTES], v1[Tile::BYTES];
     int head, slot, start, len, row0;
     att_place(a.heads, a.slots, head, slot);
-    if (!find_rows(a, a.slots - 1 - slot, start, len, row0)) return;      // the longest rows first
+    if (!find_rows<F::ROWS>(a, a.slots - 1 - slot, start, len, row0)) return;      // the longest rows first
     const int kv_head = head / (a.heads / a.kv_heads), l = threadIdx.x & 63, wave = threadIdx.x / 64;
-    const int first = row0 + 32 * wave, row = first + (l & 31);
+    const int part = wave % PARTS, first = row0 + wave / PARTS * 32, row = first + (l & 31);
     Tile tk, tv;
     tk.init(a.k_ld, a.head_dim);
     tv.init(a.v_ld, a.head_dim);
@@ -249,13 +294,14 @@ __global__ __launch_bounds__(256, 2) void attention_fwd_kernel(AttShape a, const
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[c][r] = 0.f;
-    const int end = min(len, row0 + ATT_ROWS);
+    const int end = min(len, row0 + F::ROWS);
     auto fetch = [&](lds_char *lk, lds_char *lv, int key0) {      // none is under way when the last tile has been used
         if (key0 >= end) return;
         tk.copy(lk, kp + key0 * a.k_ld, len - key0);
         tv.copy(lv, vp + key0 * a.v_ld, len - key0);
     };
-    auto work = [&](const lds_char *lk, const lds_char *lv, int key0) {
+    auto work = [&](const lds_char *lk, const lds_char *lv, int tile0) {
+        const int key0 = tile0 + 32 * B * part;
         if (key0 > first + 31 || key0 >= end) return;
         floatx16 s[B];
 #pragma unroll
@@ -263,9 +309,9 @@ __global__ __launch_bounds__(256, 2) void attention_fwd_kernel(AttShape a, const
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) s[b] = Piece<T>::mma(rd.wide(lk, b, p), qr.p[p], s[b]);
+            for (int p = 0; p < PIECES; ++p) s[b] = Piece<T>::mma(rd.wide(lk, B * part + b, p), qr.p[p], s[b]);
         }
-        if (key0 + R - 1 > first) {
+        if (key0 + 32 * B - 1 > first) {
 #pragma unroll
             for (int b = 0; b < B; ++b)
 #pragma unroll
@@ -281,7 +327,7 @@ __global__ __launch_bounds__(256, 2) void attention_fwd_kernel(AttShape a, const
         // The sums are kept relative to a maximum that may lie up to 2^8 below the true one: they are only rescaled when it falls
         // further behind, which after the first tiles is rare.
         if (__any(most > top + 8.f)) {
-            const float next = fmaxf(top, most), f = __builtin_amdgcn_exp2f(top - next);
+            const float next = fmaxf(top, most), f = top == next ? 1.f : __builtin_amdgcn_exp2f(top - next);
             sum *= f;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c)
@@ -289,18 +335,19 @@ __global__ __launch_bounds__(256, 2) void attention_fwd_kernel(AttShape a, const
                 for (int r = 0; r < 16; ++r) acc[c][r] *= f;
             top = next;
         }
+        const float base = PARTS > 1 && top == -INFINITY ? 0.f : top;      // a part of a row may see no key at all
 #pragma unroll
         for (int b = 0; b < B; ++b) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[b][r] = __builtin_amdgcn_exp2f(s[b][r] * by - top);
+                s[b][r] = __builtin_amdgcn_exp2f(s[b][r] * by - base);
                 sum += s[b][r];
             }
 #pragma unroll
             for (int p = 0; p < STEPS; ++p) {
                 const typename Piece<T>::V pr = Piece<T>::from_result(s[b], p);
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) acc[c] = Piece<T>::mma(rd.deep(lv, b, p, c), pr, acc[c]);
+                for (int c = 0; c < D / 32; ++c) acc[c] = Piece<T>::mma(rd.deep(lv, B * part + b, p, c), pr, acc[c]);
             }
         }
     };
@@ -314,25 +361,40 @@ __global__ __launch_bounds__(256, 2) void attention_fwd_kernel(AttShape a, const
         fetch(lk0, lv0, key0 + 2 * R);
         work(lk1, lv1, key0 + R);
     }
-    if (row >= len) return;
     sum = exchange_sum(sum);
-    store_row<T, D>(o + (int64_t)(start + row) * a.o_ld + (int64_t)head * a.head_dim, acc, 1.f / sum, a.head_dim, false);
-    if (l < 32) lse[(int64_t)head * a.tokens + start + row] = (top + __builtin_amdgcn_logf(sum)) * LN2;
+    float factor = 1.f;
+    if constexpr (PARTS > 1) {
+        stats[0][wave][l] = top;
+        stats[1][wave][l] = sum;
+        __syncthreads();             // and everybody is done with the tiles
+        const float mine = top;
+        top = stats[0][wave - part][l];
+#pragma unroll
+        for (int i = 1; i < PARTS; ++i) top = fmaxf(top, stats[0][wave - part + i][l]);
+        sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) sum += stats[1][wave - part + i][l] * __builtin_amdgcn_exp2f(stats[0][wave - part + i][l] - top);
+        factor = __builtin_amdgcn_exp2f(mine - top);
+    }
+    auto area = [&](int w) { return w == 0 ? lk0 : w == 1 ? lk1 : w == 2 ? lv0 : lv1; };
+    if (part == 0 && l < 32 && row < len) lse[(int64_t)head * a.tokens + start + row] = (top + __builtin_amdgcn_logf(sum)) * LN2;
+    join_and_store<T, D, PARTS>(area, acc, factor, o + (int64_t)(start + row) * a.o_ld + (int64_t)head * a.head_dim, row < len, 1.f / sum, a.head_dim, false);
 }
 
-// dq, and delta for the other kernel
-template <class T, int D>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kernel(
+// dq, and for the other kernel delta and, behind it, lse in powers of two
+template <class T, int D, int PARTS>
+__global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T) == 2 || D == 64) ? 2 : 1)) void attention_dq_kernel(
     AttShape a, const T *__restrict__ go, const T *__restrict__ q, const T *__restrict__ k, const T *__restrict__ v, const T *__restrict__ o,
     const float *__restrict__ lse, T *dq, float *__restrict__ delta, int add) {
-    constexpr int R = sizeof(T) == 2 ? 64 : 32, B = R / 32, PIECES = D * sizeof(T) / 32, STEPS = Piece<T>::STEPS;
-    typedef AttTile<T, D, R> Tile;
+    typedef AttForm<T, D, PARTS> F;
+    typedef typename F::Tile Tile;
+    constexpr int R = F::TILE, B = F::BLOCKS, PIECES = F::PIECES, STEPS = F::STEPS;
     __shared__ __attribute__((aligned(16))) char k0[Tile::BYTES], k1[Tile::BYTES], v0[Tile::BYTES], v1[Tile::BYTES];
     int head, slot, start, len, row0;
     att_place(a.heads, a.slots, head, slot);
-    if (!find_rows(a, a.slots - 1 - slot, start, len, row0)) return;
+    if (!find_rows<F::ROWS>(a, a.slots - 1 - slot, start, len, row0)) return;
     const int kv_head = head / (a.heads / a.kv_heads), l = threadIdx.x & 63, wave = threadIdx.x / 64;
-    const int first = row0 + 32 * wave, row = first + (l & 31);
+    const int part = wave % PARTS, first = row0 + wave / PARTS * 32, row = first + (l & 31);
     Tile tk, tv;
     tk.init(a.k_ld, a.head_dim);
     tv.init(a.v_ld, a.head_dim);
@@ -352,30 +414,34 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
     }
     const int64_t at = (int64_t)head * a.tokens + start + row;
     const float by = a.scale * LOG2E, ls = row < len ? lse[at] * LOG2E : 0.f;
-    if (l < 32 && row < len) delta[at] = dot;
+    if (part == 0 && l < 32 && row < len) {
+        delta[at] = dot;
+        delta[at + (int64_t)a.heads * a.tokens] = ls;
+    }
     floatx16 acc[D / 32];
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[c][r] = 0.f;
-    const int end = min(len, row0 + ATT_ROWS);
+    const int end = min(len, row0 + F::ROWS);
     auto fetch = [&](lds_char *lk, lds_char *lv, int key0) {      // none is under way when the last tile has been used
         if (key0 >= end) return;
         tk.copy(lk, kp + key0 * a.k_ld, len - key0);
         tv.copy(lv, vp + key0 * a.v_ld, len - key0);
     };
-    auto work = [&](const lds_char *lk, const lds_char *lv, int key0) {
+    auto work = [&](const lds_char *lk, const lds_char *lv, int tile0) {
+        const int key0 = tile0 + 32 * B * part;
         if (key0 > first + 31 || key0 >= end) return;
-        const bool edge = key0 + R - 1 > first;
+        const bool edge = key0 + 32 * B - 1 > first;
 #pragma unroll
         for (int b = 0; b < B; ++b) {
             floatx16 s, d;
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = d[r] = 0.f;
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) s = Piece<T>::mma(rd.wide(lk, b, p), qr.p[p], s);
+            for (int p = 0; p < PIECES; ++p) s = Piece<T>::mma(rd.wide(lk, B * part + b, p), qr.p[p], s);
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) d = Piece<T>::mma(rd.wide(lv, b, p), gr.p[p], d);
+            for (int p = 0; p < PIECES; ++p) d = Piece<T>::mma(rd.wide(lv, B * part + b, p), gr.p[p], d);
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * by - ls) * (d[r] - dot);
             if (edge) {
@@ -387,7 +453,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
             for (int p = 0; p < STEPS; ++p) {
                 const typename Piece<T>::V ds = Piece<T>::from_result(s, p);
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) acc[c] = Piece<T>::mma(rd.deep(lk, b, p, c), ds, acc[c]);
+                for (int c = 0; c < D / 32; ++c) acc[c] = Piece<T>::mma(rd.deep(lk, B * part + b, p, c), ds, acc[c]);
             }
         }
     };
@@ -401,23 +467,28 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_dq_kern
         fetch(lk0, lv0, key0 + 2 * R);
         work(lk1, lv1, key0 + R);
     }
-    if (row < len) store_row<T, D>(dq + (int64_t)(start + row) * a.q_ld + (int64_t)head * a.head_dim, acc, a.scale, a.head_dim, add);
+    if (PARTS > 1) __syncthreads();      // everybody is done with the tiles
+    auto area = [&](int w) { return w == 0 ? lk0 : w == 1 ? lk1 : w == 2 ? lv0 : lv1; };
+    join_and_store<T, D, PARTS>(area, acc, 1.f, dq + (int64_t)(start + row) * a.q_ld + (int64_t)head * a.head_dim, row < len, a.scale, a.head_dim, add);
 }
 
-// dk and dv: a wave holds 32 keys and walks along the rows behind them, head by head of the group
-template <class T, int D>
-__global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttShape a, const T *__restrict__ go, const T *__restrict__ q, const T *__restrict__ k,
-                                                               const T *__restrict__ v, const float *__restrict__ lse, const float *__restrict__ delta,
-                                                               T *dk, T *dv, int add_k, int add_v) {
-    constexpr int R = sizeof(T) == 2 ? 64 : 32, B = R / 32, PIECES = D * sizeof(T) / 32, STEPS = Piece<T>::STEPS;
-    typedef AttTile<T, D, R> Tile;
+// dk and dv: a wave holds 32 keys and walks along the rows behind them, head by head of the group.  With more than one range (grid y) a
+// workgroup takes its share of that way and leaves fp32 sums in `ranges` ([range][token][kv_head][head_dim], dk's and behind them dv's),
+// which attention_join_kernel adds up in order.
+template <class T, int D, int PARTS>
+__global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T) == 2 || D == 64) ? 2 : 1)) void attention_dkv_kernel(
+    AttShape a, const T *__restrict__ go, const T *__restrict__ q, const T *__restrict__ k, const T *__restrict__ v, const float *__restrict__ delta,
+    T *dk, T *dv, int add_k, int add_v, float *__restrict__ ranges) {
+    typedef AttForm<T, D, PARTS> F;
+    typedef typename F::Tile Tile;
+    constexpr int R = F::TILE, B = F::BLOCKS, PIECES = F::PIECES, STEPS = F::STEPS;
     __shared__ __attribute__((aligned(16))) char q0[Tile::BYTES], q1[Tile::BYTES], g0[Tile::BYTES], g1[Tile::BYTES];
-    __shared__ __attribute__((aligned(16))) float stat0[128], stat1[128];      // lse of 64 rows, delta of 64
+    __shared__ __attribute__((aligned(16))) float stat0[256], stat1[256];      // delta of a tile's rows, their lse
     int kv_head, slot, start, len, key0;
     att_place(a.kv_heads, a.slots, kv_head, slot);
-    if (!find_rows(a, slot, start, len, key0)) return;
+    if (!find_rows<F::ROWS>(a, slot, start, len, key0)) return;
     const int group = a.heads / a.kv_heads, l = threadIdx.x & 63, wave = threadIdx.x / 64;
-    const int first = key0 + 32 * wave, key = first + (l & 31);
+    const int part = wave % PARTS, first = key0 + wave / PARTS * 32, key = first + (l & 31);
     Tile tq, tg;
     tq.init(a.q_ld, a.head_dim);
     tg.init(a.o_ld, a.head_dim);
@@ -432,21 +503,23 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttShape a, const
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
         for (int r = 0; r < 16; ++r) ak[c][r] = av[c][r] = 0.f;
-    const int from = key0 / R * R, tiles = (len - from + R - 1) / R, all = tiles * group;
-    auto fetch = [&](lds_char *lq, lds_char *lg, lds_char *ls, int t) {
+    const int from = key0 / R * R, tiles = (len - from + R - 1) / R;
+    const int begin = (int)((int64_t)tiles * group * blockIdx.y / gridDim.y), all = (int)((int64_t)tiles * group * (blockIdx.y + 1) / gridDim.y);
+    auto fetch = [&](lds_char *lq, lds_char *lg, lds_char *ls, int t) {      // none is under way when the last tile has been used
         if (t >= all) return;
         const int g = t / tiles, row = from + (t - g * tiles) * R, head = kv_head * group + g;
         tq.copy(lq, q + (start + row) * a.q_ld + (int64_t)head * a.head_dim, len - row);
         tg.copy(lg, go + (start + row) * a.o_ld + (int64_t)head * a.head_dim, len - row);
-        if (wave < 2) {
-            const float *p = (wave ? delta : lse) + (int64_t)head * a.tokens + start + row;
+        // 64 rows' delta (waves 0, 1) and lse (2, 3); rows behind the sequence: 0
+        if (64 * (wave & 1) < R) {
+            const float *p = delta + (wave / 2 * a.heads + head) * (int64_t)a.tokens + start + row;
             const __amdgpu_buffer_rsrc_t r = buffer_of(p, (unsigned)min(len - row, R) * 4);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(ls + wave * 256), 4, l * 4, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(ls + wave * 256), 4, (64 * (wave & 1) + l) * 4, 0, 0, 0);
         }
     };
     auto work = [&](const lds_char *lq, const lds_char *lg, const lds_char *ls, int t) {
-        const int row = from + t % tiles * R;
-        if (t >= all || row + R - 1 < first) return;
+        const int row = from + t % tiles * R + 32 * B * part;
+        if (t >= all || row + 32 * B - 1 < first || row >= len) return;
         const bool edge = row < first + 31;
 #pragma unroll
         for (int b = 0; b < B; ++b) {
@@ -454,16 +527,16 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttShape a, const
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = d[r] = 0.f;
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) s = Piece<T>::mma(rd.wide(lq, b, p), kr.p[p], s);
+            for (int p = 0; p < PIECES; ++p) s = Piece<T>::mma(rd.wide(lq, B * part + b, p), kr.p[p], s);
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) d = Piece<T>::mma(rd.wide(lg, b, p), vr.p[p], d);
+            for (int p = 0; p < PIECES; ++p) d = Piece<T>::mma(rd.wide(lg, B * part + b, p), vr.p[p], d);
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
-                const lds_char *at = ls + (32 * b + result_row(r, l)) * 4;
-                const floatx4 x = *(const __attribute__((address_space(3))) floatx4 *)at, y = *(const __attribute__((address_space(3))) floatx4 *)(at + 256);
+                const lds_char *at = ls + (32 * (B * part + b) + result_row(r, l)) * 4;
+                const floatx4 y = *(const __attribute__((address_space(3))) floatx4 *)at, x = *(const __attribute__((address_space(3))) floatx4 *)(at + 512);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    s[r + j] = __builtin_amdgcn_exp2f(s[r + j] * by - x[j] * LOG2E);
+                    s[r + j] = __builtin_amdgcn_exp2f(s[r + j] * by - x[j]);
                     if (edge && row + 32 * b + result_row(r + j, l) < key) s[r + j] = 0.f;
                     d[r + j] = s[r + j] * (d[r + j] - y[j]);
                 }
@@ -472,15 +545,15 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttShape a, const
             for (int p = 0; p < STEPS; ++p) {
                 const typename Piece<T>::V pr = Piece<T>::from_result(s, p), ds = Piece<T>::from_result(d, p);
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) av[c] = Piece<T>::mma(rd.deep(lg, b, p, c), pr, av[c]);
+                for (int c = 0; c < D / 32; ++c) av[c] = Piece<T>::mma(rd.deep(lg, B * part + b, p, c), pr, av[c]);
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) ak[c] = Piece<T>::mma(rd.deep(lq, b, p, c), ds, ak[c]);
+                for (int c = 0; c < D / 32; ++c) ak[c] = Piece<T>::mma(rd.deep(lq, B * part + b, p, c), ds, ak[c]);
             }
         }
     };
     lds_char *lq0 = (lds_char *)q0, *lq1 = (lds_char *)q1, *lg0 = (lds_char *)g0, *lg1 = (lds_char *)g1, *ls0 = (lds_char *)stat0, *ls1 = (lds_char *)stat1;
-    fetch(lq0, lg0, ls0, 0);
-    for (int t = 0; t < all; t += 2) {
+    fetch(lq0, lg0, ls0, begin);
+    for (int t = begin; t < all; t += 2) {
         copies_arrived();
         fetch(lq1, lg1, ls1, t + 1);
         work(lq0, lg0, ls0, t);
@@ -488,9 +561,47 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttShape a, const
         fetch(lq0, lg0, ls0, t + 2);
         work(lq1, lg1, ls1, t + 1);
     }
-    if (key >= len) return;
-    store_row<T, D>(dk + (int64_t)(start + key) * a.k_ld + (int64_t)kv_head * a.head_dim, ak, a.scale, a.head_dim, add_k);
-    store_row<T, D>(dv + (int64_t)(start + key) * a.v_ld + (int64_t)kv_head * a.head_dim, av, 1.f, a.head_dim, add_v);
+    auto area = [&](int w) { return w == 0 ? lq0 : w == 1 ? lq1 : w == 2 ? lg0 : lg1; };
+    if (PARTS > 1) __syncthreads();      // everybody is done with the tiles
+    if (ranges) {
+        float *row = ranges + (((int64_t)blockIdx.y * a.tokens + start + key) * a.kv_heads + kv_head) * a.head_dim;
+        join_and_store<float, D, PARTS>(area, ak, 1.f, row, key < len, a.scale, a.head_dim, false);
+        if (PARTS > 1) __syncthreads();
+        row += (int64_t)gridDim.y * a.tokens * a.kv_heads * a.head_dim;
+        join_and_store<float, D, PARTS>(area, av, 1.f, row, key < len, 1.f, a.head_dim, false);
+        return;
+    }
+    join_and_store<T, D, PARTS>(area, ak, 1.f, dk + (int64_t)(start + key) * a.k_ld + (int64_t)kv_head * a.head_dim, key < len, a.scale, a.head_dim, add_k);
+    if (PARTS > 1) __syncthreads();
+    join_and_store<T, D, PARTS>(area, av, 1.f, dv + (int64_t)(start + key) * a.v_ld + (int64_t)kv_head * a.head_dim, key < len, 1.f, a.head_dim, add_v);
+}
+
+// dk (grid y 0) or dv (1) = the sum of its ranges, four values a thread; tokens of no sequence are left alone
+template <class T>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttShape a, const float *__restrict__ ranges, int count, T *dk, T *dv, int add_k, int add_v) {
+    const int width = a.kv_heads * a.head_dim, per_row = width / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per_row, all = (int64_t)a.tokens * width;
+    if (row >= a.tokens || row < a.cu[0] || row >= a.cu[a.seqs]) return;
+    const int c = (int)(i - row * per_row) * 4;
+    const float *p = ranges + (blockIdx.y ? count * all : 0) + row * width + c;
+    float4 v = *(const float4 *)p;
+    for (int r = 1; r < count; ++r) {
+        const float4 w = *(const float4 *)(p + r * all);
+        v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+    }
+    const bool add = blockIdx.y ? add_v : add_k;
+    T *out = blockIdx.y ? dv + row * a.v_ld + c : dk + row * a.k_ld + c;
+    if constexpr (sizeof(T) == 2) {
+        if (add) {
+            const uint2 o = *(const uint2 *)out;
+            v.x += __uint_as_float(o.x << 16); v.y += __uint_as_float(o.x & 0xffff0000u);
+            v.z += __uint_as_float(o.y << 16); v.w += __uint_as_float(o.y & 0xffff0000u);
+        }
+        *(uint2 *)out = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+    } else {
+        if (add) { const float4 o = *(const float4 *)out; v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w; }
+        *(float4 *)out = v;
+    }
 }
 
 AttShape att_shape(int dtype, const int32_t *cu, int seqs, int64_t tokens, int heads, int kv_heads, int head_dim, int64_t q_ld, int64_t k_ld,
@@ -504,10 +615,9 @@ AttShape att_shape(int dtype, const int32_t *cu, int seqs, int64_t tokens, int h
         if (ld < (int64_t)heads * head_dim || ld % step || ld >= (1 << 23)) throw KernelError("attention: row strides must hold all heads, be a multiple of 16 bytes and below 2^23 elements");
     for (int64_t ld : {k_ld, v_ld})
         if (ld < (int64_t)kv_heads * head_dim || ld % step || ld >= (1 << 23)) throw KernelError("attention: row strides must hold all heads, be a multiple of 16 bytes and below 2^23 elements");
-    const int64_t slots = tokens / ATT_ROWS + seqs;
-    if (tokens > 0x7fffffff || slots * heads > 0x7fffffff) throw KernelError("attention: too many tokens");
+    if (tokens > 0x7fffffff || (tokens / 32 + seqs) * heads > 0x7fffffff) throw KernelError("attention: too many tokens");
     if (!cu) throw KernelError("attention: null pointer");
-    return AttShape{cu, seqs, (int)tokens, heads, kv_heads, head_dim, (int)slots, q_ld, k_ld, v_ld, o_ld, scale};
+    return AttShape{cu, seqs, (int)tokens, heads, kv_heads, head_dim, 0, q_ld, k_ld, v_ld, o_ld, scale};
 }
 void check_tensors(std::initializer_list<const void *> ptrs) {
     for (const void *p : ptrs) {
@@ -516,20 +626,85 @@ void check_tensors(std::initializer_list<const void *> ptrs) {
     }
 }
 
+// Rows of the forward and the first backward kernel: 128 to a workgroup where that gives four workgroups to a CU, 64 below (bf16, forward:
+// 8 x 16 heads of 512 rows 14.4 against 15.5 us, one sequence of 4000 rows and 8 heads 40 against 51; at 4096 workgroups 64 rows take 10 %
+// longer), and 32 in fp32 with 64 columns, whose products are slow enough to hide the traffic, below two (70 against 88 us at 816 workgroups).
 template <class T, int D>
-void fwd_launch(hipStream_t st, const AttShape &a, const void *q, const void *k, const void *v, void *o, float *lse) {
-    hipLaunchKernelGGL((attention_fwd_kernel<T, D>), dim3(a.slots * a.heads), dim3(256), 0, st, a, (const T *)q, (const T *)k, (const T *)v, (T *)o, lse);
+int row_parts(const AttShape &a) {
+    const int64_t full = (int64_t)(a.tokens / 128) * a.heads;
+    if (full >= 1024 && a.tokens / a.seqs >= 128) return 1;
+    return sizeof(T) == 4 && D == 64 && full < 512 ? 4 : 2;
+}
+// The second backward kernel has fewer workgroups (key heads) with a longer way each (the rows behind a key, of every head of the group).
+// Where 128 keys to a workgroup do not give four workgroups to a CU, the way is cut into ranges of at least 16 tiles; where that gives less
+// than two, a workgroup takes 32 keys (64 in fp32 with 128 columns, whose tiles fill LDS) and ranges by the same measure.  bf16, both
+// backward kernels: 8 ragged sequences of 8192 rows, 32 / 8 heads, 1255 us uncut, 888 in four ranges, 928 with 32 keys; one of 10000, 4 / 1
+// heads, 2291, 620 (8 ranges), 820 (32 keys, 4 ranges); one of 1024, 8 heads of 64, 51, 43 (4 ranges), 24 (32 keys).
+struct KeyForm { int parts, ranges; };
+KeyForm key_form(const AttShape &a, bool fp32) {
+    const bool large = fp32 && a.head_dim > 64;
+    const int64_t full = std::max<int64_t>(1, (int64_t)(a.tokens / 128) * a.kv_heads), len = a.tokens / a.seqs, group = a.heads / a.kv_heads;
+    const auto cut = [&](int64_t groups, int64_t tile) {
+        return std::max<int64_t>(1, std::min<int64_t>({(2048 + groups - 1) / groups, len * group / tile / 16, 16}));
+    };
+    if (full >= 1024) return {1, 1};
+    const int64_t r = cut(full, fp32 ? 32 : 64);
+    if (full * r >= 512 && len >= 64) return {1, (int)r};
+    const int parts = large ? 2 : 4;
+    return {parts, (int)cut(2 * full * parts, large ? 64 : 128)};
+}
+
+template <class T, int D, int PARTS>
+void fwd_launch(hipStream_t st, AttShape a, const void *q, const void *k, const void *v, void *o, float *lse) {
+    a.slots = a.tokens / AttForm<T, D, PARTS>::ROWS + a.seqs;
+    hipLaunchKernelGGL((attention_fwd_kernel<T, D, PARTS>), dim3(a.slots * a.heads), dim3(256), 0, st, a, (const T *)q, (const T *)k, (const T *)v, (T *)o, lse);
     hip_check(hipGetLastError(), "attention forward launch");
 }
 template <class T, int D>
-void bwd_launch(hipStream_t st, const AttShape &a, const void *go, const void *q, const void *k, const void *v, const void *o, const float *lse, void *dq,
-                void *dk, void *dv, int accumulate, float *delta) {
-    hipLaunchKernelGGL((attention_dq_kernel<T, D>), dim3(a.slots * a.heads), dim3(256), 0, st, a, (const T *)go, (const T *)q, (const T *)k,
-                       (const T *)v, (const T *)o, lse, (T *)dq, delta, accumulate & 1);
+void fwd_form(hipStream_t st, const AttShape &a, const void *q, const void *k, const void *v, void *o, float *lse) {
+    const int parts = row_parts<T, D>(a);
+    if (parts == 1) fwd_launch<T, D, 1>(st, a, q, k, v, o, lse);
+    else if (parts == 2) fwd_launch<T, D, 2>(st, a, q, k, v, o, lse);
+    else if constexpr (sizeof(T) == 4 && D == 64) fwd_launch<T, D, 4>(st, a, q, k, v, o, lse);
+}
+struct BwdArgs {
+    const void *go, *q, *k, *v, *o;
+    const float *lse;
+    void *dq, *dk, *dv;
+    float *delta, *ranges;
+    int accumulate;
+};
+int64_t stat_bytes(const AttShape &a) { return (2 * (int64_t)a.heads * a.tokens * 4 + 255) / 256 * 256; }
+template <class T, int D, int PARTS>
+void dq_launch(hipStream_t st, AttShape a, const BwdArgs &b) {
+    a.slots = a.tokens / AttForm<T, D, PARTS>::ROWS + a.seqs;
+    hipLaunchKernelGGL((attention_dq_kernel<T, D, PARTS>), dim3(a.slots * a.heads), dim3(256), 0, st, a, (const T *)b.go, (const T *)b.q, (const T *)b.k,
+                       (const T *)b.v, (const T *)b.o, b.lse, (T *)b.dq, b.delta, b.accumulate & 1);
     hip_check(hipGetLastError(), "attention query gradient launch");
-    hipLaunchKernelGGL((attention_dkv_kernel<T, D>), dim3(a.slots * a.kv_heads), dim3(256), 0, st, a, (const T *)go, (const T *)q, (const T *)k,
-                       (const T *)v, lse, delta, (T *)dk, (T *)dv, accumulate & 2, accumulate & 4);
+}
+template <class T, int D, int PARTS>
+void dkv_launch(hipStream_t st, AttShape a, const BwdArgs &b, int ranges) {
+    a.slots = a.tokens / AttForm<T, D, PARTS>::ROWS + a.seqs;
+    hipLaunchKernelGGL((attention_dkv_kernel<T, D, PARTS>), dim3(a.slots * a.kv_heads, ranges), dim3(256), 0, st, a, (const T *)b.go, (const T *)b.q,
+                       (const T *)b.k, (const T *)b.v, b.delta, (T *)b.dk, (T *)b.dv, b.accumulate & 2, b.accumulate & 4, ranges > 1 ? b.ranges : nullptr);
     hip_check(hipGetLastError(), "attention key gradient launch");
+    if (ranges > 1) {
+        const int64_t blocks = ((int64_t)a.tokens * a.kv_heads * a.head_dim / 4 + 255) / 256;
+        hipLaunchKernelGGL((attention_join_kernel<T>), dim3((unsigned)blocks, 2), dim3(256), 0, st, a, b.ranges, ranges, (T *)b.dk, (T *)b.dv,
+                           b.accumulate & 2, b.accumulate & 4);
+        hip_check(hipGetLastError(), "attention join launch");
+    }
+}
+template <class T, int D>
+void bwd_form(hipStream_t st, const AttShape &a, const BwdArgs &b) {
+    const int parts = row_parts<T, D>(a);
+    if (parts == 1) dq_launch<T, D, 1>(st, a, b);
+    else if (parts == 2) dq_launch<T, D, 2>(st, a, b);
+    else if constexpr (sizeof(T) == 4 && D == 64) dq_launch<T, D, 4>(st, a, b);
+    const KeyForm f = key_form(a, sizeof(T) == 4);
+    constexpr int MANY = sizeof(T) == 4 && D == 128 ? 2 : 4;
+    if (f.parts == 1) dkv_launch<T, D, 1>(st, a, b, f.ranges);
+    else dkv_launch<T, D, MANY>(st, a, b, f.ranges);
 }
 
 }  // namespace
@@ -540,15 +715,16 @@ void attention_fwd(hipStream_t st, int dtype, const void *q, const void *k, cons
     if (!tokens) return;
     check_tensors({q, k, v, o});
     if (!lse) throw KernelError("attention: null pointer");
-    if (dtype == MONET_BF16) (head_dim <= 64 ? fwd_launch<unsigned short, 64> : fwd_launch<unsigned short, 128>)(st, a, q, k, v, o, lse);
-    else (head_dim <= 64 ? fwd_launch<float, 64> : fwd_launch<float, 128>)(st, a, q, k, v, o, lse);
+    if (dtype == MONET_BF16) (head_dim <= 64 ? fwd_form<unsigned short, 64> : fwd_form<unsigned short, 128>)(st, a, q, k, v, o, lse);
+    else (head_dim <= 64 ? fwd_form<float, 64> : fwd_form<float, 128>)(st, a, q, k, v, o, lse);
 }
 
 size_t attention_bwd_workspace_bytes(int dtype, int seqs, int64_t tokens, int heads, int kv_heads, int head_dim) {
     static const int32_t none = 0;
-    att_shape(dtype, &none, seqs, tokens, heads, kv_heads, head_dim, (int64_t)heads * head_dim, (int64_t)kv_heads * head_dim,
+    const AttShape a = att_shape(dtype, &none, seqs, tokens, heads, kv_heads, head_dim, (int64_t)heads * head_dim, (int64_t)kv_heads * head_dim,
               (int64_t)kv_heads * head_dim, (int64_t)heads * head_dim, 1.f);
-    return (size_t)(((int64_t)heads * tokens * 4 + 255) / 256 * 256);
+    const int ranges = key_form(a, dtype == MONET_F32).ranges;
+    return (size_t)(stat_bytes(a) + (ranges > 1 ? 2 * (int64_t)ranges * tokens * kv_heads * head_dim * 4 : 0));
 }
 
 void attention_bwd(hipStream_t st, int dtype, const void *go, const void *q, const void *k, const void *v, const void *o, const float *lse, void *dq,
@@ -562,9 +738,9 @@ void attention_bwd(hipStream_t st, int dtype, const void *go, const void *q, con
     if (!ws || ws_bytes < attention_bwd_workspace_bytes(dtype, seqs, tokens, heads, kv_heads, head_dim))
         throw KernelError("attention: workspace too small");
     if ((uintptr_t)ws % 256) throw KernelError("attention: the workspace must be 256-byte aligned");
-    if (dtype == MONET_BF16)
-        (head_dim <= 64 ? bwd_launch<unsigned short, 64> : bwd_launch<unsigned short, 128>)(st, a, go, q, k, v, o, lse, dq, dk, dv, accumulate, (float *)ws);
-    else (head_dim <= 64 ? bwd_launch<float, 64> : bwd_launch<float, 128>)(st, a, go, q, k, v, o, lse, dq, dk, dv, accumulate, (float *)ws);
+    const BwdArgs b{go, q, k, v, o, lse, dq, dk, dv, (float *)ws, (float *)((char *)ws + stat_bytes(a)), accumulate};
+    if (dtype == MONET_BF16) (head_dim <= 64 ? bwd_form<unsigned short, 64> : bwd_form<unsigned short, 128>)(st, a, b);
+    else (head_dim <= 64 ? bwd_form<float, 64> : bwd_form<float, 128>)(st, a, b);
 }
 
 }  // namespace monet

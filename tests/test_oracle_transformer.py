@@ -108,7 +108,7 @@ def refused(name, args, match):
     (dict(k_ld=260), "strides"), (dict(v_ld=128), "strides"), (dict(o_ld=1 << 23), "strides"), (dict(scale=0.0), "scale"),
     (dict(scale=float("nan")), "scale"), (dict(scale=float("inf")), "scale"), (dict(tokens=1 << 31), "too many"), (dict(q=P + 8), "aligned"),
     (dict(k=None), "null"), (dict(lse=None), "null"), (dict(cu=None), "null"), (dict(accumulate=8), "accumulate"), (dict(ws=None), "workspace"),
-    (dict(ws=P + 16), "workspace"), (dict(ws_bytes=8 * 100 * 4 - 1), "workspace"), (dict(go=None), "null"), (dict(dv=P + 4), "aligned"),
+    (dict(ws=P + 16), "workspace"), (dict(ws_bytes=2 * 8 * 100 * 4 - 1), "workspace"), (dict(go=None), "null"), (dict(dv=P + 4), "aligned"),
 ])
 def test_attention_refuses(change, match):
     a = dict(dtype=monet.BF16, go=P, q=P, k=P, v=P, o=P, lse=P, dq=P, dk=P, dv=P, cu=P, seqs=3, tokens=100, heads=8, kv_heads=4, head_dim=64,
