@@ -4,8 +4,9 @@
 // Backward: dl[t][v] = (exp(l[t][v] - lse[t]) - [v == label]) / count, dx = dl w, dw = dl^T x, one piece of dl at a time.
 //
 // bf16: three matrix products on the bf16 matrix cores (gemm_bf16.hpp).  The first one's epilogue keeps a maximum and a sum of
-// exponentials per row and 128 logits (forward) or writes dl, rounded to bf16 (backward: dl is the operand of two bf16 products whose
-// results are rounded to bf16 themselves; the rounding, at most 2^-8 of a value, averages out over the sums).  All sums are fp32.
+// exponentials per row and 64 or 128 logits (forward) or writes count * dl, rounded to bf16 (backward: it is the operand of two bf16
+// products whose results are rounded to bf16 themselves; the rounding, at most 2^-8 of a value, averages out over the sums.  1 / count
+// comes in behind the products: the label's entries p - 1 are near -1 and would otherwise all be rounded the same way).  Sums are fp32.
 // fp32: the convolution kernels' products, a piece of logits in the workspace at a time.
 #include <initializer_list>
 #include <vector>
@@ -69,17 +70,16 @@ struct CeStatsEpilogue {
     }
 };
 
-// dl[t][v - v0]; columns behind the vocabulary are zero up to the row's end
+// count * dl[t][v - v0]; columns behind the vocabulary are zero up to the row's end
 struct CeGradEpilogue {
     const int32_t *labels;
-    const float *lse, *inv_count;
+    const float *lse;
     unsigned short *dl;
     int64_t ld;
     int rows, piece, v0, vocab;      // `piece` logits from v0 on
     template <int MB, int NB>
     __device__ __forceinline__ void operator()(floatx16 (&acc)[MB][NB], int m0, int n0, int, int) const {
         const int l = threadIdx.x & 63;
-        const float inv = *inv_count;
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const int t = n0 + 32 * j + (l & 31);
@@ -97,7 +97,7 @@ struct CeGradEpilogue {
                     for (int q = 0; q < 4; ++q) {
                         const int v = m0 + 32 * i + result_row(r + q, l);
                         const float p = exp_of(acc[i][j][r + q] - ls);
-                        d[q] = has && v < piece ? (p - (v0 + v == label ? 1.f : 0.f)) * inv : 0.f;
+                        d[q] = has && v < piece ? p - (v0 + v == label ? 1.f : 0.f) : 0.f;
                     }
                     if (m0 + 32 * i + result_row(r, l) < ld)
                         *(uint2 *)(row + 32 * i + result_row(r, l)) = make_uint2(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]));
@@ -134,13 +134,15 @@ struct SumEpilogue {
     }
 };
 
-// out[n][m] in bf16
+// *by out[n][m] in bf16
 struct RoundEpilogue {
     unsigned short *out;
+    const float *by;
     int64_t ld;
     template <int MB, int NB>
     __device__ __forceinline__ void operator()(floatx16 (&acc)[MB][NB], int m0, int n0, int m, int n) const {
         const int l = threadIdx.x & 63;
+        const float f = *by;
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const int c = n0 + 32 * j + (l & 31);
@@ -150,7 +152,8 @@ struct RoundEpilogue {
 #pragma unroll
                 for (int r = 0; r < 16; r += 4) {
                     const int row = m0 + 32 * i + result_row(r, l);
-                    if (row < m) *(uint2 *)(out + c * ld + row) = make_uint2(pack_bf16(acc[i][j][r], acc[i][j][r + 1]), pack_bf16(acc[i][j][r + 2], acc[i][j][r + 3]));
+                    if (row < m)
+                        *(uint2 *)(out + c * ld + row) = make_uint2(pack_bf16(acc[i][j][r] * f, acc[i][j][r + 1] * f), pack_bf16(acc[i][j][r + 2] * f, acc[i][j][r + 3] * f));
                 }
         }
     }
@@ -197,20 +200,24 @@ __global__ __launch_bounds__(1024) void ce_mean_kernel(const float *__restrict__
     if (inv) *inv = counts[0] ? 1.f / counts[0] : 0.f;
 }
 
-// out = sum over ranges of part (+ out), rounded to bf16; eight values a thread
-__global__ __launch_bounds__(256) void ce_round_kernel(const float *__restrict__ part, int ranges, int64_t n, unsigned short *__restrict__ out, int add) {
+// out = *by times the sum over ranges of part (+ out), rounded to bf16; eight values a thread
+__global__ __launch_bounds__(256) void ce_round_kernel(const float *__restrict__ part, int ranges, int64_t n, const float *__restrict__ by,
+                                                       unsigned short *__restrict__ out, int add) {
     const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
     if (i >= n) return;
     float v[8] = {};
+    for (int r = 0; r < ranges; ++r) {
+        const float4 a = *(const float4 *)(part + r * n + i), b = *(const float4 *)(part + r * n + i + 4);
+        v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+    }
+    const float f = *by;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] *= f;
     if (add) {
         const uint4 o = *(const uint4 *)(out + i);
         const unsigned w[4] = {o.x, o.y, o.z, o.w};
 #pragma unroll
-        for (int q = 0; q < 4; ++q) { v[2 * q] = __uint_as_float(w[q] << 16); v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u); }
-    }
-    for (int r = 0; r < ranges; ++r) {
-        const float4 a = *(const float4 *)(part + r * n + i), b = *(const float4 *)(part + r * n + i + 4);
-        v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+        for (int q = 0; q < 4; ++q) { v[2 * q] += __uint_as_float(w[q] << 16); v[2 * q + 1] += __uint_as_float(w[q] & 0xffff0000u); }
     }
     *(uint4 *)(out + i) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
@@ -253,15 +260,16 @@ int64_t cut(int64_t n, int64_t by) { return (n + by - 1) / by; }
 
 constexpr int64_t CE_PIECE_BYTES = 256ll << 20;      // a piece of logits or of their gradient
 
-// How a call goes through the vocabulary, and its workspace: forward [hit][row_loss][part][logits (fp32)], backward
-// [inv][dx parts (bf16)][dl][parts of the fp32 products].
+// How a call goes through the vocabulary, and its workspace: forward [hit][row_loss][part][product][logits (fp32)], backward
+// [inv][dx parts (bf16) or product][dl].
 struct CePlan {
     int rows, width, vocab;
     bool bf16;
     int unit = 0;                   // bf16 forward: logits to a part
     int piece = 0;                  // logits of a piece
     int ranges = 1, chunk = 0;      // bf16 backward: of the reduction over a piece in dx
-    int dgrad_splits = 1, wgrad_splits = 1;      // fp32 backward
+    int wgrad_splits = 1;           // fp32 backward
+    int64_t product = 0;            // fp32: bytes for the products' partial results
     int64_t fixed = 0, per_col = 0;              // bytes without the pieces, and for each logit of a piece
 
     int64_t parts() const { return bf16 ? cut(vocab, unit) : pieces().size(); }
@@ -277,8 +285,10 @@ struct CePlan {
     }
 };
 
-// A reduction of `red` into rows x cols results gives few tiles where both are small: as many ranges as fill the card, of 512 indices at least.
-int ce_splits(int64_t tiles, int64_t red) { return (int)std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), red / 512, 16})); }
+// Results of few tiles leave CUs idle while their reduction is long: as many ranges as fill the card, of at least `least` indices.
+int ce_splits(int64_t tiles, int64_t red, int64_t least) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), red / least, 16}));
+}
 
 CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab) {
     if (dtype != MONET_F32 && dtype != MONET_BF16) throw KernelError("linear_ce: dtype must be MONET_F32 or MONET_BF16");
@@ -296,23 +306,24 @@ CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab) {
     const int64_t pieces = cut(vocab, std::max<int64_t>(CE_PIECE_BYTES / p.per_col / 256 * 256, 256));
     p.piece = (int)std::min<int64_t>(up(cut(vocab, pieces), 256), 1 << 20);
     if (!bf16) p.piece = std::min(p.piece, vocab);
+    const ConvShape cs{p.rows, 1, 1, width, p.piece, 1, 1, 1, 0, 1, 1};
     if (!grad) {
-        p.fixed = 2 * up(rows * 4, 256) + up(p.parts() * rows * 8, 256);
+        p.product = up((int64_t)conv_workspace_bytes(0, cs, 1), 256);
+        p.fixed = 2 * up(rows * 4, 256) + up(p.parts() * rows * 8, 256) + p.product;
         return p;
     }
     p.fixed = 256;
     if (bf16) {
-        p.ranges = ce_splits(cut(width, 128) * cut(rows, 128), p.piece);
+        p.ranges = ce_splits(cut(width, 128) * cut(rows, 128), p.piece, 512);
         p.chunk = (int)up(cut(p.piece, p.ranges), GEMM_DEPTH);
         p.ranges = (int)cut(std::min(p.piece, vocab), p.chunk);      // a later piece is no longer than the first
         if (p.ranges > 1 || p.piece < vocab) p.fixed += up(p.ranges * rows * width * 4, 256);
     } else {
-        p.dgrad_splits = ce_splits(cut(width, 128) * cut(rows, 128), p.piece);
-        p.wgrad_splits = ce_splits(cut(width, 128) * cut(p.piece, 128), rows);
-        int64_t part = 0;
-        if (p.dgrad_splits > 1) part = p.dgrad_splits * rows * width * 4;
-        if (p.wgrad_splits > 1) part = std::max(part, p.wgrad_splits * (int64_t)p.piece * width * 4);
-        p.fixed += up(part, 256);
+        p.wgrad_splits = ce_splits(cut(width, 128) * cut(p.piece, 128), rows, 64);
+        p.product = (int64_t)std::max(conv_workspace_bytes(0, cs, 1), conv_workspace_bytes(1, cs, 1));
+        if (p.wgrad_splits > 1) p.product = std::max(p.product, p.wgrad_splits * (int64_t)p.piece * width * 4);
+        p.product = up(p.product, 256);
+        p.fixed += p.product;
     }
     return p;
 }
@@ -356,11 +367,12 @@ void linear_ce_fwd(hipStream_t st, int dtype, const void *x, const void *w, cons
     if (p.bf16) {
         gemm_bf16<false, false>(st, ce_logits_shape(p, x, w, 0, vocab), CeStatsEpilogue{labels, part, hit, p.rows, vocab}, "linear_ce logits launch");
     } else {
-        float *logits = (float *)((char *)ws + p.fixed);
+        float *logits = (float *)((char *)ws + p.fixed), *product = p.product ? (float *)((char *)logits - p.product) : nullptr;
+        const size_t product_bytes = (size_t)p.product;
         const std::vector<int> at = p.pieces();
         for (size_t i = 0; i < at.size(); ++i) {
             const int piece = (i + 1 < at.size() ? at[i + 1] : vocab) - at[i];
-            conv_fwd(st, (const float *)x, (const float *)w + (int64_t)at[i] * width, logits, ce_conv_shape(p, piece));
+            conv_fwd(st, (const float *)x, (const float *)w + (int64_t)at[i] * width, logits, ce_conv_shape(p, piece), 1, product, product_bytes);
             hipLaunchKernelGGL(ce_piece_stats_kernel, dim3(p.rows), dim3(256), 0, st, logits, piece, at[i], labels, part + i * rows, hit);
             hip_check(hipGetLastError(), "linear_ce statistics launch");
         }
@@ -389,7 +401,7 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
             unsigned short *d = (unsigned short *)dl;
             const int64_t ld = up(piece, 8);
             gemm_bf16<false, false>(st, ce_logits_shape(p, x, w, v0, piece),
-                                    CeGradEpilogue{labels, lse, inv, d, ld, p.rows, piece, v0, vocab}, "linear_ce gradient launch");
+                                    CeGradEpilogue{labels, lse, d, ld, p.rows, piece, v0, vocab}, "linear_ce gradient launch");
             GemmShape g{};
             // dx[t][c] (+)= sum over v of w[v][c] dl[t][v]
             g.a = (const unsigned short *)w + (int64_t)v0 * width; g.lda = width;
@@ -397,12 +409,12 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
             g.m = width; g.n = p.rows; g.k = piece;
             g.chunk = p.chunk; g.splits = (int)cut(piece, p.chunk);
             if (p.ranges == 1 && at.size() == 1 && !accumulate)
-                gemm_bf16<true, false>(st, g, RoundEpilogue{(unsigned short *)dx, width}, "linear_ce input gradient launch");
+                gemm_bf16<true, false>(st, g, RoundEpilogue{(unsigned short *)dx, inv, width}, "linear_ce input gradient launch");
             else {
                 gemm_bf16<true, false>(st, g, SumEpilogue{parts, width, rows * width, i > 0}, "linear_ce input gradient launch");
                 if (i + 1 == at.size()) {
                     const int64_t n = rows * width;
-                    hipLaunchKernelGGL(ce_round_kernel, dim3((unsigned)cut(n, 2048)), dim3(256), 0, st, parts, p.ranges, n, (unsigned short *)dx, accumulate);
+                    hipLaunchKernelGGL(ce_round_kernel, dim3((unsigned)cut(n, 2048)), dim3(256), 0, st, parts, p.ranges, n, inv, (unsigned short *)dx, accumulate);
                     hip_check(hipGetLastError(), "linear_ce round launch");
                 }
             }
@@ -410,18 +422,19 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
             g.a = (const unsigned short *)x; g.lda = width;
             g.m = width; g.n = piece; g.k = p.rows;
             g.splits = 1; g.chunk = (int)up(rows, GEMM_DEPTH);
-            gemm_bf16<true, true>(st, g, RoundEpilogue{(unsigned short *)dw + (int64_t)v0 * width, width}, "linear_ce weight gradient launch");
+            gemm_bf16<true, true>(st, g, RoundEpilogue{(unsigned short *)dw + (int64_t)v0 * width, inv, width}, "linear_ce weight gradient launch");
         } else {
             const ConvShape cs = ce_conv_shape(p, piece);
             const float *wp = (const float *)w + (int64_t)v0 * width;
             float *d = (float *)dl;
-            const size_t part_bytes = (size_t)(p.fixed - 256);
-            conv_fwd(st, (const float *)x, wp, d, cs);
+            float *product = p.product ? parts : nullptr;
+            const size_t product_bytes = (size_t)p.product;
+            conv_fwd(st, (const float *)x, wp, d, cs, 1, product, product_bytes);
             hipLaunchKernelGGL(ce_piece_grad_kernel, dim3(p.rows, (unsigned)cut(piece, 256)), dim3(256), 0, st, d, piece, v0, labels, lse, inv, vocab);
             hip_check(hipGetLastError(), "linear_ce gradient launch");
-            conv_dgrad(st, d, wp, (float *)dx, cs, accumulate || i > 0, p.dgrad_splits, p.dgrad_splits > 1 ? parts : nullptr, p.dgrad_splits > 1 ? part_bytes : 0);
-            conv_wgrad(st, (const float *)x, d, (float *)dw + (int64_t)v0 * width, cs, p.wgrad_splits, p.wgrad_splits > 1 ? parts : nullptr,
-                       p.wgrad_splits > 1 ? part_bytes : 0);
+            conv_dgrad(st, d, wp, (float *)dx, cs, accumulate || i > 0, 1, product, product_bytes);
+            conv_wgrad(st, (const float *)x, d, (float *)dw + (int64_t)v0 * width, cs, p.wgrad_splits, p.wgrad_splits > 1 ? product : nullptr,
+                       p.wgrad_splits > 1 ? product_bytes : 0);
         }
     }
 }
