@@ -24,18 +24,22 @@ template <class T> __device__ __forceinline__ float value_of(T v);
 template <> __device__ __forceinline__ float value_of(float v) { return v; }
 template <> __device__ __forceinline__ float value_of(unsigned short v) { return bf16_float(v); }
 
+// vectors at any address that their elements may have: the hardware takes 16 bytes from and to there
+typedef float float4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned uint4_any __attribute__((ext_vector_type(4), aligned(2)));
+
 // eight neighbouring values; `have` of them exist
 template <class T>
-__device__ __forceinline__ void load8(const T *p, int have, bool vec, float (&v)[8]) {
-    if (vec && have >= 8) {
+__device__ __forceinline__ void load8(const T *p, int have, float (&v)[8]) {
+    if (have >= 8) {
         if constexpr (sizeof(T) == 4) {
-            const float4 a = *(const float4 *)p, b = *(const float4 *)(p + 4);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        } else {
-            const uint4 a = *(const uint4 *)p;
-            const unsigned w[4] = {a.x, a.y, a.z, a.w};
+            const float4_any a = *(const float4_any *)p, b = *(const float4_any *)(p + 4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+            for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+        } else {
+            const uint4_any a = *(const uint4_any *)p;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(a[i] << 16); v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u); }
         }
     } else {
 #pragma unroll
@@ -46,12 +50,12 @@ __device__ __forceinline__ void load8(const T *p, int have, bool vec, float (&v)
 // a thread takes eight columns, four threads a group
 template <class T>
 __global__ __launch_bounds__(256) void act8_pack_kernel(const T *__restrict__ x, int64_t ld, int8_t *__restrict__ code, uint8_t *__restrict__ exps,
-                                                        int64_t rows, int cols, int per_row, bool vec) {
+                                                        int64_t rows, int cols, int per_row) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per_row;
     if (row >= rows) return;
     const int c = (int)(i - row * per_row) * 8;
     float v[8];
-    load8(x + row * ld + c, cols - c, vec, v);
+    load8(x + row * ld + c, cols - c, v);
     unsigned top = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
@@ -73,7 +77,7 @@ __global__ __launch_bounds__(256) void act8_pack_kernel(const T *__restrict__ x,
 
 template <class T>
 __global__ __launch_bounds__(256) void act8_unpack_kernel(const int8_t *__restrict__ code, const uint8_t *__restrict__ exps, T *__restrict__ y, int64_t ld,
-                                                          int64_t rows, int cols, int per_row, bool vec) {
+                                                          int64_t rows, int cols, int per_row) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per_row;
     if (row >= rows) return;
     const int c = (int)(i - row * per_row) * 8, have = cols - c;
@@ -84,11 +88,11 @@ __global__ __launch_bounds__(256) void act8_unpack_kernel(const int8_t *__restri
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = (float)(int8_t)((j < 4 ? w.x : w.y) >> (8 * (j % 4))) * by;
     T *p = y + row * ld + c;
-    if (vec && have >= 8) {
+    if (have >= 8) {
         if constexpr (sizeof(T) == 4) {
-            *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
-            *(float4 *)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-        } else *(uint4 *)p = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+            *(float4_any *)p = float4_any{v[0], v[1], v[2], v[3]};
+            *(float4_any *)(p + 4) = float4_any{v[4], v[5], v[6], v[7]};
+        } else *(uint4_any *)p = uint4_any{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -110,7 +114,7 @@ struct Act8Shape {
     int64_t rows, range;       // range: elements between the partial results of two ranges
     int cols, outs, ld, tiles_m, tiles_n;
     int64_t chunk;             // rows of a range
-    bool vec, vec_out;
+    bool vec_out;
 };
 template <bool F32, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN * 64, WM *WN * 64 / 256) void act8_wgrad_kernel(Act8Shape g) {
@@ -137,7 +141,7 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN * 64 / 256) void act8_wgrad_ker
     float scale[CODES];
     typedef typename std::conditional<F32, float, unsigned short>::type T;
     float dy[F32 ? PIECES : 1][8];
-    uint4 dyw[F32 ? 1 : PIECES];
+    uintx4 dyw[F32 ? 1 : PIECES];
     auto fetch = [&](int64_t k0) {
 #pragma unroll
         for (int i = 0; i < CODES; ++i) {
@@ -154,15 +158,11 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN * 64 / 256) void act8_wgrad_ker
             const int piece = i * THREADS + threadIdx.x, kr = piece / (BN / 8), o = o0 + piece % (BN / 8) * 8;
             const int have = k0 + kr < last ? g.outs - o : 0;
             const T *p = (const T *)g.dy + (k0 + kr) * g.outs + o;
-            if constexpr (F32) load8(p, have, g.vec, dy[i]);
+            if constexpr (F32) load8(p, have, dy[i]);
+            else if (have >= 8) dyw[i] = *(const uint4_any *)p;
             else {
-                if (g.vec) dyw[i] = have >= 8 ? *(const uint4 *)p : make_uint4(0, 0, 0, 0);
-                else {
-                    unsigned w[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) w[j] = (2 * j < have ? p[2 * j] : 0u) | (2 * j + 1 < have ? (unsigned)p[2 * j + 1] << 16 : 0u);
-                    dyw[i] = make_uint4(w[0], w[1], w[2], w[3]);
-                }
+                for (int j = 0; j < 4; ++j) dyw[i][j] = (2 * j < have ? p[2 * j] : 0u) | (2 * j + 1 < have ? (unsigned)p[2 * j + 1] << 16 : 0u);
             }
         }
     };
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN * 64 / 256) void act8_wgrad_ker
                 *(bf16x8 *)(b_lds[buf][0] + at) = r.h;
                 *(bf16x8 *)(b_lds[buf][1] + at) = r.m;
                 *(bf16x8 *)(b_lds[buf][2] + at) = r.l;
-            } else *(uint4 *)(b_lds[buf][0] + at) = dyw[i];
+            } else *(uintx4 *)(b_lds[buf][0] + at) = dyw[i];
         }
     };
     auto work = [&](int buf) {
@@ -248,6 +248,59 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN * 64 / 256) void act8_wgrad_ker
     }
 }
 
+// dy as the GEMM takes it: rows of `ld` values, zero behind the last one; fp32 in three planes of pieces.  Eight values a thread.
+template <class T>
+__global__ __launch_bounds__(256) void act8_planes_kernel(const T *__restrict__ dy, unsigned short *__restrict__ out, int64_t rows, int outs, int ld) {
+    const int per_row = ld / 8;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per_row, plane = rows * ld;
+    if (row >= rows) return;
+    const int o = (int)(i - row * per_row) * 8;
+    float v[8];
+    load8(dy + row * outs + o, outs - o, v);
+    unsigned short *p = out + row * ld + o;
+    if constexpr (sizeof(T) == 4) {
+        unsigned lost = 0;
+        const PieceRow r = split_row(v, lost);
+        *(bf16x8 *)p = r.h;
+        *(bf16x8 *)(p + plane) = r.m;
+        *(bf16x8 *)(p + 2 * plane) = r.l;
+    } else *(uint4 *)p = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+}
+
+// out[n][m], one range's partial result behind the other
+struct RangeEpilogue {
+    float *out;
+    int64_t range;
+    int add;
+    bool vec;
+    template <int MB, int NB>
+    __device__ __forceinline__ void operator()(floatx16 (&acc)[MB][NB], int m0, int n0, int m, int n) const {
+        const int l = threadIdx.x & 63;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int o = n0 + 32 * j + (l & 31);
+            if (o >= n) continue;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const int c = m0 + 32 * i + result_row(r, l);
+                    float *p = out + blockIdx.y * range + (int64_t)o * m + c;
+                    if (vec) {
+                        if (c >= m) continue;
+                        float4 v = make_float4(acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]);
+                        if (add) { const float4 w = *(const float4 *)p; v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w; }
+                        *(float4 *)p = v;
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            if (c + q < m) p[q] = acc[i][j][r + q] + (add ? p[q] : 0.f);
+                    }
+                }
+        }
+    }
+};
+
 void check_shape(int64_t rows, int64_t cols) {
     if (rows < 1 || cols < 1 || cols > (1 << 24) || rows > (1ll << 40) / code_ld(cols)) throw KernelError("act8: bad shape");
 }
@@ -259,14 +312,45 @@ void check_tensor(const void *p, size_t align) {
     if ((uintptr_t)p % align) throw KernelError("act8: pointer not aligned");
 }
 
-// Results of few tiles cut the reduction over the rows into ranges until every CU has a workgroup, each of at least 256 rows.
-struct WgradPlan { int tile, splits; int64_t chunk; };
-WgradPlan wgrad_plan(int64_t rows, int cols, int outs) {
-    const int tile = gemm_tile(cols, outs);
-    const int64_t tiles = ((cols + tile - 1) / tile) * ((int64_t)(outs + tile - 1) / tile);
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({512 / tiles, rows / 256, 64}));
-    const int64_t chunk = ((rows + splits - 1) / splits + 63) / 64 * 64;
-    return {tile, (int)((rows + chunk - 1) / chunk), chunk};
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// Two forms.  Direct: one kernel from codes and dy, few launches.  Expanded: the codes as bf16 and dy's planes in the workspace, some rows
+// (a turn) at a time, and the GEMM, whose operands then need no register on their way.  Both cut the reduction over the rows into
+// ranges where the result has few tiles, until every CU has work, of at least 256 rows each; the ranges' results are added in order.
+// Measured, expanded and direct: bf16 8192 x 4096 x 4096 250 and 474 us (1.10 PFLOP/s), 16384 x 4096 x 1024 184 and 255, 4096 x 1024 x 1024
+// 34 and 32, 1024 x 512 x 512 15 and 14; fp32 (three products each) 746 and 855, 464 and 453, 55 and 44, 24 and 17.  So bf16 expands from
+// 12 GFLOP on and fp32 from 200.
+struct WgradPlan {
+    bool expanded, copy;       // copy: dy goes through the workspace (fp32, or rows that are no multiple of 16 bytes)
+    int tile, splits, ld, ldo, planes;
+    int64_t turn, chunk;       // rows of a turn, of a range
+    int64_t code_bytes, dy_bytes, part_bytes;
+    int64_t bytes() const { return code_bytes + dy_bytes + part_bytes; }
+};
+constexpr int64_t ACT8_TURN_BYTES = 256ll << 20;
+WgradPlan wgrad_plan(int dtype, int64_t rows, int cols, int outs, bool aligned) {
+    WgradPlan p{};
+    p.expanded = 2.0 * rows * cols * outs >= (dtype == MONET_F32 ? 2e11 : 1.2e10);
+    p.tile = p.expanded ? gemm_tile(cols, outs) : 128;
+    p.ld = (int)code_ld(cols);
+    p.planes = dtype == MONET_F32 ? 3 : 1;
+    p.copy = dtype == MONET_F32 || outs % 8 || !aligned;
+    p.ldo = p.copy ? (int)up(outs, 8) : outs;
+    p.turn = rows;
+    if (p.expanded) {
+        const int64_t per_row = 2 * ((int64_t)p.ld + (p.copy ? p.planes * (int64_t)p.ldo : 0));
+        const int64_t turns = (rows * per_row + ACT8_TURN_BYTES - 1) / ACT8_TURN_BYTES;
+        p.turn = up((rows + turns - 1) / turns, 64);
+        const int64_t held = std::min(p.turn, rows);
+        p.code_bytes = up(held * p.ld * 2, 256);
+        p.dy_bytes = p.copy ? up(held * p.ldo * 2 * p.planes, 256) : 0;
+    }
+    const int64_t tiles = ((cols + p.tile - 1) / p.tile) * ((int64_t)(outs + p.tile - 1) / p.tile), first = std::min(p.turn, rows);
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({(p.tile == 256 ? 256 : 512) / tiles, first / 256, 64}));
+    p.chunk = up((first + splits - 1) / splits, 64);
+    p.splits = (int)((first + p.chunk - 1) / p.chunk);
+    p.part_bytes = p.splits > 1 ? up((int64_t)p.splits * cols * outs * 4, 256) : 0;
+    return p;
 }
 
 }  // namespace
@@ -286,12 +370,11 @@ void act8_pack(hipStream_t st, int dtype, const void *x, int64_t ld, void *code,
     const int per_row = (int)(code_ld(cols) / 8);
     const int64_t blocks = (rows * per_row + 255) / 256;
     if (blocks > 0x7fffffff) throw KernelError("act8_pack: too many values");
-    const bool vec = (uintptr_t)x % 16 == 0 && ld * es % 16 == 0;
     uint8_t *exps = (uint8_t *)code + rows * code_ld(cols);
     if (dtype == MONET_F32)
-        hipLaunchKernelGGL((act8_pack_kernel<float>), dim3((unsigned)blocks), dim3(256), 0, st, (const float *)x, ld, (int8_t *)code, exps, rows, (int)cols, per_row, vec);
+        hipLaunchKernelGGL((act8_pack_kernel<float>), dim3((unsigned)blocks), dim3(256), 0, st, (const float *)x, ld, (int8_t *)code, exps, rows, (int)cols, per_row);
     else
-        hipLaunchKernelGGL((act8_pack_kernel<unsigned short>), dim3((unsigned)blocks), dim3(256), 0, st, (const unsigned short *)x, ld, (int8_t *)code, exps, rows, (int)cols, per_row, vec);
+        hipLaunchKernelGGL((act8_pack_kernel<unsigned short>), dim3((unsigned)blocks), dim3(256), 0, st, (const unsigned short *)x, ld, (int8_t *)code, exps, rows, (int)cols, per_row);
     hip_check(hipGetLastError(), "act8 pack launch");
 }
 
@@ -305,12 +388,11 @@ void act8_unpack(hipStream_t st, int dtype, const void *code, void *y, int64_t l
     const int per_row = (int)(code_ld(cols) / 8);
     const int64_t blocks = (rows * per_row + 255) / 256;
     if (blocks > 0x7fffffff) throw KernelError("act8_unpack: too many values");
-    const bool vec = (uintptr_t)y % 16 == 0 && ld * es % 16 == 0;
     const uint8_t *exps = (const uint8_t *)code + rows * code_ld(cols);
     if (dtype == MONET_F32)
-        hipLaunchKernelGGL((act8_unpack_kernel<float>), dim3((unsigned)blocks), dim3(256), 0, st, (const int8_t *)code, exps, (float *)y, ld, rows, (int)cols, per_row, vec);
+        hipLaunchKernelGGL((act8_unpack_kernel<float>), dim3((unsigned)blocks), dim3(256), 0, st, (const int8_t *)code, exps, (float *)y, ld, rows, (int)cols, per_row);
     else
-        hipLaunchKernelGGL((act8_unpack_kernel<unsigned short>), dim3((unsigned)blocks), dim3(256), 0, st, (const int8_t *)code, exps, (unsigned short *)y, ld, rows, (int)cols, per_row, vec);
+        hipLaunchKernelGGL((act8_unpack_kernel<unsigned short>), dim3((unsigned)blocks), dim3(256), 0, st, (const int8_t *)code, exps, (unsigned short *)y, ld, rows, (int)cols, per_row);
     hip_check(hipGetLastError(), "act8 unpack launch");
 }
 
@@ -318,43 +400,68 @@ size_t act8_wgrad_workspace_bytes(int dtype, int64_t rows, int64_t cols, int64_t
     check_type(dtype);
     check_shape(rows, cols);
     check_shape(rows, outs);
-    const WgradPlan p = wgrad_plan(rows, (int)cols, (int)outs);
-    return p.splits > 1 ? (size_t)p.splits * cols * outs * 4 : 0;
+    // rows of dy that begin off a 16-byte boundary are copied: room for that in any case
+    return (size_t)wgrad_plan(dtype, rows, (int)cols, (int)outs, false).bytes();
 }
 
 void act8_wgrad(hipStream_t st, int dtype, const void *code, const void *dy, float *dw, int64_t rows, int64_t cols, int64_t outs, void *ws, size_t ws_bytes) {
     const size_t need = act8_wgrad_workspace_bytes(dtype, rows, cols, outs);
-    const WgradPlan p = wgrad_plan(rows, (int)cols, (int)outs);
     const int es = dtype == MONET_F32 ? 4 : 2;
     check_tensor(code, 16);
     check_tensor(dy, es);
     check_tensor(dw, 4);
     if (need && (!ws || ws_bytes < need)) throw KernelError("act8_wgrad: workspace of " + std::to_string(ws_bytes) + " bytes, " + std::to_string(need) + " needed");
-    if (need) check_tensor(ws, 16);
-    Act8Shape g{};
-    g.code = (const int8_t *)code;
-    g.ld = (int)code_ld(cols);
-    g.exps = (const uint8_t *)code + rows * g.ld;
-    g.dy = dy;
-    g.out = p.splits > 1 ? (float *)ws : dw;
-    g.rows = rows; g.cols = (int)cols; g.outs = (int)outs;
-    g.range = cols * outs;
-    g.chunk = p.chunk;
-    g.tiles_m = (int)((cols + p.tile - 1) / p.tile);
-    g.tiles_n = (int)((outs + p.tile - 1) / p.tile);
-    g.vec = (uintptr_t)dy % 16 == 0 && outs * es % 16 == 0;
-    g.vec_out = (uintptr_t)g.out % 16 == 0 && cols % 4 == 0;
-    if ((int64_t)g.tiles_m * g.tiles_n > 0x7fffffff) throw KernelError("act8_wgrad: result too large");
-    const dim3 grid(g.tiles_m * g.tiles_n, p.splits);
-    if (dtype == MONET_F32) {
-        if (p.tile == 256) hipLaunchKernelGGL((act8_wgrad_kernel<true, 256, 256, 2, 4>), grid, dim3(512), 0, st, g);
-        else hipLaunchKernelGGL((act8_wgrad_kernel<true, 128, 128, 2, 2>), grid, dim3(256), 0, st, g);
+    if (need) check_tensor(ws, 256);
+    const WgradPlan p = wgrad_plan(dtype, rows, (int)cols, (int)outs, (uintptr_t)dy % 16 == 0);
+    float *parts = (float *)ws;
+    char *held = (char *)ws + p.part_bytes;
+    float *out = p.splits > 1 ? parts : dw;
+    const bool vec_out = (uintptr_t)out % 16 == 0 && cols % 4 == 0;
+    const int8_t *codes = (const int8_t *)code;
+    const uint8_t *exps = (const uint8_t *)code + rows * p.ld;
+    if (p.expanded) {
+        unsigned short *x = (unsigned short *)held, *planes = (unsigned short *)(held + p.code_bytes);
+        for (int64_t row = 0; row < rows; row += p.turn) {
+            const int64_t n = std::min(p.turn, rows - row);
+            const int per_row = p.ld / 8;
+            hipLaunchKernelGGL((act8_unpack_kernel<unsigned short>), dim3((unsigned)((n * per_row + 255) / 256)), dim3(256), 0, st, codes + row * p.ld,
+                               exps + row * (p.ld / GROUP), x, (int64_t)p.ld, n, p.ld, per_row);
+            hip_check(hipGetLastError(), "act8 expand launch");
+            const char *src = (const char *)dy + row * outs * es;
+            if (p.copy) {
+                const dim3 grid((unsigned)((n * (p.ldo / 8) + 255) / 256));
+                if (dtype == MONET_F32) hipLaunchKernelGGL((act8_planes_kernel<float>), grid, dim3(256), 0, st, (const float *)src, planes, n, (int)outs, p.ldo);
+                else hipLaunchKernelGGL((act8_planes_kernel<unsigned short>), grid, dim3(256), 0, st, (const unsigned short *)src, planes, n, (int)outs, p.ldo);
+                hip_check(hipGetLastError(), "act8 planes launch");
+            }
+            GemmShape g{};
+            g.a = x; g.lda = p.ld;
+            g.b = p.copy ? planes : (const unsigned short *)src; g.ldb = p.ldo;
+            g.m = (int)cols; g.n = (int)outs; g.k = (int)n;
+            g.chunk = (int)p.chunk; g.splits = (int)((n + p.chunk - 1) / p.chunk);
+            g.planes = p.planes; g.b_plane = n * p.ldo;
+            gemm_bf16<true, true>(st, g, RangeEpilogue{out, cols * outs, row > 0, vec_out}, "act8 weight gradient launch");
+        }
     } else {
-        if (p.tile == 256) hipLaunchKernelGGL((act8_wgrad_kernel<false, 256, 256, 2, 4>), grid, dim3(512), 0, st, g);
+        Act8Shape g{};
+        g.code = codes;
+        g.ld = p.ld;
+        g.exps = exps;
+        g.dy = dy;
+        g.out = out;
+        g.rows = rows; g.cols = (int)cols; g.outs = (int)outs;
+        g.range = cols * outs;
+        g.chunk = p.chunk;
+        g.tiles_m = (int)((cols + 127) / 128);
+        g.tiles_n = (int)((outs + 127) / 128);
+        g.vec_out = vec_out;
+        if ((int64_t)g.tiles_m * g.tiles_n > 0x7fffffff) throw KernelError("act8_wgrad: result too large");
+        const dim3 grid(g.tiles_m * g.tiles_n, p.splits);
+        if (dtype == MONET_F32) hipLaunchKernelGGL((act8_wgrad_kernel<true, 128, 128, 2, 2>), grid, dim3(256), 0, st, g);
         else hipLaunchKernelGGL((act8_wgrad_kernel<false, 128, 128, 2, 2>), grid, dim3(256), 0, st, g);
+        hip_check(hipGetLastError(), "act8 weight gradient launch");
     }
-    hip_check(hipGetLastError(), "act8 weight gradient launch");
-    if (p.splits > 1) split_reduce(st, (const float *)ws, dw, cols * outs, p.splits, false);
+    if (p.splits > 1) split_reduce(st, parts, dw, cols * outs, p.splits, false);
 }
 
 }  // namespace monet

@@ -15,6 +15,8 @@ struct GemmShape {
     int m, n, k;            // a row of a WIDE operand is zero from k to the next multiple of 8, where a DEEP one's rows end is no matter
     int tiles_m, tiles_n;
     int splits, chunk;      // ranges of the reduction (grid y), `chunk` indices each, a multiple of GEMM_DEPTH
+    int planes = 1;         // b is the sum of so many matrices, `b_plane` elements apart (a float's bf16 pieces, bf16_pieces.hpp)
+    int64_t b_plane = 0;
 };
 constexpr int GEMM_DEPTH = 64;      // reduction indices of a step
 
@@ -29,6 +31,7 @@ struct GemmTile {
     const unsigned short *base;
     int64_t ld;
     int rows, k;
+    unsigned whole_bytes;
     __device__ __forceinline__ void init(const unsigned short *p, int64_t ld_, int row0, int rows_all, int k_) {
         ld = ld_; k = k_;
         rows = (min(ROWS, rows_all - row0) + 7) & ~7;
@@ -45,7 +48,14 @@ struct GemmTile {
                 off[i] = row * (unsigned)ld * 2 + c * 16;
             }
         }
-        if (!DEEP) whole = buffer_of(base, (unsigned)((min(ROWS, rows_all - row0) - 1) * ld + ((k + 7) & ~7)) * 2);
+        if (!DEEP) {
+            whole_bytes = (unsigned)((min(ROWS, rows_all - row0) - 1) * ld + ((k + 7) & ~7)) * 2;
+            whole = buffer_of(base, whole_bytes);
+        }
+    }
+    __device__ __forceinline__ void move(int64_t elements) {
+        base += elements;
+        if (!DEEP) whole = buffer_of(base, whole_bytes);
     }
     __device__ __forceinline__ void copy(lds_char *lds, int k0) const {
         const int wave = threadIdx.x / 64;
@@ -141,18 +151,22 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN * 64 / 256) void gemm_bf16_kern
         }
     };
     lds_char *la0 = (lds_char *)a0, *la1 = (lds_char *)a1, *lb0 = (lds_char *)b0, *lb1 = (lds_char *)b1;
-    const int first = blockIdx.y * g.chunk, steps = (last - first + GEMM_DEPTH - 1) / GEMM_DEPTH;
-    ta.copy(la0, first);
-    tb.copy(lb0, first);
-    // two steps a turn; a step behind the last one is copied as zeros
-    for (int step = 0; step < steps; step += 2) {
+    const int first = blockIdx.y * g.chunk, each = (last - first + GEMM_DEPTH - 1) / GEMM_DEPTH, steps = each * g.planes;
+    // the next step's tiles, plane by plane; a step behind the last one is copied as zeros
+    int at = 0, left = g.planes;
+    auto fetch = [&](lds_char *a, lds_char *b) {
+        if (at == each && left > 1) { at = 0; --left; tb.move(g.b_plane); }
+        ta.copy(a, at < each ? first + at * GEMM_DEPTH : last);
+        tb.copy(b, at < each ? first + at * GEMM_DEPTH : last);
+        ++at;
+    };
+    fetch(la0, lb0);
+    for (int step = 0; step < steps; step += 2) {       // two steps a turn
         copies_arrived();
-        ta.copy(la1, first + (step + 1) * GEMM_DEPTH);
-        tb.copy(lb1, first + (step + 1) * GEMM_DEPTH);
+        fetch(la1, lb1);
         work(la0, lb0);
         copies_arrived();
-        ta.copy(la0, first + (step + 2) * GEMM_DEPTH);
-        tb.copy(lb0, first + (step + 2) * GEMM_DEPTH);
+        fetch(la0, lb0);
         work(la1, lb1);
     }
     copies_arrived();

@@ -456,6 +456,28 @@ def test_act8_wgrad_matches_64_bits(case, dtype):
         assert (guard[:4] == -7).all() and (guard[-4:] == -7).all()
 
 
+@pytest.mark.parametrize("dtype,rows,cols,outs", [(monet.BF16, 3000, 1500, 2050), (monet.BF16, 40000, 4090, 128), (monet.F32, 6100, 4100, 4101)])
+def test_act8_wgrad_of_large_layers(dtype, rows, cols, outs):
+    """Sizes that go through the workspace as bf16: all rows at once, in several turns, fp32 in three planes."""
+    torch = torch_mod()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    x = torch.randn(rows, cols, generator=g, device="cuda")
+    dy = torch.randn(rows, outs, generator=g, device="cuda").to(tdtype(dtype))
+    code = torch.zeros(monet.call("monet_act8_bytes", rows, cols), dtype=torch.uint8, device="cuda")
+    monet.call("monet_act8_pack", None, monet.F32, x.data_ptr(), cols, code.data_ptr(), rows, cols)
+    monet.call("monet_act8_unpack", None, monet.F32, code.data_ptr(), x.data_ptr(), cols, rows, cols)
+    need = monet.call("monet_act8_wgrad_workspace_bytes", dtype, rows, cols, outs)
+    assert need < 1 << 30
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    dw = torch.full((outs, cols), float("nan"), device="cuda")
+    monet.call("monet_act8_wgrad", None, dtype, code.data_ptr(), dy.data_ptr(), dw.data_ptr(), rows, cols, outs, ws.data_ptr(), need)
+    want, mag = dy.double().t() @ x.double(), dy.double().abs().t() @ x.double().abs()
+    # sums of exact products: (3 rows + 8) U at worst, a random walk in practice
+    assert ((dw.double() - want).abs() <= 1.1 * (3 * rows + 8) * U * mag).all()
+    assert ((dw.double() - want).norm() / want.norm()).item() < 2e-6
+
+
 def test_act8_wgrad_of_a_marked_group():
     """A group that stands for NaN makes its 32 columns NaN and no others."""
     torch = torch_mod()
