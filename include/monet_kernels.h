@@ -257,7 +257,7 @@ enum monet_dtype { MONET_F32 = 0, MONET_BF16 = 1 };
  * h / (heads / kv_heads).  Row i of a sequence sees its rows 0 .. i:
  *   s = scale * q k^T, lse = log sum exp s, o = exp(s - lse) v.
  * q, o [tokens][heads][head_dim]; k, v [tokens][kv_heads][head_dim]; *_ld: elements from one token to the next (heads lie
- * head_dim apart).  lse [heads][tokens] fp32.  cu_seqlens: device, seqs + 1 ascending offsets; sequence s holds tokens
+ * head_dim apart).  lse [heads][tokens] fp32 (forward: NULL if nobody needs it).  cu_seqlens: device, seqs + 1 ascending offsets; sequence s holds tokens
  * cu_seqlens[s] .. cu_seqlens[s + 1] - 1 and may be empty.  Tokens before the first and behind the last one are neither read
  * nor written, in any output.  Offsets are held to 0 .. tokens, so that others cannot lead out of the tensors.
  * Needs heads % kv_heads == 0, head_dim a multiple of 8 up to 128, scale > 0, pointers and strides that are multiples of
@@ -267,7 +267,7 @@ int monet_attention_fwd(void *stream, int dtype, const void *q, const void *k, c
                         const int32_t *cu_seqlens, int seqs, int64_t tokens, int heads, int kv_heads, int head_dim,
                         int64_t q_ld, int64_t k_ld, int64_t v_ld, int64_t o_ld, float scale);
 /* Its gradients from d(o), the inputs, o and lse: the probabilities are computed again.  dout has o's stride, dq q's, dk k's, dv v's;
- * dk and dv are the sums over a group's heads.  accumulate: bit 0, 1, 2 adds to dq, dk, dv instead of writing them.
+ * dk and dv are the sums over a group's heads.  The three results must not overlap.  accumulate: bit 0, 1, 2 adds to dq, dk, dv instead of writing them.
  * Workspace: monet_attention_bwd_workspace_bytes. */
 int monet_attention_bwd(void *stream, int dtype, const void *dout, const void *q, const void *k, const void *v, const void *o,
                         const float *lse, void *dq, void *dk, void *dv, const int32_t *cu_seqlens, int seqs, int64_t tokens,

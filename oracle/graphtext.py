@@ -42,7 +42,7 @@ class ONode:
 
     @property
     def is_aux(self):
-        return self.op in ("mask", "poolidx")
+        return self.op in ("mask", "poolidx", "lse", "act8")
 
     @property
     def persist(self):
@@ -121,7 +121,7 @@ class OGraph:
         cnt = 1
         for d in n.shape:
             cnt *= d
-        size = {"mask": 8, "poolidx": 1}.get(n.op, 4)
+        size = {"mask": 8, "poolidx": 1, "act8": 1}.get(n.op, 4)
         return align(cnt * size)
 
     def shape_of(self, ref):

@@ -62,6 +62,15 @@ def forward_op(g: OGraph, n, get, params, stats, recompute=False):
         y = nm.avgpool_fwd(x)
     elif n.op == "linear":
         y = nm.linear_fwd(x, params[n.pars[0]], params[n.pars[1]])
+        aux["act8"] = lambda: nm.act8_pack(x)
+    elif n.op == "attention":
+        q, k, v, cu = _attention_operands(n, get)
+        o, lse = nm.attention_fwd(q, k, v, cu, float(a["scale"]))
+        y = o.reshape(x.shape)
+        aux["lse"] = lambda: lse
+    elif n.op == "linearce":
+        loss, stats[n.id] = nm.linear_ce_fwd(x, params[n.pars[0]], get(n.ins[1]))
+        y = np.array([loss])
     elif n.op == "softmaxce":
         y = np.array([nm.softmaxce_fwd(x, get(n.ins[1]))])
     elif n.op == "sumloss":
@@ -69,6 +78,12 @@ def forward_op(g: OGraph, n, get, params, stats, recompute=False):
     else:
         raise ValueError(n.op)
     return y, aux
+
+
+def _attention_operands(n, get):
+    """q, k, v as [tokens, heads, dim] and the sequences' offsets."""
+    dim = int(n.attrs["dim"])
+    return tuple(get(r).reshape(get(r).shape[0], -1, dim) for r in n.ins[:3]) + (get(n.ins[3]),)
 
 
 def backward_op(g: OGraph, bop, algo, gy, get, params, stats):
@@ -133,10 +148,21 @@ def backward_op(g: OGraph, bop, algo, gy, get, params, stats):
     if kind == "avgpool_bwd":
         return {0: nm.avgpool_bwd(gy, nchw_shape(g.shape_of(n.ins[0])))}, {}
     if kind == "linear_wgrad":
-        dw, db = nm.linear_wgrad(get(n.ins[0]), gy)
+        if algo == "from_code":
+            x = nm.act8_unpack(*get(g.aux_children[n.id][0]), g.shape_of(n.ins[0])[1])
+        else:
+            x = get(n.ins[0])
+        dw, db = nm.linear_wgrad(x, gy)
         return {}, {n.pars[0]: dw, n.pars[1]: db}
     if kind == "linear_dgrad":
         return {0: nm.linear_dgrad(gy, params[n.pars[0]], nchw_shape(g.shape_of(n.ins[0])))}, {}
+    if kind == "attention_bwd":
+        q, k, v, cu = _attention_operands(n, get)
+        grads = nm.attention_bwd(gy.reshape(q.shape), q, k, v, cu, float(a["scale"]))
+        return {p: d.reshape(d.shape[0], -1) for p, d in enumerate(grads)}, {}
+    if kind == "linearce_bwd":
+        dx, dw = nm.linear_ce_bwd(get(n.ins[0]), params[n.pars[0]], get(n.ins[1]))
+        return {0: dx}, {n.pars[0]: dw}
     if kind == "softmaxce_bwd":
         return {0: nm.softmaxce_bwd(get(n.ins[0]), get(n.ins[1]))}, {}
     if kind == "sumloss_bwd":

@@ -14,6 +14,11 @@ using namespace monet;
 
 static thread_local std::string g_err;
 
+namespace monet {
+void linear_bias_add(hipStream_t st, float *y, const float *b, int N, int out);
+void linear_bias_grad(hipStream_t st, const float *dy, float *db, int N, int out);
+}
+
 struct monet_plan;
 namespace {
 void build_programs(monet_plan *p);
@@ -162,6 +167,7 @@ struct StepCtx {
     }
     float *scratch() const { return (float *)(mp->base + mp->plan.scratch_off); }
     size_t scratch_bytes() const { return (size_t)mp->plan.scratch_bytes; }
+    float *ce_lse(int node) const { return (float *)(mp->base + mp->plan.ce_lse_off.at(node)); }
     float *bn_stats(int node) const { return (float *)(mp->base + mp->plan.bn_stats_off.at(node)); }
     size_t index_of(const Launch &L) const { return (size_t)(&L - mp->plan.launches.data()); }
     bool feeds_stats(const Launch &L) const { return mp->feeds_stats[index_of(L)] != 0; }
@@ -199,6 +205,10 @@ ConvShape linear_shape(const Graph &g, const Node &n) {   // a linear layer is a
     cs.N = (int)is[0]; cs.H = 1; cs.W = 1; cs.C = (int)(numel_of(is) / is[0]);
     cs.K = (int)n.shape[1]; cs.R = 1; cs.S = 1; cs.stride = 1; cs.pad = 0; cs.P = 1; cs.Q = 1;
     return cs;
+}
+struct AttentionNode { int seqs; int64_t tokens; int heads, kv_heads, dim; float scale; };
+AttentionNode attention_node(const Graph &, const Node &n) {
+    return {n.attr_int("seqs"), n.shape[0], n.attr_int("heads"), n.attr_int("kv_heads"), n.attr_int("dim"), (float)n.attr_f("scale", 1.0)};
 }
 PoolShape pool_shape(const Graph &g, const Node &n) {
     const auto &is = g.shape_of(n.ins[0]);
@@ -276,6 +286,16 @@ void run_forward(const StepCtx &c, const Launch &L, const BnAffine *affine = nul
         const auto &is = g.shape_of(n.ins[0]);
         linear_fwd(c.st, in0, c.weights[n.pars[0]], c.weights[n.pars[1]], out, (int)is[0], (int)(numel_of(is) / is[0]), (int)n.shape[1],
                    c.scratch(), c.scratch_bytes());
+        if (L.flags & 2) act8_pack(c.st, MONET_F32, in0, is[1], c.ptr(L.a[3]), is[0], is[1]);      // the input in 8 bits for the weight gradient
+    } else if (op == "attention") {
+        const AttentionNode a = attention_node(g, n);
+        attention_fwd(c.st, MONET_F32, in0, c.ptr(L.in[1]), c.ptr(L.in[2]), out, (L.flags & 2) ? (float *)c.ptr(L.a[3]) : nullptr,
+                      (const int32_t *)c.ptr(L.in[3]), a.seqs, a.tokens, a.heads, a.kv_heads, a.dim, a.heads * a.dim, a.kv_heads * a.dim,
+                      a.kv_heads * a.dim, a.heads * a.dim, a.scale);
+    } else if (op == "linearce") {
+        const auto &is = g.shape_of(n.ins[0]);
+        linear_ce_fwd(c.st, MONET_F32, in0, c.weights[n.pars[0]], (const int32_t *)c.ptr(L.in[1]), out, c.ce_lse(L.id), is[0], (int)is[1],
+                      (int)g.params[n.pars[0]].shape[0], c.ptr(L.a[4]), (size_t)align_up(n.fimpls[L.impl].ws));
     } else if (op == "softmaxce") {
         const auto &is = g.shape_of(n.ins[0]);
         const int classes = (int)is.back();
@@ -356,7 +376,23 @@ void run_backward(const StepCtx &c, const Launch &L) {
         avgpool_bwd(c.st, gy, d0, (int)is[0], (int)(is[1] * is[2]), (int)is[3], acc0);
     } else if (kd == "linear_wgrad") {
         const auto &is = g.shape_of(n.ins[0]);
-        linear_wgrad(c.st, (const float *)dep, gy, c.grads[n.pars[0]], c.grads[n.pars[1]], (int)is[0], (int)(numel_of(is) / is[0]), (int)n.shape[1]);
+        if (im.algo == "from_code") {
+            act8_wgrad(c.st, MONET_F32, dep, gy, c.grads[n.pars[0]], is[0], is[1], n.shape[1], c.ptr(L.a[4]), (size_t)(im.ws > 0 ? align_up(im.ws) : 0));
+            linear_bias_grad(c.st, gy, c.grads[n.pars[1]], (int)is[0], (int)n.shape[1]);
+        } else
+            linear_wgrad(c.st, (const float *)dep, gy, c.grads[n.pars[0]], c.grads[n.pars[1]], (int)is[0], (int)(numel_of(is) / is[0]), (int)n.shape[1]);
+    } else if (kd == "attention_bwd") {
+        const AttentionNode a = attention_node(g, n);
+        Ref cu; cu.region = R_EXT; cu.off = -n.ins[3];
+        attention_bwd(c.st, MONET_F32, gy, c.ptr(L.dep[0]), c.ptr(L.dep[1]), c.ptr(L.dep[2]), c.ptr(L.dep[3]), (const float *)c.ptr(L.dep[4]),
+                      c.ptr(L.grad[0]), c.ptr(L.grad[1]), c.ptr(L.grad[2]), (const int32_t *)c.ptr(cu), a.seqs, a.tokens, a.heads, a.kv_heads, a.dim,
+                      a.heads * a.dim, a.kv_heads * a.dim, a.kv_heads * a.dim, a.heads * a.dim, a.scale, (int)(L.flags & 7), c.ptr(L.a[4]),
+                      (size_t)align_up(im.ws));
+    } else if (kd == "linearce_bwd") {
+        const auto &is = g.shape_of(n.ins[0]);
+        Ref lab; lab.region = R_EXT; lab.off = -n.ins[1];
+        linear_ce_bwd(c.st, MONET_F32, dep, c.weights[n.pars[0]], (const int32_t *)c.ptr(lab), c.ce_lse(b.node), d0, c.grads[n.pars[0]], is[0],
+                      (int)is[1], (int)g.params[n.pars[0]].shape[0], acc0, c.ptr(L.a[4]), (size_t)align_up(im.ws));
     } else if (kd == "linear_dgrad") {
         const auto &is = g.shape_of(n.ins[0]);
         linear_dgrad(c.st, gy, c.weights[n.pars[0]], d0, (int)is[0], (int)(numel_of(is) / is[0]), (int)n.shape[1], acc0, c.scratch(),
@@ -773,6 +809,12 @@ static double issued_conv_flops(const ConvShape &cs, const std::string &algo) {
     return 2.0 * (m + 2) * (m + 2) * tiles * cs.K * cs.C;
 }
 
+// two products over the causal pairs; the offsets live in device memory, so sequences count as equally long
+static double attention_flops(const Node &n) {
+    const double tokens = n.shape[0], len = tokens / n.attr_int("seqs", 1);
+    return 4.0 * n.shape[1] * tokens * (len + 1) / 2;
+}
+
 extern "C" int monet_plan_launch_info(const monet_plan *p, size_t index, monet_launch_info *out) {
     if (!p || !out || index >= current_program(p).size()) { g_err = "monet_plan_launch_info: bad argument"; return MONET_BAD_ARGUMENT; }
     const Graph &g = p->plan.g;
@@ -861,7 +903,19 @@ extern "C" int monet_plan_launch_info(const monet_plan *p, size_t index, monet_l
         }
         else if (b.kind == "tconv_wgrad") conv_cost(tconv_adjoint_shape(g, n), "tconv_wgrad");
         else if (b.kind == "tconv_dgrad") conv_cost(tconv_adjoint_shape(g, n), "tconv_dgrad");
-        else if (b.kind == "linear_wgrad") conv_cost(linear_shape(g, n), "linear_wgrad");
+        else if (b.kind == "linear_wgrad") {
+            conv_cost(linear_shape(g, n), b.impls[L.impl].algo == "from_code" ? "linear_wgrad_act8" : "linear_wgrad");
+            if (b.impls[L.impl].algo == "from_code") bytes -= 4.0 * numel_of(g.shape_of(n.ins[0])) - g.nodes[n.aux_children[0]].bytes;
+        } else if (b.kind == "attention_bwd") {
+            flops = 2.5 * attention_flops(n);
+            issued = 3.5 * attention_flops(n);
+            bytes = 2.0 * e + 4.0 * e + 4.0 * (numel_of(g.shape_of(n.ins[1])) + numel_of(g.shape_of(n.ins[2])));
+        } else if (b.kind == "linearce_bwd") {
+            const double rows = g.shape_of(n.ins[0])[0], w = numel_of(g.params[n.pars[0]].shape);
+            flops = 4.0 * rows * w;
+            issued = 6.0 * rows * w;
+            bytes = 8.0 * (numel_of(g.shape_of(n.ins[0])) + w);
+        }
         else if (b.kind == "linear_dgrad") conv_cost(linear_shape(g, n), "linear_dgrad");
         else if (b.kind == "bn_bwd") bytes = 5 * e;                      // reduce pass reads dy,t; apply pass reads dy,t, writes dx
         else if (b.kind == "relu_bwd" || b.kind == "relu6_bwd")
@@ -884,7 +938,17 @@ extern "C" int monet_plan_launch_info(const monet_plan *p, size_t index, monet_l
             issued = issued_conv_flops(conv_shape(g, n), n.fimpls[L.impl].algo);
         } else if (n.op == "tconv") conv_cost(tconv_adjoint_shape(g, n), "tconv_fwd");
         else if (n.op == "concat") bytes = 2 * e;
-        else if (n.op == "linear") conv_cost(linear_shape(g, n), "linear_fwd");
+        else if (n.op == "linear") {
+            conv_cost(linear_shape(g, n), "linear_fwd");
+            if (L.flags & 2) bytes += 4.0 * numel_of(g.shape_of(n.ins[0])) + g.nodes[n.aux_children[0]].bytes;
+        } else if (n.op == "attention") {
+            flops = attention_flops(n);
+            bytes = 2.0 * e + 4.0 * (numel_of(g.shape_of(n.ins[1])) + numel_of(g.shape_of(n.ins[2])));
+        } else if (n.op == "linearce") {
+            const double rows = g.shape_of(n.ins[0])[0], w = numel_of(g.params[n.pars[0]].shape);
+            flops = 2.0 * rows * w;
+            bytes = 4.0 * (numel_of(g.shape_of(n.ins[0])) + w);
+        }
         else if (n.op == "bn") {
             if (L.kind == EV_RUN_FWD) bytes = (p->stats_fed[ps.a] ? 2 : 3) * e;   // statistics pass (unless fed by the convolution) + apply pass
             else { bytes = 2 * e; label = "bn_apply"; }                  // recomputation reuses the statistics
@@ -921,9 +985,6 @@ extern "C" int monet_plan_read_timing(monet_plan *p, float *ms, size_t n) {
 
 // ------------------------------------------------------------------ linear layer = 1x1 convolution + bias
 namespace monet {
-
-void linear_bias_add(hipStream_t st, float *y, const float *b, int N, int out);
-void linear_bias_grad(hipStream_t st, const float *dy, float *db, int N, int out);
 
 // A batch of a few hundred rows gives a handful of output tiles: the reduction is cut into ranges (partial
 // results in the caller's scratch, added in range order) until about a thousand workgroups exist.

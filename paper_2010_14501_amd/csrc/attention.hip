@@ -377,7 +377,7 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS ? 2 : 1)) vo
         factor = __builtin_amdgcn_exp2f(mine - top);
     }
     auto area = [&](int w) { return w == 0 ? lk0 : w == 1 ? lk1 : w == 2 ? lv0 : lv1; };
-    if (part == 0 && l < 32 && row < len) lse[(int64_t)head * a.tokens + start + row] = (top + __builtin_amdgcn_logf(sum)) * LN2;
+    if (lse && part == 0 && l < 32 && row < len) lse[(int64_t)head * a.tokens + start + row] = (top + __builtin_amdgcn_logf(sum)) * LN2;
     join_and_store<T, D, PARTS>(area, acc, factor, o + (int64_t)(start + row) * a.o_ld + (int64_t)head * a.head_dim, row < len, 1.f / sum, a.head_dim, false);
 }
 
@@ -714,7 +714,6 @@ void attention_fwd(hipStream_t st, int dtype, const void *q, const void *k, cons
     const AttShape a = att_shape(dtype, cu, seqs, tokens, heads, kv_heads, head_dim, q_ld, k_ld, v_ld, o_ld, scale);
     if (!tokens) return;
     check_tensors({q, k, v, o});
-    if (!lse) throw KernelError("attention: null pointer");
     if (dtype == MONET_BF16) (head_dim <= 64 ? fwd_form<unsigned short, 64> : fwd_form<unsigned short, 128>)(st, a, q, k, v, o, lse);
     else (head_dim <= 64 ? fwd_form<float, 64> : fwd_form<float, 128>)(st, a, q, k, v, o, lse);
 }

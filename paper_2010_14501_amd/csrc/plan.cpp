@@ -110,9 +110,9 @@ void Graph::parse(const std::string &text) {
                 n.pars = parse_refs(take(a, "par"));
                 n.shape = parse_dims(take(a, "shape"));
                 n.attrs = a;
-                n.aux = (n.op == "mask" || n.op == "poolidx");
+                n.aux = (n.op == "mask" || n.op == "poolidx" || n.op == "lse" || n.op == "act8");
                 n.persist = n.attr_int("persist") == 1;
-                int64_t esz = n.op == "mask" ? 8 : (n.op == "poolidx" ? 1 : 4);
+                int64_t esz = n.op == "mask" ? 8 : (n.op == "poolidx" || n.op == "act8" ? 1 : 4);
                 n.bytes = n.persist ? 0 : align_up(numel(n.shape) * esz);
                 for (int j : n.ins)
                     if (j >= n.id || -j >= (int)exts.size())
@@ -261,7 +261,15 @@ static void check_declared_deps(const Graph &g) {
             else if (b.kind == "dwconv_wgrad") { known = algo == "direct"; input0(); }
             else if (b.kind == "dwconv_dgrad") { known = algo == "direct"; }
             else if (b.kind == "concat_bwd") { known = algo == "copy"; }
-            else if (b.kind == "linear_wgrad") { known = algo == "gemm"; input0(); }
+            else if (b.kind == "linear_wgrad") {
+                if (algo == "gemm") input0(); else if (algo == "from_code") aux0(); else known = false;
+            }
+            else if (b.kind == "attention_bwd") {
+                known = algo == "fused";
+                want = {n.ins[0], n.ins[1], n.ins[2], n.id};
+                aux0();
+            }
+            else if (b.kind == "linearce_bwd") { known = algo == "pieces"; input0(); }
             else if (b.kind == "linear_dgrad") { known = algo == "gemm"; }
             else if (b.kind == "bn_bwd") {
                 if (algo == "from_input") input0(); else if (algo == "from_output") want.push_back(n.id); else known = false;
@@ -279,6 +287,39 @@ static void check_declared_deps(const Graph &g) {
             if (node_deps(g, k, (int)l) != want)
                 throw PlanError(MONET_BAD_GRAPH, "backward operator " + std::to_string(k) + " (" + algo + "): declared dependencies differ from what the kernel reads");
         }
+    }
+}
+
+// Shapes that the kernels of a transformer's operators take from the graph text.
+static void check_transformer_nodes(const Graph &g) {
+    for (const Node &n : g.nodes) {
+        auto need = [&](bool ok, const char *what) {
+            if (!ok) throw PlanError(MONET_BAD_GRAPH, "node " + std::to_string(n.id) + " (" + n.op + "): " + what);
+        };
+        const Node *aux = n.aux_children.empty() ? nullptr : &g.nodes[n.aux_children[0]];
+        auto offsets = [&](int ref, int64_t count) {
+            return ref <= 0 && g.exts[-ref].dtype == "i32" && numel(g.exts[-ref].shape) == count;
+        };
+        if (n.op == "attention") {
+            const int64_t heads = n.attr_int("heads"), kv = n.attr_int("kv_heads"), dim = n.attr_int("dim"), seqs = n.attr_int("seqs");
+            need(heads > 0 && kv > 0 && heads % kv == 0 && dim > 0 && seqs > 0, "heads, kv_heads, dim and seqs must be positive, heads a multiple of kv_heads");
+            need(n.ins.size() == 4 && n.ins[0] > 0 && n.ins[1] > 0 && n.ins[2] > 0, "inputs are three nodes and the sequences' offsets");
+            need(n.ins[0] != n.ins[1] && n.ins[0] != n.ins[2] && n.ins[1] != n.ins[2], "queries, keys and values must be three tensors");
+            need(n.shape.size() == 2 && n.shape[1] == heads * dim && g.shape_of(n.ins[0]) == n.shape, "queries and output must be tokens x (heads * dim)");
+            const std::vector<int64_t> kv_shape{n.shape[0], kv * dim};
+            need(g.shape_of(n.ins[1]) == kv_shape && g.shape_of(n.ins[2]) == kv_shape, "keys and values must be tokens x (kv_heads * dim)");
+            need(offsets(n.ins[3], seqs + 1), "offsets must be an external i32 tensor of seqs + 1 values");
+            need(aux && aux->op == "lse" && numel(aux->shape) == heads * n.shape[0], "needs an intermediate lse of heads x tokens");
+        } else if (n.op == "linearce") {
+            need(n.persist && n.ins.size() == 2 && n.ins[0] > 0 && n.pars.size() == 1, "is a persistent node with an input, labels and a parameter");
+            const auto &x = g.shape_of(n.ins[0]), &w = g.params[n.pars[0]].shape;
+            need(x.size() == 2 && w.size() == 2 && x[1] == w[1], "input rows x width and parameter vocab x width do not fit");
+            need(offsets(n.ins[1], x[0]), "labels must be an external i32 tensor of one value per row");
+        } else if (n.op == "linear" && aux) {
+            const auto &x = g.shape_of(n.ins[0]);
+            need(aux->op == "act8" && x.size() == 2 && numel(aux->shape) == x[0] * ((x[1] + 31) / 32) * 33, "the 8-bit copy of an input rows x cols has rows * ceil(cols / 32) * 33 bytes");
+        } else if (aux && (aux->op == "lse" || aux->op == "act8"))
+            need(false, "does not write such an intermediate");
     }
 }
 
@@ -517,7 +558,10 @@ void Plan::lower() {
         L.kind = kind; L.id = i; L.impl = l;
         L.flags = (im.inplace ? 1u : 0u) | (emit.empty() ? 0u : 2u);
         begin_launch(chainable(L));
-        for (size_t p = 0; p < n.ins.size() && p < 2; ++p) L.a[p] = fwd_ref(n.ins[p], who);
+        for (size_t p = 0; p < n.ins.size() && p < 4; ++p) {
+            L.in[p] = fwd_ref(n.ins[p], who);
+            if (p < 2) L.a[p] = L.in[p];
+        }
         if (n.persist) { L.a[2].region = R_PERSIST; L.a[2].off = loss_off; }
         else if (im.inplace) L.a[2] = L.a[0];
         else {
@@ -614,7 +658,10 @@ void Plan::lower() {
             if (gi == grads.end()) throw PlanError(MONET_BAD_GRAPH, who + " has no incoming gradient");
             L.a[0].region = R_ARENA; L.a[0].off = gi->second.first;
         }
-        for (int d : D) fwd_ref(d, who);
+        for (size_t i = 0; i < D.size(); ++i) {
+            const Ref r = fwd_ref(D[i], who);
+            if (i < 5) L.dep[i] = r;
+        }
         if (!D.empty()) L.a[1] = fwd_ref(D[0], who);
         else if (b.kind.size() > 6 && b.kind.compare(b.kind.size() - 6, 6, "_wgrad") == 0) L.a[1] = fwd_ref(n.ins[0], who);
         uint32_t acc = 0;
@@ -627,7 +674,11 @@ void Plan::lower() {
                 grads[j] = {off, g.nodes[j].bytes};
                 gj = grads.find(j);
             }
-            if (p < 2) { L.a[2 + p].region = R_ARENA; L.a[2 + p].off = gj->second.first; }
+            Ref r;
+            r.region = R_ARENA;
+            r.off = gj->second.first;
+            if (p < 2) L.a[2 + p] = r;
+            if (p < 3) L.grad[p] = r;
         }
         L.flags = acc;
         int64_t wsb = im.ws > 0 ? align_up(im.ws) : 0, wso = 0;
@@ -746,16 +797,20 @@ void Plan::closed_form() {
 
 void Plan::build(const std::string &graph_text, const std::string &schedule_text) {
     g.parse(graph_text);
+    check_transformer_nodes(g);
     check_declared_deps(g);
     sch.parse(schedule_text, g);
     validate();
-    // constant region: loss scalar, BatchNorm statistics, reduction scratch
+    // constant region: loss scalar, BatchNorm statistics, a vocabulary loss's lse, reduction scratch
     int64_t off = 0;
     loss_off = off; off += kAlign;
     for (int i = 1; i <= g.N(); ++i)
         if (g.nodes[i].op == "bn") {
             bn_stats_off[i] = off;
             off += align_up(2 * g.nodes[i].shape.back() * 4);
+        } else if (g.nodes[i].op == "linearce") {
+            ce_lse_off[i] = off;
+            off += align_up(g.shape_of(g.nodes[i].ins[0])[0] * 4);
         }
     scratch_off = off;
     // holds the partial results of the two-level reductions; the largest user is BatchNorm's forward statistics

@@ -103,6 +103,8 @@ struct Launch {
     // backward: a[0] incoming gradient; a[1] forward dependency; a[2], a[3] gradient outputs
     //           for input 0 / 1; a[4] workspace
     Ref a[5];
+    Ref in[4];             // forward: every input (a[0], a[1] are the first two)
+    Ref dep[5], grad[3];   // backward: every dependency (a[1] is the first), the gradient of every input (a[2], a[3] the first two)
 };
 
 struct PoisonFill {
@@ -122,6 +124,7 @@ struct Plan {
     // (event index, node, is_grad) -> offset, for tests that read tensors back
     std::vector<std::map<std::pair<int, int>, int64_t>> where;   // per launch: live tensor offsets
     std::map<int, int64_t> bn_stats_off;   // node -> offset in the persistent region
+    std::map<int, int64_t> ce_lse_off;     // the same for the lse of a vocabulary loss's rows
     int64_t loss_off = 0;
     int64_t scratch_off = 0, scratch_bytes = 0;
     int64_t persistent_bytes = 0;

@@ -116,7 +116,7 @@ def test_attention_refuses(change, match):
     a.update(change)
     shape = ["cu", "seqs", "tokens", "heads", "kv_heads", "head_dim", "q_ld", "k_ld", "v_ld", "o_ld", "scale"]
     refused("monet_attention_bwd", [None] + [a[n] for n in ["dtype", "go", "q", "k", "v", "o", "lse", "dq", "dk", "dv"] + shape + ["accumulate", "ws", "ws_bytes"]], match)
-    if not set(change) & {"accumulate", "ws", "ws_bytes", "go", "dv"}:
+    if not set(change) & {"accumulate", "ws", "ws_bytes", "go", "dv", "lse"}:      # the forward pass takes lse = NULL
         refused("monet_attention_fwd", [None] + [a[n] for n in ["dtype", "q", "k", "v", "o", "lse"] + shape], match)
 
 

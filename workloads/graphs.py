@@ -54,7 +54,7 @@ class Node:
 
 
 class Graph:
-    AUX_OPS = ("mask", "poolidx")
+    AUX_OPS = ("mask", "poolidx", "lse", "act8")
 
     def __init__(self):
         self.exts = []      # (ref, name, dtype, shape)
@@ -63,6 +63,7 @@ class Graph:
         self.fimpls = {}    # node id -> [dict]
         self.bops = []      # dict(k, kind, node)
         self.bimpls = {}    # k -> [dict]
+        self.ext_values = {}  # ref -> values of an external tensor that are part of the workload (sequence offsets)
         self.blocks = []    # [(name, [node ids])]  (builder-side grouping for schedule helpers)
         self._cur_block = None
 
@@ -316,8 +317,10 @@ class Graph:
                            [("dwconv_wgrad", [dict(algo="direct", deps=[x] if x > 0 else [], ws=0, cost=(bi + bo) * c)])])
         return i
 
-    def linear(self, x, out, name="fc"):
-        """Fully connected layer over the flattened input; a 4-D input N,H,W,C gets weights out,H,W,C."""
+    def linear(self, x, out, name="fc", code=False):
+        """Fully connected layer over the flattened input; a 4-D input N,H,W,C gets weights out,H,W,C.
+        `code` (2-D inputs computed by a node; the caller holds its own anyway): the layer offers an intermediate node, its input in 8 bits, and a weight gradient from it:
+        held from the forward pass, it takes a quarter of what the input takes."""
         shp = self.shape_of(x)
         N, I = shp[0], numel(shp[1:])
         w = self.param(name + ".w", (out,) + tuple(shp[1:]))
@@ -325,8 +328,40 @@ class Graph:
         i = self._add("linear", [x], [w, b], (N, out))
         flop = 2.0 * N * I * out
         self.fimpls[i] = [dict(algo="gemm", ws=0, cost=flop)]
+        wg = [dict(algo="gemm", deps=[x] if x > 0 else [], ws=0, cost=flop)]
+        if code and x > 0:
+            assert len(shp) == 2
+            c = self._add("act8", [i], [], (N * -(-I // 32) * 33,))
+            wg.append(dict(algo="from_code", deps=[c], ws=_library_bytes("monet_act8_wgrad_workspace_bytes", 0, N, I, out), cost=flop * 0.5))
         self._pending_bops(i, [("linear_dgrad", [dict(algo="gemm", deps=[], ws=0, cost=flop)])] if x > 0 else [],
-                           [("linear_wgrad", [dict(algo="gemm", deps=[x] if x > 0 else [], ws=0, cost=flop)])])
+                           [("linear_wgrad", wg)])
+        return i
+
+    def attention(self, q, k, v, cu, heads, kv_heads, scale=None):
+        """Causal attention over packed sequences: q [tokens, heads * dim], k and v [tokens, kv_heads * dim], cu an external
+        i32 tensor with the sequences' offsets.  The forward pass leaves lse [heads, tokens] as an intermediate node, from which
+        the backward pass computes the probabilities again."""
+        tokens, width = self.shape_of(q)
+        dim, seqs = width // heads, self.shape_of(cu)[0] - 1
+        i = self._add("attention", [q, k, v, cu], [], (tokens, width), heads=heads, kv_heads=kv_heads, dim=dim, seqs=seqs,
+                      scale=float(dim ** -0.5 if scale is None else scale))
+        lse = self._add("lse", [i], [], (heads, tokens))
+        flop = 4.0 * width * tokens * (tokens / seqs + 1) / 2
+        self.fimpls[i] = [dict(algo="fused", ws=0, cost=flop)]
+        ws = _library_bytes("monet_attention_bwd_workspace_bytes", 0, seqs, tokens, heads, kv_heads, dim)
+        self._pending_bops(i, [("attention_bwd", [dict(algo="fused", deps=[q, k, v, i, lse], ws=ws, cost=3.5 * flop)])])
+        return i
+
+    def linearce(self, x, labels, vocab, name="head"):
+        """Loss: softmax cross entropy of a linear layer without bias over `vocab` classes, in pieces of them; rows whose label is
+        outside the vocabulary carry none.  The logits are never held."""
+        rows, width = self.shape_of(x)
+        w = self.param(name + ".w", (vocab, width))
+        i = self._add("linearce", [x, labels], [w], (1,), persist=1)
+        flop = 2.0 * rows * width * vocab
+        self.fimpls[i] = [dict(algo="pieces", ws=_library_bytes("monet_linear_ce_workspace_bytes", 0, 0, rows, width, vocab), cost=flop)]
+        ws = _library_bytes("monet_linear_ce_workspace_bytes", 1, 0, rows, width, vocab)
+        self._pending_bops(i, [("linearce_bwd", [dict(algo="pieces", deps=[x], ws=ws, cost=3 * flop)])])
         return i
 
     def softmaxce(self, x, labels):
@@ -409,6 +444,12 @@ class Graph:
                         rec += f" {kk}={v}"
                 out.append(rec)
         return "\n".join(out) + "\n"
+
+
+def _library_bytes(name, *args):
+    """A workspace as the kernel library asks for it."""
+    from paper_2010_14501_amd import monet
+    return _align(monet.call(name, *args))
 
 
 def conv_split_plan(rows, cols, reduction, classes=1, out_elems=None):
@@ -698,4 +739,31 @@ def googlenet(batch=320, hw=224, classes=1000, stem=(64, 64, 192), inceptions=GO
     f = g.linear(p, classes, name="fc")
     g.softmaxce(f, labels)
     g.end_block()
+    return g
+
+
+def transformer(lens=(40, 1, 23), width=64, heads=4, kv_heads=2, hidden=128, layers=2, vocab=300, code=True):
+    """Decoder-shaped network over packed sequences of the given lengths: per layer attention between linear layers and two linear layers
+    around a ReLU, each behind a residual add, and the vocabulary loss.  The input is the embedded tokens; no normalisation.  With `code`
+    every linear layer offers its input in 8 bits."""
+    g = Graph()
+    tokens, dim = sum(lens), width // heads
+    x = g.ext("embedded", "f32", (tokens, width))
+    labels = g.ext("labels", "i32", (tokens,))
+    cu = g.ext("cu_seqlens", "i32", (len(lens) + 1,))
+    g.ext_values[cu] = [sum(lens[:i]) for i in range(len(lens) + 1)]
+    for layer in range(layers):
+        g.begin_block(f"layer{layer}")
+        name = f"l{layer}."
+        if layer == 0:
+            x = g.linear(x, width, name="in", code=code)
+        q = g.linear(x, heads * dim, name=name + "q", code=code)
+        k = g.linear(x, kv_heads * dim, name=name + "k", code=code)
+        v = g.linear(x, kv_heads * dim, name=name + "v", code=code)
+        o = g.linear(g.attention(q, k, v, cu, heads, kv_heads), width, name=name + "o", code=code)
+        x = g.add(x, o)
+        h = g.linear(g.relu(g.linear(x, hidden, name=name + "up", code=code)), width, name=name + "down", code=code)
+        x = g.add(x, h)
+        g.end_block()
+    g.linearce(x, labels, vocab)
     return g

@@ -46,7 +46,7 @@ def node_bytes(g: Graph, i):
     count = 1
     for d in n.shape:
         count *= d
-    return _align({"mask": 8, "poolidx": 1}.get(n.op, 4) * count)
+    return _align({"mask": 8, "poolidx": 1, "act8": 1}.get(n.op, 4) * count)
 
 
 class _Vars:

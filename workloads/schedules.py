@@ -42,6 +42,8 @@ WINOGRAD2_VARIANTS = dict(DEFAULT_VARIANTS, conv_wgrad=("winograd", "splitk"), c
                           conv_fwd=("winograd", "igemm_splitk"))
 # every convolution with a filter larger than 1x1 through the explicit patch matrix (forward and filter gradient)
 IM2COL_VARIANTS = dict(DEFAULT_VARIANTS, conv_wgrad=("im2col", "splitk"), conv_fwd=("im2col", "igemm_splitk"))
+# a transformer's linear layers from their inputs in 8 bits
+CODE_VARIANTS = dict(DEFAULT_VARIANTS, linear_wgrad="from_code")
 STANDARD_VARIANTS = dict(
     bn_bwd="from_input", relu_bwd="from_output", relu6_bwd="from_output", maxpool_bwd="from_input",
     conv_wgrad=("winograd4", "winograd", "splitk"), tconv_wgrad="splitk", conv_dgrad=("winograd4f", "winograd4", "winograd", "igemm_splitk"),
@@ -367,3 +369,21 @@ def googlenet_alternate_schedule(g: Graph, variants=None):
     the others are recomputed from the kept block outputs around them."""
     keep = {b for b in range(len(g.blocks)) if b % 2 == 0} | {len(g.blocks) - 1}
     return block_checkpoint_schedule(g, keep, variants)
+
+
+def code_set(g: Graph):
+    """What a transformer holds when every linear layer's weight gradient reads its input in 8 bits: the 8-bit inputs, sign masks,
+    block outputs, and attention's output and row statistics.  Queries, keys and values are computed again from the block's input."""
+    F = block_output_set(g)
+    for n in g.nodes:
+        if n.op == "attention":
+            F |= {n.id, g.aux_of(n.id)}
+        elif n.op in ("act8", "mask"):
+            F.add(n.id)
+    return F
+
+
+def code_schedule(g: Graph, variants=None):
+    """Schedule of code_set: linear inputs in 8 bits, projections recomputed."""
+    variants = CODE_VARIANTS if variants is None else variants
+    return expand(g, code_set(g), choose_bimpls(g, variants), allow_inplace=variants.get("inplace", True))

@@ -22,8 +22,12 @@ def make_inputs(g: Graph, seed=0, gamma_beta="unit"):
     for n in g.nodes:
         if n.op == "softmaxce":
             classes = g.shape_of(n.ins[0])[-1]
+        elif n.op == "linearce":
+            classes = g.params[n.pars[0]][2][0]
     for ref, name, dt, shp in g.exts:
-        if dt == "f32":
+        if ref in g.ext_values:
+            exts[ref] = np.asarray(g.ext_values[ref], dtype=np.int32)
+        elif dt == "f32":
             exts[ref] = rng.standard_normal(shp, dtype=np.float32)
         else:
             exts[ref] = rng.integers(0, classes, size=shp, dtype=np.int32)
