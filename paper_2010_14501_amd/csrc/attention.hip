@@ -8,11 +8,12 @@
 // The products are worked as their transposes, so that a lane of the matrix instruction holds 16 scores of one row: the row's maximum and
 // sum need one exchange between the wave's halves, and the scores leave the first product where the second one reads its operand (the
 // order of a reduction's indices is free as long as both operands agree).  The other operand of the second product runs across the
-// reduction and is read from LDS by ds_read_b64_tr_b16 (bf16) or by single floats.
+// reduction and is read from LDS by ds_read_b64_tr_b16.
 //
-// bf16: v_mfma_f32_32x32x16_bf16; p and ds are rounded to bf16 between the products (at most 2^-8 of a value each, which averages
-// out over the sums: the results' own rounding to bf16 costs more).  fp32: v_mfma_f32_32x32x2_f32, nothing is rounded below fp32.  Scores, maxima, sums
-// and gradients are fp32 in both.
+// Everything runs on v_mfma_f32_32x32x16_bf16.  bf16: p and ds are rounded to bf16 between the products (at most 2^-8 of a value each, which
+// averages out over the sums: the results' own rounding to bf16 costs more).  fp32: every operand in three bf16 pieces and a product in
+// six terms (bf16_pieces.hpp), 2^-24 of it at worst, in 192 cycles where the fp32 instruction takes 512; tiles are split on their way to
+// LDS, results in registers.  An infinity comes out as NaN there.  Scores, maxima, sums and gradients are fp32 in both.
 //
 // Backward is two kernels without atomics, so results do not depend on the order of anything: the first walks along the keys of 128
 // rows (dq, and delta on the way), the second along the rows and the group's heads of 128 keys (dk, dv).  That computes the scores
@@ -30,21 +31,23 @@ namespace {
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
-// What a lane holds of an operand, 16 bytes, and the product of two such pieces: 16 reduction indices in bf16, 8 in fp32.
+// What a lane holds of an operand at 16 reduction indices, and the product of two of these.
 template <class T> struct Piece;
 template <> struct Piece<unsigned short> {
     typedef bf16x8 V;
-    static constexpr int STEPS = 2;      // pieces along 32 reduction indices
-    static __device__ __forceinline__ floatx16 mma(V a, V b, floatx16 c) { return mfma_bf16(a, b, c); }
+    static constexpr int PLANES = 1;
+    static __device__ __forceinline__ V plane(const V &v, int) { return v; }
+    static __device__ __forceinline__ floatx16 mma(const V &a, const V &b, floatx16 c) { return mfma_bf16(a, b, c); }
     // results 8 s .. 8 s + 7 of a lane as an operand
     static __device__ __forceinline__ V from_result(const floatx16 &p, int s) {
         const uintx4 w{pack_bf16(p[8 * s], p[8 * s + 1]), pack_bf16(p[8 * s + 2], p[8 * s + 3]), pack_bf16(p[8 * s + 4], p[8 * s + 5]),
                        pack_bf16(p[8 * s + 6], p[8 * s + 7])};
         return __builtin_bit_cast(V, w);
     }
-    static __device__ __forceinline__ float dot(V a, V b) {
+    static __device__ __forceinline__ V load(const unsigned short *p) { return *(const V *)p; }
+    static __device__ __forceinline__ float dot(const unsigned short *a, const unsigned short *b) {
         float s = 0.f;
-        const uintx4 x = __builtin_bit_cast(uintx4, a), y = __builtin_bit_cast(uintx4, b);
+        const uintx4 x = *(const uintx4 *)a, y = *(const uintx4 *)b;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             s += __uint_as_float(x[i] << 16) * __uint_as_float(y[i] << 16);
@@ -54,96 +57,145 @@ template <> struct Piece<unsigned short> {
     }
 };
 template <> struct Piece<float> {
-    typedef floatx4 V;
-    static constexpr int STEPS = 4;
-    static __device__ __forceinline__ floatx16 mma(V a, V b, floatx16 c) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
-        return c;
+    typedef PieceRow V;
+    static constexpr int PLANES = 3;
+    static __device__ __forceinline__ floatx16 mma(const V &a, const V &b, floatx16 c) {
+        c = mfma_bf16(a.l, b.h, c);
+        c = mfma_bf16(a.h, b.l, c);
+        c = mfma_bf16(a.m, b.m, c);
+        c = mfma_bf16(a.m, b.h, c);
+        c = mfma_bf16(a.h, b.m, c);
+        return mfma_bf16(a.h, b.h, c);
     }
-    static __device__ __forceinline__ V from_result(const floatx16 &p, int s) { return V{p[4 * s], p[4 * s + 1], p[4 * s + 2], p[4 * s + 3]}; }
-    static __device__ __forceinline__ float dot(V a, V b) { return a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]; }
+    static __device__ __forceinline__ V from_result(const floatx16 &p, int s) {
+        const float v[8] = {p[8 * s], p[8 * s + 1], p[8 * s + 2], p[8 * s + 3], p[8 * s + 4], p[8 * s + 5], p[8 * s + 6], p[8 * s + 7]};
+        unsigned lost = 0;
+        return split_row(v, lost);
+    }
+    static __device__ __forceinline__ V load(const float *p) {
+        const float4 a = *(const float4 *)p, b = *(const float4 *)(p + 4);
+        const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        unsigned lost = 0;
+        return split_row(v, lost);
+    }
+    static __device__ __forceinline__ float dot(const float *a, const float *b) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += a[i] * b[i];
+        return s;
+    }
 };
 
-// A tile of R rows of D values in LDS: strips of 128 bytes, each R rows of eight 16-byte pieces turned by the row (tile_bf16.hpp).
-template <class T, int D, int R>
-struct AttTile {
-    static constexpr int STRIPS = D * (int)sizeof(T) / 128, BYTES = R * 128 * STRIPS, COPIES = BYTES / (256 * 16);
+// A tile of R rows of D values in LDS, as bf16 (fp32: a plane for each piece): strips of 64 columns, each R rows of 128 bytes in eight
+// pieces turned by the row (tile_bf16.hpp).
+template <class T, int D, int R> struct AttTile;
+template <int D, int R>
+struct AttTile<unsigned short, D, R> {         // straight from memory to LDS
+    static constexpr int BYTES = R * D * 2, COPIES = BYTES / (256 * 16);
     unsigned off[COPIES];
     int64_t ld;
     int used;               // bytes of a row that exist
     __device__ __forceinline__ void init(int64_t ld_, int head_dim) {
         ld = ld_;
-        used = head_dim * (int)sizeof(T);
+        used = head_dim * 2;
 #pragma unroll
         for (int i = 0; i < COPIES; ++i) {
             const unsigned piece = i * 256 + threadIdx.x, strip = piece / (R * 8), row = piece / 8 % R, c = (piece % 8) ^ wide_turn(row);
             const unsigned col = strip * 128 + c * 16;
-            off[i] = (int)col < used ? row * (unsigned)(ld * sizeof(T)) + col : BUFFER_ABSENT;
+            off[i] = (int)col < used ? row * (unsigned)(ld * 2) + col : BUFFER_ABSENT;
         }
     }
     // rows of which `left` exist; the others arrive as zeros
-    __device__ __forceinline__ void copy(lds_char *lds, const T *rows, int left) const {
-        const __amdgpu_buffer_rsrc_t r = buffer_of(rows, left > 0 ? (unsigned)((min(left, R) - 1) * ld * sizeof(T)) + used : 0u);
+    __device__ __forceinline__ void copy(lds_char *lds, const unsigned short *rows, int left) const {
+        const __amdgpu_buffer_rsrc_t r = buffer_of(rows, left > 0 ? (unsigned)((min(left, R) - 1) * ld * 2) + used : 0u);
         const int wave = threadIdx.x / 64;
 #pragma unroll
         for (int i = 0; i < COPIES; ++i) copy_to_lds(r, lds + (i * 256 + wave * 64) * 16, off[i], 0);
     }
 };
+template <int D, int R>
+struct AttTile<float, D, R> {                  // through registers, where it is split
+    static constexpr int PLANE = R * D * 2, BYTES = 3 * PLANE, COPIES = R * D / (256 * 8);
+    float4 held[COPIES][2];
+    int64_t ld;
+    int head_dim;
+    __device__ __forceinline__ void init(int64_t ld_, int head_dim_) {
+        ld = ld_;
+        head_dim = head_dim_;
+    }
+    __device__ __forceinline__ void load(const float *rows, int left) {
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+            const int piece = i * 256 + threadIdx.x, row = piece / (D / 8), col = piece % (D / 8) * 8;
+            held[i][0] = held[i][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (row < left && col < head_dim) {
+                const float *p = rows + row * ld + col;
+                held[i][0] = *(const float4 *)p;
+                held[i][1] = *(const float4 *)(p + 4);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(lds_char *lds) const {
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+            const int piece = i * 256 + threadIdx.x, row = piece / (D / 8), c = piece % (D / 8);
+            const float4 a = held[i][0], b = held[i][1];
+            const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            unsigned lost = 0;
+            const PieceRow r = split_row(v, lost);
+            lds_char *p = lds + (c >> 3) * R * 128 + row * 128 + (((c & 7) ^ (int)wide_turn(row)) << 4);
+            typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+            *(lds_bf16x8 *)p = r.h;
+            *(lds_bf16x8 *)(p + PLANE) = r.m;
+            *(lds_bf16x8 *)(p + 2 * PLANE) = r.l;
+        }
+    }
+};
 // where a lane reads such tiles
-template <class T, int R>
+template <class T, int D, int R>
 struct AttReader {
-    static constexpr bool BF16 = sizeof(T) == 2;
-    unsigned wide_at[4], deep_at[BF16 ? 4 : 8];
+    static constexpr int PLANE = R * D * 2;
+    typedef typename Piece<T>::V V;
+    unsigned wide_at[4], deep_at[4];
     __device__ __forceinline__ void init() {
         const unsigned l = threadIdx.x & 63, h = l >> 5;
 #pragma unroll
         for (int s = 0; s < 4; ++s) wide_at[s] = (l & 31) * 128 + (((2 * s + h) ^ wide_turn(l & 31)) << 4);
-        if (BF16) {
 #pragma unroll
-            for (int p = 0; p < 4; ++p) {      // bit 0: rows + 8, bit 1: columns + 32
-                const unsigned row = 4 * h + ((l & 15) >> 2) + 8 * (p & 1), c = 4 * (p >> 1) + 2 * ((l >> 4) & 1) + ((l & 3) >> 1);
-                deep_at[p] = row * 128 + ((c ^ wide_turn(row)) << 4) + (l & 1) * 8;
-            }
-        } else {
-#pragma unroll
-            for (int p = 0; p < 8; ++p) {      // bits 0, 1: row of four, bit 2: rows + 8
-                const unsigned row = 4 * h + (p & 3) + 8 * (p >> 2);
-                deep_at[p] = row * 128 + ((((l & 31) >> 2) ^ wide_turn(row)) << 4) + (l & 3) * 4;
-            }
+        for (int p = 0; p < 4; ++p) {      // bit 0: rows + 8, bit 1: columns + 32
+            const unsigned row = 4 * h + ((l & 15) >> 2) + 8 * (p & 1), c = 4 * (p >> 1) + 2 * ((l >> 4) & 1) + ((l & 3) >> 1);
+            deep_at[p] = row * 128 + ((c ^ wide_turn(row)) << 4) + (l & 1) * 8;
         }
     }
-    // rows 32 b + (l & 31), piece s along the row
-    __device__ __forceinline__ typename Piece<T>::V wide(const lds_char *t, int b, int s) const {
-        return *(const __attribute__((address_space(3))) typename Piece<T>::V *)(t + wide_at[s & 3] + b * 32 * 128 + (s >> 2) * R * 128);
+    // rows 32 b + (l & 31), 16 columns from 16 s on
+    __device__ __forceinline__ V wide(const lds_char *t, int b, int s) const {
+        const lds_char *p = t + wide_at[s & 3] + b * 32 * 128 + (s >> 2) * R * 128;
+        if constexpr (sizeof(T) == 2) return read_wide(p);
+        else return PieceRow{read_wide(p), read_wide(p + PLANE), read_wide(p + 2 * PLANE)};
     }
     // columns 32 c + (l & 31), the rows of 32 b .. that results of step s hold
-    __device__ __forceinline__ typename Piece<T>::V deep(const lds_char *t, int b, int s, int c) const {
-        if constexpr (BF16) {
-            const lds_char *p = t + (c >> 1) * R * 128 + (32 * b + 16 * s) * 128;
-            return join(read_turned(p + deep_at[2 * (c & 1)]), read_turned(p + deep_at[2 * (c & 1) + 1]));
-        } else {
-            const lds_char *p = t + c * R * 128 + (32 * b + 16 * (s >> 1)) * 128;
-            floatx4 v;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = *(const __attribute__((address_space(3))) float *)(p + deep_at[4 * (s & 1) + j]);
-            return v;
-        }
+    __device__ __forceinline__ V deep(const lds_char *t, int b, int s, int c) const {
+        const lds_char *p = t + (c >> 1) * R * 128 + (32 * b + 16 * s) * 128;
+        const unsigned x = deep_at[2 * (c & 1)], y = deep_at[2 * (c & 1) + 1];
+        if constexpr (sizeof(T) == 2) return join(read_turned(p + x), read_turned(p + y));
+        else
+            return PieceRow{join(read_turned(p + x), read_turned(p + y)), join(read_turned(p + PLANE + x), read_turned(p + PLANE + y)),
+                            join(read_turned(p + 2 * PLANE + x), read_turned(p + 2 * PLANE + y))};
     }
 };
 
 // The pieces of row l & 31 of 32 rows (of which `left` exist) straight from memory
 template <class T, int D>
 struct RowPieces {
-    typename Piece<T>::V p[D * sizeof(T) / 32];
+    typename Piece<T>::V p[D / 16];
     __device__ __forceinline__ void load(const T *rows, int64_t ld, int left, int head_dim) {
         const int l = threadIdx.x & 63;
         const T *row = rows + (l & 31) * ld;
 #pragma unroll
-        for (int s = 0; s < (int)(D * sizeof(T) / 32); ++s) {
-            const int col = (2 * s + (l >> 5)) * (int)(16 / sizeof(T));
+        for (int s = 0; s < D / 16; ++s) {
+            const int col = (2 * s + (l >> 5)) * 8;
             p[s] = typename Piece<T>::V{};
-            if ((l & 31) < left && col < head_dim) p[s] = *(const typename Piece<T>::V *)(row + col);
+            if ((l & 31) < left && col < head_dim) p[s] = Piece<T>::load(row + col);
         }
     }
 };
@@ -161,9 +213,12 @@ struct AttShape {
 template <class T, int D, int PARTS>
 struct AttForm {
     static constexpr int ROWS = 128 / PARTS, BLOCKS = sizeof(T) == 2 && PARTS == 1 ? 2 : 1, TILE = 32 * BLOCKS * PARTS;
-    static constexpr int PIECES = D * (int)sizeof(T) / 32, STEPS = Piece<T>::STEPS;
+    static constexpr int PIECES = D / 16, STEPS = 2;
     typedef AttTile<T, D, TILE> Tile;
-    static constexpr bool TWO_GROUPS = 4 * Tile::BYTES <= 64 << 10;      // two workgroups in a CU's LDS
+    // bf16: two tiles of each of two tensors, copied to while the others are read; fp32: one of each, which registers hold the next of
+    static constexpr int BUFFERS = sizeof(T) == 2 ? 2 : 1;
+    static constexpr bool TWO_GROUPS = 2 * BUFFERS * Tile::BYTES <= 72 << 10;      // two workgroups in a CU's LDS
+    static constexpr int AREA = D / 32 * 16 * 256;                       // a wave's results
 };
 
 // Sequence s owns the slots from cu[s] / ROWS + s on: at least one for every ROWS rows begun, whatever the lengths, so the grid
@@ -273,7 +328,8 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS ? 2 : 1)) vo
     typedef typename F::Tile Tile;
     constexpr int R = F::TILE, B = F::BLOCKS, PIECES = F::PIECES, STEPS = F::STEPS;
     __shared__ float stats[2][4][64];
-    __shared__ __attribute__((aligned(16))) char k0[Tile::BYTES], k1[Tile::BYTES], v0[Tile::BYTES], v1[Tile::BYTES];
+    constexpr int BYTES = Tile::BYTES, SECOND = F::BUFFERS == 2 ? BYTES : 16;
+    __shared__ __attribute__((aligned(16))) char k0[BYTES], k1[SECOND], v0[BYTES], v1[SECOND];
     int head, slot, start, len, row0;
     att_place(a.heads, a.slots, head, slot);
     if (!find_rows<F::ROWS>(a, a.slots - 1 - slot, start, len, row0)) return;      // the longest rows first
@@ -282,7 +338,7 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS ? 2 : 1)) vo
     Tile tk, tv;
     tk.init(a.k_ld, a.head_dim);
     tv.init(a.v_ld, a.head_dim);
-    AttReader<T, R> rd;
+    AttReader<T, D, R> rd;
     rd.init();
     const T *kp = k + start * a.k_ld + (int64_t)kv_head * a.head_dim, *vp = v + start * a.v_ld + (int64_t)kv_head * a.head_dim;
     RowPieces<T, D> qr;
@@ -295,11 +351,6 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS ? 2 : 1)) vo
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[c][r] = 0.f;
     const int end = min(len, row0 + F::ROWS);
-    auto fetch = [&](lds_char *lk, lds_char *lv, int key0) {      // none is under way when the last tile has been used
-        if (key0 >= end) return;
-        tk.copy(lk, kp + key0 * a.k_ld, len - key0);
-        tv.copy(lv, vp + key0 * a.v_ld, len - key0);
-    };
     auto work = [&](const lds_char *lk, const lds_char *lv, int tile0) {
         const int key0 = tile0 + 32 * B * part;
         if (key0 > first + 31 || key0 >= end) return;
@@ -352,14 +403,35 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS ? 2 : 1)) vo
         }
     };
     lds_char *lk0 = (lds_char *)k0, *lk1 = (lds_char *)k1, *lv0 = (lds_char *)v0, *lv1 = (lds_char *)v1;
-    fetch(lk0, lv0, 0);
-    for (int key0 = 0; key0 < end; key0 += 2 * R) {
-        copies_arrived();
-        fetch(lk1, lv1, key0 + R);
-        work(lk0, lv0, key0);
-        copies_arrived();
-        fetch(lk0, lv0, key0 + 2 * R);
-        work(lk1, lv1, key0 + R);
+    if constexpr (F::BUFFERS == 2) {
+        auto fetch = [&](lds_char *lk, lds_char *lv, int key0) {      // none is under way when the last tile has been used
+            if (key0 >= end) return;
+            tk.copy(lk, kp + key0 * a.k_ld, len - key0);
+            tv.copy(lv, vp + key0 * a.v_ld, len - key0);
+        };
+        fetch(lk0, lv0, 0);
+        for (int key0 = 0; key0 < end; key0 += 2 * R) {
+            copies_arrived();
+            fetch(lk1, lv1, key0 + R);
+            work(lk0, lv0, key0);
+            copies_arrived();
+            fetch(lk0, lv0, key0 + 2 * R);
+            work(lk1, lv1, key0 + R);
+        }
+    } else {
+        tk.load(kp, len);
+        tv.load(vp, len);
+        for (int key0 = 0; key0 < end; key0 += R) {
+            __syncthreads();
+            tk.store(lk0);
+            tv.store(lv0);
+            __syncthreads();
+            if (key0 + R < end) {
+                tk.load(kp + (key0 + R) * a.k_ld, len - key0 - R);
+                tv.load(vp + (key0 + R) * a.v_ld, len - key0 - R);
+            }
+            work(lk0, lv0, key0);
+        }
     }
     sum = exchange_sum(sum);
     float factor = 1.f;
@@ -376,7 +448,11 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS ? 2 : 1)) vo
         for (int i = 0; i < PARTS; ++i) sum += stats[1][wave - part + i][l] * __builtin_amdgcn_exp2f(stats[0][wave - part + i][l] - top);
         factor = __builtin_amdgcn_exp2f(mine - top);
     }
-    auto area = [&](int w) { return w == 0 ? lk0 : w == 1 ? lk1 : w == 2 ? lv0 : lv1; };
+    auto area = [&](int w) {
+        if (F::BUFFERS == 2) return w == 0 ? lk0 : w == 1 ? lk1 : w == 2 ? lv0 : lv1;
+        return (w < 2 ? lk0 : lv0) + (w & 1) * F::AREA;
+    };
+    static_assert(PARTS == 1 || BYTES >= F::AREA * (F::BUFFERS == 2 ? 1 : 2), "");
     if (lse && part == 0 && l < 32 && row < len) lse[(int64_t)head * a.tokens + start + row] = (top + __builtin_amdgcn_logf(sum)) * LN2;
     join_and_store<T, D, PARTS>(area, acc, factor, o + (int64_t)(start + row) * a.o_ld + (int64_t)head * a.head_dim, row < len, 1.f / sum, a.head_dim, false);
 }
@@ -389,7 +465,8 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
     typedef AttForm<T, D, PARTS> F;
     typedef typename F::Tile Tile;
     constexpr int R = F::TILE, B = F::BLOCKS, PIECES = F::PIECES, STEPS = F::STEPS;
-    __shared__ __attribute__((aligned(16))) char k0[Tile::BYTES], k1[Tile::BYTES], v0[Tile::BYTES], v1[Tile::BYTES];
+    constexpr int BYTES = Tile::BYTES, SECOND = F::BUFFERS == 2 ? BYTES : 16;
+    __shared__ __attribute__((aligned(16))) char k0[BYTES], k1[SECOND], v0[BYTES], v1[SECOND];
     int head, slot, start, len, row0;
     att_place(a.heads, a.slots, head, slot);
     if (!find_rows<F::ROWS>(a, a.slots - 1 - slot, start, len, row0)) return;
@@ -398,20 +475,22 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
     Tile tk, tv;
     tk.init(a.k_ld, a.head_dim);
     tv.init(a.v_ld, a.head_dim);
-    AttReader<T, R> rd;
+    AttReader<T, D, R> rd;
     rd.init();
     const T *kp = k + start * a.k_ld + (int64_t)kv_head * a.head_dim, *vp = v + start * a.v_ld + (int64_t)kv_head * a.head_dim;
     RowPieces<T, D> qr, gr;
     qr.load(q + (start + first) * a.q_ld + (int64_t)head * a.head_dim, a.q_ld, len - first, a.head_dim);
     gr.load(go + (start + first) * a.o_ld + (int64_t)head * a.head_dim, a.o_ld, len - first, a.head_dim);
     float dot = 0.f;
-    {
-        RowPieces<T, D> orow;
-        orow.load(o + (start + first) * a.o_ld + (int64_t)head * a.head_dim, a.o_ld, len - first, a.head_dim);
+    if (row < len) {
+        const int64_t at = (start + row) * a.o_ld + (int64_t)head * a.head_dim;
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p) dot += Piece<T>::dot(orow.p[p], gr.p[p]);
-        dot = exchange_sum(dot);
+        for (int p = 0; p < PIECES; ++p) {
+            const int col = (2 * p + (l >> 5)) * 8;
+            if (col < a.head_dim) dot += Piece<T>::dot(o + at + col, go + at + col);
+        }
     }
+    dot = exchange_sum(dot);
     const int64_t at = (int64_t)head * a.tokens + start + row;
     const float by = a.scale * LOG2E, ls = row < len ? lse[at] * LOG2E : 0.f;
     if (part == 0 && l < 32 && row < len) {
@@ -424,11 +503,6 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[c][r] = 0.f;
     const int end = min(len, row0 + F::ROWS);
-    auto fetch = [&](lds_char *lk, lds_char *lv, int key0) {      // none is under way when the last tile has been used
-        if (key0 >= end) return;
-        tk.copy(lk, kp + key0 * a.k_ld, len - key0);
-        tv.copy(lv, vp + key0 * a.v_ld, len - key0);
-    };
     auto work = [&](const lds_char *lk, const lds_char *lv, int tile0) {
         const int key0 = tile0 + 32 * B * part;
         if (key0 > first + 31 || key0 >= end) return;
@@ -458,17 +532,42 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
         }
     };
     lds_char *lk0 = (lds_char *)k0, *lk1 = (lds_char *)k1, *lv0 = (lds_char *)v0, *lv1 = (lds_char *)v1;
-    fetch(lk0, lv0, 0);
-    for (int key0 = 0; key0 < end; key0 += 2 * R) {
-        copies_arrived();
-        fetch(lk1, lv1, key0 + R);
-        work(lk0, lv0, key0);
-        copies_arrived();
-        fetch(lk0, lv0, key0 + 2 * R);
-        work(lk1, lv1, key0 + R);
+    if constexpr (F::BUFFERS == 2) {
+        auto fetch = [&](lds_char *lk, lds_char *lv, int key0) {      // none is under way when the last tile has been used
+            if (key0 >= end) return;
+            tk.copy(lk, kp + key0 * a.k_ld, len - key0);
+            tv.copy(lv, vp + key0 * a.v_ld, len - key0);
+        };
+        fetch(lk0, lv0, 0);
+        for (int key0 = 0; key0 < end; key0 += 2 * R) {
+            copies_arrived();
+            fetch(lk1, lv1, key0 + R);
+            work(lk0, lv0, key0);
+            copies_arrived();
+            fetch(lk0, lv0, key0 + 2 * R);
+            work(lk1, lv1, key0 + R);
+        }
+    } else {
+        tk.load(kp, len);
+        tv.load(vp, len);
+        for (int key0 = 0; key0 < end; key0 += R) {
+            __syncthreads();
+            tk.store(lk0);
+            tv.store(lv0);
+            __syncthreads();
+            if (key0 + R < end) {
+                tk.load(kp + (key0 + R) * a.k_ld, len - key0 - R);
+                tv.load(vp + (key0 + R) * a.v_ld, len - key0 - R);
+            }
+            work(lk0, lv0, key0);
+        }
     }
     if (PARTS > 1) __syncthreads();      // everybody is done with the tiles
-    auto area = [&](int w) { return w == 0 ? lk0 : w == 1 ? lk1 : w == 2 ? lv0 : lv1; };
+    auto area = [&](int w) {
+        if (F::BUFFERS == 2) return w == 0 ? lk0 : w == 1 ? lk1 : w == 2 ? lv0 : lv1;
+        return (w < 2 ? lk0 : lv0) + (w & 1) * F::AREA;
+    };
+    static_assert(PARTS == 1 || BYTES >= F::AREA * (F::BUFFERS == 2 ? 1 : 2), "");
     join_and_store<T, D, PARTS>(area, acc, 1.f, dq + (int64_t)(start + row) * a.q_ld + (int64_t)head * a.head_dim, row < len, a.scale, a.head_dim, add);
 }
 
@@ -482,7 +581,8 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
     typedef AttForm<T, D, PARTS> F;
     typedef typename F::Tile Tile;
     constexpr int R = F::TILE, B = F::BLOCKS, PIECES = F::PIECES, STEPS = F::STEPS;
-    __shared__ __attribute__((aligned(16))) char q0[Tile::BYTES], q1[Tile::BYTES], g0[Tile::BYTES], g1[Tile::BYTES];
+    constexpr int BYTES = Tile::BYTES, SECOND = F::BUFFERS == 2 ? BYTES : 16;
+    __shared__ __attribute__((aligned(16))) char q0[BYTES], q1[SECOND], g0[BYTES], g1[SECOND];
     __shared__ __attribute__((aligned(16))) float stat0[256], stat1[256];      // delta of a tile's rows, their lse
     int kv_head, slot, start, len, key0;
     att_place(a.kv_heads, a.slots, kv_head, slot);
@@ -492,7 +592,7 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
     Tile tq, tg;
     tq.init(a.q_ld, a.head_dim);
     tg.init(a.o_ld, a.head_dim);
-    AttReader<T, R> rd;
+    AttReader<T, D, R> rd;
     rd.init();
     RowPieces<T, D> kr, vr;
     kr.load(k + (start + first) * a.k_ld + (int64_t)kv_head * a.head_dim, a.k_ld, len - first, a.head_dim);
@@ -505,18 +605,13 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
         for (int r = 0; r < 16; ++r) ak[c][r] = av[c][r] = 0.f;
     const int from = key0 / R * R, tiles = (len - from + R - 1) / R;
     const int begin = (int)((int64_t)tiles * group * blockIdx.y / gridDim.y), all = (int)((int64_t)tiles * group * (blockIdx.y + 1) / gridDim.y);
-    auto fetch = [&](lds_char *lq, lds_char *lg, lds_char *ls, int t) {      // none is under way when the last tile has been used
-        if (t >= all) return;
-        const int g = t / tiles, row = from + (t - g * tiles) * R, head = kv_head * group + g;
-        tq.copy(lq, q + (start + row) * a.q_ld + (int64_t)head * a.head_dim, len - row);
-        tg.copy(lg, go + (start + row) * a.o_ld + (int64_t)head * a.head_dim, len - row);
-        // 64 rows' delta (waves 0, 1) and lse (2, 3); rows behind the sequence: 0
-        if (64 * (wave & 1) < R) {
-            const float *p = delta + (wave / 2 * a.heads + head) * (int64_t)a.tokens + start + row;
-            const __amdgpu_buffer_rsrc_t r = buffer_of(p, (unsigned)min(len - row, R) * 4);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(ls + wave * 256), 4, (64 * (wave & 1) + l) * 4, 0, 0, 0);
-        }
+    auto place = [&](int t, int &head, int &row) {
+        const int g = t / tiles;
+        head = kv_head * group + g;
+        row = from + (t - g * tiles) * R;
     };
+    // fp32: one product's operands at a time, or they do not fit the registers
+    auto narrow = [] { if (sizeof(T) == 4) __builtin_amdgcn_sched_barrier(0); };
     auto work = [&](const lds_char *lq, const lds_char *lg, const lds_char *ls, int t) {
         const int row = from + t % tiles * R + 32 * B * part;
         if (t >= all || row + 32 * B - 1 < first || row >= len) return;
@@ -528,8 +623,10 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
             for (int r = 0; r < 16; ++r) s[r] = d[r] = 0.f;
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) s = Piece<T>::mma(rd.wide(lq, B * part + b, p), kr.p[p], s);
+            narrow();
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) d = Piece<T>::mma(rd.wide(lg, B * part + b, p), vr.p[p], d);
+            narrow();
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 const lds_char *at = ls + (32 * (B * part + b) + result_row(r, l)) * 4;
@@ -548,20 +645,60 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
                 for (int c = 0; c < D / 32; ++c) av[c] = Piece<T>::mma(rd.deep(lg, B * part + b, p, c), pr, av[c]);
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) ak[c] = Piece<T>::mma(rd.deep(lq, B * part + b, p, c), ds, ak[c]);
+                narrow();
             }
         }
     };
     lds_char *lq0 = (lds_char *)q0, *lq1 = (lds_char *)q1, *lg0 = (lds_char *)g0, *lg1 = (lds_char *)g1, *ls0 = (lds_char *)stat0, *ls1 = (lds_char *)stat1;
-    fetch(lq0, lg0, ls0, begin);
-    for (int t = begin; t < all; t += 2) {
-        copies_arrived();
-        fetch(lq1, lg1, ls1, t + 1);
-        work(lq0, lg0, ls0, t);
-        copies_arrived();
-        fetch(lq0, lg0, ls0, t + 2);
-        work(lq1, lg1, ls1, t + 1);
+    if constexpr (F::BUFFERS == 2) {
+        auto fetch = [&](lds_char *lq, lds_char *lg, lds_char *ls, int t) {      // none is under way when the last tile has been used
+            if (t >= all) return;
+            int head, row;
+            place(t, head, row);
+            tq.copy(lq, q + (start + row) * a.q_ld + (int64_t)head * a.head_dim, len - row);
+            tg.copy(lg, go + (start + row) * a.o_ld + (int64_t)head * a.head_dim, len - row);
+            // 64 rows' delta (waves 0, 1) and lse (2, 3); rows behind the sequence: 0
+            if (64 * (wave & 1) < R) {
+                const float *p = delta + (wave / 2 * a.heads + head) * (int64_t)a.tokens + start + row;
+                const __amdgpu_buffer_rsrc_t r = buffer_of(p, (unsigned)min(len - row, R) * 4);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(ls + wave * 256), 4, (64 * (wave & 1) + l) * 4, 0, 0, 0);
+            }
+        };
+        fetch(lq0, lg0, ls0, begin);
+        for (int t = begin; t < all; t += 2) {
+            copies_arrived();
+            fetch(lq1, lg1, ls1, t + 1);
+            work(lq0, lg0, ls0, t);
+            copies_arrived();
+            fetch(lq0, lg0, ls0, t + 2);
+            work(lq1, lg1, ls1, t + 1);
+        }
+    } else {
+        float stat = 0.f;            // threads 0 .. 127: a row's delta, 128 .. 255: its lse
+        const int stat_row = threadIdx.x & 127;
+        auto load = [&](int t) {
+            int head, row;
+            place(t, head, row);
+            tq.load(q + (start + row) * a.q_ld + (int64_t)head * a.head_dim, len - row);
+            tg.load(go + (start + row) * a.o_ld + (int64_t)head * a.head_dim, len - row);
+            stat = stat_row < R && row + stat_row < len ? delta[((int64_t)(threadIdx.x / 128) * a.heads + head) * a.tokens + start + row + stat_row] : 0.f;
+        };
+        if (begin < all) load(begin);
+        for (int t = begin; t < all; ++t) {
+            __syncthreads();
+            tq.store(lq0);
+            tg.store(lg0);
+            stat0[threadIdx.x] = stat;
+            __syncthreads();
+            if (t + 1 < all) load(t + 1);
+            work(lq0, lg0, ls0, t);
+        }
     }
-    auto area = [&](int w) { return w == 0 ? lq0 : w == 1 ? lq1 : w == 2 ? lg0 : lg1; };
+    auto area = [&](int w) {
+        if (F::BUFFERS == 2) return w == 0 ? lq0 : w == 1 ? lq1 : w == 2 ? lg0 : lg1;
+        return (w < 2 ? lq0 : lg0) + (w & 1) * F::AREA;
+    };
+    static_assert(PARTS == 1 || BYTES >= F::AREA * (F::BUFFERS == 2 ? 1 : 2), "");
     if (PARTS > 1) __syncthreads();      // everybody is done with the tiles
     if (ranges) {
         float *row = ranges + (((int64_t)blockIdx.y * a.tokens + start + key) * a.kv_heads + kv_head) * a.head_dim;
@@ -626,32 +763,31 @@ void check_tensors(std::initializer_list<const void *> ptrs) {
     }
 }
 
-// Rows of the forward and the first backward kernel: 128 to a workgroup where that gives four workgroups to a CU, 64 below (bf16, forward:
-// 8 x 16 heads of 512 rows 14.4 against 15.5 us, one sequence of 4000 rows and 8 heads 40 against 51; at 4096 workgroups 64 rows take 10 %
-// longer), and 32 in fp32 with 64 columns, whose products are slow enough to hide the traffic, below two (70 against 88 us at 816 workgroups).
+// Rows of the forward and the first backward kernel: 128 to a workgroup where that gives four workgroups to a CU (fp32 with 128 columns, whose
+// tiles take more of LDS: two), 64 below.  Forward, 64 and 128 rows: bf16 8 x 16 heads of 512 rows 14.4 and 15.5 us, one sequence of 4000 rows
+// and 8 heads 40 and 51, two of 8192 and 32 heads 1190 and 1084; fp32 4 x 16 heads of 512 rows 28 and 36, one of 4096 and 32 heads of 128 1135 and 813.
 template <class T, int D>
 int row_parts(const AttShape &a) {
     const int64_t full = (int64_t)(a.tokens / 128) * a.heads;
-    if (full >= 1024 && a.tokens / a.seqs >= 128) return 1;
-    return sizeof(T) == 4 && D == 64 && full < 512 ? 4 : 2;
+    return full >= (sizeof(T) == 4 && D == 128 ? 512 : 1024) && a.tokens / a.seqs >= 128 ? 1 : 2;
 }
 // The second backward kernel has fewer workgroups (key heads) with a longer way each (the rows behind a key, of every head of the group).
-// Where 128 keys to a workgroup do not give four workgroups to a CU, the way is cut into ranges of at least 16 tiles; where that gives less
-// than two, a workgroup takes 32 keys (64 in fp32 with 128 columns, whose tiles fill LDS) and ranges by the same measure.  bf16, both
-// backward kernels: 8 ragged sequences of 8192 rows, 32 / 8 heads, 1255 us uncut, 888 in four ranges, 928 with 32 keys; one of 10000, 4 / 1
-// heads, 2291, 620 (8 ranges), 820 (32 keys, 4 ranges); one of 1024, 8 heads of 64, 51, 43 (4 ranges), 24 (32 keys).
+// Where 128 keys to a workgroup do not give four workgroups to a CU, the way is cut into ranges.  bf16, where that gives less than two: a
+// workgroup takes 32 keys.  Both backward kernels: bf16, 8 ragged sequences of 8192 rows, 32 / 8 heads, 1255 us uncut, 888 in four ranges, 928
+// with 32 keys; one of 10000, 4 / 1 heads, 2291, 620 (8 ranges), 820 (32 keys, 4 ranges); one of 1024, 8 heads of 64, 51, 43 (4 ranges), 24
+// (32 keys).  fp32, 2048 ragged rows, 12 / 4 heads of 64: 587, 196 (16 ranges), 223 (32 keys, 4 ranges); 4 x 512 rows, 16 heads: 126, 110 (2), 124.
 struct KeyForm { int parts, ranges; };
 KeyForm key_form(const AttShape &a, bool fp32) {
-    const bool large = fp32 && a.head_dim > 64;
-    const int64_t full = std::max<int64_t>(1, (int64_t)(a.tokens / 128) * a.kv_heads), len = a.tokens / a.seqs, group = a.heads / a.kv_heads;
-    const auto cut = [&](int64_t groups, int64_t tile) {
-        return std::max<int64_t>(1, std::min<int64_t>({(2048 + groups - 1) / groups, len * group / tile / 16, 16}));
+    const int64_t full = std::max<int64_t>(1, (int64_t)(a.tokens / 128) * a.kv_heads), way = (int64_t)(a.tokens / a.seqs) * (a.heads / a.kv_heads);
+    // ranges until there are `enough` workgroups, of at least `least` rows of the way
+    const auto cut = [&](int64_t groups, int64_t enough, int64_t least) {
+        return std::max<int64_t>(1, std::min<int64_t>({(enough + groups - 1) / groups, way / least, 16}));
     };
+    if (fp32) return {1, (int)cut(full, 1024, 192)};
     if (full >= 1024) return {1, 1};
-    const int64_t r = cut(full, fp32 ? 32 : 64);
-    if (full * r >= 512 && len >= 64) return {1, (int)r};
-    const int parts = large ? 2 : 4;
-    return {parts, (int)cut(2 * full * parts, large ? 64 : 128)};
+    const int64_t r = cut(full, 2048, 1024);
+    if (full * r >= 512 && a.tokens / a.seqs >= 64) return {1, (int)r};
+    return {4, (int)cut(4 * full, 1024, 2048)};
 }
 
 template <class T, int D, int PARTS>
@@ -664,8 +800,7 @@ template <class T, int D>
 void fwd_form(hipStream_t st, const AttShape &a, const void *q, const void *k, const void *v, void *o, float *lse) {
     const int parts = row_parts<T, D>(a);
     if (parts == 1) fwd_launch<T, D, 1>(st, a, q, k, v, o, lse);
-    else if (parts == 2) fwd_launch<T, D, 2>(st, a, q, k, v, o, lse);
-    else if constexpr (sizeof(T) == 4 && D == 64) fwd_launch<T, D, 4>(st, a, q, k, v, o, lse);
+    else fwd_launch<T, D, 2>(st, a, q, k, v, o, lse);
 }
 struct BwdArgs {
     const void *go, *q, *k, *v, *o;
@@ -699,12 +834,10 @@ template <class T, int D>
 void bwd_form(hipStream_t st, const AttShape &a, const BwdArgs &b) {
     const int parts = row_parts<T, D>(a);
     if (parts == 1) dq_launch<T, D, 1>(st, a, b);
-    else if (parts == 2) dq_launch<T, D, 2>(st, a, b);
-    else if constexpr (sizeof(T) == 4 && D == 64) dq_launch<T, D, 4>(st, a, b);
+    else dq_launch<T, D, 2>(st, a, b);
     const KeyForm f = key_form(a, sizeof(T) == 4);
-    constexpr int MANY = sizeof(T) == 4 && D == 128 ? 2 : 4;
-    if (f.parts == 1) dkv_launch<T, D, 1>(st, a, b, f.ranges);
-    else dkv_launch<T, D, MANY>(st, a, b, f.ranges);
+    if (sizeof(T) == 4 || f.parts == 1) dkv_launch<T, D, 1>(st, a, b, f.ranges);
+    else if constexpr (sizeof(T) == 2) dkv_launch<T, D, 4>(st, a, b, f.ranges);
 }
 
 }  // namespace
