@@ -159,18 +159,27 @@ struct RoundEpilogue {
     }
 };
 
-// 64 tokens a workgroup, 16 threads to a token: lse and the row's loss from the parts of its logits
-__global__ __launch_bounds__(1024) void ce_merge_kernel(const float2 *__restrict__ part, int parts, const float *__restrict__ hit,
-                                                        const int32_t *__restrict__ labels, float *__restrict__ lse, float *__restrict__ row_loss,
-                                                        int rows, int vocab) {
-    __shared__ Soft seg[16][64];
-    const int l = threadIdx.x % 64, s = threadIdx.x / 64, t = blockIdx.x * 64 + l;
+// 16 tokens a workgroup, 16 threads to a token: lse and the row's loss from the parts of its logits
+__global__ __launch_bounds__(256) void ce_merge_kernel(const float2 *__restrict__ part, int parts, const float *__restrict__ hit,
+                                                       const int32_t *__restrict__ labels, float *__restrict__ lse, float *__restrict__ row_loss,
+                                                       int rows, int vocab) {
+    __shared__ Soft seg[16][16];
+    const int l = threadIdx.x % 16, s = threadIdx.x / 16, t = blockIdx.x * 16 + l;
     Soft a{-INFINITY, 0.f};
-    if (t < rows)
-        for (int b = s; b < parts; b += 16) {
+    if (t < rows) {
+        int b = s;
+        for (; b + 48 < parts; b += 64) {
+            float2 v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = part[(int64_t)(b + 16 * q) * rows + t];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) a = soft_join(a, Soft{v[q].x, v[q].y});
+        }
+        for (; b < parts; b += 16) {
             const float2 v = part[(int64_t)b * rows + t];
             a = soft_join(a, Soft{v.x, v.y});
         }
+    }
     seg[s][l] = a;
     __syncthreads();
     if (s || t >= rows) return;
@@ -377,7 +386,7 @@ void linear_ce_fwd(hipStream_t st, int dtype, const void *x, const void *w, cons
             hip_check(hipGetLastError(), "linear_ce statistics launch");
         }
     }
-    hipLaunchKernelGGL(ce_merge_kernel, dim3((unsigned)cut(rows, 64)), dim3(1024), 0, st, part, (int)p.parts(), hit, labels, lse, row_loss, p.rows, vocab);
+    hipLaunchKernelGGL(ce_merge_kernel, dim3((unsigned)cut(rows, 16)), dim3(256), 0, st, part, (int)p.parts(), hit, labels, lse, row_loss, p.rows, vocab);
     hip_check(hipGetLastError(), "linear_ce merge launch");
     hipLaunchKernelGGL(ce_mean_kernel, dim3(1), dim3(1024), 0, st, row_loss, labels, p.rows, vocab, loss, (float *)nullptr);
     hip_check(hipGetLastError(), "linear_ce mean launch");
