@@ -31,6 +31,16 @@ namespace {
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
+// The rows of a 32 x 32 result that lie before `limit` are not the lane's key's: their probabilities are 0.  The limit passes through a register of
+// its own inside the branch that this stands in, or the compiler compares for every tile what only those on the diagonal need.
+__device__ __forceinline__ void clear_before(floatx16 &s, int limit) {
+    limit -= 4 * ((threadIdx.x & 63) >> 5);
+    asm volatile("" : "+v"(limit));
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+        if ((r & 3) + 8 * (r >> 2) < limit) s[r] = 0.f;
+}
+
 // What a lane holds of an operand at 16 reduction indices, and the product of two of these.
 template <class T> struct Piece;
 template <> struct Piece<unsigned short> {
@@ -587,7 +597,7 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
     int kv_head, slot, start, len, key0;
     att_place(a.kv_heads, a.slots, kv_head, slot);
     if (!find_rows<F::ROWS>(a, slot, start, len, key0)) return;
-    const int group = a.heads / a.kv_heads, l = threadIdx.x & 63, wave = threadIdx.x / 64;
+    const int group = a.heads / a.kv_heads, l = threadIdx.x & 63, wave = D > 64 ? threadIdx.x / 64 : __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int part = wave % PARTS, first = key0 + wave / PARTS * 32, key = first + (l & 31);
     Tile tq, tg;
     tq.init(a.q_ld, a.head_dim);
@@ -634,9 +644,16 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     s[r + j] = __builtin_amdgcn_exp2f(s[r + j] * by - x[j]);
-                    if (edge && row + 32 * b + result_row(r + j, l) < key) s[r + j] = 0.f;
-                    d[r + j] = s[r + j] * (d[r + j] - y[j]);
+                    if (D > 64 && edge && row + 32 * b + result_row(r + j, l) < key) s[r + j] = 0.f;
+                    d[r + j] = D > 64 ? s[r + j] * (d[r + j] - y[j]) : d[r + j] - y[j];
                 }
+            }
+            // 64 wide in a branch of its own: 185 us (bf16, two sequences of 4096 rows, 16 heads of 64), in the loop above 229.  128 wide the loop's
+            // form leaves the registers alone: 2.80 ms (two sequences of 8192, 32 heads of 128 on 8), the branch with its limit 3.35
+            if (D <= 64) {
+                if (edge) clear_before(s, key - row - 32 * b);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) d[r] *= s[r];
             }
 #pragma unroll
             for (int p = 0; p < STEPS; ++p) {
