@@ -9,6 +9,7 @@
 // comes in behind the products: the label's entries p - 1 are near -1 and would otherwise all be rounded the same way).  Sums are fp32.
 // fp32: the convolution kernels' products, a piece of logits in the workspace at a time.
 #include <initializer_list>
+#include <type_traits>
 #include <vector>
 
 #include "../../include/monet_kernels.h"
@@ -231,17 +232,26 @@ __global__ __launch_bounds__(256) void ce_round_kernel(const float *__restrict__
     *(uint4 *)(out + i) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 
-// fp32: maximum and sum of a row's piece of logits, and the label's logit
+// fp32: maximum and sum of CE_SEGMENT logits of a row's piece (grid y: which), and the label's logit.  The logits are read once, into registers; a
+// row's segments go to different workgroups, since there may be a single row (92544 logits of it: 4.6 us, with one workgroup to a row 122).
+constexpr int CE_SEGMENT = 4096;
 __global__ __launch_bounds__(256) void ce_piece_stats_kernel(const float *__restrict__ logits, int piece, int v0, const int32_t *__restrict__ labels,
                                                              float2 *__restrict__ part, float *__restrict__ hit) {
     __shared__ Soft seg[256];
     const int64_t t = blockIdx.x;
     const float *row = logits + t * piece;
-    float top = -INFINITY;
-    for (int v = threadIdx.x; v < piece; v += 256) top = fmaxf(top, row[v]);
+    const int from = blockIdx.y * CE_SEGMENT, to = min(piece, from + CE_SEGMENT);
+    float x[CE_SEGMENT / 256], top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < CE_SEGMENT / 256; ++i) {
+        const int v = from + i * 256 + threadIdx.x;
+        x[i] = v < to ? row[v] : -INFINITY;
+        top = fmaxf(top, x[i]);
+    }
     const float base = top == -INFINITY ? 0.f : fminf(top, 3.4028235e38f);
     float sum = 0.f;
-    for (int v = threadIdx.x; v < piece; v += 256) sum += exp_of(row[v] - base);
+#pragma unroll
+    for (int i = 0; i < CE_SEGMENT / 256; ++i) sum += exp_of(x[i] - base);      // an index that does not exist: e^-inf, 0
     if (top == INFINITY) { top = 3.4028235e38f; sum = INFINITY; }
     seg[threadIdx.x] = Soft{top, sum};
     for (int w = 128; w; w /= 2) {
@@ -249,9 +259,9 @@ __global__ __launch_bounds__(256) void ce_piece_stats_kernel(const float *__rest
         if ((int)threadIdx.x < w) seg[threadIdx.x] = soft_join(seg[threadIdx.x], seg[threadIdx.x + w]);
     }
     if (threadIdx.x) return;
-    part[t] = make_float2(seg[0].m, seg[0].s);
+    part[blockIdx.y * (int64_t)gridDim.x + t] = make_float2(seg[0].m, seg[0].s);
     const int label = labels[t] - v0;
-    if (label >= 0 && label < piece) hit[t] = row[label];
+    if (label >= from && label < to) hit[t] = row[label];
 }
 // fp32: dl in the place of the logits
 __global__ __launch_bounds__(256) void ce_piece_grad_kernel(float *__restrict__ logits, int piece, int v0, const int32_t *__restrict__ labels,
@@ -264,10 +274,76 @@ __global__ __launch_bounds__(256) void ce_piece_grad_kernel(float *__restrict__ 
     *at = (unsigned)label < (unsigned)vocab ? (exp_of(*at - lse[t]) - (v0 + v == label ? 1.f : 0.f)) * *inv_count : 0.f;
 }
 
+// fp32 and few rows: dx += dl W, which reads all of W for rows * 2 operations an entry.  A matrix tile would be mostly empty, and its few
+// workgroups wait for memory; here a workgroup sums 256 columns over `per` entries of the piece on the vector units, rows from scalar
+// registers, and leaves part[range][row][column].  11 rows, 1120 columns, 41104 entries (184 MB): 48 us (3.8 TB/s), the convolutions'
+// tiles 91; 1 row, 144 columns, 92544 entries: 9 us, the tiles 188.
+constexpr int CE_FEW_ROWS = 16;
+template <int ROWS>
+__global__ __launch_bounds__(256) void ce_few_rows_kernel(const float *__restrict__ dl, int piece, const float *__restrict__ w, int width, int rows, int per,
+                                                          float *__restrict__ part) {
+    __shared__ float sums[4][ROWS][256];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x & 63, c0 = blockIdx.x * 256;
+    const int from = blockIdx.y * per, to = min(piece, from + per);
+    int col[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) col[j] = min(c0 + 64 * j + l, width - 1);
+    float acc[ROWS][4] = {};
+    auto add = [&](int v, auto n) {      // entries v .. v + n - 1; rows that do not exist take the last one's dl and are not stored
+        constexpr int N = decltype(n)::value;
+        float x[N][4];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[i][j] = w[(int64_t)(v + i) * width + col[j]];
+#pragma unroll
+        for (int t = 0; t < ROWS; ++t) {
+            const float *d = dl + (int64_t)min(t, rows - 1) * piece + v;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[t][j] = fmaf(d[i], x[i][j], acc[t][j]);
+        }
+    };
+    int v = from + 4 * wave;
+    for (; v + 4 <= to; v += 16) add(v, std::integral_constant<int, 4>());
+    for (const int end = min(to, v + 4); v < end; ++v) add(v, std::integral_constant<int, 1>());
+#pragma unroll
+    for (int t = 0; t < ROWS; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sums[wave][t][64 * j + l] = acc[t][j];
+    __syncthreads();
+    const int c = threadIdx.x;
+    if (c0 + c >= width) return;
+    for (int t = 0; t < rows; ++t)
+        part[((int64_t)blockIdx.y * rows + t) * width + c0 + c] = (sums[0][t][c] + sums[1][t][c]) + (sums[2][t][c] + sums[3][t][c]);
+}
+// out (+)= the sum over the ranges of part, in a fixed order: sixteen waves take a share of the ranges each
+__global__ __launch_bounds__(1024) void ce_few_rows_join_kernel(const float *__restrict__ part, int ranges, int n, float *__restrict__ out, int add) {
+    __shared__ float sums[16][64];
+    const int wave = threadIdx.x / 64, l = threadIdx.x & 63, i = blockIdx.x * 64 + l;
+    float sum = 0.f;
+    if (i < n) {
+#pragma unroll 8
+        for (int r = wave; r < ranges; r += 16) sum += part[(int64_t)r * n + i];
+    }
+    sums[wave][l] = sum;
+    __syncthreads();
+    if (wave || i >= n) return;
+#pragma unroll
+    for (int w = 1; w < 16; ++w) sum += sums[w][l];
+    out[i] = add ? out[i] + sum : sum;
+}
+
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 int64_t cut(int64_t n, int64_t by) { return (n + by - 1) / by; }
 
 constexpr int64_t CE_PIECE_BYTES = 256ll << 20;      // a piece of logits or of their gradient
+
+// Results of few tiles leave CUs idle while their reduction is long: as many ranges as fill the card, of at least `least` indices.
+int ce_splits(int64_t tiles, int64_t red, int64_t least) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), red / least, 16}));
+}
 
 // How a call goes through the vocabulary, and its workspace: forward [hit][row_loss][part][product][logits (fp32)], backward
 // [inv][dx parts (bf16) or product][dl].
@@ -277,12 +353,15 @@ struct CePlan {
     int unit = 0;                   // bf16 forward: logits to a part
     int piece = 0;                  // logits of a piece
     int ranges = 1, chunk = 0;      // bf16 backward: of the reduction over a piece in dx
-    int wgrad_splits = 1;           // fp32 backward
     int64_t product = 0;            // fp32: bytes for the products' partial results
     int64_t fixed = 0, per_col = 0;              // bytes without the pieces, and for each logit of a piece
 
-    int64_t parts() const { return bf16 ? cut(vocab, unit) : pieces().size(); }
     int64_t bytes() const { return fixed + per_col * piece; }
+    int wgrad_splits(int piece) const { return ce_splits(cut(width, 128) * cut(piece, 128), rows, 64); }
+    bool few_rows() const { return rows <= CE_FEW_ROWS; }
+    int few_per(int piece) const {      // entries of W for a workgroup: four workgroups to a CU
+        return (int)up(cut(piece, std::max<int64_t>(1, std::min<int64_t>(1024 / cut(width, 256), cut(piece, 64)))), 16);
+    }
     // where the pieces begin, and the vocabulary's end.  fp32: the products read 16 bytes at a time where the piece is a multiple of
     // 16, so what a large vocabulary has over that is a piece of its own
     std::vector<int> pieces() const {
@@ -290,14 +369,17 @@ struct CePlan {
         const int tail = !bf16 && vocab > 4096 ? vocab % 16 : 0;
         for (int v = 0; v < vocab - tail; v += piece) at.push_back(v);
         if (tail) at.push_back(vocab - tail);
+        at.push_back(vocab);
         return at;
     }
+    int64_t parts() const {
+        if (bf16) return cut(vocab, unit);
+        const std::vector<int> at = pieces();
+        int64_t n = 0;
+        for (size_t i = 0; i + 1 < at.size(); ++i) n += cut(at[i + 1] - at[i], CE_SEGMENT);
+        return n;
+    }
 };
-
-// Results of few tiles leave CUs idle while their reduction is long: as many ranges as fill the card, of at least `least` indices.
-int ce_splits(int64_t tiles, int64_t red, int64_t least) {
-    return (int)std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), red / least, 16}));
-}
 
 CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab) {
     if (dtype != MONET_F32 && dtype != MONET_BF16) throw KernelError("linear_ce: dtype must be MONET_F32 or MONET_BF16");
@@ -328,9 +410,13 @@ CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab) {
         p.ranges = (int)cut(std::min(p.piece, vocab), p.chunk);      // a later piece is no longer than the first
         if (p.ranges > 1 || p.piece < vocab) p.fixed += up(p.ranges * rows * width * 4, 256);
     } else {
-        p.wgrad_splits = ce_splits(cut(width, 128) * cut(p.piece, 128), rows, 64);
-        p.product = (int64_t)std::max(conv_workspace_bytes(0, cs, 1), conv_workspace_bytes(1, cs, 1));
-        if (p.wgrad_splits > 1) p.product = std::max(p.product, p.wgrad_splits * (int64_t)p.piece * width * 4);
+        p.product = (int64_t)std::max(conv_workspace_bytes(0, cs, 1), p.few_rows() ? 0 : conv_workspace_bytes(1, cs, 1));
+        const std::vector<int> at = p.pieces();
+        for (size_t i = 0; i + 1 < at.size(); ++i) {
+            const int64_t piece = at[i + 1] - at[i], splits = p.wgrad_splits((int)piece);
+            if (splits > 1) p.product = std::max(p.product, splits * piece * width * 4);
+            if (p.few_rows()) p.product = std::max(p.product, cut(piece, p.few_per((int)piece)) * rows * width * 4);
+        }
         p.product = up(p.product, 256);
         p.fixed += p.product;
     }
@@ -379,11 +465,13 @@ void linear_ce_fwd(hipStream_t st, int dtype, const void *x, const void *w, cons
         float *logits = (float *)((char *)ws + p.fixed), *product = p.product ? (float *)((char *)logits - p.product) : nullptr;
         const size_t product_bytes = (size_t)p.product;
         const std::vector<int> at = p.pieces();
-        for (size_t i = 0; i < at.size(); ++i) {
-            const int piece = (i + 1 < at.size() ? at[i + 1] : vocab) - at[i];
+        int64_t done = 0;      // parts
+        for (size_t i = 0; i + 1 < at.size(); ++i) {
+            const int piece = at[i + 1] - at[i], segments = (int)cut(piece, CE_SEGMENT);
             conv_fwd(st, (const float *)x, (const float *)w + (int64_t)at[i] * width, logits, ce_conv_shape(p, piece), 1, product, product_bytes);
-            hipLaunchKernelGGL(ce_piece_stats_kernel, dim3(p.rows), dim3(256), 0, st, logits, piece, at[i], labels, part + i * rows, hit);
+            hipLaunchKernelGGL(ce_piece_stats_kernel, dim3(p.rows, segments), dim3(256), 0, st, logits, piece, at[i], labels, part + done * rows, hit);
             hip_check(hipGetLastError(), "linear_ce statistics launch");
+            done += segments;
         }
     }
     hipLaunchKernelGGL(ce_merge_kernel, dim3((unsigned)cut(rows, 16)), dim3(256), 0, st, part, (int)p.parts(), hit, labels, lse, row_loss, p.rows, vocab);
@@ -404,8 +492,8 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
     const std::vector<int> at = p.pieces();
     char *dl = (char *)ws + p.fixed;
     float *parts = (float *)((char *)ws + 256);
-    for (size_t i = 0; i < at.size(); ++i) {
-        const int v0 = at[i], piece = (i + 1 < at.size() ? at[i + 1] : vocab) - v0;
+    for (size_t i = 0; i + 1 < at.size(); ++i) {
+        const int v0 = at[i], piece = at[i + 1] - v0;
         if (p.bf16) {
             unsigned short *d = (unsigned short *)dl;
             const int64_t ld = up(piece, 8);
@@ -417,11 +505,11 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
             g.b = d; g.ldb = ld;
             g.m = width; g.n = p.rows; g.k = piece;
             g.chunk = p.chunk; g.splits = (int)cut(piece, p.chunk);
-            if (p.ranges == 1 && at.size() == 1 && !accumulate)
+            if (p.ranges == 1 && at.size() == 2 && !accumulate)
                 gemm_bf16<true, false>(st, g, RoundEpilogue{(unsigned short *)dx, inv, width}, "linear_ce input gradient launch");
             else {
                 gemm_bf16<true, false>(st, g, SumEpilogue{parts, width, rows * width, i > 0}, "linear_ce input gradient launch");
-                if (i + 1 == at.size()) {
+                if (i + 2 == at.size()) {
                     const int64_t n = rows * width;
                     hipLaunchKernelGGL(ce_round_kernel, dim3((unsigned)cut(n, 2048)), dim3(256), 0, st, parts, p.ranges, n, inv, (unsigned short *)dx, accumulate);
                     hip_check(hipGetLastError(), "linear_ce round launch");
@@ -441,9 +529,21 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
             conv_fwd(st, (const float *)x, wp, d, cs, 1, product, product_bytes);
             hipLaunchKernelGGL(ce_piece_grad_kernel, dim3(p.rows, (unsigned)cut(piece, 256)), dim3(256), 0, st, d, piece, v0, labels, lse, inv, vocab);
             hip_check(hipGetLastError(), "linear_ce gradient launch");
-            conv_dgrad(st, d, wp, (float *)dx, cs, accumulate || i > 0, 1, product, product_bytes);
-            conv_wgrad(st, (const float *)x, d, (float *)dw + (int64_t)v0 * width, cs, p.wgrad_splits, p.wgrad_splits > 1 ? product : nullptr,
-                       p.wgrad_splits > 1 ? product_bytes : 0);
+            if (p.few_rows()) {
+                const int per = p.few_per(piece), ranges = (int)cut(piece, per), n = p.rows * width;
+                const dim3 grid((unsigned)cut(width, 256), ranges);
+                if (rows <= 4)
+                    hipLaunchKernelGGL(ce_few_rows_kernel<4>, grid, dim3(256), 0, st, d, piece, wp, width, p.rows, per, product);
+                else
+                    hipLaunchKernelGGL(ce_few_rows_kernel<CE_FEW_ROWS>, grid, dim3(256), 0, st, d, piece, wp, width, p.rows, per, product);
+                hip_check(hipGetLastError(), "linear_ce input gradient launch");
+                hipLaunchKernelGGL(ce_few_rows_join_kernel, dim3((unsigned)cut(n, 64)), dim3(1024), 0, st, product, ranges, n, (float *)dx, accumulate || i > 0);
+                hip_check(hipGetLastError(), "linear_ce input gradient sum launch");
+            } else {
+                conv_dgrad(st, d, wp, (float *)dx, cs, accumulate || i > 0, 1, product, product_bytes);
+            }
+            const int splits = p.wgrad_splits(piece);
+            conv_wgrad(st, (const float *)x, d, (float *)dw + (int64_t)v0 * width, cs, splits, splits > 1 ? product : nullptr, splits > 1 ? product_bytes : 0);
         }
     }
 }

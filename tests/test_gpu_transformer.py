@@ -333,6 +333,13 @@ def test_linear_ce_matches_64_bits(case, dtype):
 
 
 @pytest.mark.parametrize("dtype", [monet.F32, monet.BF16])
+@pytest.mark.parametrize("case", [(1, 144, 8209), (4, 40, 4096), (5, 264, 4113), (16, 1032, 12304), (17, 520, 4097)])
+def test_linear_ce_of_few_rows(case, dtype):
+    """Few rows take the input's gradient over ranges of the vocabulary; a row's logits in segments of 4096."""
+    test_linear_ce_matches_64_bits(case, dtype)
+
+
+@pytest.mark.parametrize("dtype", [monet.F32, monet.BF16])
 def test_linear_ce_without_a_label(dtype):
     torch = torch_mod()
     x, w = torch.randn(20, 64, device="cuda").to(tdtype(dtype)), torch.randn(300, 64, device="cuda").to(tdtype(dtype))
