@@ -345,6 +345,16 @@ int ce_splits(int64_t tiles, int64_t red, int64_t least) {
     return (int)std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), red / least, 16}));
 }
 
+// Ranges of the reduction over a piece in dx = dl W.  Large tiles (gemm_tile) where ranges of 4096 entries or more make whole rounds of one to a CU
+// (a range's fp32 sums cost 8 bytes of traffic for each result) and few of their entries lie outside the result: backward pass of 512 rows,
+// 2048 columns, 100000 entries 830 us, with small tiles 997; 4096 rows, 2048 columns, 50176 entries 2459 and 2542.  Small ones otherwise:
+// 4000 rows, 1600 columns, 50257 entries (112 large tiles; three ranges are 1.3 rounds) 2126 us, with large ones 2248.
+int ce_input_ranges(int64_t rows, int64_t width, int piece) {
+    const int64_t large = cut(width, 256) * cut(rows, 256), ranges = cut(256, large);
+    if (ranges <= 16 && piece / ranges >= 4096 && 5 * rows * width * ranges >= 4 * 65536 * up(large * ranges, 256)) return (int)ranges;
+    return ce_splits(cut(width, 128) * cut(rows, 128), piece, 512);
+}
+
 // How a call goes through the vocabulary, and its workspace: forward [hit][row_loss][part][product][logits (fp32)], backward
 // [inv][dx parts (bf16) or product][dl].
 struct CePlan {
@@ -405,7 +415,7 @@ CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab) {
     }
     p.fixed = 256;
     if (bf16) {
-        p.ranges = ce_splits(cut(width, 128) * cut(rows, 128), p.piece, 512);
+        p.ranges = ce_input_ranges(rows, width, p.piece);
         p.chunk = (int)up(cut(p.piece, p.ranges), GEMM_DEPTH);
         p.ranges = (int)cut(std::min(p.piece, vocab), p.chunk);      // a later piece is no longer than the first
         if (p.ranges > 1 || p.piece < vocab) p.fixed += up(p.ranges * rows * width * 4, 256);
