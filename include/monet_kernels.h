@@ -261,13 +261,14 @@ enum monet_dtype { MONET_F32 = 0, MONET_BF16 = 1 };
  * cu_seqlens[s] .. cu_seqlens[s + 1] - 1 and may be empty.  Tokens before the first and behind the last one are neither read
  * nor written, in any output.  Offsets are held to 0 .. tokens, so that others cannot lead out of the tensors.
  * Needs heads % kv_heads == 0, head_dim a multiple of 8 up to 128, scale > 0, pointers and strides that are multiples of
- * 16 bytes, tokens below 2^31.  tokens == 0 is allowed and does nothing.  A sequence's infinities and NaNs stay in that sequence.
- * Within it, one in k or v reaches the rows from its own on and may reach up to 127 rows before it. */
+ * 16 bytes, tokens below 2^31, (tokens / 64 + seqs) * heads below 2^24; o must not overlap an input.  tokens == 0 is allowed and does nothing.  A sequence's infinities and NaNs stay in that sequence.
+ * Within it, one in k or v reaches the rows from its own on and may reach up to 127 rows before it.  fp32: the products go through
+ * three bf16 pieces of each operand, exact from 2^-110 up; an infinity in a tensor comes out as NaN. */
 int monet_attention_fwd(void *stream, int dtype, const void *q, const void *k, const void *v, void *o, float *lse,
                         const int32_t *cu_seqlens, int seqs, int64_t tokens, int heads, int kv_heads, int head_dim,
                         int64_t q_ld, int64_t k_ld, int64_t v_ld, int64_t o_ld, float scale);
 /* Its gradients from d(o), the inputs, o and lse: the probabilities are computed again.  dout has o's stride, dq q's, dk k's, dv v's;
- * dk and dv are the sums over a group's heads.  The three results must not overlap.  accumulate: bit 0, 1, 2 adds to dq, dk, dv instead of writing them.
+ * dk and dv are the sums over a group's heads.  The three results must overlap neither each other nor an input.  accumulate: bit 0, 1, 2 adds to dq, dk, dv instead of writing them.
  * Workspace: monet_attention_bwd_workspace_bytes. */
 int monet_attention_bwd(void *stream, int dtype, const void *dout, const void *q, const void *k, const void *v, const void *o,
                         const float *lse, void *dq, void *dk, void *dv, const int32_t *cu_seqlens, int seqs, int64_t tokens,
@@ -278,12 +279,12 @@ int64_t monet_attention_bwd_workspace_bytes(int dtype, int seqs, int64_t tokens,
 /* Softmax cross entropy of a linear layer over a large vocabulary, in pieces of the vocabulary; the logits x w^T are not kept.
  * x [rows][width], w [vocab][width], labels [rows]; a row whose label is outside 0 .. vocab - 1 carries no loss and no gradient.
  *   lse[row] = log sum exp of the row's logits (all rows);  loss = mean over the rows with a label of lse - logit[label], 0 if there are none.
- * Needs, for bf16, width % 8 == 0 and 16-byte aligned x and w; rows at most 2^24, width 2^20, vocab 2^28.
+ * Needs, for bf16, width % 8 == 0 and 16-byte aligned x and w; rows below 2^24, width at most 2^20, vocab 2^28.
  * ws_bytes >= monet_linear_ce_workspace_bytes(grad = 0, ...). */
 int monet_linear_ce_fwd(void *stream, int dtype, const void *x, const void *w, const int32_t *labels, float *loss, float *lse,
                         int64_t rows, int width, int vocab, void *ws, size_t ws_bytes);
 /* The mean loss's gradients: dx [rows][width] (added to if accumulate != 0), dw [vocab][width] (written), in the tensors' type.
- * The logits are computed again from x, w and lse, a piece at a time, and a piece's gradient is held in the workspace.  bf16: it is
+ * Neither overlaps the other or an input.  The logits are computed again from x, w and lse, a piece at a time, and a piece's gradient is held in the workspace.  bf16: it is
  * rounded to bf16 there, the sums over it are fp32.  ws_bytes >= monet_linear_ce_workspace_bytes(grad = 1, ...), which is also
  * enough for the forward call. */
 int monet_linear_ce_bwd(void *stream, int dtype, const void *x, const void *w, const int32_t *labels, const float *lse, void *dx,
@@ -294,7 +295,7 @@ int64_t monet_linear_ce_workspace_bytes(int grad, int dtype, int64_t rows, int w
  * smallest from e = -126 up with max|x| / 2^e < 127.5, and a code is x / 2^e rounded to nearest, ties to even.  A group with an
  * infinity or a NaN stands for NaN throughout.  code: monet_act8_bytes(rows, cols) bytes, 16-byte aligned: rows of
  * round_up(cols, 32) signed codes (zero behind the last column), then rows of one byte e + 127 per group.  ld: elements from one
- * row of x (y) to the next.  code * 2^e is exact in fp32 and bf16, so unpack rounds nothing. */
+ * row of x (y) to the next; rows * round_up(cols, 32) below 2^35.  code * 2^e is exact in fp32 and bf16, so unpack rounds nothing. */
 int64_t monet_act8_bytes(int64_t rows, int64_t cols);
 int monet_act8_pack(void *stream, int dtype, const void *x, int64_t ld, void *code, int64_t rows, int64_t cols);
 int monet_act8_unpack(void *stream, int dtype, const void *code, void *y, int64_t ld, int64_t rows, int64_t cols);

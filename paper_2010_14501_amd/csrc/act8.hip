@@ -330,15 +330,15 @@ struct WgradPlan {
 constexpr int64_t ACT8_TURN_BYTES = 256ll << 20;
 WgradPlan wgrad_plan(int dtype, int64_t rows, int cols, int outs, bool aligned) {
     WgradPlan p{};
-    p.expanded = 2.0 * rows * cols * outs >= (dtype == MONET_F32 ? 2e11 : 1.2e10);
-    p.tile = p.expanded ? gemm_tile(cols, outs) : 128;
     p.ld = (int)code_ld(cols);
+    p.expanded = 2.0 * rows * cols * outs >= (dtype == MONET_F32 ? 2e11 : 1.2e10) && std::max<int64_t>(p.ld, up(outs, 8)) < GEMM_MOST_LD;
+    p.tile = p.expanded ? gemm_tile(cols, outs) : 128;
     p.planes = dtype == MONET_F32 ? 3 : 1;
     p.copy = dtype == MONET_F32 || outs % 8 || !aligned;
     p.ldo = p.copy ? (int)up(outs, 8) : outs;
     p.turn = rows;
     if (p.expanded) {
-        const int64_t per_row = 2 * ((int64_t)p.ld + (p.copy ? p.planes * (int64_t)p.ldo : 0));
+        const int64_t per_row = 2 * (p.ld + p.planes * up(outs, 8));      // as if dy were copied: turns and ranges do not depend on where it lies
         const int64_t turns = (rows * per_row + ACT8_TURN_BYTES - 1) / ACT8_TURN_BYTES;
         p.turn = up((rows + turns - 1) / turns, 64);
         const int64_t held = std::min(p.turn, rows);
@@ -369,7 +369,7 @@ void act8_pack(hipStream_t st, int dtype, const void *x, int64_t ld, void *code,
     if (ld < cols) throw KernelError("act8_pack: row stride below the number of columns");
     const int per_row = (int)(code_ld(cols) / 8);
     const int64_t blocks = (rows * per_row + 255) / 256;
-    if (blocks > 0x7fffffff) throw KernelError("act8_pack: too many values");
+    if (blocks >= 1 << 24) throw KernelError("act8_pack: too many values");
     uint8_t *exps = (uint8_t *)code + rows * code_ld(cols);
     if (dtype == MONET_F32)
         hipLaunchKernelGGL((act8_pack_kernel<float>), dim3((unsigned)blocks), dim3(256), 0, st, (const float *)x, ld, (int8_t *)code, exps, rows, (int)cols, per_row);
@@ -387,7 +387,7 @@ void act8_unpack(hipStream_t st, int dtype, const void *code, void *y, int64_t l
     if (ld < cols) throw KernelError("act8_unpack: row stride below the number of columns");
     const int per_row = (int)(code_ld(cols) / 8);
     const int64_t blocks = (rows * per_row + 255) / 256;
-    if (blocks > 0x7fffffff) throw KernelError("act8_unpack: too many values");
+    if (blocks >= 1 << 24) throw KernelError("act8_unpack: too many values");
     const uint8_t *exps = (const uint8_t *)code + rows * code_ld(cols);
     if (dtype == MONET_F32)
         hipLaunchKernelGGL((act8_unpack_kernel<float>), dim3((unsigned)blocks), dim3(256), 0, st, (const int8_t *)code, exps, (float *)y, ld, rows, (int)cols, per_row);
@@ -455,7 +455,7 @@ void act8_wgrad(hipStream_t st, int dtype, const void *code, const void *dy, flo
         g.tiles_m = (int)((cols + 127) / 128);
         g.tiles_n = (int)((outs + 127) / 128);
         g.vec_out = vec_out;
-        if ((int64_t)g.tiles_m * g.tiles_n > 0x7fffffff) throw KernelError("act8_wgrad: result too large");
+        if ((int64_t)g.tiles_m * g.tiles_n >= 1 << 24) throw KernelError("act8_wgrad: result too large");
         const dim3 grid(g.tiles_m * g.tiles_n, p.splits);
         if (dtype == MONET_F32) hipLaunchKernelGGL((act8_wgrad_kernel<true, 128, 128, 2, 2>), grid, dim3(256), 0, st, g);
         else hipLaunchKernelGGL((act8_wgrad_kernel<false, 128, 128, 2, 2>), grid, dim3(256), 0, st, g);

@@ -769,7 +769,7 @@ AttShape att_shape(int dtype, const int32_t *cu, int seqs, int64_t tokens, int h
         if (ld < (int64_t)heads * head_dim || ld % step || ld >= (1 << 23)) throw KernelError("attention: row strides must hold all heads, be a multiple of 16 bytes and below 2^23 elements");
     for (int64_t ld : {k_ld, v_ld})
         if (ld < (int64_t)kv_heads * head_dim || ld % step || ld >= (1 << 23)) throw KernelError("attention: row strides must hold all heads, be a multiple of 16 bytes and below 2^23 elements");
-    if (tokens > 0x7fffffff || (tokens / 32 + seqs) * heads > 0x7fffffff) throw KernelError("attention: too many tokens");
+    if (tokens > 0x7fffffff || (tokens / 64 + seqs) * heads >= 1 << 24) throw KernelError("attention: too many tokens");
     if (!cu) throw KernelError("attention: null pointer");
     return AttShape{cu, seqs, (int)tokens, heads, kv_heads, head_dim, 0, q_ld, k_ld, v_ld, o_ld, scale};
 }

@@ -173,13 +173,16 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN * 64 / 256) void gemm_bf16_kern
     epi(acc, tm * BM + wm, tn * BN + wn, g.m, g.n);
 }
 
+constexpr int64_t GEMM_MOST_LD = 1 << 23;      // row strides are below this: 256 rows in 32 bits of a buffer's offset
+
 // Tiles of 256 x 256 (8 waves) where they give every CU one, of 128 x 128 (4 waves, two workgroups a CU) otherwise.
 inline int gemm_tile(int64_t m, int64_t n, int splits = 1) { return ((m + 255) / 256) * ((n + 255) / 256) * splits >= 256 ? 256 : 128; }
 template <bool A_DEEP, bool B_DEEP, class Epi>
 void gemm_bf16(hipStream_t st, GemmShape g, const Epi &epi, const char *what) {
-    const auto tiles = [&](int64_t b) { return ((g.m + b - 1) / b) * ((g.n + b - 1) / b); };
+    const auto tiles = [&](int64_t b) { return (g.m + b - 1) / b * ((g.n + b - 1) / b); };
     const int b = gemm_tile(g.m, g.n, g.splits);
-    if (g.lda >= (1 << 23) || g.ldb >= (1 << 23) || g.lda % 8 || g.ldb % 8 || tiles(128) > 0x7fffffff) throw KernelError(std::string(what) + ": operand too large");
+    // a launch takes less than 2^32 threads
+    if (g.lda >= GEMM_MOST_LD || g.ldb >= GEMM_MOST_LD || g.lda % 8 || g.ldb % 8 || tiles(b) >= (b == 256 ? 1 << 23 : 1 << 24)) throw KernelError(std::string(what) + ": operand too large");
     g.tiles_m = (g.m + b - 1) / b;
     g.tiles_n = (g.n + b - 1) / b;
     const dim3 grid(g.tiles_m * g.tiles_n, g.splits);

@@ -396,7 +396,7 @@ CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab) {
     if (rows < 1 || width < 1 || vocab < 1) throw KernelError("linear_ce: bad shape");
     const bool bf16 = dtype == MONET_BF16;
     if (bf16 && width % 8) throw KernelError("linear_ce: bf16 needs a width that is a multiple of 8");
-    if (rows > (1 << 24) || width > (1 << 20) || vocab > (1 << 28)) throw KernelError("linear_ce: shape too large");
+    if (rows >= (1 << 24) || width > (1 << 20) || vocab > (1 << 28)) throw KernelError("linear_ce: shape too large");
     CePlan p{(int)rows, width, vocab, bf16};
     if (bf16 && !grad) {
         p.unit = gemm_tile(vocab, rows) / 2;
@@ -406,7 +406,7 @@ CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab) {
     p.per_col = up(rows * (bf16 ? 2 : 4), 256);
     const int64_t pieces = cut(vocab, std::max<int64_t>(CE_PIECE_BYTES / p.per_col / 256 * 256, 256));
     p.piece = (int)std::min<int64_t>(up(cut(vocab, pieces), 256), 1 << 20);
-    if (!bf16) p.piece = std::min(p.piece, vocab);
+    if (!bf16) p.piece = std::min<int64_t>({p.piece, vocab, std::max<int64_t>(((1ll << 32) - (1 << 21)) / (4 * (int64_t)width) / 256 * 256, 256)});      // the products address a piece of w with 32 bits
     const ConvShape cs{p.rows, 1, 1, width, p.piece, 1, 1, 1, 0, 1, 1};
     if (!grad) {
         p.product = up((int64_t)conv_workspace_bytes(0, cs, 1), 256);

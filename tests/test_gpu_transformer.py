@@ -485,6 +485,49 @@ def test_act8_wgrad_of_large_layers(dtype, rows, cols, outs):
     assert ((dw.double() - want).norm() / want.norm()).item() < 2e-6
 
 
+def test_act8_wgrad_stays_in_its_workspace():
+    """dy that the products read where it lies (bf16, rows of 16 bytes) takes no other turns than dy that is copied."""
+    torch = torch_mod()
+    rows, cols, outs = 32000, 4096, 160          # rows of codes alone would fit one turn, with dy beside them they take two
+    g = torch.Generator(device="cuda")
+    g.manual_seed(6)
+    x = torch.randn(rows, cols, generator=g, device="cuda")
+    dy = torch.randn(rows * outs + 8, generator=g, device="cuda").bfloat16()
+    code = torch.zeros(monet.call("monet_act8_bytes", rows, cols), dtype=torch.uint8, device="cuda")
+    monet.call("monet_act8_pack", None, monet.F32, x.data_ptr(), cols, code.data_ptr(), rows, cols)
+    monet.call("monet_act8_unpack", None, monet.F32, code.data_ptr(), x.data_ptr(), cols, rows, cols)
+    need = monet.call("monet_act8_wgrad_workspace_bytes", monet.BF16, rows, cols, outs)
+    ws = torch.full((need + (256 << 20),), 7, dtype=torch.uint8, device="cuda")
+    for shift in (0, 1):
+        src = dy[shift:shift + rows * outs].view(rows, outs)
+        dw = torch.full((outs, cols), float("nan"), device="cuda")
+        monet.call("monet_act8_wgrad", None, monet.BF16, code.data_ptr(), src.data_ptr(), dw.data_ptr(), rows, cols, outs, ws.data_ptr(), need)
+        assert (ws[need:] == 7).all()
+        want, mag = src.double().t() @ x.double(), src.double().abs().t() @ x.double().abs()
+        assert ((dw.double() - want).abs() <= 1.1 * (3 * rows + 8) * U * mag).all()
+
+
+def test_act8_wgrad_of_very_wide_rows():
+    """Rows of 2^23 columns and more are beyond the reach of the large products' addresses: the other form takes them."""
+    torch = torch_mod()
+    rows, cols, outs = 16, (1 << 23) + 5, 48
+    g = torch.Generator(device="cuda")
+    g.manual_seed(7)
+    x = torch.randn(rows, cols, generator=g, device="cuda").bfloat16()
+    dy = torch.randn(rows, outs, generator=g, device="cuda").bfloat16()
+    code = torch.zeros(monet.call("monet_act8_bytes", rows, cols), dtype=torch.uint8, device="cuda")
+    monet.call("monet_act8_pack", None, monet.BF16, x.data_ptr(), cols, code.data_ptr(), rows, cols)
+    monet.call("monet_act8_unpack", None, monet.BF16, code.data_ptr(), x.data_ptr(), cols, rows, cols)
+    need = monet.call("monet_act8_wgrad_workspace_bytes", monet.BF16, rows, cols, outs)
+    ws = torch.zeros(max(need, 16), dtype=torch.uint8, device="cuda")
+    dw = torch.full((outs, cols), float("nan"), device="cuda")
+    monet.call("monet_act8_wgrad", None, monet.BF16, code.data_ptr(), dy.data_ptr(), dw.data_ptr(), rows, cols, outs, ws.data_ptr(), need)
+    for at in (slice(0, 5000), slice(cols // 2, cols // 2 + 5000), slice(cols - 5000, cols)):
+        want, mag = dy.double().t() @ x[:, at].double(), dy.double().abs().t() @ x[:, at].double().abs()
+        assert ((dw[:, at].double() - want).abs() <= 1.1 * (rows + 8) * U * mag).all()
+    assert torch.isfinite(dw).all()
+
+
 def test_act8_wgrad_of_a_marked_group():
     """A group that stands for NaN makes its 32 columns NaN and no others."""
     torch = torch_mod()
@@ -500,3 +543,100 @@ def test_act8_wgrad_of_a_marked_group():
     monet.call("monet_act8_wgrad", None, monet.BF16, code.data_ptr(), dy.data_ptr(), dw.data_ptr(), rows, cols, outs, ws.data_ptr(), need)
     bad = torch.isnan(dw)
     assert bad[:, 32:64].all() and not bad[:, :32].any() and not bad[:, 64:].any()
+
+
+# ---------------------------------------------------------------------- large and busy
+def test_attention_beyond_32_bits():
+    """Rows of 2^22 elements that hold every tensor side by side: offsets pass 2^32 elements, and the results are those of compact tensors."""
+    torch = torch_mod()
+    n, heads, kv_heads, dim, ld = 1200, 2, 1, 64, 1 << 22
+    g = torch.Generator(device="cuda")
+    g.manual_seed(8)
+    cu = torch.tensor([0, 700, 1200], dtype=torch.int32, device="cuda")
+    q, do = (torch.randn(n, heads * dim, generator=g, device="cuda").bfloat16() for _ in range(2))
+    k, v = (torch.randn(n, kv_heads * dim, generator=g, device="cuda").bfloat16() for _ in range(2))
+    want = attention_call(monet.BF16, q, k, v, do, cu, heads, kv_heads, dim, 0.125)
+    wide = torch.empty(n, ld, dtype=torch.bfloat16, device="cuda")
+    at = {name: wide[:, 1024 * i:1024 * i + t.shape[1]] for i, (name, t) in enumerate(
+        dict(q=q, k=k, v=v, do=do, o=q, dq=q, dk=k, dv=v).items())}
+    for name, t in dict(q=q, k=k, v=v, do=do).items():
+        at[name].copy_(t)
+    lse = torch.empty(heads, n, device="cuda")
+    need = monet.call("monet_attention_bwd_workspace_bytes", monet.BF16, 2, n, heads, kv_heads, dim)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    shape = (2, n, heads, kv_heads, dim, ld, ld, ld, ld, 0.125)
+    p = {name: t.data_ptr() for name, t in at.items()}
+    monet.call("monet_attention_fwd", None, monet.BF16, p["q"], p["k"], p["v"], p["o"], lse.data_ptr(), cu.data_ptr(), *shape)
+    monet.call("monet_attention_bwd", None, monet.BF16, p["do"], p["q"], p["k"], p["v"], p["o"], lse.data_ptr(), p["dq"], p["dk"], p["dv"],
+               cu.data_ptr(), *shape, 0, ws.data_ptr(), need)
+    for a, b in zip((at["o"], lse, at["dq"], at["dk"], at["dv"]), want):
+        assert torch.equal(a.reshape(-1), b.reshape(-1))
+
+
+@pytest.mark.parametrize("dtype", [monet.F32, monet.BF16])
+def test_linear_ce_beyond_32_bits(dtype):
+    """x and dx of more than 2^31 elements: the last rows' lse and gradient, and dw's, against 64 bits."""
+    torch = torch_mod()
+    rows, width, vocab = 530000, 4096, 40
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    x = torch.randn(rows, width, generator=g, device="cuda", dtype=tdtype(dtype))
+    w = (torch.randn(vocab, width, generator=g, device="cuda") * 0.02).to(tdtype(dtype))
+    lab = torch.randint(0, vocab, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    loss, lse, dx, dw = linear_ce_call(dtype, x, w, lab)
+    wd, total, bound = w.double(), torch.zeros(vocab, width, device="cuda", dtype=torch.float64), torch.zeros(vocab, width, device="cuda", dtype=torch.float64)
+    mean = 0.0
+    rp = R if dtype == monet.BF16 else 0.0
+    for at in range(0, rows, 53000):
+        xs, ls = x[at:at + 53000].double(), lab[at:at + 53000].long()
+        logits = xs @ wd.t()
+        want = torch.logsumexp(logits, 1)
+        # a logit is off by (width + 2) U of its terms' sum, at most 0.02 * 4096 or so in all; what follows adds a few U
+        err = (width + vocab + 16) * U * (xs.abs() @ wd.abs().t()).max(1).values
+        assert ((lse[at:at + 53000].double() - want).abs() <= 1.1 * err).all()
+        mean += (want - logits.gather(1, ls[:, None])[:, 0]).sum().item()
+        dl = torch.exp(logits - want[:, None])
+        edl = dl * (2 * err[:, None] + 8 * U)
+        dl[torch.arange(dl.shape[0], device="cuda"), ls] -= 1.0
+        edl += (rp + 4 * U) * dl.abs()
+        d = dl @ wd / rows
+        ed = (edl + (vocab + 8) * U * dl.abs()) @ wd.abs() / rows + rp * d.abs()
+        assert ((dx[at:at + 53000].double() - d).abs() <= 1.1 * ed + 1e-30).all()
+        total += dl.t() @ xs / rows
+        bound += (edl + (rows + 8) * U * dl.abs()).t() @ xs.abs() / rows
+    assert ((dw.double() - total).abs() <= 1.1 * (bound + rp * total.abs())).all()
+    assert abs(loss.item() - mean / rows) < 1e-5 * mean / rows
+
+
+def test_calls_on_two_streams_at_once():
+    """Calls that share their inputs and run at the same time, each with results and a workspace of its own."""
+    torch = torch_mod()
+    rng = np.random.default_rng(13)
+    heads, dim, n = 4, 64, 2000
+    ref, gpu = attention_inputs(rng, n, heads, heads, dim, monet.BF16)
+    cu = torch.tensor([0, 900, 2000], dtype=torch.int32, device="cuda")
+    x = torch.randn(n, 256, device="cuda")
+    w = torch.randn(5003, 256, device="cuda") * 0.1
+    lab = torch.randint(-1, 5003, (n,), device="cuda", dtype=torch.int32)
+    dy = torch.randn(n, 320, device="cuda")
+
+    def all_of_them():
+        code = torch.zeros(monet.call("monet_act8_bytes", n, 256), dtype=torch.uint8, device="cuda")
+        need = monet.call("monet_act8_wgrad_workspace_bytes", monet.F32, n, 256, 320)
+        ws, dw = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda"), torch.empty(320, 256, device="cuda")
+        s = torch.cuda.current_stream().cuda_stream
+        monet.call("monet_act8_pack", s, monet.F32, x.data_ptr(), 256, code.data_ptr(), n, 256)
+        monet.call("monet_act8_wgrad", s, monet.F32, code.data_ptr(), dy.data_ptr(), dw.data_ptr(), n, 256, 320, ws.data_ptr(), need)
+        out = [code, dw, *linear_ce_call(monet.F32, x, w, lab), *linear_ce_call(monet.BF16, x.bfloat16(), w.bfloat16(), lab)]
+        return out + list(attention_call(monet.BF16, *gpu, cu, heads, heads, dim, 0.125)), ws
+    want, _ = all_of_them()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        got = []
+        for st in streams:
+            with torch.cuda.stream(st):
+                got.append(all_of_them())
+        torch.cuda.synchronize()
+        for out, _ in got:
+            assert all(torch.equal(a, b) for a, b in zip(out, want))

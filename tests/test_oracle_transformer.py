@@ -164,5 +164,15 @@ def test_act8_refuses(name, args, match):
     refused(name, args, match)
 
 
+def test_calls_of_more_threads_than_a_launch_takes_are_refused():
+    tail = [8 * 64, 4 * 64, 4 * 64, 8 * 64, 0.125]
+    refused("monet_attention_fwd", [None, monet.BF16, P, P, P, P, P, P, 3, 1 << 27, 8, 4, 64] + tail, "too many")
+    refused("monet_attention_fwd", [None, monet.BF16, P, P, P, P, P, P, 1 << 21, 64, 8, 4, 64] + tail, "too many")
+    refused("monet_linear_ce_fwd", [None, monet.F32, P, P, P, P, P, 1 << 24, 64, 1000, P, 1 << 40], "too large")
+    refused("monet_linear_ce_fwd", [None, monet.BF16, P, P, P, P, P, (1 << 24) - 1, 64, 1 << 28, P, 1 << 60], "too large")
+    for name, args in (("monet_act8_pack", (P, 1 << 24, P)), ("monet_act8_unpack", (P, P, 1 << 24))):
+        refused(name, [None, monet.BF16, *args, 1 << 11, 1 << 24], "too many")
+
+
 def test_act8_bytes():
     assert monet.call("monet_act8_bytes", 5, 32) == 5 * 33 and monet.call("monet_act8_bytes", 5, 33) == 5 * 66
