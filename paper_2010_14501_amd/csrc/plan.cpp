@@ -303,6 +303,7 @@ static void check_transformer_nodes(const Graph &g) {
         if (n.op == "attention") {
             const int64_t heads = n.attr_int("heads"), kv = n.attr_int("kv_heads"), dim = n.attr_int("dim"), seqs = n.attr_int("seqs");
             need(heads > 0 && kv > 0 && heads % kv == 0 && dim > 0 && seqs > 0, "heads, kv_heads, dim and seqs must be positive, heads a multiple of kv_heads");
+            need(dim % 8 == 0 && dim <= 128, "dim must be a multiple of 8 up to 128");
             need(n.ins.size() == 4 && n.ins[0] > 0 && n.ins[1] > 0 && n.ins[2] > 0, "inputs are three nodes and the sequences' offsets");
             need(n.ins[0] != n.ins[1] && n.ins[0] != n.ins[2] && n.ins[1] != n.ins[2], "queries, keys and values must be three tensors");
             need(n.shape.size() == 2 && n.shape[1] == heads * dim && g.shape_of(n.ins[0]) == n.shape, "queries and output must be tokens x (heads * dim)");

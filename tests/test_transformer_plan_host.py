@@ -67,6 +67,7 @@ def test_gradients_agree_over_schedules_and_with_differences():
     ("heads=4 kv_heads=2 dim=16", "heads=4 kv_heads=3 dim=16", "multiple of kv_heads"),
     ("heads=4 kv_heads=2 dim=16", "heads=4 kv_heads=2 dim=8", "tokens x"),
     ("heads=4 kv_heads=2 dim=16", "heads=4 kv_heads=1 dim=16", "keys and values"),
+    ("heads=4 kv_heads=2 dim=16", "heads=16 kv_heads=8 dim=4", "multiple of 8"),
     ("seqs=3", "seqs=4", "offsets"),
     ("ext -2 cu_seqlens i32 4", "ext -2 cu_seqlens f32 4", "offsets"),
     ("ext -1 labels i32 64", "ext -1 labels i32 63", "labels"),
