@@ -31,6 +31,8 @@ namespace {
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
+__device__ __forceinline__ int uniform_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }      // in a scalar register, as is what follows from it
+
 // The rows of a 32 x 32 result that lie before `limit` are not the lane's key's: their probabilities are 0.  The limit passes through a register of
 // its own inside the branch that this stands in, or the compiler compares for every tile what only those on the diagonal need.
 __device__ __forceinline__ void clear_before(floatx16 &s, int limit) {
@@ -101,26 +103,29 @@ template <> struct Piece<float> {
 template <class T, int D, int R> struct AttTile;
 template <int D, int R>
 struct AttTile<unsigned short, D, R> {         // straight from memory to LDS
-    static constexpr int BYTES = R * D * 2, COPIES = BYTES / (256 * 16);
-    unsigned off[COPIES];
+    // a copy takes 32 rows of a strip; the turns repeat after 16, so a strip's offsets serve all of its copies
+    static constexpr int BYTES = R * D * 2, STRIPS = D / 64;
+    unsigned off[STRIPS];
     int64_t ld;
     int used;               // bytes of a row that exist
     __device__ __forceinline__ void init(int64_t ld_, int head_dim) {
         ld = ld_;
         used = head_dim * 2;
 #pragma unroll
-        for (int i = 0; i < COPIES; ++i) {
-            const unsigned piece = i * 256 + threadIdx.x, strip = piece / (R * 8), row = piece / 8 % R, c = (piece % 8) ^ wide_turn(row);
-            const unsigned col = strip * 128 + c * 16;
+        for (int i = 0; i < STRIPS; ++i) {
+            const unsigned row = threadIdx.x / 8, col = i * 128 + (((threadIdx.x % 8) ^ wide_turn(row)) << 4);
             off[i] = (int)col < used ? row * (unsigned)(ld * 2) + col : BUFFER_ABSENT;
         }
     }
     // rows of which `left` exist; the others arrive as zeros
     __device__ __forceinline__ void copy(lds_char *lds, const unsigned short *rows, int left) const {
-        const __amdgpu_buffer_rsrc_t r = buffer_of(rows, left > 0 ? (unsigned)((min(left, R) - 1) * ld * 2) + used : 0u);
-        const int wave = threadIdx.x / 64;
+        const int wave = uniform_wave();
 #pragma unroll
-        for (int i = 0; i < COPIES; ++i) copy_to_lds(r, lds + (i * 256 + wave * 64) * 16, off[i], 0);
+        for (int row = 0; row < R; row += 32) {
+            const __amdgpu_buffer_rsrc_t r = buffer_of(rows + row * ld, left > row ? (unsigned)((min(left - row, 32) - 1) * ld * 2) + used : 0u);
+#pragma unroll
+            for (int i = 0; i < STRIPS; ++i) copy_to_lds(r, lds + (i * R + row) * 128 + wave * 1024, off[i], 0);
+        }
     }
 };
 template <int D, int R>
@@ -597,7 +602,7 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
     int kv_head, slot, start, len, key0;
     att_place(a.kv_heads, a.slots, kv_head, slot);
     if (!find_rows<F::ROWS>(a, slot, start, len, key0)) return;
-    const int group = a.heads / a.kv_heads, l = threadIdx.x & 63, wave = D > 64 ? threadIdx.x / 64 : __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int group = a.heads / a.kv_heads, l = threadIdx.x & 63, wave = D > 64 ? threadIdx.x / 64 : uniform_wave();
     const int part = wave % PARTS, first = key0 + wave / PARTS * 32, key = first + (l & 31);
     Tile tq, tg;
     tq.init(a.q_ld, a.head_dim);
@@ -608,6 +613,7 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
     kr.load(k + (start + first) * a.k_ld + (int64_t)kv_head * a.head_dim, a.k_ld, len - first, a.head_dim);
     vr.load(v + (start + first) * a.v_ld + (int64_t)kv_head * a.head_dim, a.v_ld, len - first, a.head_dim);
     const float by = a.scale * LOG2E;
+    const int limit = key - 4 * (l >> 5);
     floatx16 ak[D / 32], av[D / 32];
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
@@ -644,7 +650,7 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     s[r + j] = __builtin_amdgcn_exp2f(s[r + j] * by - x[j]);
-                    if (D > 64 && edge && row + 32 * b + result_row(r + j, l) < key) s[r + j] = 0.f;
+                    if (D > 64 && edge && row + 32 * b + result_row(r + j, 0) < limit) s[r + j] = 0.f;
                     d[r + j] = D > 64 ? s[r + j] * (d[r + j] - y[j]) : d[r + j] - y[j];
                 }
             }
@@ -675,10 +681,11 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
             tq.copy(lq, q + (start + row) * a.q_ld + (int64_t)head * a.head_dim, len - row);
             tg.copy(lg, go + (start + row) * a.o_ld + (int64_t)head * a.head_dim, len - row);
             // 64 rows' delta (waves 0, 1) and lse (2, 3); rows behind the sequence: 0
-            if (64 * (wave & 1) < R) {
-                const float *p = delta + (wave / 2 * a.heads + head) * (int64_t)a.tokens + start + row;
+            const int w = uniform_wave();
+            if (64 * (w & 1) < R) {
+                const float *p = delta + (w / 2 * a.heads + head) * (int64_t)a.tokens + start + row;
                 const __amdgpu_buffer_rsrc_t r = buffer_of(p, (unsigned)min(len - row, R) * 4);
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(ls + wave * 256), 4, (64 * (wave & 1) + l) * 4, 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(ls + w * 256), 4, (64 * (w & 1) + l) * 4, 0, 0, 0);
             }
         };
         fetch(lq0, lg0, ls0, begin);
