@@ -654,8 +654,8 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
                     d[r + j] = D > 64 ? s[r + j] * (d[r + j] - y[j]) : d[r + j] - y[j];
                 }
             }
-            // 64 wide in a branch of its own: 185 us (bf16, two sequences of 4096 rows, 16 heads of 64), in the loop above 229.  128 wide the loop's
-            // form leaves the registers alone: 2.80 ms (two sequences of 8192, 32 heads of 128 on 8), the branch with its limit 3.35
+            // 64 wide in a branch of its own: 185 us (bf16, two sequences of 4096 rows, 16 heads of 64), in the loop above 229.  128 wide the branch's
+            // limit does not fit the registers: 42 spilled in the loop, where a reload waits for the copies under way; the form above none
             if (D <= 64) {
                 if (edge) clear_before(s, key - row - 32 * b);
 #pragma unroll
@@ -797,9 +797,8 @@ int row_parts(const AttShape &a) {
 }
 // The second backward kernel has fewer workgroups (key heads) with a longer way each (the rows behind a key, of every head of the group).
 // Where 128 keys to a workgroup do not give four workgroups to a CU, the way is cut into ranges.  bf16, where that gives less than two: a
-// workgroup takes 32 keys.  Both backward kernels: bf16, 8 ragged sequences of 8192 rows, 32 / 8 heads, 1255 us uncut, 888 in four ranges, 928
-// with 32 keys; one of 10000, 4 / 1 heads, 2291, 620 (8 ranges), 820 (32 keys, 4 ranges); one of 1024, 8 heads of 64, 51, 43 (4 ranges), 24
-// (32 keys).  fp32, 2048 ragged rows, 12 / 4 heads of 64: 587, 196 (16 ranges), 223 (32 keys, 4 ranges); 4 x 512 rows, 16 heads: 126, 110 (2), 124.
+// workgroup takes 32 keys.  Both backward kernels: bf16, 8 ragged sequences of 8192 rows, 32 / 8 heads, 994 us uncut, 837 in two ranges, 953
+// with 32 keys; one of 10000, 4 / 1 heads, 1865, 559 (14 ranges), 794 (32 keys, 4 ranges); one of 1024, 8 heads of 64, 47 and 28 (32 keys).  fp32, 2048 ragged rows, 12 / 4 heads of 64: 587, 196 (16 ranges), 223 (32 keys, 4 ranges); 4 x 512 rows, 16 heads: 126, 110 (2), 124.
 struct KeyForm { int parts, ranges; };
 KeyForm key_form(const AttShape &a, bool fp32) {
     const int64_t full = std::max<int64_t>(1, (int64_t)(a.tokens / 128) * a.kv_heads), way = (int64_t)(a.tokens / a.seqs) * (a.heads / a.kv_heads);
@@ -809,7 +808,7 @@ KeyForm key_form(const AttShape &a, bool fp32) {
     };
     if (fp32) return {1, (int)cut(full, 1024, 192)};
     if (full >= 1024) return {1, 1};
-    const int64_t r = cut(full, 2048, 1024);
+    const int64_t r = cut(full, 1024, 1024);
     if (full * r >= 512 && a.tokens / a.seqs >= 64) return {1, (int)r};
     return {4, (int)cut(4 * full, 1024, 2048)};
 }
