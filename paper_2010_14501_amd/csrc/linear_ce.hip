@@ -160,12 +160,13 @@ struct RoundEpilogue {
     }
 };
 
-// 16 tokens a workgroup, 16 threads to a token: lse and the row's loss from the parts of its logits
-__global__ __launch_bounds__(256) void ce_merge_kernel(const float2 *__restrict__ part, int parts, const float *__restrict__ hit,
-                                                       const int32_t *__restrict__ labels, float *__restrict__ lse, float *__restrict__ row_loss,
-                                                       int rows, int vocab) {
-    __shared__ Soft seg[16][16];
-    const int l = threadIdx.x % 16, s = threadIdx.x / 16, t = blockIdx.x * 16 + l;
+// 16 threads to a token: lse and the row's loss from the parts of its logits.  TOKENS = 64: the only workgroup, which takes the mean as well.
+template <int TOKENS>
+__global__ __launch_bounds__(TOKENS * 16) void ce_merge_kernel(const float2 *__restrict__ part, int parts, const float *__restrict__ hit,
+                                                               const int32_t *__restrict__ labels, float *__restrict__ lse,
+                                                               float *__restrict__ row_loss, float *__restrict__ loss, int rows, int vocab) {
+    __shared__ Soft seg[16][TOKENS];
+    const int l = threadIdx.x % TOKENS, s = threadIdx.x / TOKENS, t = blockIdx.x * TOKENS + l;
     Soft a{-INFINITY, 0.f};
     if (t < rows) {
         int b = s;
@@ -183,11 +184,21 @@ __global__ __launch_bounds__(256) void ce_merge_kernel(const float2 *__restrict_
     }
     seg[s][l] = a;
     __syncthreads();
-    if (s || t >= rows) return;
-    for (int b = 1; b < 16; ++b) a = soft_join(a, seg[b][l]);
-    const float ls = a.m + logf(a.s);
-    lse[t] = ls;
-    row_loss[t] = (unsigned)labels[t] < (unsigned)vocab ? ls - hit[t] : 0.f;
+    if (s) return;
+    float mine = 0.f;
+    const bool has = t < rows && (unsigned)labels[t] < (unsigned)vocab;
+    if (t < rows) {
+        for (int b = 1; b < 16; ++b) a = soft_join(a, seg[b][l]);
+        const float ls = a.m + logf(a.s);
+        lse[t] = ls;
+        mine = has ? ls - hit[t] : 0.f;
+        if (TOKENS < 64) row_loss[t] = mine;
+    }
+    if (TOKENS < 64) return;
+    double sum = mine;       // one wave by now
+    for (int w = 32; w; w /= 2) sum += __shfl_xor(sum, w);
+    const int count = __popcll(__ballot(has));
+    if (l == 0) *loss = count ? (float)(sum / count) : 0.f;
 }
 
 // the number of rows with a label (inv: its reciprocal, 0 for none) and the mean of their losses; sums in a fixed order
@@ -263,28 +274,41 @@ __global__ __launch_bounds__(256) void ce_piece_stats_kernel(const float *__rest
     const int label = labels[t] - v0;
     if (label >= from && label < to) hit[t] = row[label];
 }
-// fp32: dl in the place of the logits
+// fp32: dl in the place of the logits.  COUNT: with up to 1024 rows every workgroup counts the labels itself, a launch less.
+template <bool COUNT>
 __global__ __launch_bounds__(256) void ce_piece_grad_kernel(float *__restrict__ logits, int piece, int v0, const int32_t *__restrict__ labels,
-                                                            const float *__restrict__ lse, const float *__restrict__ inv_count, int vocab) {
+                                                            const float *__restrict__ lse, const float *__restrict__ inv_count, int rows, int vocab) {
+    __shared__ int counts[4];
+    float inv;
+    if (COUNT) {
+        int count = 0;
+        for (int t = threadIdx.x; t < rows; t += 256) count += (unsigned)labels[t] < (unsigned)vocab;
+        for (int w = 32; w; w /= 2) count += __shfl_xor(count, w);
+        if (threadIdx.x % 64 == 0) counts[threadIdx.x / 64] = count;
+        __syncthreads();
+        count = counts[0] + counts[1] + counts[2] + counts[3];
+        inv = count ? 1.f / count : 0.f;
+    } else inv = *inv_count;
     const int64_t t = blockIdx.x;
     const int v = blockIdx.y * 256 + threadIdx.x;
     if (v >= piece) return;
     const int label = labels[t];
     float *at = logits + t * piece + v;
-    *at = (unsigned)label < (unsigned)vocab ? (exp_of(*at - lse[t]) - (v0 + v == label ? 1.f : 0.f)) * *inv_count : 0.f;
+    *at = (unsigned)label < (unsigned)vocab ? (exp_of(*at - lse[t]) - (v0 + v == label ? 1.f : 0.f)) * inv : 0.f;
 }
 
 // fp32 and few rows: dx += dl W, which reads all of W for rows * 2 operations an entry.  A matrix tile would be mostly empty, and its few
 // workgroups wait for memory; here a workgroup sums 256 columns over `per` entries of the piece on the vector units, rows from scalar
 // registers, and leaves part[range][row][column].  11 rows, 1120 columns, 41104 entries (184 MB): 48 us (3.8 TB/s), the convolutions'
 // tiles 91; 1 row, 144 columns, 92544 entries: 9 us, the tiles 188.
+// Twice as many rows (grid z) read W twice: backward pass of 24 rows, 512 columns, 1000 entries 27 us, with the tiles 30; but 20 rows, 4096 columns, 32000 entries 595 us (tiles 500).
 constexpr int CE_FEW_ROWS = 16;
 template <int ROWS>
 __global__ __launch_bounds__(256) void ce_few_rows_kernel(const float *__restrict__ dl, int piece, const float *__restrict__ w, int width, int rows, int per,
                                                           float *__restrict__ part) {
     __shared__ float sums[4][ROWS][256];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x & 63, c0 = blockIdx.x * 256;
-    const int from = blockIdx.y * per, to = min(piece, from + per);
+    const int from = blockIdx.y * per, to = min(piece, from + per), t0 = blockIdx.z * ROWS;
     int col[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) col[j] = min(c0 + 64 * j + l, width - 1);
@@ -298,7 +322,7 @@ __global__ __launch_bounds__(256) void ce_few_rows_kernel(const float *__restric
             for (int j = 0; j < 4; ++j) x[i][j] = w[(int64_t)(v + i) * width + col[j]];
 #pragma unroll
         for (int t = 0; t < ROWS; ++t) {
-            const float *d = dl + (int64_t)min(t, rows - 1) * piece + v;
+            const float *d = dl + (int64_t)min(t0 + t, rows - 1) * piece + v;
 #pragma unroll
             for (int i = 0; i < N; ++i)
 #pragma unroll
@@ -315,8 +339,8 @@ __global__ __launch_bounds__(256) void ce_few_rows_kernel(const float *__restric
     __syncthreads();
     const int c = threadIdx.x;
     if (c0 + c >= width) return;
-    for (int t = 0; t < rows; ++t)
-        part[((int64_t)blockIdx.y * rows + t) * width + c0 + c] = (sums[0][t][c] + sums[1][t][c]) + (sums[2][t][c] + sums[3][t][c]);
+    for (int t = 0; t < min(ROWS, rows - t0); ++t)
+        part[((int64_t)blockIdx.y * rows + t0 + t) * width + c0 + c] = (sums[0][t][c] + sums[1][t][c]) + (sums[2][t][c] + sums[3][t][c]);
 }
 // out (+)= the sum over the ranges of part, in a fixed order: sixteen waves take a share of the ranges each
 __global__ __launch_bounds__(1024) void ce_few_rows_join_kernel(const float *__restrict__ part, int ranges, int n, float *__restrict__ out, int add) {
@@ -368,7 +392,7 @@ struct CePlan {
 
     int64_t bytes() const { return fixed + per_col * piece; }
     int wgrad_splits(int piece) const { return ce_splits(cut(width, 128) * cut(piece, 128), rows, 64); }
-    bool few_rows() const { return rows <= CE_FEW_ROWS; }
+    bool few_rows(int piece) const { return rows <= CE_FEW_ROWS || (rows <= 2 * CE_FEW_ROWS && (int64_t)piece * width <= 1 << 20); }      // twice: where W stays in L2
     int few_per(int piece) const {      // entries of W for a workgroup: four workgroups to a CU
         return (int)up(cut(piece, std::max<int64_t>(1, std::min<int64_t>(1024 / cut(width, 256), cut(piece, 64)))), 16);
     }
@@ -420,12 +444,12 @@ CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab) {
         p.ranges = (int)cut(std::min(p.piece, vocab), p.chunk);      // a later piece is no longer than the first
         if (p.ranges > 1 || p.piece < vocab) p.fixed += up(p.ranges * rows * width * 4, 256);
     } else {
-        p.product = (int64_t)std::max(conv_workspace_bytes(0, cs, 1), p.few_rows() ? 0 : conv_workspace_bytes(1, cs, 1));
+        p.product = (int64_t)std::max(conv_workspace_bytes(0, cs, 1), p.few_rows(p.piece) ? 0 : conv_workspace_bytes(1, cs, 1));
         const std::vector<int> at = p.pieces();
         for (size_t i = 0; i + 1 < at.size(); ++i) {
             const int64_t piece = at[i + 1] - at[i], splits = p.wgrad_splits((int)piece);
             if (splits > 1) p.product = std::max(p.product, splits * piece * width * 4);
-            if (p.few_rows()) p.product = std::max(p.product, cut(piece, p.few_per((int)piece)) * rows * width * 4);
+            if (p.few_rows((int)piece)) p.product = std::max(p.product, cut(piece, p.few_per((int)piece)) * rows * width * 4);
         }
         p.product = up(p.product, 256);
         p.fixed += p.product;
@@ -484,7 +508,12 @@ void linear_ce_fwd(hipStream_t st, int dtype, const void *x, const void *w, cons
             done += segments;
         }
     }
-    hipLaunchKernelGGL(ce_merge_kernel, dim3((unsigned)cut(rows, 16)), dim3(256), 0, st, part, (int)p.parts(), hit, labels, lse, row_loss, p.rows, vocab);
+    if (rows <= 64 && rows * p.parts() <= 1 << 14) {      // few enough for one workgroup: a launch less
+        hipLaunchKernelGGL(ce_merge_kernel<64>, dim3(1), dim3(1024), 0, st, part, (int)p.parts(), hit, labels, lse, row_loss, loss, p.rows, vocab);
+        hip_check(hipGetLastError(), "linear_ce merge launch");
+        return;
+    }
+    hipLaunchKernelGGL(ce_merge_kernel<16>, dim3((unsigned)cut(rows, 16)), dim3(256), 0, st, part, (int)p.parts(), hit, labels, lse, row_loss, loss, p.rows, vocab);
     hip_check(hipGetLastError(), "linear_ce merge launch");
     hipLaunchKernelGGL(ce_mean_kernel, dim3(1), dim3(1024), 0, st, row_loss, labels, p.rows, vocab, loss, (float *)nullptr);
     hip_check(hipGetLastError(), "linear_ce mean launch");
@@ -497,8 +526,11 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
     check_aligned(p, {x, w, dx, dw});
     if (!labels || !lse) throw KernelError("linear_ce: null pointer");
     float *inv = (float *)ws;
-    hipLaunchKernelGGL(ce_mean_kernel, dim3(1), dim3(1024), 0, st, (const float *)nullptr, labels, p.rows, vocab, (float *)nullptr, inv);
-    hip_check(hipGetLastError(), "linear_ce count launch");
+    const bool count = p.bf16 || rows > 1024;
+    if (count) {
+        hipLaunchKernelGGL(ce_mean_kernel, dim3(1), dim3(1024), 0, st, (const float *)nullptr, labels, p.rows, vocab, (float *)nullptr, inv);
+        hip_check(hipGetLastError(), "linear_ce count launch");
+    }
     const std::vector<int> at = p.pieces();
     char *dl = (char *)ws + p.fixed;
     float *parts = (float *)((char *)ws + 256);
@@ -537,15 +569,16 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
             float *product = p.product ? parts : nullptr;
             const size_t product_bytes = (size_t)p.product;
             conv_fwd(st, (const float *)x, wp, d, cs, 1, product, product_bytes);
-            hipLaunchKernelGGL(ce_piece_grad_kernel, dim3(p.rows, (unsigned)cut(piece, 256)), dim3(256), 0, st, d, piece, v0, labels, lse, inv, vocab);
+            hipLaunchKernelGGL((count ? ce_piece_grad_kernel<false> : ce_piece_grad_kernel<true>), dim3(p.rows, (unsigned)cut(piece, 256)), dim3(256), 0, st, d, piece, v0,
+                               labels, lse, inv, p.rows, vocab);
             hip_check(hipGetLastError(), "linear_ce gradient launch");
-            if (p.few_rows()) {
+            if (p.few_rows(piece)) {
                 const int per = p.few_per(piece), ranges = (int)cut(piece, per), n = p.rows * width;
                 const dim3 grid((unsigned)cut(width, 256), ranges);
                 if (rows <= 4)
                     hipLaunchKernelGGL(ce_few_rows_kernel<4>, grid, dim3(256), 0, st, d, piece, wp, width, p.rows, per, product);
                 else
-                    hipLaunchKernelGGL(ce_few_rows_kernel<CE_FEW_ROWS>, grid, dim3(256), 0, st, d, piece, wp, width, p.rows, per, product);
+                    hipLaunchKernelGGL(ce_few_rows_kernel<CE_FEW_ROWS>, dim3(grid.x, grid.y, (unsigned)cut(rows, CE_FEW_ROWS)), dim3(256), 0, st, d, piece, wp, width, p.rows, per, product);
                 hip_check(hipGetLastError(), "linear_ce input gradient launch");
                 hipLaunchKernelGGL(ce_few_rows_join_kernel, dim3((unsigned)cut(n, 64)), dim3(1024), 0, st, product, ranges, n, (float *)dx, accumulate || i > 0);
                 hip_check(hipGetLastError(), "linear_ce input gradient sum launch");
