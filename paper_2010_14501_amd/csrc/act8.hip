@@ -47,7 +47,8 @@ __device__ __forceinline__ void load8(const T *p, int have, float (&v)[8]) {
     }
 }
 
-// a thread takes eight columns, four threads a group
+// A thread takes eight columns, four threads a group.  Bound by memory: 16384 x 4096 in fp32, 337 MB, 71 to 78 us (4.3 to 4.8 TB/s), and back 56
+// (6.0 TB/s, part of it from the last-level cache).
 template <class T>
 __global__ __launch_bounds__(256) void act8_pack_kernel(const T *__restrict__ x, int64_t ld, int8_t *__restrict__ code, uint8_t *__restrict__ exps,
                                                         int64_t rows, int cols, int per_row) {
@@ -105,7 +106,9 @@ __global__ __launch_bounds__(256) void act8_unpack_kernel(const int8_t *__restri
 
 // dw[o][c] = sum over rows of dy[row][o] x[row][c]: both operands run across the reduction (DEEP tiles, tile_bf16.hpp).  The codes become
 // bf16 on their way to LDS: a byte u = code + 128 to a float, then u 2^e - 128 2^e in one exact multiply-add.  bf16 dy goes in as it is,
-// fp32 dy in three pieces (bf16_pieces.hpp), three instructions a product and nothing lost above 2^-110.
+// fp32 dy in three pieces (bf16_pieces.hpp), three instructions a product and nothing lost above 2^-110.  128 x 128 results to a workgroup of four
+// waves, two workgroups a CU.  One of these has its conversions and its barrier while the other one multiplies; that, not memory, bounds it:
+// 4096 x 2048 x 1024 40 us in bf16 (431 TFLOP/s), 68 in fp32 (254, times three).
 struct Act8Shape {
     const int8_t *code;
     const uint8_t *exps;
@@ -116,7 +119,8 @@ struct Act8Shape {
     int64_t chunk;             // rows of a range
     bool vec_out;
 };
-template <bool F32, int BM, int BN, int WM, int WN>
+// WORDS: dy's rows begin on words, which a buffer's loads need.
+template <bool F32, bool WORDS, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN * 64, WM *WN * 64 / 256) void act8_wgrad_kernel(Act8Shape g) {
     constexpr int THREADS = WM * WN * 64, DEPTH = F32 ? 32 : 64, PLANES = F32 ? 3 : 1, MB = BM / WM / 32, NB = BN / WN / 32;
     constexpr int CODES = BM * DEPTH / 16 / THREADS, PIECES = BN * DEPTH / 8 / THREADS;
@@ -137,42 +141,57 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN * 64 / 256) void act8_wgrad_ker
         for (int j = 0; j < NB; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-    uint4 codes[CODES];
-    float scale[CODES];
+    // A step's operands on their way.  What lies behind a row's end, the next row's beginning, only reaches results that are not stored; rows
+    // behind the range arrive as zeros.
+    struct Held {
+        uintx4 codes[CODES], dy[PIECES][F32 ? 2 : 1];
+        unsigned exps[CODES];
+    } held0, held1;
     typedef typename std::conditional<F32, float, unsigned short>::type T;
-    float dy[F32 ? PIECES : 1][8];
-    uintx4 dyw[F32 ? 1 : PIECES];
-    auto fetch = [&](int64_t k0) {
+    unsigned code_at[CODES], exp_at[CODES], dy_at[PIECES];
+#pragma unroll
+    for (int i = 0; i < CODES; ++i) {
+        const unsigned piece = i * THREADS + threadIdx.x, kr = piece / (BM / 16), c = c0 + piece % (BM / 16) * 16;
+        code_at[i] = kr * g.ld + c;
+        exp_at[i] = kr * (g.ld / GROUP) + c / GROUP;
+    }
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const unsigned piece = i * THREADS + threadIdx.x, kr = piece / (BN / 8), o = o0 + piece % (BN / 8) * 8;
+        dy_at[i] = (kr * g.outs + o) * sizeof(T);
+    }
+    auto fetch = [&](Held &h, int64_t k0) {
+        const unsigned left = (unsigned)max(min(last - k0, (int64_t)DEPTH), (int64_t)0);
+        const __amdgpu_buffer_rsrc_t rc = buffer_of(g.code + k0 * g.ld, left * g.ld), re = buffer_of(g.exps + k0 * (g.ld / GROUP), left * (g.ld / GROUP)),
+                                     rd = buffer_of((const T *)g.dy + k0 * g.outs, left * g.outs * (unsigned)sizeof(T));
 #pragma unroll
         for (int i = 0; i < CODES; ++i) {
-            const int piece = i * THREADS + threadIdx.x, kr = piece / (BM / 16), c = c0 + piece % (BM / 16) * 16;
-            codes[i] = make_uint4(0, 0, 0, 0);
-            scale[i] = 0.f;
-            if (k0 + kr < last && c < g.ld) {
-                codes[i] = *(const uint4 *)(g.code + (k0 + kr) * g.ld + c);
-                scale[i] = __uint_as_float((unsigned)g.exps[(k0 + kr) * (g.ld / GROUP) + c / GROUP] << 23);
-            }
+            h.codes[i] = __builtin_bit_cast(uintx4, __builtin_amdgcn_raw_buffer_load_b128(rc, code_at[i], 0, 0));
+            h.exps[i] = __builtin_amdgcn_raw_buffer_load_b8(re, exp_at[i], 0, 0);
         }
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const int piece = i * THREADS + threadIdx.x, kr = piece / (BN / 8), o = o0 + piece % (BN / 8) * 8;
-            const int have = k0 + kr < last ? g.outs - o : 0;
-            const T *p = (const T *)g.dy + (k0 + kr) * g.outs + o;
-            if constexpr (F32) load8(p, have, dy[i]);
-            else if (have >= 8) dyw[i] = *(const uint4_any *)p;
-            else {
+            if constexpr (WORDS) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) dyw[i][j] = (2 * j < have ? p[2 * j] : 0u) | (2 * j + 1 < have ? (unsigned)p[2 * j + 1] << 16 : 0u);
+                for (int j = 0; j < (F32 ? 2 : 1); ++j) h.dy[i][j] = __builtin_bit_cast(uintx4, __builtin_amdgcn_raw_buffer_load_b128(rd, dy_at[i] + 16 * j, 0, 0));
+            } else {
+                const int piece = i * THREADS + threadIdx.x, kr = piece / (BN / 8), o = o0 + piece % (BN / 8) * 8, have = kr < (int)left ? g.outs - o : 0;
+                const unsigned short *p = (const unsigned short *)g.dy + (k0 + kr) * g.outs + o;
+                if (have >= 8) h.dy[i][0] = *(const uint4_any *)p;
+                else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) h.dy[i][0][j] = (2 * j < have ? p[2 * j] : 0u) | (2 * j + 1 < have ? (unsigned)p[2 * j + 1] << 16 : 0u);
+                }
             }
         }
     };
     auto place = [](int kr, int c, int row_bytes) { return kr * row_bytes + ((((c >> 1) ^ (int)deep_turn(kr)) << 1) | (c & 1)) * 16; };
-    auto store = [&](int buf) {
+    auto store = [&](const Held &h, int buf) {
 #pragma unroll
         for (int i = 0; i < CODES; ++i) {
             const int piece = i * THREADS + threadIdx.x, kr = piece / (BM / 16), c = piece % (BM / 16) * 2;
-            const unsigned w[4] = {codes[i].x ^ 0x80808080u, codes[i].y ^ 0x80808080u, codes[i].z ^ 0x80808080u, codes[i].w ^ 0x80808080u};
-            const float s = scale[i], mid = -128.f * s;
+            const unsigned w[4] = {h.codes[i][0] ^ 0x80808080u, h.codes[i][1] ^ 0x80808080u, h.codes[i][2] ^ 0x80808080u, h.codes[i][3] ^ 0x80808080u};
+            const float s = __uint_as_float(h.exps[i] << 23), mid = -128.f * s;
             unsigned out[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -189,11 +208,14 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN * 64 / 256) void act8_wgrad_ker
             const int piece = i * THREADS + threadIdx.x, kr = piece / (BN / 8), at = place(kr, piece % (BN / 8), BN * 2);
             if constexpr (F32) {
                 unsigned lost = 0;
-                const PieceRow r = split_row(dy[i], lost);
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(h.dy[i][j / 4][j % 4]);
+                const PieceRow r = split_row(v, lost);
                 *(bf16x8 *)(b_lds[buf][0] + at) = r.h;
                 *(bf16x8 *)(b_lds[buf][1] + at) = r.m;
                 *(bf16x8 *)(b_lds[buf][2] + at) = r.l;
-            } else *(uintx4 *)(b_lds[buf][0] + at) = dyw[i];
+            } else *(uintx4 *)(b_lds[buf][0] + at) = h.dy[i][0];
         }
     };
     auto work = [&](int buf) {
@@ -216,14 +238,19 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN * 64 / 256) void act8_wgrad_ker
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    fetch(first);
-    store(0);
+    // two steps ahead of the products: a step takes less time than its loads (5003 rows, 1000 columns, 777 outputs, fp32: 46 us, one step ahead 52)
+    fetch(held0, first);
+    fetch(held1, first + DEPTH);
+    store(held0, 0);
     __syncthreads();
-    int buf = 0;
-    for (int64_t k0 = first; k0 < last; k0 += DEPTH, buf ^= 1) {
-        fetch(k0 + DEPTH);       // behind the last step: nothing, as zeros
-        work(buf);
-        store(buf ^ 1);
+    for (int64_t k0 = first; k0 < last; k0 += 2 * DEPTH) {
+        fetch(held0, k0 + 2 * DEPTH);
+        work(0);
+        store(held1, 1);
+        __syncthreads();
+        fetch(held1, k0 + 3 * DEPTH);
+        if (k0 + DEPTH < last) work(1);
+        store(held0, 0);
         __syncthreads();
     }
     const int l = threadIdx.x & 63;
@@ -317,9 +344,10 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 // Two forms.  Direct: one kernel from codes and dy, few launches.  Expanded: the codes as bf16 and dy's planes in the workspace, some rows
 // (a turn) at a time, and the GEMM, whose operands then need no register on their way.  Both cut the reduction over the rows into
 // ranges where the result has few tiles, until every CU has work, of at least 256 rows each; the ranges' results are added in order.
-// Measured, expanded and direct: bf16 8192 x 4096 x 4096 250 and 474 us (1.10 PFLOP/s), 16384 x 4096 x 1024 184 and 255, 4096 x 1024 x 1024
-// 34 and 32, 1024 x 512 x 512 15 and 14; fp32 (three products each) 746 and 855, 464 and 453, 55 and 44, 24 and 17.  So bf16 expands from
-// 12 GFLOP on and fp32 from 200.
+// Measured, expanded and direct: bf16 8192 x 4096 x 4096 256 and 406 us (1.08 PFLOP/s), 8192 x 2048 x 2048 100 and 110, 4096 x 2048 x 1024
+// 47 and 40, 1024 x 512 x 512 15 and 12; fp32 (three products each) 8192 x 4096 x 4096 726 and 824, 16384 x 4096 x 1024 460 and 422,
+// 4096 x 1024 x 1024 61 and 42.  So bf16 expands from 40 GFLOP on and fp32 from 200.  The expanded form is bound by the matrix instructions'
+// power, the direct one by the conversions and barriers between them.
 struct WgradPlan {
     bool expanded, copy;       // copy: dy goes through the workspace (fp32, or rows that are no multiple of 16 bytes)
     int tile, splits, ld, ldo, planes;
@@ -331,7 +359,7 @@ constexpr int64_t ACT8_TURN_BYTES = 256ll << 20;
 WgradPlan wgrad_plan(int dtype, int64_t rows, int cols, int outs, bool aligned) {
     WgradPlan p{};
     p.ld = (int)code_ld(cols);
-    p.expanded = 2.0 * rows * cols * outs >= (dtype == MONET_F32 ? 2e11 : 1.2e10) && std::max<int64_t>(p.ld, up(outs, 8)) < GEMM_MOST_LD;
+    p.expanded = 2.0 * rows * cols * outs >= (dtype == MONET_F32 ? 2e11 : 4e10) && std::max<int64_t>(p.ld, up(outs, 8)) < GEMM_MOST_LD;
     p.tile = p.expanded ? gemm_tile(cols, outs) : 128;
     p.planes = dtype == MONET_F32 ? 3 : 1;
     p.copy = dtype == MONET_F32 || outs % 8 || !aligned;
@@ -457,8 +485,9 @@ void act8_wgrad(hipStream_t st, int dtype, const void *code, const void *dy, flo
         g.vec_out = vec_out;
         if ((int64_t)g.tiles_m * g.tiles_n >= 1 << 24) throw KernelError("act8_wgrad: result too large");
         const dim3 grid(g.tiles_m * g.tiles_n, p.splits);
-        if (dtype == MONET_F32) hipLaunchKernelGGL((act8_wgrad_kernel<true, 128, 128, 2, 2>), grid, dim3(256), 0, st, g);
-        else hipLaunchKernelGGL((act8_wgrad_kernel<false, 128, 128, 2, 2>), grid, dim3(256), 0, st, g);
+        if (dtype == MONET_F32) hipLaunchKernelGGL((act8_wgrad_kernel<true, true, 128, 128, 2, 2>), grid, dim3(256), 0, st, g);
+        else if ((uintptr_t)dy % 4 == 0 && outs % 2 == 0) hipLaunchKernelGGL((act8_wgrad_kernel<false, true, 128, 128, 2, 2>), grid, dim3(256), 0, st, g);
+        else hipLaunchKernelGGL((act8_wgrad_kernel<false, false, 128, 128, 2, 2>), grid, dim3(256), 0, st, g);
         hip_check(hipGetLastError(), "act8 weight gradient launch");
     }
     if (p.splits > 1) split_reduce(st, parts, dw, cols * outs, p.splits, false);

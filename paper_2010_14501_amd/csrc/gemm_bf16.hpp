@@ -1,8 +1,12 @@
-// C = A B^T on bf16 operands with fp32 sums: the products of the vocabulary loss.
+// C = A B^T on bf16 operands with fp32 sums: the products of the vocabulary loss, and large weight gradients of 8-bit inputs.
 //
 // The result's rows (m) are the index that is contiguous in memory, its columns (n) the other one, since a lane of the matrix
 // instruction holds four neighbouring rows of one column.  Either operand may run along the reduction (WIDE: [row][k]) or across it
 // (DEEP: [k][row]); both reach LDS in 16-byte copies that pass no register and are read there without conflicts (tile_bf16.hpp).
+//
+// Bound by the matrix instructions under the power limit: they alone, from registers, reach 1.4 PFLOP/s in this loop (the clock falls), 8192 x 8192 x
+// 4096 0.96 to 1.02, the loss's products of 8192 x 4096 x 131072 1.19 to 1.27 (MFMA pipes busy 60 % of the cycles).  Tried without a gain: operands
+// of the next step read early, wave priorities, four stages of 32 indices, copies through registers, four waves of 128 x 128.
 #pragma once
 #include "kernels.hpp"
 #include "tile_bf16.hpp"

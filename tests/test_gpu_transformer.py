@@ -485,6 +485,10 @@ def test_act8_wgrad_of_large_layers(dtype, rows, cols, outs):
     assert ((dw.double() - want).norm() / want.norm()).item() < 2e-6
 
 
+def test_act8_wgrad_of_a_larger_layer():
+    test_act8_wgrad_of_large_layers(monet.BF16, 8200, 2050, 1300)
+
+
 def test_act8_wgrad_stays_in_its_workspace():
     """dy that the products read where it lies (bf16, rows of 16 bytes) takes no other turns than dy that is copied."""
     torch = torch_mod()
@@ -510,7 +514,7 @@ def test_act8_wgrad_stays_in_its_workspace():
 def test_act8_wgrad_of_very_wide_rows():
     """Rows of 2^23 columns and more are beyond the reach of the large products' addresses: the other form takes them."""
     torch = torch_mod()
-    rows, cols, outs = 16, (1 << 23) + 5, 48
+    rows, cols, outs = 16, (1 << 23) + 5, 160
     g = torch.Generator(device="cuda")
     g.manual_seed(7)
     x = torch.randn(rows, cols, generator=g, device="cuda").bfloat16()
