@@ -1,7 +1,7 @@
 // Causal attention over packed sequences with grouped heads.
 //
 //   s[i][j] = scale q[i] . k[j] for j <= i of the same sequence,  lse[i] = log sum_j exp s[i][j],  p = exp(s - lse),  o[i] = sum_j p[i][j] v[j]
-//   delta[i] = do[i] . o[i],  ds = p (do v^T - delta),  dq = scale ds k,  dk = scale ds^T q,  dv = p^T do  (dk, dv summed over a group's heads)
+//   delta[i] = do[i] . o[i] = sum_j p[i][j] (do[i] . v[j]),  ds = p (do v^T - delta),  dq = scale ds k,  dk = scale ds^T q,  dv = p^T do  (dk, dv summed over a group's heads)
 //
 // Nothing of size length x length is kept: the forward pass leaves lse, the backward pass computes p again.
 //
@@ -11,7 +11,7 @@
 // reduction and is read from LDS by ds_read_b64_tr_b16.
 //
 // Everything runs on v_mfma_f32_32x32x16_bf16.  bf16: p and ds are rounded to bf16 between the products, at most 2^-8 of a value each.  Rounding
-// the results alone leaves them 1.7e-3 off (Frobenius norm; 8 ragged sequences of 8192 rows), with this o is 2.0e-3 and dq and dk are 2.5e-3 off;
+// the results alone leaves them 1.7e-3 off (Frobenius norm; 8 ragged sequences of 8192 rows), with this o is 2.0e-3 and dq and dk are 2.4e-3 off;
 // ds in two pieces would take nine products for seven.  fp32: every operand in three bf16 pieces and a product in
 // six terms (bf16_pieces.hpp), 2^-24 of it at worst, in 192 cycles where the fp32 instruction takes 512; tiles are split on their way to
 // LDS, results in registers.  An infinity comes out as NaN there.  Scores, maxima, sums and gradients are fp32 in both.
@@ -37,6 +37,10 @@ constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ int uniform_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }      // in a scalar register, as is what follows from it
+
+// bf16: delta = sum of p dp, from fp32, in the rows of a sequence before this one; from o, rounded to bf16, in the others.  What rounding o moves delta by
+// goes into ds of all keys alike, which few keys do not average out: dq and dk of sequences of a few rows are 2.4e-3 off so, from o throughout 4.2e-3.
+constexpr int FEW_KEYS = 128;
 
 // The rows of a 32 x 32 result that lie before `limit` are not the lane's key's: their probabilities are 0.  The limit passes through a register of
 // its own inside the branch that this stands in, or the compiler compares for every tile what only those on the diagonal need.
@@ -513,6 +517,38 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
     dot = exchange_sum(dot);
     const int64_t at = (int64_t)head * a.tokens + start + row;
     const float by = a.scale * LOG2E, ls = row < len ? lse[at] * LOG2E : 0.f;
+    const int end = min(len, row0 + F::ROWS);
+    if constexpr (sizeof(T) == 2) {
+        if (row0 < FEW_KEYS) {
+            __shared__ float sums[4][32];
+            float sum = 0.f;
+            for (int key0 = 0; key0 < end; key0 += R) {
+                __syncthreads();
+                tk.copy((lds_char *)k0, kp + key0 * a.k_ld, len - key0);
+                tv.copy((lds_char *)v0, vp + key0 * a.v_ld, len - key0);
+                copies_arrived();
+#pragma unroll
+                for (int b = 0; b < B; ++b) {
+                    floatx16 s, d;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = d[r] = 0.f;
+#pragma unroll
+                    for (int p = 0; p < PIECES; ++p) s = Piece<T>::mma(rd.wide((lds_char *)k0, B * part + b, p), qr.p[p], s);
+#pragma unroll
+                    for (int p = 0; p < PIECES; ++p) d = Piece<T>::mma(rd.wide((lds_char *)v0, B * part + b, p), gr.p[p], d);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (key0 + 32 * (B * part + b) + result_row(r, l) <= row) sum += __builtin_amdgcn_exp2f(s[r] * by - ls) * d[r];
+                }
+            }
+            sum = exchange_sum(sum);
+            if (l < 32) sums[wave][l] = sum;
+            __syncthreads();
+            dot = 0.f;
+#pragma unroll
+            for (int w = 0; w < PARTS; ++w) dot += sums[wave / PARTS * PARTS + w][l & 31];
+        }
+    }
     if (part == 0 && l < 32 && row < len) {
         delta[at] = dot;
         delta[at + (int64_t)a.heads * a.tokens] = ls;
@@ -522,7 +558,6 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[c][r] = 0.f;
-    const int end = min(len, row0 + F::ROWS);
     auto work = [&](const lds_char *lk, const lds_char *lv, int tile0) {
         const int key0 = tile0 + 32 * B * part;
         if (key0 > first + 31 || key0 >= end) return;

@@ -192,6 +192,23 @@ def test_attention_special_values_stay_in_their_sequence(dtype):
         assert not torch.isfinite(g[70:120]).all()
 
 
+@pytest.mark.parametrize("lens,dim", [([3, 1, 2, 8, 7, 1, 5, 4] * 8, 64), ([127, 129, 64, 65], 128)])
+def test_attention_gradients_of_short_sequences(lens, dim):
+    """bf16: ds and the result are each rounded once.  A rounding is off by half a step at most and evenly spread: 2^-8 / sqrt(3) of a value at its
+    worst in the root of the mean square, sqrt(2) times that for two.  What the rounding of o would add to it has no room."""
+    rng = np.random.default_rng(15)
+    heads, kv_heads, n = 8, 2, sum(lens)
+    ref, gpu = attention_inputs(rng, n, heads, kv_heads, dim, monet.BF16)
+    cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    torch = torch_mod()
+    got = attention_call(monet.BF16, *gpu, torch.from_numpy(cu).cuda(), heads, kv_heads, dim, dim ** -0.5)
+    q, k, v, do = ref
+    want = nm.attention_bwd(do, q, k, v, cu, dim ** -0.5)
+    for name, g, w in zip(("dq", "dk", "dv"), got[2:], want):
+        w = w.reshape(n, -1)
+        assert np.linalg.norm(host(g) - w) < 2.0 ** -8 * (2 / 3) ** 0.5 * np.linalg.norm(w), name
+
+
 @pytest.mark.parametrize("dtype", [monet.F32, monet.BF16])
 def test_attention_repeats_accumulates_and_replays(dtype):
     torch = torch_mod()
