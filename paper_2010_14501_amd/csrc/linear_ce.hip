@@ -342,6 +342,68 @@ __global__ __launch_bounds__(256) void ce_few_rows_kernel(const float *__restric
     for (int t = 0; t < min(ROWS, rows - t0); ++t)
         part[((int64_t)blockIdx.y * rows + t0 + t) * width + c0 + c] = (sums[0][t][c] + sums[1][t][c]) + (sums[2][t][c] + sums[3][t][c]);
 }
+// The logits of up to eight rows, bound by reading W as well: a wave takes eight entries, its lanes 256 columns of them at a time; the rows come from the
+// vector cache, where a workgroup's waves share them.  Then ROWS x 8 sums over 64 lanes: each step exchanges half of them and keeps the other
+// half.  Forward pass, 1 row, 2024 columns, 41311 entries (334 MB): 90 us (3.8 TB/s), with the convolutions' tiles 164; 6 rows, 2552, 38183: 162 and
+// 194; but 11 rows, 1120, 41119: 214 and 86, the rows' loads outnumber W's; 3 rows, 64 columns, 500 entries, 16 workgroups: 13.1 and 11.3.
+constexpr int CE_FEW_ENTRIES = 8;
+template <int ROWS>
+__global__ __launch_bounds__(256) void ce_few_logits_kernel(const float *__restrict__ x, const float *__restrict__ w, int width, int rows, int piece,
+                                                            float *__restrict__ logits) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x & 63;
+    const int v0 = (blockIdx.x * 4 + wave) * CE_FEW_ENTRIES;
+    if (v0 >= piece) return;
+    float sum[ROWS * CE_FEW_ENTRIES] = {};      // [row][entry]; rows and entries that do not exist repeat the last one and are not stored
+    auto add = [&](int c, auto whole) {
+        constexpr int N = decltype(whole)::value ? 4 : 1;
+        float e[CE_FEW_ENTRIES][N];
+#pragma unroll
+        for (int i = 0; i < CE_FEW_ENTRIES; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) e[i][j] = w[(int64_t)min(v0 + i, piece - 1) * width + c + 64 * j];
+#pragma unroll
+        for (int t = 0; t < ROWS; ++t) {
+            const float *row = x + (int64_t)min(t, rows - 1) * width + c;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float f = row[64 * j];
+#pragma unroll
+                for (int i = 0; i < CE_FEW_ENTRIES; ++i) sum[t * CE_FEW_ENTRIES + i] = fmaf(f, e[i][j], sum[t * CE_FEW_ENTRIES + i]);
+            }
+        }
+    };
+    int c = l;
+    for (; c - l + 256 <= width; c += 256) add(c, std::true_type());
+    for (; c < width; c += 64) add(c, std::false_type());
+    // lane l ends with the LEFT sums from l * LEFT on, or, of fewer than 64, ALIKE neighbouring lanes with the same one
+    constexpr int ALL = ROWS * CE_FEW_ENTRIES, LEFT = ALL > 64 ? ALL / 64 : 1, ALIKE = ALL < 64 ? 64 / ALL : 1;
+#pragma unroll
+    for (int k = 0; k < 6; ++k) {
+        const int step = 32 >> k, n = ALL >> (k + 1);
+        const bool high = l & step;
+        if (n == 0) sum[0] += __shfl_xor(sum[0], step);
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float keep = high ? sum[i + n] : sum[i], send = high ? sum[i] : sum[i + n];
+            sum[i] = keep + __shfl_xor(send, step);
+        }
+    }
+    if (l % ALIKE) return;
+#pragma unroll
+    for (int i = 0; i < LEFT; ++i) {
+        const int at = l / ALIKE * LEFT + i, t = at / CE_FEW_ENTRIES, v = v0 + at % CE_FEW_ENTRIES;
+        if (t < rows && v < piece) logits[(int64_t)t * piece + v] = sum[i];
+    }
+}
+bool ce_few_logits(hipStream_t st, const float *x, const float *w, int width, int rows, int piece, float *logits) {
+    if (rows > 8 || piece < 8192) return false;
+    const unsigned groups = (unsigned)((piece + 4 * CE_FEW_ENTRIES - 1) / (4 * CE_FEW_ENTRIES));
+    if (rows <= 4) hipLaunchKernelGGL(ce_few_logits_kernel<4>, dim3(groups), dim3(256), 0, st, x, w, width, rows, piece, logits);
+    else hipLaunchKernelGGL(ce_few_logits_kernel<8>, dim3(groups), dim3(256), 0, st, x, w, width, rows, piece, logits);
+    hip_check(hipGetLastError(), "linear_ce logits launch");
+    return true;
+}
+
 // out (+)= the sum over the ranges of part, in a fixed order: sixteen waves take a share of the ranges each
 __global__ __launch_bounds__(1024) void ce_few_rows_join_kernel(const float *__restrict__ part, int ranges, int n, float *__restrict__ out, int add) {
     __shared__ float sums[16][64];
@@ -502,7 +564,8 @@ void linear_ce_fwd(hipStream_t st, int dtype, const void *x, const void *w, cons
         int64_t done = 0;      // parts
         for (size_t i = 0; i + 1 < at.size(); ++i) {
             const int piece = at[i + 1] - at[i], segments = (int)cut(piece, CE_SEGMENT);
-            conv_fwd(st, (const float *)x, (const float *)w + (int64_t)at[i] * width, logits, ce_conv_shape(p, piece), 1, product, product_bytes);
+            const float *wp = (const float *)w + (int64_t)at[i] * width;
+            if (!ce_few_logits(st, (const float *)x, wp, width, p.rows, piece, logits)) conv_fwd(st, (const float *)x, wp, logits, ce_conv_shape(p, piece), 1, product, product_bytes);
             hipLaunchKernelGGL(ce_piece_stats_kernel, dim3(p.rows, segments), dim3(256), 0, st, logits, piece, at[i], labels, part + done * rows, hit);
             hip_check(hipGetLastError(), "linear_ce statistics launch");
             done += segments;
@@ -568,7 +631,7 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
             float *d = (float *)dl;
             float *product = p.product ? parts : nullptr;
             const size_t product_bytes = (size_t)p.product;
-            conv_fwd(st, (const float *)x, wp, d, cs, 1, product, product_bytes);
+            if (!ce_few_logits(st, (const float *)x, wp, width, p.rows, piece, d)) conv_fwd(st, (const float *)x, wp, d, cs, 1, product, product_bytes);
             hipLaunchKernelGGL((count ? ce_piece_grad_kernel<false> : ce_piece_grad_kernel<true>), dim3(p.rows, (unsigned)cut(piece, 256)), dim3(256), 0, st, d, piece, v0,
                                labels, lse, inv, p.rows, vocab);
             hip_check(hipGetLastError(), "linear_ce gradient launch");

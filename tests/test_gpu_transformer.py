@@ -350,7 +350,8 @@ def test_linear_ce_matches_64_bits(case, dtype):
 
 
 @pytest.mark.parametrize("dtype", [monet.F32, monet.BF16])
-@pytest.mark.parametrize("case", [(1, 144, 8209), (4, 40, 4096), (5, 264, 4113), (16, 1032, 12304), (17, 520, 4097)])
+@pytest.mark.parametrize("case", [(1, 144, 8209), (4, 40, 4096), (5, 264, 4113), (16, 1032, 12304), (17, 520, 4097),
+                                  (3, 40, 9001), (4, 264, 8192), (7, 328, 8215), (8, 1288, 8200)])
 def test_linear_ce_of_few_rows(case, dtype):
     """Few rows take the input's gradient over ranges of the vocabulary; a row's logits in segments of 4096."""
     test_linear_ce_matches_64_bits(case, dtype)
