@@ -7,7 +7,7 @@
 // exponentials per row and 64 or 128 logits (forward) or writes count * dl, rounded to bf16 (backward: it is the operand of two bf16
 // products whose results are rounded to bf16 themselves; the rounding, at most 2^-8 of a value, averages out over the sums.  1 / count
 // comes in behind the products: the label's entries p - 1 are near -1 and would otherwise all be rounded the same way).  Sums are fp32.
-// fp32: the convolution kernels' products, a piece of logits in the workspace at a time.
+// fp32: the convolution kernels' products, a piece of logits in the workspace at a time; with few rows two of them on the vector units.
 #include <initializer_list>
 #include <type_traits>
 #include <vector>
