@@ -135,11 +135,12 @@ struct SumEpilogue {
     }
 };
 
-// *by out[n][m] in bf16
+// out[n][m] = *by times the sums (+ out), rounded to bf16
 struct RoundEpilogue {
     unsigned short *out;
     const float *by;
     int64_t ld;
+    bool add;
     template <int MB, int NB>
     __device__ __forceinline__ void operator()(floatx16 (&acc)[MB][NB], int m0, int n0, int m, int n) const {
         const int l = threadIdx.x & 63;
@@ -153,8 +154,15 @@ struct RoundEpilogue {
 #pragma unroll
                 for (int r = 0; r < 16; r += 4) {
                     const int row = m0 + 32 * i + result_row(r, l);
-                    if (row < m)
-                        *(uint2 *)(out + c * ld + row) = make_uint2(pack_bf16(acc[i][j][r] * f, acc[i][j][r + 1] * f), pack_bf16(acc[i][j][r + 2] * f, acc[i][j][r + 3] * f));
+                    if (row >= m) continue;
+                    uint2 *p = (uint2 *)(out + c * ld + row);
+                    float v[4] = {acc[i][j][r] * f, acc[i][j][r + 1] * f, acc[i][j][r + 2] * f, acc[i][j][r + 3] * f};
+                    if (add) {
+                        const uint2 o = *p;
+                        v[0] += __uint_as_float(o.x << 16); v[1] += __uint_as_float(o.x & 0xffff0000u);
+                        v[2] += __uint_as_float(o.y << 16); v[3] += __uint_as_float(o.y & 0xffff0000u);
+                    }
+                    *p = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
                 }
         }
     }
@@ -610,8 +618,8 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
             g.b = d; g.ldb = ld;
             g.m = width; g.n = p.rows; g.k = piece;
             g.chunk = p.chunk; g.splits = (int)cut(piece, p.chunk);
-            if (p.ranges == 1 && at.size() == 2 && !accumulate)
-                gemm_bf16<true, false>(st, g, RoundEpilogue{(unsigned short *)dx, inv, width}, "linear_ce input gradient launch");
+            if (p.ranges == 1 && at.size() == 2)      // the workspace holds no sums then
+                gemm_bf16<true, false>(st, g, RoundEpilogue{(unsigned short *)dx, inv, width, accumulate}, "linear_ce input gradient launch");
             else {
                 gemm_bf16<true, false>(st, g, SumEpilogue{parts, width, rows * width, i > 0}, "linear_ce input gradient launch");
                 if (i + 2 == at.size()) {
@@ -624,7 +632,7 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
             g.a = (const unsigned short *)x; g.lda = width;
             g.m = width; g.n = piece; g.k = p.rows;
             g.splits = 1; g.chunk = (int)up(rows, GEMM_DEPTH);
-            gemm_bf16<true, true>(st, g, RoundEpilogue{(unsigned short *)dw + (int64_t)v0 * width, inv, width}, "linear_ce weight gradient launch");
+            gemm_bf16<true, true>(st, g, RoundEpilogue{(unsigned short *)dw + (int64_t)v0 * width, inv, width, false}, "linear_ce weight gradient launch");
         } else {
             const ConvShape cs = ce_conv_shape(p, piece);
             const float *wp = (const float *)w + (int64_t)v0 * width;
