@@ -295,7 +295,8 @@ int64_t monet_linear_ce_workspace_bytes(int grad, int dtype, int64_t rows, int w
  * smallest from e = -126 up with max|x| / 2^e < 127.5, and a code is x / 2^e rounded to nearest, ties to even.  A group with an
  * infinity or a NaN stands for NaN throughout.  code: monet_act8_bytes(rows, cols) bytes, 16-byte aligned: rows of
  * round_up(cols, 32) signed codes (zero behind the last column), then rows of one byte e + 127 per group.  ld: elements from one
- * row of x (y) to the next; rows * round_up(cols, 32) below 2^35.  code * 2^e is exact in fp32 and bf16, so unpack rounds nothing. */
+ * row of x (y) to the next; rows * round_up(cols, 32) below 2^35.  code * 2^e is exact in fp32 and bf16, so unpack rounds nothing;
+ * only 2^128, which values beyond 63.5 * 2^122 are rounded to, is an infinity in both. */
 int64_t monet_act8_bytes(int64_t rows, int64_t cols);
 int monet_act8_pack(void *stream, int dtype, const void *x, int64_t ld, void *code, int64_t rows, int64_t cols);
 int monet_act8_unpack(void *stream, int dtype, const void *code, void *y, int64_t ld, int64_t rows, int64_t cols);

@@ -105,9 +105,10 @@ __global__ __launch_bounds__(256) void act8_unpack_kernel(const int8_t *__restri
 }
 
 // dw[o][c] = sum over rows of dy[row][o] x[row][c]: both operands run across the reduction (DEEP tiles, tile_bf16.hpp).  The codes become
-// bf16 on their way to LDS: a byte u = code + 128 to a float, then u 2^e - 128 2^e in one exact multiply-add.  bf16 dy goes in as it is,
-// fp32 dy in three pieces (bf16_pieces.hpp), three instructions a product and nothing lost above 2^-110.  128 x 128 results to a workgroup of four
-// waves, two workgroups a CU.  One of these has its conversions and its barrier while the other one multiplies; that, not memory, bounds it:
+// bf16 on their way to LDS: a signed byte to a float, times 2^e, both exact.  (By way of code + 128 and a multiply-add, as many instructions,
+// 128 2^e is infinite in groups that reach 2^127.)  bf16 dy goes in as it is, fp32 dy in three pieces (bf16_pieces.hpp), three instructions a
+// product and nothing lost above 2^-110.  128 x 128 results to a workgroup of four waves, two workgroups a CU.  One of these has its
+// conversions and its barrier while the other one multiplies; that, not memory, bounds it:
 // 4096 x 2048 x 1024 40 us in bf16 (431 TFLOP/s), 68 in fp32 (254, times three).
 struct Act8Shape {
     const int8_t *code;
@@ -190,13 +191,12 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN * 64 / 256) void act8_wgrad_ker
 #pragma unroll
         for (int i = 0; i < CODES; ++i) {
             const int piece = i * THREADS + threadIdx.x, kr = piece / (BM / 16), c = piece % (BM / 16) * 2;
-            const unsigned w[4] = {h.codes[i][0] ^ 0x80808080u, h.codes[i][1] ^ 0x80808080u, h.codes[i][2] ^ 0x80808080u, h.codes[i][3] ^ 0x80808080u};
-            const float s = __uint_as_float(h.exps[i] << 23), mid = -128.f * s;
+            const float s = __uint_as_float(h.exps[i] << 23);
             unsigned out[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const unsigned b = w[j / 2] >> (16 * (j % 2));
-                const float lo = fmaf((float)(b & 0xffu), s, mid), hi = fmaf((float)((b >> 8) & 0xffu), s, mid);
+                const unsigned b = h.codes[i][j / 2] >> (16 * (j % 2));
+                const float lo = (float)(int8_t)b * s, hi = (float)(int8_t)(b >> 8) * s;
                 out[j] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
             }
             char *p = a_lds[buf] + place(kr, c, BM * 2);

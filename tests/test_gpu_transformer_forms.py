@@ -53,3 +53,34 @@ def test_linear_ce_adds_to_dx_and_leaves_dw(case, dtype):
     # one more rounding of the sum (fp32: of each piece's sum)
     r = R if dtype == monet.BF16 else 8 * U
     within(host(added), total, bound[2] + 1.1 * r * (np.abs(total) + np.abs(host(start))), "added dx")
+
+
+# ---------------------------------------------------------------------- 8-bit activations
+@pytest.mark.parametrize("dtype", [monet.F32, monet.BF16])
+@pytest.mark.parametrize("rows,cols,outs", [(70, 96, 40), (2000, 4090, 2500)])
+def test_act8_wgrad_of_groups_up_to_the_largest_numbers(dtype, rows, cols, outs):
+    """Groups whose maximum lies at 2^115 to 2^127.98 (the largest that rounds to a code times a power below 2^128 is 63.5 2^122): both forms of
+    the weight gradient, directly from the codes and (the larger case in bf16) through the workspace."""
+    torch = torch_mod()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(22)
+    groups = -(-cols // 32)
+    top = torch.exp2(torch.linspace(115.0, 127.98, groups, device="cuda", dtype=torch.float64))
+    x = torch.rand(rows, groups * 32, generator=g, device="cuda", dtype=torch.float64) * 2 - 1
+    x[:, ::32] = 1.0
+    x = (x.view(rows, groups, 32) * top[:, None]).view(rows, -1)[:, :cols].float().contiguous()
+    dy = (torch.randn(rows, outs, generator=g, device="cuda") * (1e-2 / rows)).to(tdtype(dtype))
+    code = torch.zeros(monet.call("monet_act8_bytes", rows, cols), dtype=torch.uint8, device="cuda")
+    back = torch.empty_like(x)
+    monet.call("monet_act8_pack", None, monet.F32, x.data_ptr(), cols, code.data_ptr(), rows, cols)
+    monet.call("monet_act8_unpack", None, monet.F32, code.data_ptr(), back.data_ptr(), cols, rows, cols)
+    # half a step of a group, 2^e with max / 2^e >= 63.75
+    step = torch.exp2(torch.floor(torch.log2(top)) - 5).repeat_interleave(32)[:cols]
+    assert torch.isfinite(back).all() and ((back.double() - x.double()).abs() <= 0.5 * step).all()
+    need = monet.call("monet_act8_wgrad_workspace_bytes", dtype, rows, cols, outs)
+    ws = torch.full((max(need, 16),), 255, dtype=torch.uint8, device="cuda")
+    dw = torch.full((outs, cols), float("nan"), device="cuda")
+    monet.call("monet_act8_wgrad", None, dtype, code.data_ptr(), dy.data_ptr(), dw.data_ptr(), rows, cols, outs, ws.data_ptr(), need)
+    want, mag = dy.double().t() @ back.double(), dy.double().abs().t() @ back.double().abs()
+    assert torch.isfinite(dw).all()
+    assert ((dw.double() - want).abs() <= 1.1 * (3 * rows + 8) * U * mag).all()
