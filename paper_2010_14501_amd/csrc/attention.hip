@@ -410,7 +410,7 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS ? 2 : 1)) vo
                 for (int r = 0; r < 16; ++r) acc[c][r] *= f;
             top = next;
         }
-        const float base = PARTS > 1 && top == -INFINITY ? 0.f : top;      // a part of a row may see no key at all
+        const float base = top == -INFINITY ? 0.f : top;      // no key yet that has a weight: a part of a row may see none, scores may be -infinity
 #pragma unroll
         for (int b = 0; b < B; ++b) {
 #pragma unroll

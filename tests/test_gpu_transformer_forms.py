@@ -84,3 +84,43 @@ def test_act8_wgrad_of_groups_up_to_the_largest_numbers(dtype, rows, cols, outs)
     want, mag = dy.double().t() @ back.double(), dy.double().abs().t() @ back.double().abs()
     assert torch.isfinite(dw).all()
     assert ((dw.double() - want).abs() <= 1.1 * (3 * rows + 8) * U * mag).all()
+
+
+# ---------------------------------------------------------------------- attention: special values
+@pytest.mark.parametrize("dtype", [monet.F32, monet.BF16])
+@pytest.mark.parametrize("heads,kv_heads,dim,tokens", [(2, 1, 64, 200), (32, 4, 64, 4224), (2, 1, 128, 200), (32, 4, 128, 4224)])
+def test_attention_of_scores_that_overflow_to_minus_infinity(dtype, heads, kv_heads, dim, tokens):
+    """The first 150 keys' scores are beyond -3.4e38 for every row behind them: weight 0 there, whichever form the sizes choose (4224 rows and 32
+    heads: 128 rows to a workgroup).  The rows before see such keys only, and have no result that means anything."""
+    torch = torch_mod()
+    rng = np.random.default_rng(23)
+    blind = 150
+    q = np.zeros((tokens, heads, dim), np.float32)
+    k = (rng.standard_normal((tokens, kv_heads, dim)) * 2.0 ** -60).astype(np.float32)
+    v = rng.standard_normal((tokens, kv_heads, dim)).astype(np.float32)
+    q[:, :, 0] = 2.0 ** 64                             # scores of the others: 2^64 2^-60 n / 8, about 2
+    k[:blind, :, :] = 0.0
+    k[:blind, :, 0] = -2.0 ** 70
+    q, tq = rounded(q.reshape(tokens, -1), dtype)
+    k, tk = rounded(k.reshape(tokens, -1), dtype)
+    v, tv = rounded(v.reshape(tokens, -1), dtype)
+    o, lse = torch.full_like(tq, -7.0), torch.full((heads, tokens), -7.0, device="cuda")
+    cu = torch.tensor([0, tokens], dtype=torch.int32, device="cuda")
+    monet.call("monet_attention_fwd", torch.cuda.current_stream().cuda_stream, dtype, tq.data_ptr(), tk.data_ptr(), tv.data_ptr(), o.data_ptr(),
+               lse.data_ptr(), cu.data_ptr(), 1, tokens, heads, kv_heads, dim, heads * dim, kv_heads * dim, kv_heads * dim, heads * dim, 0.125)
+    # all heads of a group are alike, and so are a row's scores but for its key
+    for h in range(0, heads, heads // kv_heads):
+        kv = h * kv_heads // heads
+        s = (0.125 * q.reshape(tokens, heads, dim)[0, h, 0] * k.reshape(tokens, kv_heads, dim)[blind:, kv, 0])
+        e = np.exp(s - s.max())
+        total = np.cumsum(e)
+        w = v.reshape(tokens, kv_heads, dim)[blind:, kv]
+        want, want_lse = np.cumsum(e[:, None] * w, 0) / total[:, None], s.max() + np.log(total)
+        mag = np.cumsum(e[:, None] * np.abs(w), 0) / total[:, None]
+        # a score is one product (two roundings, and the exponential's; the difference from the maximum), the sums run over the keys; bf16 rounds
+        # the weights and the result
+        n = np.arange(1, tokens - blind + 1)[:, None]
+        es = 8 * U * np.abs(s).max() * 2 + (n + 24) * U
+        r = R if dtype == monet.BF16 else 0.0
+        within(host(o).reshape(tokens, heads, dim)[blind:, h], want, 1.1 * ((2 * es + 2 * r) * mag) + 1e-30, "o")
+        within(host(lse)[h, blind:], want_lse, (es + 4 * U * np.abs(want_lse)[:, None])[:, 0] + 1e-30, "lse")
