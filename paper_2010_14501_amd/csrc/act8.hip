@@ -388,16 +388,21 @@ size_t act8_bytes(int64_t rows, int64_t cols) {
     return (size_t)(rows * (code_ld(cols) / GROUP) * (GROUP + 1));
 }
 
+// a launch of eight values a thread takes less than 2^24 workgroups
+void act8_check_values(int64_t rows, int64_t cols) {
+    check_shape(rows, cols);
+    if ((rows * (code_ld(cols) / 8) + 255) / 256 >= 1 << 24) throw KernelError("act8: too many values");
+}
+
 void act8_pack(hipStream_t st, int dtype, const void *x, int64_t ld, void *code, int64_t rows, int64_t cols) {
     check_type(dtype);
-    check_shape(rows, cols);
+    act8_check_values(rows, cols);
     const int es = dtype == MONET_F32 ? 4 : 2;
     check_tensor(x, es);
     check_tensor(code, 16);
     if (ld < cols) throw KernelError("act8_pack: row stride below the number of columns");
     const int per_row = (int)(code_ld(cols) / 8);
     const int64_t blocks = (rows * per_row + 255) / 256;
-    if (blocks >= 1 << 24) throw KernelError("act8_pack: too many values");
     uint8_t *exps = (uint8_t *)code + rows * code_ld(cols);
     if (dtype == MONET_F32)
         hipLaunchKernelGGL((act8_pack_kernel<float>), dim3((unsigned)blocks), dim3(256), 0, st, (const float *)x, ld, (int8_t *)code, exps, rows, (int)cols, per_row);
@@ -408,14 +413,13 @@ void act8_pack(hipStream_t st, int dtype, const void *x, int64_t ld, void *code,
 
 void act8_unpack(hipStream_t st, int dtype, const void *code, void *y, int64_t ld, int64_t rows, int64_t cols) {
     check_type(dtype);
-    check_shape(rows, cols);
+    act8_check_values(rows, cols);
     const int es = dtype == MONET_F32 ? 4 : 2;
     check_tensor(y, es);
     check_tensor(code, 16);
     if (ld < cols) throw KernelError("act8_unpack: row stride below the number of columns");
     const int per_row = (int)(code_ld(cols) / 8);
     const int64_t blocks = (rows * per_row + 255) / 256;
-    if (blocks >= 1 << 24) throw KernelError("act8_unpack: too many values");
     const uint8_t *exps = (const uint8_t *)code + rows * code_ld(cols);
     if (dtype == MONET_F32)
         hipLaunchKernelGGL((act8_unpack_kernel<float>), dim3((unsigned)blocks), dim3(256), 0, st, (const int8_t *)code, exps, (float *)y, ld, rows, (int)cols, per_row);

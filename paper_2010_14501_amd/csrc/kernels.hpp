@@ -235,6 +235,7 @@ void linear_ce_fwd(hipStream_t st, int dtype, const void *x, const void *w, cons
 void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *labels, const float *lse, void *dx, void *dw,
                    int64_t rows, int width, int vocab, bool accumulate, void *ws, size_t ws_bytes);
 size_t act8_bytes(int64_t rows, int64_t cols);
+void act8_check_values(int64_t rows, int64_t cols);      // refuses what pack and unpack refuse
 void act8_pack(hipStream_t st, int dtype, const void *x, int64_t ld, void *code, int64_t rows, int64_t cols);
 void act8_unpack(hipStream_t st, int dtype, const void *code, void *y, int64_t ld, int64_t rows, int64_t cols);
 size_t act8_wgrad_workspace_bytes(int dtype, int64_t rows, int64_t cols, int64_t outs);

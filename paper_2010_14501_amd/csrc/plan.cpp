@@ -3,6 +3,9 @@
 // -> event trace, kernel launch list with resolved arena offsets, predicted peak.
 #include "plan.hpp"
 
+#include "../../include/monet_kernels.h"
+#include "kernels.hpp"
+
 #include <algorithm>
 #include <deque>
 #include <sstream>
@@ -290,20 +293,42 @@ static void check_declared_deps(const Graph &g) {
     }
 }
 
-// Shapes that the kernels of a transformer's operators take from the graph text.
+// What the kernels of a transformer's operators take from the graph text: shapes within their limits, workspaces that are large enough, backward
+// operators at the nodes they belong to.  A step so finds nothing to refuse between its launches.
 static void check_transformer_nodes(const Graph &g) {
     for (const Node &n : g.nodes) {
-        auto need = [&](bool ok, const char *what) {
-            if (!ok) throw PlanError(MONET_BAD_GRAPH, "node " + std::to_string(n.id) + " (" + n.op + "): " + what);
+        const std::string who = "node " + std::to_string(n.id) + " (" + n.op + "): ";
+        auto need = [&](bool ok, const std::string &what) {
+            if (!ok) throw PlanError(MONET_BAD_GRAPH, who + what);
         };
         const Node *aux = n.aux_children.empty() ? nullptr : &g.nodes[n.aux_children[0]];
         auto offsets = [&](int ref, int64_t count) {
             return ref <= 0 && g.exts[-ref].dtype == "i32" && numel(g.exts[-ref].shape) == count;
         };
+        // the kernels' own limits, by asking for a workspace
+        auto workspace = [&](auto bytes) -> int64_t {
+            try {
+                return (int64_t)bytes();
+            } catch (const KernelError &e) {
+                throw PlanError(MONET_BAD_GRAPH, who + e.what());
+            }
+        };
+        auto enough = [&](int64_t ws, int64_t bytes) {
+            need((ws > 0 ? align_up(ws) : 0) >= bytes, "a workspace of " + std::to_string(ws) + " bytes is declared, " + std::to_string(bytes) + " are needed");
+        };
+        // every implementation of this node's backward operators of that kind
+        auto each_impl = [&](const char *kind, const char *algo, int64_t bytes) {
+            for (const Bop &b : g.bops)
+                if (b.node == n.id && b.kind == kind)
+                    for (const BwdImpl &im : b.impls)
+                        if (im.algo == algo) enough(im.ws, bytes);
+        };
         if (n.op == "attention") {
             const int64_t heads = n.attr_int("heads"), kv = n.attr_int("kv_heads"), dim = n.attr_int("dim"), seqs = n.attr_int("seqs");
             need(heads > 0 && kv > 0 && heads % kv == 0 && dim > 0 && seqs > 0, "heads, kv_heads, dim and seqs must be positive, heads a multiple of kv_heads");
             need(dim % 8 == 0 && dim <= 128, "dim must be a multiple of 8 up to 128");
+            const float scale = (float)n.attr_f("scale", 1.0);
+            need(scale > 0.f && scale <= 1e30f, "scale must be positive and finite");
             need(n.ins.size() == 4 && n.ins[0] > 0 && n.ins[1] > 0 && n.ins[2] > 0, "inputs are three nodes and the sequences' offsets");
             need(n.ins[0] != n.ins[1] && n.ins[0] != n.ins[2] && n.ins[1] != n.ins[2], "queries, keys and values must be three tensors");
             need(n.shape.size() == 2 && n.shape[1] == heads * dim && g.shape_of(n.ins[0]) == n.shape, "queries and output must be tokens x (heads * dim)");
@@ -311,16 +336,38 @@ static void check_transformer_nodes(const Graph &g) {
             need(g.shape_of(n.ins[1]) == kv_shape && g.shape_of(n.ins[2]) == kv_shape, "keys and values must be tokens x (kv_heads * dim)");
             need(offsets(n.ins[3], seqs + 1), "offsets must be an external i32 tensor of seqs + 1 values");
             need(aux && aux->op == "lse" && numel(aux->shape) == heads * n.shape[0], "needs an intermediate lse of heads x tokens");
+            each_impl("attention_bwd", "fused", workspace([&] {
+                return attention_bwd_workspace_bytes(MONET_F32, (int)seqs, n.shape[0], (int)heads, (int)kv, (int)dim);
+            }));
         } else if (n.op == "linearce") {
             need(n.persist && n.ins.size() == 2 && n.ins[0] > 0 && n.pars.size() == 1, "is a persistent node with an input, labels and a parameter");
             const auto &x = g.shape_of(n.ins[0]), &w = g.params[n.pars[0]].shape;
             need(x.size() == 2 && w.size() == 2 && x[1] == w[1], "input rows x width and parameter vocab x width do not fit");
             need(offsets(n.ins[1], x[0]), "labels must be an external i32 tensor of one value per row");
+            need(x[1] <= INT32_MAX && w[0] <= INT32_MAX, "width or vocabulary too large");
+            const auto bytes = [&](bool grad) { return workspace([&] { return linear_ce_workspace_bytes(grad, MONET_F32, x[0], (int)x[1], (int)w[0]); }); };
+            for (const FwdImpl &im : n.fimpls) enough(im.ws, bytes(false));
+            each_impl("linearce_bwd", "pieces", bytes(true));
         } else if (n.op == "linear" && aux) {
             const auto &x = g.shape_of(n.ins[0]);
             need(aux->op == "act8" && x.size() == 2 && numel(aux->shape) == x[0] * ((x[1] + 31) / 32) * 33, "the 8-bit copy of an input rows x cols has rows * ceil(cols / 32) * 33 bytes");
+            need(n.shape.size() == 2, "output must be rows x outputs");
+            each_impl("linear_wgrad", "from_code", workspace([&] {
+                act8_check_values(x[0], x[1]);
+                return act8_wgrad_workspace_bytes(MONET_F32, x[0], x[1], n.shape[1]);
+            }));
         } else if (aux && (aux->op == "lse" || aux->op == "act8"))
             need(false, "does not write such an intermediate");
+    }
+    for (const Bop &b : g.bops) {
+        const Node &n = g.nodes[b.node];
+        auto belongs = [&](bool ok) {
+            if (!ok) throw PlanError(MONET_BAD_GRAPH, "backward operator " + std::to_string(b.k) + " (" + b.kind + ") does not belong to node " + std::to_string(n.id) + " (" + n.op + ")");
+        };
+        if (b.kind == "attention_bwd") belongs(n.op == "attention");
+        if (b.kind == "linearce_bwd") belongs(n.op == "linearce");
+        for (const BwdImpl &im : b.impls)
+            if (im.algo == "from_code") belongs(b.kind == "linear_wgrad" && n.op == "linear");
     }
 }
 

@@ -84,3 +84,58 @@ def test_graph_texts_that_do_not_fit_are_refused(old, new, match):
     assert old in text, [line for line in text.splitlines() if line.split()[0] in ("ext", "param") or "attention" in line]
     with pytest.raises(M.MonetError, match=match):
         M.Plan(text.replace(old, new, 1), schedules.store_everything_schedule(g).text())
+
+
+@pytest.mark.parametrize("old,new,match", [
+    ("seqs=3 scale=0.25", "seqs=3 scale=0", "scale"),
+    ("seqs=3 scale=0.25", "seqs=3 scale=-0.25", "scale"),
+    ("seqs=3 scale=0.25", "seqs=3 scale=nan", "scale"),
+    ("seqs=3 scale=0.25", "seqs=3 scale=inf", "scale"),
+    ("deps=2,4,6,8,9 ws=2048", "deps=2,4,6,8,9 ws=1792", "2048 are needed"),
+    ("deps=2,4,6,8,9 ws=2048", "deps=2,4,6,8,9 ws=-1000", "2048 are needed"),
+    ("fimpl 38 0 algo=pieces ws=77824", "fimpl 38 0 algo=pieces ws=77568", "77824 are needed"),
+    ("deps=37 ws=339200", "deps=37 ws=338944", "339200 are needed"),
+    ("bop 8 attention_bwd node=8", "bop 8 attention_bwd node=6", "does not belong"),
+    ("bop 34 linearce_bwd node=38", "bop 34 linearce_bwd node=37", "does not belong"),
+    ("bop 1 linear_wgrad node=1", "bop 1 attention_bwd node=1", "does not belong"),
+    ("bimpl 14 0 algo=copy", "bimpl 14 0 algo=from_code", "does not belong"),
+])
+def test_graph_texts_that_a_step_would_refuse_are_refused_when_loaded(old, new, match):
+    """A step that finds something to refuse has launched what comes before it: scales, declared workspaces and the nodes of backward operators
+    are looked at when the text is."""
+    g = graphs.transformer()
+    text = g.text()
+    if old.startswith("bimpl 14"):
+        old = next(line for line in text.splitlines() if line.startswith("bimpl 14 0 ")).split(" deps=")[0]
+    assert text.count(old) >= 1, old
+    M.Plan(text, schedules.store_everything_schedule(g).text())
+    with pytest.raises(M.MonetError, match=match):
+        M.Plan(text.replace(old, new, 1), schedules.store_everything_schedule(g).text())
+
+
+def test_workspaces_of_codes_are_checked_when_a_graph_is_loaded():
+    """From 512 rows on the weight gradient from 8 bits is summed in ranges, which need a workspace: twice 64 x 64 fp32 sums here."""
+    g = graphs.transformer(lens=(1024,), layers=1)
+    text = g.text()
+    old = [line for line in text.splitlines() if "algo=from_code" in line][0]
+    ws = int(old.split(" ws=")[1].split()[0])
+    assert ws >= 2 * 64 * 64 * 4
+    sch = schedules.store_everything_schedule(g).text()
+    M.Plan(text, sch)
+    for less in (0, ws - 256):
+        with pytest.raises(M.MonetError, match="are needed"):
+            M.Plan(text.replace(old, old.replace(f" ws={ws}", f" ws={less}"), 1), sch)
+
+
+def test_attention_of_more_heads_and_tokens_than_a_launch_takes_is_refused_when_loaded():
+    """(tokens / 64 + seqs) * heads has to stay below 2^24; nothing of that size is allocated here."""
+    g = graphs.transformer(code=False)
+    sch = schedules.store_everything_schedule(g).text()
+    text = g.text()
+    tokens = (1 << 28) + 64
+    for kind in ("64x64", "64x32", "64x128"):
+        text = text.replace(f" shape={kind}", f" shape={tokens}x{kind[3:]}")
+    text = text.replace("shape=4x64", f"shape=4x{tokens}")
+    text = text.replace("ext -1 labels i32 64", f"ext -1 labels i32 {tokens}").replace("ext 0 embedded f32 64x64", f"ext 0 embedded f32 {tokens}x64")
+    with pytest.raises(M.MonetError, match="too many"):
+        M.Plan(text, sch)
