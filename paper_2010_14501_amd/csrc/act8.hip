@@ -378,6 +378,7 @@ WgradPlan wgrad_plan(int dtype, int64_t rows, int cols, int outs, bool aligned) 
     p.chunk = up((first + splits - 1) / splits, 64);
     p.splits = (int)((first + p.chunk - 1) / p.chunk);
     p.part_bytes = p.splits > 1 ? up((int64_t)p.splits * cols * outs * 4, 256) : 0;
+    if (p.expanded ? !gemm_fits(cols, outs, p.splits, p.ld, up(outs, 8)) : tiles >= 1 << 24) throw KernelError("act8_wgrad: result too large");
     return p;
 }
 
@@ -487,7 +488,6 @@ void act8_wgrad(hipStream_t st, int dtype, const void *code, const void *dy, flo
         g.tiles_m = (int)((cols + 127) / 128);
         g.tiles_n = (int)((outs + 127) / 128);
         g.vec_out = vec_out;
-        if ((int64_t)g.tiles_m * g.tiles_n >= 1 << 24) throw KernelError("act8_wgrad: result too large");
         const dim3 grid(g.tiles_m * g.tiles_n, p.splits);
         if (dtype == MONET_F32) hipLaunchKernelGGL((act8_wgrad_kernel<true, true, 128, 128, 2, 2>), grid, dim3(256), 0, st, g);
         else if ((uintptr_t)dy % 4 == 0 && outs % 2 == 0) hipLaunchKernelGGL((act8_wgrad_kernel<false, true, 128, 128, 2, 2>), grid, dim3(256), 0, st, g);

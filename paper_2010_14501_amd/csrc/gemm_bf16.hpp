@@ -181,12 +181,15 @@ constexpr int64_t GEMM_MOST_LD = 1 << 23;      // row strides are below this: 25
 
 // Tiles of 256 x 256 (8 waves) where they give every CU one, of 128 x 128 (4 waves, two workgroups a CU) otherwise.
 inline int gemm_tile(int64_t m, int64_t n, int splits = 1) { return ((m + 255) / 256) * ((n + 255) / 256) * splits >= 256 ? 256 : 128; }
+// Whether a launch takes so many tiles (less than 2^32 threads) and the addresses such strides.
+inline bool gemm_fits(int64_t m, int64_t n, int splits, int64_t lda, int64_t ldb) {
+    const int64_t b = gemm_tile(m, n, splits), tiles = ((m + b - 1) / b) * ((n + b - 1) / b);
+    return lda < GEMM_MOST_LD && ldb < GEMM_MOST_LD && lda % 8 == 0 && ldb % 8 == 0 && tiles < (b == 256 ? 1 << 23 : 1 << 24);
+}
 template <bool A_DEEP, bool B_DEEP, class Epi>
 void gemm_bf16(hipStream_t st, GemmShape g, const Epi &epi, const char *what) {
-    const auto tiles = [&](int64_t b) { return (g.m + b - 1) / b * ((g.n + b - 1) / b); };
+    if (!gemm_fits(g.m, g.n, g.splits, g.lda, g.ldb)) throw KernelError(std::string(what) + ": operand too large");
     const int b = gemm_tile(g.m, g.n, g.splits);
-    // a launch takes less than 2^32 threads
-    if (g.lda >= GEMM_MOST_LD || g.ldb >= GEMM_MOST_LD || g.lda % 8 || g.ldb % 8 || tiles(b) >= (b == 256 ? 1 << 23 : 1 << 24)) throw KernelError(std::string(what) + ": operand too large");
     g.tiles_m = (g.m + b - 1) / b;
     g.tiles_n = (g.n + b - 1) / b;
     const dim3 grid(g.tiles_m * g.tiles_n, g.splits);

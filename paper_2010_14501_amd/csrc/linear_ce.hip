@@ -493,6 +493,7 @@ CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab) {
     if (rows >= (1 << 24) || width > (1 << 20) || vocab > (1 << 28)) throw KernelError("linear_ce: shape too large");
     CePlan p{(int)rows, width, vocab, bf16};
     if (bf16 && !grad) {
+        if (!gemm_fits(vocab, rows, 1, width, width)) throw KernelError("linear_ce: rows * vocab too large");
         p.unit = gemm_tile(vocab, rows) / 2;
         p.fixed = 2 * up(rows * 4, 256) + up(p.parts() * rows * 8, 256);
         return p;
@@ -510,6 +511,9 @@ CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab) {
     p.fixed = 256;
     if (bf16) {
         p.ranges = ce_input_ranges(rows, width, p.piece);
+        const int64_t ld = up(p.piece, 8);
+        if (!gemm_fits(p.piece, rows, 1, width, width) || !gemm_fits(width, rows, p.ranges, width, ld) || !gemm_fits(width, p.piece, 1, width, ld))
+            throw KernelError("linear_ce: rows * width too large");      // before anything is launched
         p.chunk = (int)up(cut(p.piece, p.ranges), GEMM_DEPTH);
         p.ranges = (int)cut(std::min(p.piece, vocab), p.chunk);      // a later piece is no longer than the first
         if (p.ranges > 1 || p.piece < vocab) p.fixed += up(p.ranges * rows * width * 4, 256);

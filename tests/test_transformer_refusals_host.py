@@ -1,0 +1,26 @@
+"""Calls that the transformer operators refuse before anything is enqueued, which needs no GPU: the addresses are never read."""
+import pytest
+
+from paper_2010_14501_amd import monet
+
+P = 1 << 20
+
+
+def test_linear_ce_refuses_large_products_before_its_first_launch():
+    rows, width = (1 << 24) - 1, 1 << 20
+    with pytest.raises(monet.MonetError, match="too large"):
+        monet.call("monet_linear_ce_workspace_bytes", 1, monet.BF16, rows, width, 64)
+    with pytest.raises(monet.MonetError, match="too large"):
+        monet.call("monet_linear_ce_bwd", None, monet.BF16, P, P, P, P, P, P, rows, width, 64, 0, P, 1 << 60)
+    # rows x width tiles of 256: 2^23 are too many, a row less of them is not
+    assert monet.call("monet_linear_ce_workspace_bytes", 1, monet.BF16, ((1 << 15) - 1) * 256, 1 << 16, 64) > 0
+    with pytest.raises(monet.MonetError, match="too large"):
+        monet.call("monet_linear_ce_workspace_bytes", 1, monet.BF16, (1 << 15) * 256, 1 << 16, 64)
+
+
+def test_act8_wgrad_refuses_large_results_before_its_first_launch():
+    for cols, outs in ((1 << 22, 1 << 22), (1 << 24, 1 << 24)):          # through the workspace, and directly
+        with pytest.raises(monet.MonetError, match="too large"):
+            monet.call("monet_act8_wgrad_workspace_bytes", monet.BF16, 64, cols, outs)
+        with pytest.raises(monet.MonetError, match="too large"):
+            monet.call("monet_act8_wgrad", None, monet.BF16, P, P, P, 64, cols, outs, P, 1 << 60)
