@@ -260,8 +260,8 @@ enum monet_dtype { MONET_F32 = 0, MONET_BF16 = 1 };
  * head_dim apart).  lse [heads][tokens] fp32 (forward: NULL if nobody needs it).  cu_seqlens: device, seqs + 1 ascending offsets; sequence s holds tokens
  * cu_seqlens[s] .. cu_seqlens[s + 1] - 1 and may be empty.  Tokens before the first and behind the last one are neither read
  * nor written, in any output.  Offsets are held to 0 .. tokens, so that others cannot lead out of the tensors.
- * Needs heads % kv_heads == 0, head_dim a multiple of 8 up to 128, scale > 0, pointers and strides that are multiples of
- * 16 bytes, tokens below 2^31, (tokens / 64 + seqs) * heads below 2^24; o must not overlap an input.  tokens == 0 is allowed and does nothing.  A sequence's infinities and NaNs stay in that sequence.
+ * Needs heads % kv_heads == 0, head_dim a multiple of 8 up to 128, scale > 0, tensors and strides that are multiples of
+ * 16 bytes (lse and offsets of 4), tokens below 2^31, (tokens / 64 + seqs) * heads below 2^24; o must not overlap an input.  tokens == 0 is allowed and does nothing.  A sequence's infinities and NaNs stay in that sequence.
  * Within it, one in k or v reaches the rows from its own on and may reach up to 127 rows before it.  fp32: the products go through
  * three bf16 pieces of each operand, exact from 2^-110 up; an infinity in a tensor comes out as NaN. */
 int monet_attention_fwd(void *stream, int dtype, const void *q, const void *k, const void *v, void *o, float *lse,
@@ -279,7 +279,7 @@ int64_t monet_attention_bwd_workspace_bytes(int dtype, int seqs, int64_t tokens,
 /* Softmax cross entropy of a linear layer over a large vocabulary, in pieces of the vocabulary; the logits x w^T are not kept.
  * x [rows][width], w [vocab][width], labels [rows]; a row whose label is outside 0 .. vocab - 1 carries no loss and no gradient.
  *   lse[row] = log sum exp of the row's logits (all rows);  loss = mean over the rows with a label of lse - logit[label], 0 if there are none.
- * Needs, for bf16, width % 8 == 0 and 16-byte aligned x and w; rows below 2^24, width at most 2^20, vocab 2^28.
+ * Needs, for bf16, width % 8 == 0 and 16-byte aligned tensors (everything else: 4 bytes); rows below 2^24, width at most 2^20, vocab 2^28.
  * ws_bytes >= monet_linear_ce_workspace_bytes(grad = 0, ...). */
 int monet_linear_ce_fwd(void *stream, int dtype, const void *x, const void *w, const int32_t *labels, float *loss, float *lse,
                         int64_t rows, int width, int vocab, void *ws, size_t ws_bytes);

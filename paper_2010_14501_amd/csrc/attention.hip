@@ -818,6 +818,7 @@ AttShape att_shape(int dtype, const int32_t *cu, int seqs, int64_t tokens, int h
         if (ld < (int64_t)kv_heads * head_dim || ld % step || ld >= (1 << 23)) throw KernelError("attention: row strides must hold all heads, be a multiple of 16 bytes and below 2^23 elements");
     if (tokens > 0x7fffffff || (tokens / 64 + seqs) * heads >= 1 << 24) throw KernelError("attention: too many tokens");
     if (!cu) throw KernelError("attention: null pointer");
+    if ((uintptr_t)cu % 4) throw KernelError("attention: offsets and lse must be 4-byte aligned");
     return AttShape{cu, seqs, (int)tokens, heads, kv_heads, head_dim, 0, q_ld, k_ld, v_ld, o_ld, scale};
 }
 void check_tensors(std::initializer_list<const void *> ptrs) {
@@ -825,6 +826,9 @@ void check_tensors(std::initializer_list<const void *> ptrs) {
         if (!p) throw KernelError("attention: null pointer");
         if ((uintptr_t)p % 16) throw KernelError("attention: tensors must be 16-byte aligned");
     }
+}
+void check_lse(const float *lse) {
+    if ((uintptr_t)lse % 4) throw KernelError("attention: offsets and lse must be 4-byte aligned");
 }
 
 // Rows of the forward and the first backward kernel: 128 to a workgroup where that gives four workgroups to a CU (fp32 with 128 columns, whose
@@ -910,6 +914,7 @@ void attention_fwd(hipStream_t st, int dtype, const void *q, const void *k, cons
     const AttShape a = att_shape(dtype, cu, seqs, tokens, heads, kv_heads, head_dim, q_ld, k_ld, v_ld, o_ld, scale);
     if (!tokens) return;
     check_tensors({q, k, v, o});
+    check_lse(lse);
     if (dtype == MONET_BF16) (head_dim <= 64 ? fwd_form<unsigned short, 64> : fwd_form<unsigned short, 128>)(st, a, q, k, v, o, lse);
     else (head_dim <= 64 ? fwd_form<float, 64> : fwd_form<float, 128>)(st, a, q, k, v, o, lse);
 }
@@ -929,6 +934,7 @@ void attention_bwd(hipStream_t st, int dtype, const void *go, const void *q, con
     if (!tokens) return;
     check_tensors({go, q, k, v, o, dq, dk, dv});
     if (!lse) throw KernelError("attention: null pointer");
+    check_lse(lse);
     if (accumulate & ~7) throw KernelError("attention: accumulate has one bit each for dq, dk and dv");
     if (!ws || ws_bytes < attention_bwd_workspace_bytes(dtype, seqs, tokens, heads, kv_heads, head_dim))
         throw KernelError("attention: workspace too small");

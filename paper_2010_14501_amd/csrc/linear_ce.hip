@@ -538,7 +538,13 @@ void check_ws(const CePlan &p, const void *ws, size_t ws_bytes) {
 void check_aligned(const CePlan &p, std::initializer_list<const void *> ptrs) {
     for (const void *q : ptrs) {
         if (!q) throw KernelError("linear_ce: null pointer");
-        if ((uintptr_t)q % (p.bf16 ? 16 : 4)) throw KernelError("linear_ce: bf16 tensors must be 16-byte aligned");
+        if ((uintptr_t)q % (p.bf16 ? 16 : 4)) throw KernelError(p.bf16 ? "linear_ce: bf16 tensors must be 16-byte aligned" : "linear_ce: fp32 tensors must be 4-byte aligned");
+    }
+}
+void check_words(std::initializer_list<const void *> ptrs) {
+    for (const void *q : ptrs) {
+        if (!q) throw KernelError("linear_ce: null pointer");
+        if ((uintptr_t)q % 4) throw KernelError("linear_ce: labels, loss and lse must be 4-byte aligned");
     }
 }
 
@@ -564,7 +570,7 @@ void linear_ce_fwd(hipStream_t st, int dtype, const void *x, const void *w, cons
     const CePlan p = ce_plan(false, dtype, rows, width, vocab);
     check_ws(p, ws, ws_bytes);
     check_aligned(p, {x, w});
-    if (!labels || !loss || !lse) throw KernelError("linear_ce: null pointer");
+    check_words({labels, loss, lse});
     float *hit = (float *)ws, *row_loss = hit + up(rows, 64);
     float2 *part = (float2 *)(row_loss + up(rows, 64));
     if (p.bf16) {
@@ -599,7 +605,7 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
     const CePlan p = ce_plan(true, dtype, rows, width, vocab);
     check_ws(p, ws, ws_bytes);
     check_aligned(p, {x, w, dx, dw});
-    if (!labels || !lse) throw KernelError("linear_ce: null pointer");
+    check_words({labels, lse});
     float *inv = (float *)ws;
     const bool count = p.bf16 || rows > 1024;
     if (count) {

@@ -24,3 +24,25 @@ def test_act8_wgrad_refuses_large_results_before_its_first_launch():
             monet.call("monet_act8_wgrad_workspace_bytes", monet.BF16, 64, cols, outs)
         with pytest.raises(monet.MonetError, match="too large"):
             monet.call("monet_act8_wgrad", None, monet.BF16, P, P, P, 64, cols, outs, P, 1 << 60)
+
+
+@pytest.mark.parametrize("name", ["lse", "cu"])
+def test_attention_refuses_numbers_off_their_alignment(name):
+    a = dict(lse=P, cu=P)
+    a[name] = P + 2
+    shape = (a["cu"], 3, 100, 8, 4, 64, 512, 256, 256, 512, 0.125)
+    with pytest.raises(monet.MonetError, match="4-byte aligned"):
+        monet.call("monet_attention_fwd", None, monet.BF16, P, P, P, P, a["lse"], *shape)
+    with pytest.raises(monet.MonetError, match="4-byte aligned"):
+        monet.call("monet_attention_bwd", None, monet.BF16, P, P, P, P, P, a["lse"], P, P, P, *shape, 0, P, 1 << 30)
+
+
+@pytest.mark.parametrize("name", ["labels", "loss", "lse", "x"])
+def test_linear_ce_refuses_numbers_off_their_alignment(name):
+    a = dict(labels=P, loss=P, lse=P, x=P)
+    a[name] = P + 1
+    with pytest.raises(monet.MonetError, match="4-byte aligned"):
+        monet.call("monet_linear_ce_fwd", None, monet.F32, a["x"], P, a["labels"], a["loss"], a["lse"], 50, 64, 1000, P, 1 << 30)
+    if name != "loss":
+        with pytest.raises(monet.MonetError, match="4-byte aligned"):
+            monet.call("monet_linear_ce_bwd", None, monet.F32, a["x"], P, a["labels"], a["lse"], P, P, 50, 64, 1000, 0, P, 1 << 30)
