@@ -289,9 +289,11 @@ void run_forward(const StepCtx &c, const Launch &L, const BnAffine *affine = nul
         if (L.flags & 2) act8_pack(c.st, MONET_F32, in0, is[1], c.ptr(L.a[3]), is[0], is[1]);      // the input in 8 bits for the weight gradient
     } else if (op == "attention") {
         const AttentionNode a = attention_node(g, n);
+        const int32_t *cu = (const int32_t *)c.ptr(L.in[3]);
+        // the operators around take every row: none may be what the arena held before
+        attention_clear_outside(c.st, cu, a.seqs, a.tokens, {{out, a.heads * a.dim}});
         attention_fwd(c.st, MONET_F32, in0, c.ptr(L.in[1]), c.ptr(L.in[2]), out, (L.flags & 2) ? (float *)c.ptr(L.a[3]) : nullptr,
-                      (const int32_t *)c.ptr(L.in[3]), a.seqs, a.tokens, a.heads, a.kv_heads, a.dim, a.heads * a.dim, a.kv_heads * a.dim,
-                      a.kv_heads * a.dim, a.heads * a.dim, a.scale);
+                      cu, a.seqs, a.tokens, a.heads, a.kv_heads, a.dim, a.heads * a.dim, a.kv_heads * a.dim, a.kv_heads * a.dim, a.heads * a.dim, a.scale);
     } else if (op == "linearce") {
         const auto &is = g.shape_of(n.ins[0]);
         linear_ce_fwd(c.st, MONET_F32, in0, c.weights[n.pars[0]], (const int32_t *)c.ptr(L.in[1]), out, c.ce_lse(L.id), is[0], (int)is[1],
@@ -384,6 +386,10 @@ void run_backward(const StepCtx &c, const Launch &L) {
     } else if (kd == "attention_bwd") {
         const AttentionNode a = attention_node(g, n);
         Ref cu; cu.region = R_EXT; cu.off = -n.ins[3];
+        // of the gradients that are written, not added to
+        auto written = [&](int p) { return (L.flags >> p & 1) ? nullptr : (float *)c.ptr(L.grad[p]); };
+        attention_clear_outside(c.st, (const int32_t *)c.ptr(cu), a.seqs, a.tokens,
+                                {{written(0), a.heads * a.dim}, {written(1), a.kv_heads * a.dim}, {written(2), a.kv_heads * a.dim}});
         attention_bwd(c.st, MONET_F32, gy, c.ptr(L.dep[0]), c.ptr(L.dep[1]), c.ptr(L.dep[2]), c.ptr(L.dep[3]), (const float *)c.ptr(L.dep[4]),
                       c.ptr(L.grad[0]), c.ptr(L.grad[1]), c.ptr(L.grad[2]), (const int32_t *)c.ptr(cu), a.seqs, a.tokens, a.heads, a.kv_heads, a.dim,
                       a.heads * a.dim, a.kv_heads * a.dim, a.kv_heads * a.dim, a.heads * a.dim, a.scale, (int)(L.flags & 7), c.ptr(L.a[4]),

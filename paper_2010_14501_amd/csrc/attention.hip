@@ -805,6 +805,18 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttShape a, const f
     }
 }
 
+// Rows in front of the first sequence and behind the last one of up to three tensors (grid y): zero.  Nothing to do where the offsets cover
+// all tokens, which only the device knows.
+struct OutsideRows { float *p[3]; int width[3]; };
+__global__ __launch_bounds__(256) void attention_clear_outside_kernel(const int32_t *__restrict__ cu, int seqs, int tokens, OutsideRows r) {
+    const int first = min(max(cu[0], 0), tokens), behind = min(max(cu[seqs], first), tokens), per_row = r.width[blockIdx.y] / 4;
+    const int64_t all = (int64_t)(first + tokens - behind) * per_row;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t at = i < (int64_t)first * per_row ? i : i + (int64_t)(behind - first) * per_row;
+        ((float4 *)r.p[blockIdx.y])[at] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+}
+
 AttShape att_shape(int dtype, const int32_t *cu, int seqs, int64_t tokens, int heads, int kv_heads, int head_dim, int64_t q_ld, int64_t k_ld,
                    int64_t v_ld, int64_t o_ld, float scale) {
     if (dtype != MONET_F32 && dtype != MONET_BF16) throw KernelError("attention: dtype must be MONET_F32 or MONET_BF16");
@@ -917,6 +929,16 @@ void attention_fwd(hipStream_t st, int dtype, const void *q, const void *k, cons
     check_lse(lse);
     if (dtype == MONET_BF16) (head_dim <= 64 ? fwd_form<unsigned short, 64> : fwd_form<unsigned short, 128>)(st, a, q, k, v, o, lse);
     else (head_dim <= 64 ? fwd_form<float, 64> : fwd_form<float, 128>)(st, a, q, k, v, o, lse);
+}
+
+void attention_clear_outside(hipStream_t st, const int32_t *cu, int seqs, int64_t tokens, std::initializer_list<std::pair<float *, int>> tensors) {
+    OutsideRows r{};
+    int n = 0;
+    for (const auto &t : tensors)
+        if (t.first) { r.p[n] = t.first; r.width[n++] = t.second; }
+    if (!n || !tokens) return;
+    hipLaunchKernelGGL(attention_clear_outside_kernel, dim3(64, n), dim3(256), 0, st, cu, seqs, (int)tokens, r);
+    hip_check(hipGetLastError(), "attention clear launch");
 }
 
 size_t attention_bwd_workspace_bytes(int dtype, int seqs, int64_t tokens, int heads, int kv_heads, int head_dim) {

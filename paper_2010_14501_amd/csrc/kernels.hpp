@@ -6,8 +6,10 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <initializer_list>
 #include <stdexcept>
 #include <string>
+#include <utility>
 
 namespace monet {
 
@@ -229,6 +231,8 @@ size_t attention_bwd_workspace_bytes(int dtype, int seqs, int64_t tokens, int he
 void attention_bwd(hipStream_t st, int dtype, const void *go, const void *q, const void *k, const void *v, const void *o, const float *lse, void *dq,
                    void *dk, void *dv, const int32_t *cu, int seqs, int64_t tokens, int heads, int kv_heads, int head_dim, int64_t q_ld, int64_t k_ld,
                    int64_t v_ld, int64_t o_ld, float scale, int accumulate, void *ws, size_t ws_bytes);
+// zero in the tokens of no sequence: up to three contiguous fp32 tensors [tokens][width] (null: none)
+void attention_clear_outside(hipStream_t st, const int32_t *cu, int seqs, int64_t tokens, std::initializer_list<std::pair<float *, int>> tensors);
 size_t linear_ce_workspace_bytes(bool grad, int dtype, int64_t rows, int width, int vocab);
 void linear_ce_fwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *labels, float *loss, float *lse, int64_t rows,
                    int width, int vocab, void *ws, size_t ws_bytes);

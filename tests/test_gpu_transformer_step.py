@@ -75,3 +75,25 @@ def test_captured_steps_replay():
         graph.replay()
         got = a.grads_numpy()
         assert a.loss_value() == loss and all(np.array_equal(got[p], want[p]) for p in got)
+
+
+@pytest.mark.parametrize("which", SCHEDULES)
+def test_transformer_step_of_a_padded_batch(which):
+    """Offsets that leave tokens in front of the first sequence and behind the last one: attention's output and its gradients are zero there, whatever
+    the memory held, so that the linear layers around it sum over zeros."""
+    g = NETS["long"]()
+    sch = SCHEDULES[which](g)
+    exts, params = tensors.make_inputs(g, seed=7)
+    cu = next(iter(g.ext_values))
+    tokens = exts[cu][-1]
+    exts[cu] = np.array([5, 140, 140, 170, tokens - 37], dtype=np.int32)
+    exts[-1][:5] = -1
+    exts[-1][tokens - 30:] = -1                    # seven tokens of no sequence keep their label
+    oe, op = tensors.oracle_inputs(exts, params)
+    want = osch.interpret(g.text(), sch.text(), oe, op)
+    run = StepRunner(g.text(), sch.text(), exts, params, poison=True)
+    for poison in (True, False):
+        run.plan.set_poison(poison)
+        assert run.step() == want["peak"]
+        assert abs(run.loss_value() - want["loss"]) < ACT_TOL * abs(want["loss"])
+        compare(g, run.grads_numpy(), want, 1e-3 if "codes" in which else 1e-4)
