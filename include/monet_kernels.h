@@ -261,7 +261,7 @@ enum monet_dtype { MONET_F32 = 0, MONET_BF16 = 1 };
  * cu_seqlens[s] .. cu_seqlens[s + 1] - 1 and may be empty.  Tokens before the first and behind the last one are neither read
  * nor written, in any output.  Offsets are held to 0 .. tokens, so that others cannot lead out of the tensors.
  * Needs heads % kv_heads == 0, head_dim a multiple of 8 up to 128, scale > 0, tensors and strides that are multiples of
- * 16 bytes (lse and offsets of 4), tokens below 2^31, (tokens / 64 + seqs) * heads below 2^24; o must not overlap an input.  tokens == 0 is allowed and does nothing.  A sequence's infinities and NaNs stay in that sequence.
+ * 16 bytes (lse and offsets of 4), tokens below 2^31, (tokens / 64 + seqs + 8) * heads below 2^24 - 2^11; o must not overlap an input.  tokens == 0 is allowed and does nothing.  A sequence's infinities and NaNs stay in that sequence.
  * Within it, one in k or v reaches the rows from its own on and may reach up to 127 rows before it.  fp32: the products go through
  * three bf16 pieces of each operand, exact from 2^-110 up; an infinity in a tensor comes out as NaN. */
 int monet_attention_fwd(void *stream, int dtype, const void *q, const void *k, const void *v, void *o, float *lse,

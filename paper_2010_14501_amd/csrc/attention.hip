@@ -243,6 +243,8 @@ struct AttForm {
     static constexpr int BUFFERS = sizeof(T) == 2 ? 2 : 1;
     static constexpr bool TWO_GROUPS = 2 * BUFFERS * Tile::BYTES <= 72 << 10;      // two workgroups in a CU's LDS
     static constexpr int AREA = D / 32 * 16 * 256;                       // a wave's results
+    static constexpr int RANGE_TILES = sizeof(T) == 2 ? 16 : 6;          // dk, dv: the most tiles of rows to a range
+    static constexpr int RANGE_ROWS = RANGE_TILES * TILE;
 };
 
 // Sequence s owns the slots from cu[s] / ROWS + s on: at least one for every ROWS rows begun, whatever the lengths, so the grid
@@ -268,13 +270,32 @@ __device__ __forceinline__ bool find_rows(const AttShape &a, int slot, int &star
     row0 = (slot - (start / ROWS + lo)) * ROWS;
     return row0 < len;
 }
-// Workgroups go round the eight XCDs in turn; each gets a connected range of (head, slot), so that a group's keys and values stay in
-// one L2.
-__device__ __forceinline__ void att_place(int heads, int slots, int &head, int &slot) {
-    const int all = heads * slots, x = blockIdx.x % 8, t = x * (all / 8) + min(x, all % 8) + blockIdx.x / 8;
-    head = t / slots;
-    slot = t - head * slots;
-}
+// Workgroups go round the eight XCDs in turn.  Where the heads can be dealt out evenly, each XCD gets whole heads, so that a group's keys and
+// values stay in one L2.  Otherwise runs of slots (128 rows) are dealt out, the heads of a run side by side: a connected eighth of the slots may
+// hold nothing but empty sequences, or the shortest ways of all.  Both backward kernels, fp32, 4096 rows, 4 / 1 heads of 64: 320 us, with
+// connected eighths 359, and with 63 empty sequences behind them 332 and 616; but 16 sequences of 256 rows, heads of 128: 128 and 111.
+template <int ROWS>
+struct AttPlace {
+    static constexpr int RUN = 128 / ROWS;
+    static unsigned groups(int heads, int slots) {
+        if (heads % 8 == 0) return (unsigned)heads * slots;
+        const unsigned runs = (unsigned)heads * ((slots + RUN - 1) / RUN);
+        return (runs + 7) / 8 * 8 * RUN;
+    }
+    static __device__ __forceinline__ bool find(int heads, int slots, int &head, int &slot) {
+        const int x = blockIdx.x % 8, y = blockIdx.x / 8;
+        if (heads % 8 == 0) {
+            const int t = x * (heads / 8 * slots) + y;
+            head = t / slots;
+            slot = t - head * slots;
+            return true;
+        }
+        const int u = y / RUN * 8 + x, run = u / heads;
+        head = u - run * heads;
+        slot = run * RUN + y % RUN;
+        return slot < slots;
+    }
+};
 
 __device__ __forceinline__ float exchange_max(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -355,7 +376,7 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS ? 2 : 1)) vo
     constexpr int BYTES = Tile::BYTES, SECOND = F::BUFFERS == 2 ? BYTES : 16;
     __shared__ __attribute__((aligned(16))) char k0[BYTES], k1[SECOND], v0[BYTES], v1[SECOND];
     int head, slot, start, len, row0;
-    att_place(a.heads, a.slots, head, slot);
+    if (!AttPlace<F::ROWS>::find(a.heads, a.slots, head, slot)) return;
     if (!find_rows<F::ROWS>(a, a.slots - 1 - slot, start, len, row0)) return;      // the longest rows first
     const int kv_head = head / (a.heads / a.kv_heads), l = threadIdx.x & 63, wave = threadIdx.x / 64;
     const int part = wave % PARTS, first = row0 + wave / PARTS * 32, row = first + (l & 31);
@@ -492,7 +513,7 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
     constexpr int BYTES = Tile::BYTES, SECOND = F::BUFFERS == 2 ? BYTES : 16;
     __shared__ __attribute__((aligned(16))) char k0[BYTES], k1[SECOND], v0[BYTES], v1[SECOND];
     int head, slot, start, len, row0;
-    att_place(a.heads, a.slots, head, slot);
+    if (!AttPlace<F::ROWS>::find(a.heads, a.slots, head, slot)) return;
     if (!find_rows<F::ROWS>(a, a.slots - 1 - slot, start, len, row0)) return;
     const int kv_head = head / (a.heads / a.kv_heads), l = threadIdx.x & 63, wave = threadIdx.x / 64;
     const int part = wave % PARTS, first = row0 + wave / PARTS * 32, row = first + (l & 31);
@@ -626,13 +647,14 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
     join_and_store<T, D, PARTS>(area, acc, 1.f, dq + (int64_t)(start + row) * a.q_ld + (int64_t)head * a.head_dim, row < len, a.scale, a.head_dim, add);
 }
 
-// dk and dv: a wave holds 32 keys and walks along the rows behind them, head by head of the group.  With more than one range (grid y) a
-// workgroup takes its share of that way and leaves fp32 sums in `ranges` ([range][token][kv_head][head_dim], dk's and behind them dv's),
-// which attention_join_kernel adds up in order.
+// dk and dv: a wave holds 32 keys and walks along the rows behind them, head by head of the group.  Where the grid has more than one range (y),
+// a way is cut into as many as it has room for: each workgroup takes its share and leaves fp32 sums in `ranges` ([range][token][kv_head]
+// [head_dim], dk's and behind them dv's), which attention_join_kernel adds up in order; `counts` tells it a token's number of ranges.  A way too
+// short for two is one workgroup's, which writes the results, and the others of its keys end at once.
 template <class T, int D, int PARTS>
 __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T) == 2 || D == 64) ? 2 : 1)) void attention_dkv_kernel(
     AttShape a, const T *__restrict__ go, const T *__restrict__ q, const T *__restrict__ k, const T *__restrict__ v, const float *__restrict__ delta,
-    T *dk, T *dv, int add_k, int add_v, float *__restrict__ ranges) {
+    T *dk, T *dv, int add_k, int add_v, float *__restrict__ ranges, int32_t *__restrict__ counts) {
     typedef AttForm<T, D, PARTS> F;
     typedef typename F::Tile Tile;
     constexpr int R = F::TILE, B = F::BLOCKS, PIECES = F::PIECES, STEPS = F::STEPS;
@@ -640,10 +662,12 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
     __shared__ __attribute__((aligned(16))) char q0[BYTES], q1[SECOND], g0[BYTES], g1[SECOND];
     __shared__ __attribute__((aligned(16))) float stat0[256], stat1[256];      // delta of a tile's rows, their lse
     int kv_head, slot, start, len, key0;
-    att_place(a.kv_heads, a.slots, kv_head, slot);
+    if (!AttPlace<F::ROWS>::find(a.kv_heads, a.slots, kv_head, slot)) return;
     if (!find_rows<F::ROWS>(a, slot, start, len, key0)) return;
     const int group = a.heads / a.kv_heads, l = threadIdx.x & 63, wave = D > 64 ? threadIdx.x / 64 : uniform_wave();
     const int part = wave % PARTS, first = key0 + wave / PARTS * 32, key = first + (l & 31);
+    const int from = key0 / R * R, tiles = (len - from + R - 1) / R, count = min((int)gridDim.y, (tiles * group + F::RANGE_TILES - 1) / F::RANGE_TILES);
+    if ((int)blockIdx.y >= count) return;
     Tile tq, tg;
     tq.init(a.q_ld, a.head_dim);
     tg.init(a.o_ld, a.head_dim);
@@ -659,8 +683,7 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
         for (int r = 0; r < 16; ++r) ak[c][r] = av[c][r] = 0.f;
-    const int from = key0 / R * R, tiles = (len - from + R - 1) / R;
-    const int begin = (int)((int64_t)tiles * group * blockIdx.y / gridDim.y), all = (int)((int64_t)tiles * group * (blockIdx.y + 1) / gridDim.y);
+    const int begin = (int)((int64_t)tiles * group * blockIdx.y / count), all = (int)((int64_t)tiles * group * (blockIdx.y + 1) / count);
     auto place = [&](int t, int &head, int &row) {
         const int g = t / tiles;
         head = kv_head * group + g;
@@ -764,7 +787,8 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
     };
     static_assert(PARTS == 1 || BYTES >= F::AREA * (F::BUFFERS == 2 ? 1 : 2), "");
     if (PARTS > 1) __syncthreads();      // everybody is done with the tiles
-    if (ranges) {
+    if (ranges && blockIdx.y == 0 && kv_head == 0 && part == 0 && l < 32 && key < len) counts[start + key] = count;
+    if (count > 1) {
         float *row = ranges + (((int64_t)blockIdx.y * a.tokens + start + key) * a.kv_heads + kv_head) * a.head_dim;
         join_and_store<float, D, PARTS>(area, ak, 1.f, row, key < len, a.scale, a.head_dim, false);
         if (PARTS > 1) __syncthreads();
@@ -777,14 +801,17 @@ __global__ __launch_bounds__(256, (AttForm<T, D, PARTS>::TWO_GROUPS && (sizeof(T
     join_and_store<T, D, PARTS>(area, av, 1.f, dv + (int64_t)(start + key) * a.v_ld + (int64_t)kv_head * a.head_dim, key < len, 1.f, a.head_dim, add_v);
 }
 
-// dk (grid y 0) or dv (1) = the sum of its ranges, four values a thread; tokens of no sequence are left alone
+// dk (grid y 0) or dv (1) = the sum of its ranges where there is more than one, four values a thread; tokens of no sequence are left alone
 template <class T>
-__global__ __launch_bounds__(256) void attention_join_kernel(AttShape a, const float *__restrict__ ranges, int count, T *dk, T *dv, int add_k, int add_v) {
+__global__ __launch_bounds__(256) void attention_join_kernel(AttShape a, const float *__restrict__ ranges, const int32_t *__restrict__ counts, int most, T *dk,
+                                                             T *dv, int add_k, int add_v) {
     const int width = a.kv_heads * a.head_dim, per_row = width / 4;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per_row, all = (int64_t)a.tokens * width;
     if (row >= a.tokens || row < a.cu[0] || row >= a.cu[a.seqs]) return;
+    const int count = min(counts[row], most);
+    if (count < 2) return;
     const int c = (int)(i - row * per_row) * 4;
-    const float *p = ranges + (blockIdx.y ? count * all : 0) + row * width + c;
+    const float *p = ranges + (blockIdx.y ? most * all : 0) + row * width + c;
     float4 v = *(const float4 *)p;
     for (int r = 1; r < count; ++r) {
         const float4 w = *(const float4 *)(p + r * all);
@@ -828,7 +855,8 @@ AttShape att_shape(int dtype, const int32_t *cu, int seqs, int64_t tokens, int h
         if (ld < (int64_t)heads * head_dim || ld % step || ld >= (1 << 23)) throw KernelError("attention: row strides must hold all heads, be a multiple of 16 bytes and below 2^23 elements");
     for (int64_t ld : {k_ld, v_ld})
         if (ld < (int64_t)kv_heads * head_dim || ld % step || ld >= (1 << 23)) throw KernelError("attention: row strides must hold all heads, be a multiple of 16 bytes and below 2^23 elements");
-    if (tokens > 0x7fffffff || (tokens / 64 + seqs) * heads >= 1 << 24) throw KernelError("attention: too many tokens");
+    // a launch takes less than 2^24 workgroups; what comes on top of a workgroup for 64 rows or a sequence: runs of slots, 32 keys to a workgroup
+    if (tokens > 0x7fffffff || (tokens / 64 + seqs + 8) * heads >= (1 << 24) - (1 << 11)) throw KernelError("attention: too many tokens");
     if (!cu) throw KernelError("attention: null pointer");
     if ((uintptr_t)cu % 4) throw KernelError("attention: offsets and lse must be 4-byte aligned");
     return AttShape{cu, seqs, (int)tokens, heads, kv_heads, head_dim, 0, q_ld, k_ld, v_ld, o_ld, scale};
@@ -844,35 +872,44 @@ void check_lse(const float *lse) {
 }
 
 // Rows of the forward and the first backward kernel: 128 to a workgroup where that gives four workgroups to a CU (fp32 with 128 columns, whose
-// tiles take more of LDS: two), 64 below.  Forward, 64 and 128 rows: bf16 8 x 16 heads of 512 rows 14.4 and 15.5 us, one sequence of 4000 rows
-// and 8 heads 40 and 51, two of 8192 and 32 heads 1190 and 1084; fp32 4 x 16 heads of 512 rows 28 and 36, one of 4096 and 32 heads of 128 1135 and 813.
+// tiles take more of LDS: two), 64 below.  How long the sequences are does not matter for it, and the host does not know.  Forward, 64 and 128
+// rows: bf16 8 x 16 heads of 512 rows 14.4 and 15.5 us, one sequence of 4000 rows and 8 heads 40 and 51, two of 8192 and 32 heads 1190 and 1084,
+// 82 of 100 rows and 32 heads of 128 72 and 56; fp32 4 x 16 heads of 512 rows 28 and 36, one of 4096 and 32 heads of 128 1135 and 813, 205 of 40
+// and 32 heads of 128 320 and 213 (where its backward kernel loses what this one gains).
 template <class T, int D>
 int row_parts(const AttShape &a) {
     const int64_t full = (int64_t)(a.tokens / 128) * a.heads;
-    return full >= (sizeof(T) == 4 && D == 128 ? 512 : 1024) && a.tokens / a.seqs >= 128 ? 1 : 2;
+    return full >= (sizeof(T) == 4 && D == 128 ? 512 : 1024) ? 1 : 2;
 }
 // The second backward kernel has fewer workgroups (key heads) with a longer way each (the rows behind a key, of every head of the group).
-// Where 128 keys to a workgroup do not give four workgroups to a CU, the way is cut into ranges.  bf16, where that gives less than two: a
-// workgroup takes 32 keys.  Both backward kernels: bf16, 8 ragged sequences of 8192 rows, 32 / 8 heads, 994 us uncut, 837 in two ranges, 953
-// with 32 keys; one of 10000, 4 / 1 heads, 1865, 559 (14 ranges), 794 (32 keys, 4 ranges); one of 1024, 8 heads of 64, 47 and 28 (32 keys).  fp32, 2048 ragged rows, 12 / 4 heads of 64: 587, 196 (16 ranges), 223 (32 keys, 4 ranges); 4 x 512 rows, 16 heads: 126, 110 (2), 124.
+// Where 128 keys to a workgroup do not give four workgroups to a CU, ways are cut into ranges, each as its own length asks for
+// (attention_dkv_kernel): the launch has as many as the longest way there can be, all tokens in one sequence, has room for.  So empty and tiny
+// sequences, of which padded offsets have many, take no ranges from a long one.  bf16: with less than one workgroup to a CU, and unless
+// sequences of the mean length give ranges for two, a workgroup takes 32 keys.  Both backward kernels, us:
+//   bf16, 10000 rows, 4 / 1 heads: uncut 1865, 14 ranges 559, 32 keys in 4 ranges 794;  1024 rows, 8 heads of 64: 47, with 32 keys 28
+//   fp32, 2048 ragged rows, 12 / 4 heads of 64: 587 uncut, 16 ranges 158
+//   as the mean length has it, and so: bf16, 4000 rows and nine empty sequences, 8 / 1 heads of 64, 291 and 123; 12000 and 255 empty, 4 / 1 heads
+//   of 128, 2000 and 770; fp32, 6000 and 63 empty, 16 / 4 heads of 128, 7900 and 4310; 5000, 3, 900 and 2000 rows, 8 / 4 heads of 128, 2450 and
+//   2040; but bf16, 32 sequences of 128 rows, 32 / 4 heads of 64, 63 and 74: workgroups that find no range to work on, and a launch to join none
+//   bf16, 128 and 32 keys: 256 sequences of 32 rows, 16 / 4 heads of 128, 139 and 187; 16 of 256, 4 / 1 heads of 128, 71 and 42
 struct KeyForm { int parts, ranges; };
 KeyForm key_form(const AttShape &a, bool fp32) {
-    const int64_t full = std::max<int64_t>(1, (int64_t)(a.tokens / 128) * a.kv_heads), way = (int64_t)(a.tokens / a.seqs) * (a.heads / a.kv_heads);
-    // ranges until there are `enough` workgroups, of at least `least` rows of the way
-    const auto cut = [&](int64_t groups, int64_t enough, int64_t least) {
-        return std::max<int64_t>(1, std::min<int64_t>({(enough + groups - 1) / groups, way / least, 16}));
+    const int64_t full = std::max<int64_t>(1, (int64_t)(a.tokens / 128) * a.kv_heads), group = a.heads / a.kv_heads, mean = a.tokens / a.seqs;
+    // ranges until there are 1024 workgroups, if a way of so many rows has room for them
+    const auto cut = [](int64_t groups, int64_t way, int64_t least) {
+        return std::max<int64_t>(1, std::min<int64_t>({(1024 + groups - 1) / groups, (way + least - 1) / least, 16}));
     };
-    if (fp32) return {1, (int)cut(full, 1024, 192)};
-    if (full >= 1024) return {1, 1};
-    const int64_t r = cut(full, 1024, 1024);
-    if (full * r >= 512 && a.tokens / a.seqs >= 64) return {1, (int)r};
-    return {4, (int)cut(4 * full, 1024, 2048)};
+    const int64_t longest = a.tokens * group;
+    if (fp32) return {1, (int)cut(full, longest, AttForm<float, 64, 1>::RANGE_ROWS)};
+    constexpr int LEAST = AttForm<unsigned short, 64, 1>::RANGE_ROWS;
+    if (full >= 256 || (mean >= 64 && full * cut(full, mean * group, LEAST) >= 512)) return {1, full >= 1024 ? 1 : (int)cut(full, longest, LEAST)};
+    return {4, (int)cut(4 * full, longest, AttForm<unsigned short, 64, 4>::RANGE_ROWS)};
 }
 
 template <class T, int D, int PARTS>
 void fwd_launch(hipStream_t st, AttShape a, const void *q, const void *k, const void *v, void *o, float *lse) {
     a.slots = a.tokens / AttForm<T, D, PARTS>::ROWS + a.seqs;
-    hipLaunchKernelGGL((attention_fwd_kernel<T, D, PARTS>), dim3(a.slots * a.heads), dim3(256), 0, st, a, (const T *)q, (const T *)k, (const T *)v, (T *)o, lse);
+    hipLaunchKernelGGL((attention_fwd_kernel<T, D, PARTS>), dim3(AttPlace<AttForm<T, D, PARTS>::ROWS>::groups(a.heads, a.slots)), dim3(256), 0, st, a, (const T *)q, (const T *)k, (const T *)v, (T *)o, lse);
     hip_check(hipGetLastError(), "attention forward launch");
 }
 template <class T, int D>
@@ -886,25 +923,27 @@ struct BwdArgs {
     const float *lse;
     void *dq, *dk, *dv;
     float *delta, *ranges;
+    int32_t *counts;
     int accumulate;
 };
+int64_t count_bytes(const AttShape &a) { return ((int64_t)a.tokens * 4 + 255) / 256 * 256; }
 int64_t stat_bytes(const AttShape &a) { return (2 * (int64_t)a.heads * a.tokens * 4 + 255) / 256 * 256; }
 template <class T, int D, int PARTS>
 void dq_launch(hipStream_t st, AttShape a, const BwdArgs &b) {
     a.slots = a.tokens / AttForm<T, D, PARTS>::ROWS + a.seqs;
-    hipLaunchKernelGGL((attention_dq_kernel<T, D, PARTS>), dim3(a.slots * a.heads), dim3(256), 0, st, a, (const T *)b.go, (const T *)b.q, (const T *)b.k,
+    hipLaunchKernelGGL((attention_dq_kernel<T, D, PARTS>), dim3(AttPlace<AttForm<T, D, PARTS>::ROWS>::groups(a.heads, a.slots)), dim3(256), 0, st, a, (const T *)b.go, (const T *)b.q, (const T *)b.k,
                        (const T *)b.v, (const T *)b.o, b.lse, (T *)b.dq, b.delta, b.accumulate & 1);
     hip_check(hipGetLastError(), "attention query gradient launch");
 }
 template <class T, int D, int PARTS>
 void dkv_launch(hipStream_t st, AttShape a, const BwdArgs &b, int ranges) {
     a.slots = a.tokens / AttForm<T, D, PARTS>::ROWS + a.seqs;
-    hipLaunchKernelGGL((attention_dkv_kernel<T, D, PARTS>), dim3(a.slots * a.kv_heads, ranges), dim3(256), 0, st, a, (const T *)b.go, (const T *)b.q,
-                       (const T *)b.k, (const T *)b.v, b.delta, (T *)b.dk, (T *)b.dv, b.accumulate & 2, b.accumulate & 4, ranges > 1 ? b.ranges : nullptr);
+    hipLaunchKernelGGL((attention_dkv_kernel<T, D, PARTS>), dim3(AttPlace<AttForm<T, D, PARTS>::ROWS>::groups(a.kv_heads, a.slots), ranges), dim3(256), 0, st, a, (const T *)b.go, (const T *)b.q,
+                       (const T *)b.k, (const T *)b.v, b.delta, (T *)b.dk, (T *)b.dv, b.accumulate & 2, b.accumulate & 4, ranges > 1 ? b.ranges : nullptr, b.counts);
     hip_check(hipGetLastError(), "attention key gradient launch");
     if (ranges > 1) {
         const int64_t blocks = ((int64_t)a.tokens * a.kv_heads * a.head_dim / 4 + 255) / 256;
-        hipLaunchKernelGGL((attention_join_kernel<T>), dim3((unsigned)blocks, 2), dim3(256), 0, st, a, b.ranges, ranges, (T *)b.dk, (T *)b.dv,
+        hipLaunchKernelGGL((attention_join_kernel<T>), dim3((unsigned)blocks, 2), dim3(256), 0, st, a, b.ranges, b.counts, ranges, (T *)b.dk, (T *)b.dv,
                            b.accumulate & 2, b.accumulate & 4);
         hip_check(hipGetLastError(), "attention join launch");
     }
@@ -946,7 +985,7 @@ size_t attention_bwd_workspace_bytes(int dtype, int seqs, int64_t tokens, int he
     const AttShape a = att_shape(dtype, &none, seqs, tokens, heads, kv_heads, head_dim, (int64_t)heads * head_dim, (int64_t)kv_heads * head_dim,
               (int64_t)kv_heads * head_dim, (int64_t)heads * head_dim, 1.f);
     const int ranges = key_form(a, dtype == MONET_F32).ranges;
-    return (size_t)(stat_bytes(a) + (ranges > 1 ? 2 * (int64_t)ranges * tokens * kv_heads * head_dim * 4 : 0));
+    return (size_t)(stat_bytes(a) + (ranges > 1 ? count_bytes(a) + 2 * (int64_t)ranges * tokens * kv_heads * head_dim * 4 : 0));
 }
 
 void attention_bwd(hipStream_t st, int dtype, const void *go, const void *q, const void *k, const void *v, const void *o, const float *lse, void *dq,
@@ -961,7 +1000,8 @@ void attention_bwd(hipStream_t st, int dtype, const void *go, const void *q, con
     if (!ws || ws_bytes < attention_bwd_workspace_bytes(dtype, seqs, tokens, heads, kv_heads, head_dim))
         throw KernelError("attention: workspace too small");
     if ((uintptr_t)ws % 256) throw KernelError("attention: the workspace must be 256-byte aligned");
-    const BwdArgs b{go, q, k, v, o, lse, dq, dk, dv, (float *)ws, (float *)((char *)ws + stat_bytes(a)), accumulate};
+    char *behind = (char *)ws + stat_bytes(a);
+    const BwdArgs b{go, q, k, v, o, lse, dq, dk, dv, (float *)ws, (float *)(behind + count_bytes(a)), (int32_t *)behind, accumulate};
     if (dtype == MONET_BF16) (head_dim <= 64 ? bwd_form<unsigned short, 64> : bwd_form<unsigned short, 128>)(st, a, b);
     else (head_dim <= 64 ? bwd_form<float, 64> : bwd_form<float, 128>)(st, a, b);
 }

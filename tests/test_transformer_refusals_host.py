@@ -46,3 +46,14 @@ def test_linear_ce_refuses_numbers_off_their_alignment(name):
     if name != "loss":
         with pytest.raises(monet.MonetError, match="4-byte aligned"):
             monet.call("monet_linear_ce_bwd", None, monet.F32, a["x"], P, a["labels"], a["lse"], P, P, 50, 64, 1000, 0, P, 1 << 30)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim,tokens", [(4, 1, 64, 12000), (8, 1, 64, 4000), (16, 4, 128, 6000), (32, 8, 128, 5000)])
+def test_empty_sequences_take_no_ranges_from_a_long_one(heads, kv_heads, dim, tokens):
+    """The way along the rows behind a key is cut into ranges whose sums the workspace holds.  Offsets that are padded with empty sequences must not
+    make the same tokens go uncut: no fewer ranges in fp32, and two at least in bf16."""
+    sums = 2 * tokens * kv_heads * dim * 4
+    need = lambda dtype, seqs: monet.call("monet_attention_bwd_workspace_bytes", dtype, seqs, tokens, heads, kv_heads, dim)   # noqa: E731
+    for seqs in (1, 10, 64, 256):
+        assert need(monet.F32, seqs) == need(monet.F32, 1) > 2 * sums
+        assert need(monet.BF16, seqs) > 2 * sums
