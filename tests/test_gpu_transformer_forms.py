@@ -5,7 +5,7 @@ import pytest
 
 from oracle import numerics as nm
 from paper_2010_14501_amd import monet
-from test_gpu_transformer import R, U, host, linear_ce_bounds, rounded, tdtype, torch_mod, within
+from test_gpu_transformer import R, U, attention_call, host, linear_ce_bounds, rounded, tdtype, torch_mod, within
 
 pytestmark = pytest.mark.gpu
 
@@ -124,3 +124,120 @@ def test_attention_of_scores_that_overflow_to_minus_infinity(dtype, heads, kv_he
         r = R if dtype == monet.BF16 else 0.0
         within(host(o).reshape(tokens, heads, dim)[blind:, h], want, 1.1 * ((2 * es + 2 * r) * mag) + 1e-30, "o")
         within(host(lse)[h, blind:], want_lse, (es + 4 * U * np.abs(want_lse)[:, None])[:, 0] + 1e-30, "lse")
+
+
+# ---------------------------------------------------------------------- attention: the forms that sizes choose between
+def attention_group(q, k, v, do, scale, dtype):
+    """One sequence and one key / value head with its group of query heads, in 64 bits on the GPU: (results, bounds) of o [group, n, dim], lse
+    [group, n], dq, dk [n, dim], dv.  The bounds propagate to first order, times 1.1 for the rest: a sum of n products in fp32 is off by (n + 2) U
+    of their magnitudes, exponential and logarithm by 4 U, bf16 rounds the probabilities, ds and the results by R."""
+    torch = torch_mod()
+    group, n, dim = q.shape
+    rp = R if dtype == monet.BF16 else 0.0
+    seen = torch.ones(n, n, dtype=torch.bool, device="cuda").tril()
+    zero = lambda *s: torch.zeros(*s, dtype=torch.float64, device="cuda")   # noqa: E731
+    out = [zero(group, n, dim), zero(group, n), zero(group, n, dim), zero(n, dim), zero(n, dim)]
+    bound = [t.clone() for t in out]
+    for h in range(group):
+        qs, gs = q[h], do[h]
+        s = (scale * (qs @ k.t())).masked_fill(~seen, float("-inf"))
+        lse = torch.logsumexp(s, 1)
+        p = torch.exp(s - lse[:, None])
+        o, dp = p @ v, gs @ v.t()
+        delta = (p * dp).sum(1, keepdim=True)
+        ds = p * (dp - delta)
+        out[0][h], out[1][h], out[2][h] = o, lse, scale * (ds @ k)
+        out[3] += scale * (ds.t() @ qs)
+        out[4] += p.t() @ gs
+        smax = (scale * (qs.abs() @ k.abs().t()) * seen).amax(1)
+        es = (dim + 8) * U * smax + 4 * U * lse.abs()
+        el = es + (n + 16) * U + 4 * U * lse.abs()
+        ep = (es + el + 8 * U)[:, None] * p
+        eo = (ep + (rp + (n + 8) * U) * p) @ v.abs() + (2 * es + (n + 16) * U)[:, None] * o.abs()
+        eo = eo + rp * o.abs()
+        edp = (dim + 2) * U * (gs.abs() @ v.abs().t())
+        edelta = (gs.abs() * eo).sum(1, keepdim=True) + (dim + 2) * U * (gs.abs() * o.abs()).sum(1, keepdim=True)
+        eds = ep * (dp - delta).abs() + p * (edp + edelta + 2 * U * (dp.abs() + delta.abs())) + rp * ds.abs()
+        bound[0][h], bound[1][h] = eo, el
+        bound[2][h] = scale * ((eds + (n + 4) * U * ds.abs()) @ k.abs()) + rp * out[2][h].abs()
+        bound[3] += scale * ((eds + (group * n + 4) * U * ds.abs()).t() @ qs.abs())
+        bound[4] += (ep + (rp + (group * n + 4) * U) * p).t() @ gs.abs()
+    bound[3] += rp * out[3].abs()
+    bound[4] += rp * out[4].abs()
+    return out, [1.1 * b + 1e-30 for b in bound]
+
+
+LONG, TAIL = [2125, 1, 0, 1990, 129, 300], [0] * 20
+FORMS = {
+    # name: lengths, heads, kv_heads, dim, whether dk and dv are summed over ranges (fp32, bf16)
+    "128_rows_128_keys_64": (LONG, 32, 32, 64, (False, False)),              # from 1024 workgroups of 128 rows (keys) on
+    "128_rows_128_keys_128": (LONG, 32, 32, 128, (False, False)),
+    "128_rows_ranges_40": (LONG, 32, 8, 40, (True, True)),
+    "128_rows_ranges_128": (LONG, 32, 8, 128, (True, True)),
+    "128_rows_ranges_of_padded_offsets": (LONG + TAIL, 32, 8, 96, (True, True)),
+    "64_rows_32_keys_ranges_64": ([2100, 40, 0, 65], 2, 1, 64, (True, True)),
+    "64_rows_32_keys_ranges_128": ([1500, 700], 4, 1, 128, (True, True)),
+    "64_rows_32_keys_padded_offsets": ([0, 0, 1800, 3] + [0] * 60, 6, 2, 64, (True, True)),
+    "64_rows_32_keys": ([500, 300, 224, 64, 7], 16, 16, 72, (True, False)),
+    "64_rows_128_keys_ranges": ([1300, 1295], 32, 8, 128, (True, True)),     # the mean length gives ranges for two workgroups to a CU
+    "short_128_rows": ([100] * 41 + [17, 1, 32, 128, 255], 32, 8, 64, (True, True)),
+}
+
+
+@pytest.mark.parametrize("dtype", [monet.F32, monet.BF16])
+@pytest.mark.parametrize("form", FORMS)
+def test_attention_forms_match_64_bits(form, dtype):
+    """Every form of the three kernels, with tokens in front of the sequences and behind them, rows longer than the heads need, written and added to;
+    every row of the first, the last and a middle key head and of their groups."""
+    torch = torch_mod()
+    lens, heads, kv_heads, dim, ranges = FORMS[form]
+    before, behind, pad = 3, 5, 8
+    n = sum(lens) + before + behind
+    cu_h = [before + sum(lens[:i]) for i in range(len(lens) + 1)]
+    cu = torch.tensor(cu_h, dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(24)
+    gpu = []
+    for h in (heads, kv_heads, kv_heads, heads):
+        t = torch.randn(n, h * dim + pad, generator=g, device="cuda").to(tdtype(dtype))
+        t[:before] = float("nan")
+        t[n - behind:] = float("nan")
+        gpu.append(t)
+    scale = dim ** -0.5
+    need = monet.call("monet_attention_bwd_workspace_bytes", dtype, len(lens), n, heads, kv_heads, dim)
+    assert (need >= 4 * n * kv_heads * dim * 4) == ranges[dtype], need
+    one = attention_call(dtype, *gpu, cu, heads, kv_heads, dim, scale)
+    start = torch.randn(n, heads * dim + pad, generator=g, device="cuda").to(tdtype(dtype))
+    added = attention_call(dtype, *gpu, cu, heads, kv_heads, dim, scale, accumulate=7, start=start)
+    names = ("o", "lse", "dq", "dk", "dv")
+    for name, t, u in zip(names, one, added):
+        if name == "lse":
+            assert (t[:, :before] == -7).all() and (t[:, n - behind:] == -7).all()
+            assert torch.equal(t, u)
+            continue
+        used = (heads if name in ("o", "dq") else kv_heads) * dim
+        assert (t[:before] == -7).all() and (t[n - behind:] == -7).all() and (t[:, used:] == -7).all(), name
+        if name == "o":
+            assert torch.equal(t, u)
+            continue
+        base = start[:, :t.shape[1]]
+        rows = slice(before, n - behind)
+        assert torch.equal(u[:before], base[:before]) and torch.equal(u[n - behind:], base[n - behind:]) and torch.equal(u[:, used:], base[:, used:])
+        # t is the rounded gradient, u the rounded sum
+        x, y, z = base[rows, :used].double(), t[rows, :used].double(), u[rows, :used].double()
+        r = R if dtype == monet.BF16 else U
+        assert ((z - x - y).abs() <= 1.01 * r * ((x + y).abs() + y.abs()) + 1e-30).all(), name
+    group = heads // kv_heads
+    split = lambda t, h: t[:, :h * dim].view(n, h, dim).transpose(0, 1).double()   # noqa: E731
+    q, do, o, dq = (split(t, heads) for t in (gpu[0], gpu[3], one[0], one[2]))
+    k, v, dk, dv = (split(t, kv_heads) for t in (gpu[1], gpu[2], one[3], one[4]))
+    for kv in sorted({0, kv_heads // 2, kv_heads - 1}):
+        hs = slice(kv * group, (kv + 1) * group)
+        for a, b in zip(cu_h[:-1], cu_h[1:]):
+            if a == b:
+                continue
+            want, bound = attention_group(q[hs, a:b], k[kv, a:b], v[kv, a:b], do[hs, a:b], scale, dtype)
+            got = (o[hs, a:b], one[1][hs, a:b].double(), dq[hs, a:b], dk[kv, a:b], dv[kv, a:b])
+            for name, x, w, e in zip(names, got, want, bound):
+                over = (x - w).abs() - e
+                assert (over <= 0).all(), (name, kv, a, b, (x - w).abs().max().item(), over.max().item())
