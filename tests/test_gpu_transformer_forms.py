@@ -55,6 +55,91 @@ def test_linear_ce_adds_to_dx_and_leaves_dw(case, dtype):
     within(host(added), total, bound[2] + 1.1 * r * (np.abs(total) + np.abs(host(start))), "added dx")
 
 
+def linear_ce_reference(x, w, lab, dtype, rows_at_a_time):
+    """On the GPU, in 64 bits, some rows at a time: (loss, lse, dx, dw) and bounds, from the same arithmetic as linear_ce_bounds."""
+    torch = torch_mod()
+    rp = R if dtype == monet.BF16 else 0.0
+    (rows, width), vocab = x.shape, w.shape[0]
+    wd = w.double()
+    wa = wd.abs()
+    count = max(1, int(((lab >= 0) & (lab < vocab)).sum()))
+    zero = lambda *s: torch.zeros(*s, dtype=torch.float64, device="cuda")   # noqa: E731
+    out, bound = [zero(1), zero(rows), zero(rows, width), zero(vocab, width)], [zero(1), zero(rows), zero(rows, width), zero(vocab, width)]
+    for a in range(0, rows, rows_at_a_time):
+        part = slice(a, min(rows, a + rows_at_a_time))
+        xs, ls = x[part].double(), lab[part].long()
+        logits = xs @ wd.t()
+        lse = torch.logsumexp(logits, 1)
+        m = logits.abs().amax(1)
+        el = (width + 2) * U * (xs.abs() @ wa.t()).amax(1)
+        els = el + 4 * U * m + (vocab + 16) * U + 4 * U * lse.abs()
+        has = torch.nonzero((ls >= 0) & (ls < vocab))[:, 0]
+        out[0] += (lse[has] - logits[has, ls[has]]).sum() / count
+        bound[0] += (els + el + 2 * U * m)[has].sum() / count
+        out[1][part], bound[1][part] = lse, els
+        p = torch.zeros_like(logits)
+        p[has] = torch.exp(logits[has] - lse[has, None])
+        edl = p * (el + els + 4 * U * m + 8 * U)[:, None]
+        p[has, ls[has]] -= 1.0
+        edl += (rp + 4 * U) * p.abs()
+        out[2][part] = p @ wd / count
+        bound[2][part] = (edl + (vocab + 8) * U * p.abs()) @ wa / count
+        out[3] += p.t() @ xs / count
+        bound[3] += (edl + (rows + 8) * U * p.abs()).t() @ xs.abs() / count
+        del logits, p, edl
+    bound[0] += 2 * U * out[0].abs()
+    for i in (2, 3):
+        bound[i] += rp * out[i].abs()
+    return out, [1.1 * b + 1e-30 for b in bound]
+
+
+@pytest.mark.parametrize("dtype,rows,width,vocab,at_a_time,sums", [
+    # 13 pieces of 61696 entries in 16 ranges each, the last one of 58485 in 15 (the offsets of its sums are the first one's)
+    (monet.BF16, 2048, 8, 798837, 128, 16),
+    # two pieces of 50176 entries, each in 8 ranges of large tiles
+    (monet.BF16, 2048, 1024, 100001, 512, 8),
+    # three pieces of 3328 entries and one of three
+    (monet.F32, 20000, 64, 9507, 2500, None),
+    # pieces whose weights stay below 4 GiB, and the rest: 5120 and 980 entries (those of a few rows, which are read directly, and those of more)
+    (monet.F32, 33, 200000, 6100, 33, None),
+    (monet.F32, 7, 200000, 6100, 7, None),
+])
+def test_linear_ce_over_pieces_and_ranges(dtype, rows, width, vocab, at_a_time, sums):
+    """Several pieces of the vocabulary, with dx's sums held over several ranges of each, or in large tiles; dx written and added to."""
+    torch = torch_mod()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(25)
+    x = torch.randn(rows, width, generator=g, device="cuda").to(tdtype(dtype))
+    w = torch.empty(vocab, width, dtype=tdtype(dtype), device="cuda")
+    for a in range(0, vocab, 1 << 15):
+        part = w[a:a + (1 << 15)]
+        part.copy_(torch.randn(part.shape, generator=g, device="cuda") * (1.5 * width ** -0.5))
+    lab = torch.randint(-1, vocab, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    lab[0] = vocab - 1
+    if sums:      # the workspace holds dx's sums of so many ranges, and a piece of the gradient besides
+        need = monet.call("monet_linear_ce_workspace_bytes", 1, dtype, rows, width, vocab)
+        assert need < rows * vocab * 2 and need >= sums * rows * width * 4 + rows * 2 * vocab // -(-vocab * rows * 2 // (256 << 20))
+    loss, lse = torch.empty(1, device="cuda"), torch.empty(rows, device="cuda")
+    dx, dw = linear_ce_gradients(dtype, x, w, lab)
+    need = monet.call("monet_linear_ce_workspace_bytes", 0, dtype, rows, width, vocab)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    s = torch.cuda.current_stream().cuda_stream
+    monet.call("monet_linear_ce_fwd", s, dtype, x.data_ptr(), w.data_ptr(), lab.data_ptr(), loss.data_ptr(), lse.data_ptr(), rows, width, vocab,
+               ws.data_ptr(), need)
+    del ws
+    want, bound = linear_ce_reference(x, w, lab, dtype, at_a_time)
+    for name, got, ref, b in zip(("loss", "lse", "dx", "dw"), (loss, lse, dx, dw), want, bound):
+        over = (got.double() - ref).abs() - b
+        assert (over <= 0).all(), (name, over.max().item())
+        del over
+    start = (torch.randn(rows, width, generator=g, device="cuda") * 0.1).to(x.dtype)
+    added, dw_too = linear_ce_gradients(dtype, x, w, lab, start)
+    assert torch.equal(dw, dw_too)
+    total = start.double() + want[2]
+    r = R if dtype == monet.BF16 else 8 * U      # fp32: a rounding for each piece
+    assert ((added.double() - total).abs() <= bound[2] + 1.1 * r * (total.abs() + start.double().abs())).all()
+
+
 # ---------------------------------------------------------------------- 8-bit activations
 @pytest.mark.parametrize("dtype", [monet.F32, monet.BF16])
 @pytest.mark.parametrize("rows,cols,outs", [(70, 96, 40), (2000, 4090, 2500)])
