@@ -55,6 +55,37 @@ def test_linear_ce_adds_to_dx_and_leaves_dw(case, dtype):
     within(host(added), total, bound[2] + 1.1 * r * (np.abs(total) + np.abs(host(start))), "added dx")
 
 
+@pytest.mark.parametrize("rows,width,vocab", [(1, 1, 1), (5, 1, 37), (9, 3, 5003), (17, 5, 211), (70, 7, 8200), (33, 63, 4099), (130, 65, 129), (6, 131, 9001)])
+def test_linear_ce_of_odd_widths_off_16_bytes(rows, width, vocab):
+    """fp32 takes any width, and tensors that begin on any word."""
+    torch = torch_mod()
+    rng = np.random.default_rng(26)
+    x, tx = rounded(rng.standard_normal((rows, width), dtype=np.float32), monet.F32)
+    w, tw = rounded(rng.standard_normal((vocab, width), dtype=np.float32) * np.float32(2.0 / np.sqrt(width)), monet.F32)
+    labels = rng.integers(-1, vocab, rows).astype(np.int32)
+    lab = torch.from_numpy(labels).cuda()
+    want = nm.linear_ce_bwd(x, w, labels)
+    bound = linear_ce_bounds(x, w, labels, monet.F32)[2:]
+    for off in (0, 1, 3):
+        def shifted(t):
+            hold = torch.full((t.numel() + 8,), -7.0, device="cuda")
+            at = hold[off:off + t.numel()].view(t.shape)
+            at.copy_(t)
+            return hold, at
+        (_, ax), (_, aw), (hx, dx), (hw, dw) = shifted(tx), shifted(tw), shifted(tx), shifted(tw)
+        need = monet.call("monet_linear_ce_workspace_bytes", 1, monet.F32, rows, width, vocab)
+        ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+        loss, lse = torch.empty(1, device="cuda"), torch.empty(rows, device="cuda")
+        s = torch.cuda.current_stream().cuda_stream
+        monet.call("monet_linear_ce_fwd", s, monet.F32, ax.data_ptr(), aw.data_ptr(), lab.data_ptr(), loss.data_ptr(), lse.data_ptr(), rows, width,
+                   vocab, ws.data_ptr(), need)
+        monet.call("monet_linear_ce_bwd", s, monet.F32, ax.data_ptr(), aw.data_ptr(), lab.data_ptr(), lse.data_ptr(), dx.data_ptr(), dw.data_ptr(),
+                   rows, width, vocab, 0, ws.data_ptr(), need)
+        for name, hold, got, ref, b in (("dx", hx, dx, want[0], bound[0]), ("dw", hw, dw, want[1], bound[1])):
+            within(host(got), ref, b, (name, off))
+            assert (hold[:off] == -7).all() and (hold[off + got.numel():] == -7).all()
+
+
 def linear_ce_reference(x, w, lab, dtype, rows_at_a_time):
     """On the GPU, in 64 bits, some rows at a time: (loss, lse, dx, dw) and bounds, from the same arithmetic as linear_ce_bounds."""
     torch = torch_mod()
@@ -326,3 +357,64 @@ def test_attention_forms_match_64_bits(form, dtype):
             for name, x, w, e in zip(names, got, want, bound):
                 over = (x - w).abs() - e
                 assert (over <= 0).all(), (name, kv, a, b, (x - w).abs().max().item(), over.max().item())
+
+
+# ---------------------------------------------------------------------- captured calls
+@pytest.mark.parametrize("dtype", [monet.F32, monet.BF16])
+def test_captured_calls_replay(dtype):
+    """The vocabulary loss over several pieces, 8-bit activations and (bf16: both forms of) their weight gradient in two graphs that share one workspace,
+    replayed in turn between eager calls with another one: every replay gives the eager results, and follows inputs that change."""
+    torch = torch_mod()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(27)
+    rows, width, vocab, outs = 3000, 1504, 50001, 5000
+    mk = lambda *s: torch.randn(*s, generator=g, device="cuda").to(tdtype(dtype))   # noqa: E731
+    x, w, dy = mk(rows, width), mk(vocab, width) * width ** -0.5, mk(rows, outs)
+    lab = torch.randint(-1, vocab, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    narrow = dy[:, :96].contiguous()
+    need = max(monet.call("monet_linear_ce_workspace_bytes", 1, dtype, rows, width, vocab),
+               monet.call("monet_act8_wgrad_workspace_bytes", dtype, rows, width, outs), monet.call("monet_act8_wgrad_workspace_bytes", dtype, rows, width, 96))
+    code_bytes = monet.call("monet_act8_bytes", rows, width)
+
+    def outputs():
+        f = lambda *s: torch.full(s, -7.0, device="cuda")   # noqa: E731
+        return dict(loss=f(1), lse=f(rows), dx=torch.full_like(x, -7.0), dw=torch.full_like(w, -7.0)), dict(
+            code=torch.full((code_bytes,), 9, dtype=torch.uint8, device="cuda"), y=torch.full_like(x, -7.0), wide=f(outs, width), narrow=f(96, width))
+
+    def loss_calls(t, ws):
+        s = torch.cuda.current_stream().cuda_stream
+        monet.call("monet_linear_ce_fwd", s, dtype, x.data_ptr(), w.data_ptr(), lab.data_ptr(), t["loss"].data_ptr(), t["lse"].data_ptr(), rows, width,
+                   vocab, ws.data_ptr(), need)
+        monet.call("monet_linear_ce_bwd", s, dtype, x.data_ptr(), w.data_ptr(), lab.data_ptr(), t["lse"].data_ptr(), t["dx"].data_ptr(),
+                   t["dw"].data_ptr(), rows, width, vocab, 0, ws.data_ptr(), need)
+
+    def code_calls(t, ws):
+        s = torch.cuda.current_stream().cuda_stream
+        monet.call("monet_act8_pack", s, dtype, x.data_ptr(), width, t["code"].data_ptr(), rows, width)
+        monet.call("monet_act8_unpack", s, dtype, t["code"].data_ptr(), t["y"].data_ptr(), width, rows, width)
+        for name, src, n in (("wide", dy, outs), ("narrow", narrow, 96)):
+            monet.call("monet_act8_wgrad", s, dtype, t["code"].data_ptr(), src.data_ptr(), t[name].data_ptr(), rows, width, n, ws.data_ptr(), need)
+
+    shared, other = (torch.full((need,), 255, dtype=torch.uint8, device="cuda") for _ in range(2))
+    a, b = outputs()
+    graphs = []
+    torch.cuda.synchronize()
+    for calls, t in ((loss_calls, a), (code_calls, b)):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            calls(t, shared)
+        graphs.append(graph)
+    for turn in range(3):
+        ea, eb = outputs()
+        for t in (a, b):
+            for v in t.values():
+                v.fill_(5)
+        for graph, calls, t in zip(graphs, (loss_calls, code_calls), (ea, eb)):
+            graph.replay()
+            calls(t, other)
+        torch.cuda.synchronize()
+        for t, e in ((a, ea), (b, eb)):
+            for name in t:
+                assert torch.equal(t[name], e[name]), (turn, name)
+        x.mul_(1.5)
+        lab.copy_(lab.flip(0))
