@@ -262,14 +262,18 @@ enum monet_dtype { MONET_F32 = 0, MONET_BF16 = 1 };
  * nor written, in any output.  Offsets are held to 0 .. tokens, so that others cannot lead out of the tensors.
  * Needs heads % kv_heads == 0, head_dim a multiple of 8 up to 128, scale > 0, tensors and strides that are multiples of
  * 16 bytes (lse and offsets of 4), tokens below 2^31, (tokens / 64 + seqs + 8) * heads below 2^24 - 2^11; o must not overlap an input.  tokens == 0 is allowed and does nothing.  A sequence's infinities and NaNs stay in that sequence.
- * Within it, one in k or v reaches the rows from its own on and may reach up to 127 rows before it.  fp32: the products go through
- * three bf16 pieces of each operand, exact from 2^-110 up; an infinity in a tensor comes out as NaN. */
+ * Within it, one in k or v reaches the rows from its own on and may reach up to 127 rows before it.  bf16: scores and sums are fp32, a probability
+ * is rounded to bf16 (2^-8 of it at most) before it meets v.  fp32: the products go through three bf16 pieces of each operand, exact from
+ * 2^-110 up; an infinity in a tensor comes out as NaN. */
 int monet_attention_fwd(void *stream, int dtype, const void *q, const void *k, const void *v, void *o, float *lse,
                         const int32_t *cu_seqlens, int seqs, int64_t tokens, int heads, int kv_heads, int head_dim,
                         int64_t q_ld, int64_t k_ld, int64_t v_ld, int64_t o_ld, float scale);
 /* Its gradients from d(o), the inputs, o and lse: the probabilities are computed again.  dout has o's stride, dq q's, dk k's, dv v's;
- * dk and dv are the sums over a group's heads.  The three results must overlap neither each other nor an input.  accumulate: bit 0, 1, 2 adds to dq, dk, dv instead of writing them.
- * Workspace: monet_attention_bwd_workspace_bytes. */
+ * dk and dv are the sums over a group's heads.  The three results must overlap neither each other nor an input.  accumulate: bit 0, 1, 2
+ * adds to dq, dk, dv instead of writing them.  bf16: probabilities and ds = p (dout v^T - delta) are rounded to bf16 before the second products;
+ * delta is summed in fp32 from the probabilities in a sequence's first 128 rows, where few keys average its error out, and is dout . o, with o
+ * as it was rounded, in the others.  Results are off by 2.4e-3 (Frobenius norm; their own rounding alone 1.7e-3).  An infinity or a NaN may
+ * reach up to 127 rows or keys beyond those that it belongs to, in its sequence.  Workspace: monet_attention_bwd_workspace_bytes. */
 int monet_attention_bwd(void *stream, int dtype, const void *dout, const void *q, const void *k, const void *v, const void *o,
                         const float *lse, void *dq, void *dk, void *dv, const int32_t *cu_seqlens, int seqs, int64_t tokens,
                         int heads, int kv_heads, int head_dim, int64_t q_ld, int64_t k_ld, int64_t v_ld, int64_t o_ld,
@@ -279,6 +283,7 @@ int64_t monet_attention_bwd_workspace_bytes(int dtype, int seqs, int64_t tokens,
 /* Softmax cross entropy of a linear layer over a large vocabulary, in pieces of the vocabulary; the logits x w^T are not kept.
  * x [rows][width], w [vocab][width], labels [rows]; a row whose label is outside 0 .. vocab - 1 carries no loss and no gradient.
  *   lse[row] = log sum exp of the row's logits (all rows);  loss = mean over the rows with a label of lse - logit[label], 0 if there are none.
+ * dw is a sum over all rows, with weight 0 for those without a label: x has to be finite in these too.
  * Needs, for bf16, width % 8 == 0 and 16-byte aligned tensors (everything else: 4 bytes); rows below 2^24, width at most 2^20, vocab 2^28.
  * ws_bytes >= monet_linear_ce_workspace_bytes(grad = 0, ...). */
 int monet_linear_ce_fwd(void *stream, int dtype, const void *x, const void *w, const int32_t *labels, float *loss, float *lse,

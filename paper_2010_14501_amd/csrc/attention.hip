@@ -18,11 +18,14 @@
 //
 // Backward is two kernels without atomics, so results do not depend on the order of anything: the first walks along the keys of 128
 // rows (dq, and delta on the way), the second along the rows and the group's heads of 128 keys (dk, dv).  That computes the scores
-// and do v^T twice, seven products for five.
+// and do v^T twice, seven products for five; bf16 computes them a third time for a sequence's first 128 rows (FEW_KEYS).
 //
-// What bounds it, two sequences of 8192 rows, 32 heads of 128 on 8, bf16: forward 1.09 ms (1.01 PFLOP/s), dq 1.52 (1.08 of its three products), dk and
-// dv 2.36 (0.93 of four).  MFMA pipes busy 52, 57 and 51 % of the cycles at 1.9 GHz, which the power limit leaves of 2.4; vector instructions
-// 44, 36 and 34 %, LDS 39, 38 and 45 % without a conflict.  fp32, one of 4096 rows: 0.85, 1.43 and 2.50 ms (162, 145 and 110 TFLOP/s).
+// What bounds it, two sequences of 8192 rows, 32 heads of 128 on 8, bf16: forward 1.05 ms (1.05 PFLOP/s), dq 1.5 (1.1 of its three products), dk and
+// dv 2.2 (1.0 of four).  MFMA pipes busy 51, 58 and 51 % of the cycles at 1.8 to 1.9 GHz, which the power limit leaves of 2.4; vector instructions
+// 43, 36 and 34 %, LDS 38, 39 and 44 % without a conflict.  Eight ragged sequences of as many rows in all keep the pipes busy 38, 41 and 32 % at
+// 2.1 GHz: no power limit there, but the longest ways, which end alone.  fp32, one of 4096 rows: 0.84, 1.33 and 2.30 ms (164, 155 and 120 TFLOP/s),
+// pipes busy 44, 39 and 29 %; one of 1347 rows and one of 700, 12 heads of 64: 15 to 20 %, with 6 to 10 vector instructions, most of them for the
+// pieces, to a matrix instruction.
 #include <initializer_list>
 
 #include "../../include/monet_kernels.h"
@@ -40,6 +43,8 @@ __device__ __forceinline__ int uniform_wave() { return __builtin_amdgcn_readfirs
 
 // bf16: delta = sum of p dp, from fp32, in the rows of a sequence before this one; from o, rounded to bf16, in the others.  What rounding o moves delta by
 // goes into ds of all keys alike, which few keys do not average out: dq and dk of sequences of a few rows are 2.4e-3 off so, from o throughout 4.2e-3.
+// It costs two products more in those rows.  Both backward kernels, 32 / 8 heads of 128: 128 sequences of 64 rows 171 us, without it 161; 64 of 128
+// 254 and 227; 142 of 1 to 60 rows 151 and 134; 16 of 512 259 and 255; the eight ragged ones the same.
 constexpr int FEW_KEYS = 128;
 
 // The rows of a 32 x 32 result that lie before `limit` are not the lane's key's: their probabilities are 0.  The limit passes through a register of

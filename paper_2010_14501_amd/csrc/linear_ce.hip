@@ -309,7 +309,9 @@ __global__ __launch_bounds__(256) void ce_piece_grad_kernel(float *__restrict__ 
 // workgroups wait for memory; here a workgroup sums 256 columns over `per` entries of the piece on the vector units, rows from scalar
 // registers, and leaves part[range][row][column].  11 rows, 1120 columns, 41104 entries (184 MB): 48 us (3.8 TB/s), the convolutions'
 // tiles 91; 1 row, 144 columns, 92544 entries: 9 us, the tiles 188.
-// Twice as many rows (grid z) read W twice: backward pass of 24 rows, 512 columns, 1000 entries 27 us, with the tiles 30; but 20 rows, 4096 columns, 32000 entries 595 us (tiles 500).
+// Twice as many rows (grid z) read W twice, which pays where it stays in L2; backward pass of 24 rows, with this kernel and with the tiles, us: 128
+// columns and 1009 entries 26 and 33, 512 and 2000 27 and 29, 1024 and 1024 30.5 and 30.9, 1024 and 2048 32 and 31, 2048 and 4000 52 and 45, 4096
+// and 32000 575 and 469.  So up to 2^20 weights; of narrower layers also beyond (512 and 16000: 54 and 69; 256 and 32000: 56 and 101), not taken.
 constexpr int CE_FEW_ROWS = 16;
 template <int ROWS>
 __global__ __launch_bounds__(256) void ce_few_rows_kernel(const float *__restrict__ dl, int piece, const float *__restrict__ w, int width, int rows, int per,
