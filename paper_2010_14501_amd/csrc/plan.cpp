@@ -349,6 +349,7 @@ static void check_transformer_nodes(const Graph &g) {
             for (const FwdImpl &im : n.fimpls) enough(im.ws, bytes(false));
             each_impl("linearce_bwd", "pieces", bytes(true));
         } else if (n.op == "linear" && aux) {
+            need(n.ins.size() == 1 && n.pars.size() == 2, "has one input, a weight and a bias");
             const auto &x = g.shape_of(n.ins[0]);
             need(aux->op == "act8" && x.size() == 2 && numel(aux->shape) == x[0] * ((x[1] + 31) / 32) * 33, "the 8-bit copy of an input rows x cols has rows * ceil(cols / 32) * 33 bytes");
             need(n.shape.size() == 2, "output must be rows x outputs");

@@ -99,6 +99,8 @@ def test_graph_texts_that_do_not_fit_are_refused(old, new, match):
     ("bop 34 linearce_bwd node=38", "bop 34 linearce_bwd node=37", "does not belong"),
     ("bop 1 linear_wgrad node=1", "bop 1 attention_bwd node=1", "does not belong"),
     ("bimpl 14 0 algo=copy", "bimpl 14 0 algo=from_code", "does not belong"),
+    ("node 4 linear in=1 par=4,5", "node 4 linear in=- par=4,5", "one input"),
+    ("node 4 linear in=1 par=4,5", "node 4 linear in=1 par=4", "one input"),
 ])
 def test_graph_texts_that_a_step_would_refuse_are_refused_when_loaded(old, new, match):
     """A step that finds something to refuse has launched what comes before it: scales, declared workspaces and the nodes of backward operators
