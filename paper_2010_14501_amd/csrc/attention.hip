@@ -896,6 +896,7 @@ int row_parts(const AttShape &a) {
 //   as the mean length has it, and so: bf16, 4000 rows and nine empty sequences, 8 / 1 heads of 64, 291 and 123; 12000 and 255 empty, 4 / 1 heads
 //   of 128, 2000 and 770; fp32, 6000 and 63 empty, 16 / 4 heads of 128, 7900 and 4310; 5000, 3, 900 and 2000 rows, 8 / 4 heads of 128, 2450 and
 //   2040; but bf16, 32 sequences of 128 rows, 32 / 4 heads of 64, 63 and 74: workgroups that find no range to work on, and a launch to join none
+//   bf16, 32 keys in one range and up to two, heads of 128: 4 sequences of 1024 rows, 4 / 4 heads, 54 and 64; 6000 and 63 empty, 16 / 4 heads, 1063 and 755
 //   bf16, 128 and 32 keys: 256 sequences of 32 rows, 16 / 4 heads of 128, 139 and 187; 16 of 256, 4 / 1 heads of 128, 71 and 42
 struct KeyForm { int parts, ranges; };
 KeyForm key_form(const AttShape &a, bool fp32) {
@@ -907,8 +908,10 @@ KeyForm key_form(const AttShape &a, bool fp32) {
     const int64_t longest = a.tokens * group;
     if (fp32) return {1, (int)cut(full, longest, AttForm<float, 64, 1>::RANGE_ROWS)};
     constexpr int LEAST = AttForm<unsigned short, 64, 1>::RANGE_ROWS;
-    if (full >= 256 || (mean >= 64 && full * cut(full, mean * group, LEAST) >= 512)) return {1, full >= 1024 ? 1 : (int)cut(full, longest, LEAST)};
-    return {4, (int)cut(4 * full, longest, AttForm<unsigned short, 64, 4>::RANGE_ROWS)};
+    if (full >= 256 || (mean >= 64 && full * std::min<int64_t>(mean * group / LEAST, 16) >= 512)) return {1, full >= 1024 ? 1 : (int)cut(full, longest, LEAST)};
+    constexpr int LEAST4 = AttForm<unsigned short, 64, 4>::RANGE_ROWS;
+    if (longest < (4 * full >= 512 ? 8 : 2) * LEAST4) return {4, 1};      // two ranges at most, of ways that are not long
+    return {4, (int)cut(4 * full, longest, LEAST4)};
 }
 
 template <class T, int D, int PARTS>
