@@ -384,15 +384,15 @@ WgradPlan wgrad_plan(int dtype, int64_t rows, int cols, int outs, bool aligned) 
 
 }  // namespace
 
-size_t act8_bytes(int64_t rows, int64_t cols) {
-    check_shape(rows, cols);
-    return (size_t)(rows * (code_ld(cols) / GROUP) * (GROUP + 1));
-}
-
 // a launch of eight values a thread takes less than 2^24 workgroups
 void act8_check_values(int64_t rows, int64_t cols) {
     check_shape(rows, cols);
     if ((rows * (code_ld(cols) / 8) + 255) / 256 >= 1 << 24) throw KernelError("act8: too many values");
+}
+
+size_t act8_bytes(int64_t rows, int64_t cols) {
+    act8_check_values(rows, cols);
+    return (size_t)(rows * (code_ld(cols) / GROUP) * (GROUP + 1));
 }
 
 void act8_pack(hipStream_t st, int dtype, const void *x, int64_t ld, void *code, int64_t rows, int64_t cols) {

@@ -896,7 +896,8 @@ int row_parts(const AttShape &a) {
 //   as the mean length has it, and so: bf16, 4000 rows and nine empty sequences, 8 / 1 heads of 64, 291 and 123; 12000 and 255 empty, 4 / 1 heads
 //   of 128, 2000 and 770; fp32, 6000 and 63 empty, 16 / 4 heads of 128, 7900 and 4310; 5000, 3, 900 and 2000 rows, 8 / 4 heads of 128, 2450 and
 //   2040; but bf16, 32 sequences of 128 rows, 32 / 4 heads of 64, 63 and 74: workgroups that find no range to work on, and a launch to join none
-//   bf16, 32 keys in one range and up to two, heads of 128: 4 sequences of 1024 rows, 4 / 4 heads, 54 and 64; 6000 and 63 empty, 16 / 4 heads, 1063 and 755
+//   bf16, 32 keys in one range and up to two: 4 sequences of 1024 rows, 4 / 4 heads of 128, 61 and 64; 3258 rows, 8 / 8 heads of 40, 77 and 84; 6000
+//   and 63 empty, 16 / 4 heads of 128, 1063 and 755
 //   bf16, 128 and 32 keys: 256 sequences of 32 rows, 16 / 4 heads of 128, 139 and 187; 16 of 256, 4 / 1 heads of 128, 71 and 42
 struct KeyForm { int parts, ranges; };
 KeyForm key_form(const AttShape &a, bool fp32) {

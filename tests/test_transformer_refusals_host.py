@@ -57,3 +57,13 @@ def test_empty_sequences_take_no_ranges_from_a_long_one(heads, kv_heads, dim, to
     for seqs in (1, 10, 64, 256):
         assert need(monet.F32, seqs) == need(monet.F32, 1) > 2 * sums
         assert need(monet.BF16, seqs) > 2 * sums
+
+
+def test_act8_bytes_refuses_what_pack_refuses():
+    """2^35 codes are more than a launch takes; one row fewer is not."""
+    rows, cols = 1 << 11, 1 << 24
+    with pytest.raises(monet.MonetError, match="too many"):
+        monet.call("monet_act8_pack", None, monet.BF16, P, cols, P, rows, cols)
+    with pytest.raises(monet.MonetError, match="too many"):
+        monet.call("monet_act8_bytes", rows, cols)
+    assert monet.call("monet_act8_bytes", rows - 1, cols) == (rows - 1) * cols // 32 * 33
