@@ -273,7 +273,7 @@ def _rope_own(s):
 def _linear_distill_own(s):
     c, x, w = s["case"], s["x"], s["w"]
     rows, width, vocab, k, heat = c["rows"], c["width"], c["vocab"], c["top"], c["temperature"]
-    loss, lse, mass, delta = (torch.empty(*n, device=DEV) for n in ((), (rows,), (rows,), (rows, k)))
+    loss, lse, mass, delta = (torch.empty(n, device=DEV) for n in ((), (rows,), (rows,), (rows, k)))
     need = _call("monet_linear_distill_workspace_bytes", 1 if c["grad"] else 0, _dtype(s["t"]), rows, width, vocab, k)
     ws = _ws(need)
     shape = (rows, width, vocab, k, heat)
