@@ -245,7 +245,7 @@ int monet_softmaxce_rows_bwd(void *stream, const float *logits, const int32_t *l
                              int64_t rows, int classes, int accumulate);
 
 /* ---- a transformer's training step ----------------------------------------------------------------------------
- * The three operators below take fp32 or bf16 tensors (bfloat16: the upper half of an fp32 number), row by row; statistics
+ * The operators below take fp32 or bf16 tensors (bfloat16: the upper half of an fp32 number), row by row; statistics
  * and sums are fp32.  Their backward passes hold little: no probabilities, no logits, inputs in 8 bits.  Workspaces are device
  * memory owned by the caller, 256-byte aligned, contents irrelevant before and after a call; calls that overlap in time need
  * workspaces of their own.  Everything else may be shared.  Results do not depend on the order in which anything runs: two
@@ -295,6 +295,54 @@ int monet_linear_ce_fwd(void *stream, int dtype, const void *x, const void *w, c
 int monet_linear_ce_bwd(void *stream, int dtype, const void *x, const void *w, const int32_t *labels, const float *lse, void *dx,
                         void *dw, int64_t rows, int width, int vocab, int accumulate, void *ws, size_t ws_bytes);
 int64_t monet_linear_ce_workspace_bytes(int grad, int dtype, int64_t rows, int width, int vocab);
+
+/* The same layer against a teacher's top logits: row r has `top` entries, vocabulary index index[r][j] with the teacher's logit target[r][j] (fp32).
+ * An index outside 0 .. vocab - 1 is no entry; an entry whose logit is -infinity has no weight.  With T the temperature and z = x w^T / T,
+ *   p = exp(target / T - n), n = log sum exp of the row's target / T, or target_lse[r] (NULL: none) where the teacher's own normaliser
+ *   over its whole vocabulary is known;  mass[r] = sum p (1 without target_lse; 0 in a row without weight),  lse[r] = log sum exp z (all rows);
+ *   loss = T^2 * mean over the rows with mass != 0 of sum_j p_j (log p_j + lse - z[index_j]), 0 if there are none;
+ *   delta[r][j] = mass exp(z[index_j] - lse) - (sum of p at that index), the gradient of the row's sum by z there (0 where there is no entry).
+ * An index may come more than once in a row.  x, w, loss, lse, sizes and workspaces as for linear_ce (dw is a sum over all rows: x has to be
+ * finite in all of them); mass [rows], delta [rows][top] fp32, both needed by the backward call; top 1 to 1024; fp32 tensors, index and numbers 4-byte aligned.
+ * ws_bytes >= monet_linear_distill_workspace_bytes(grad = 0, ...). */
+int monet_linear_distill_fwd(void *stream, int dtype, const void *x, const void *w, const int32_t *index, const float *target, const float *target_lse,
+                             float *loss, float *lse, float *mass, float *delta, int64_t rows, int width, int vocab, int top, float temperature, void *ws,
+                             size_t ws_bytes);
+/* That loss's gradients, as for linear_ce: dx (added to if accumulate != 0), dw (written).  ws_bytes >= monet_linear_distill_workspace_bytes(grad = 1, ...),
+ * which is also enough for the forward call. */
+int monet_linear_distill_bwd(void *stream, int dtype, const void *x, const void *w, const int32_t *index, const float *lse, const float *mass,
+                             const float *delta, void *dx, void *dw, int64_t rows, int width, int vocab, int top, float temperature, int accumulate,
+                             void *ws, size_t ws_bytes);
+int64_t monet_linear_distill_workspace_bytes(int grad, int dtype, int64_t rows, int width, int vocab, int top);
+
+/* Layer norm over rows of `cols` values (variance biased): y = (x - mean) rstd gamma + beta, rstd = 1 / sqrt(var + eps).
+ * x, y: rows x_ld, y_ld elements apart; gamma, beta [cols] of type param_dtype (a monet_dtype; NULL: 1 and 0).
+ * stats [rows][2]: mean and rstd, fp32, for the backward call (NULL if nobody needs them; 8-byte aligned).  y may be x (same stride).
+ * rows below 2^31, cols at most 2^20, strides below 2^31, any alignment of an element; rows == 0 is allowed.  An infinity or a NaN stays in its row. */
+int monet_layernorm_fwd(void *stream, int dtype, int param_dtype, const void *x, const void *gamma, const void *beta, void *y, float *stats, int64_t rows,
+                        int cols, int64_t x_ld, int64_t y_ld, float eps);
+/* Its gradients from dy, the input and stats: dx (may be dy, with the same stride), dgamma and dbeta [cols] of type param_dtype (sums over the rows; of no
+ * rows: 0); any of the three may be NULL.  Otherwise no result overlaps another one or an input.  accumulate: bit 0, 1, 2 adds to dx, dgamma, dbeta
+ * instead of writing them.  The workspace is needed where dgamma or dbeta is. */
+int monet_layernorm_bwd(void *stream, int dtype, int param_dtype, const void *dy, const void *x, const void *gamma, const float *stats, void *dx, void *dgamma,
+                        void *dbeta, int64_t rows, int cols, int64_t dy_ld, int64_t x_ld, int64_t dx_ld, int accumulate, void *ws, size_t ws_bytes);
+int64_t monet_layernorm_bwd_workspace_bytes(int dtype, int64_t rows, int cols);
+
+/* Rotary positions.  x, y [tokens][heads][head_dim], tokens x_ld, y_ld elements apart (heads lie head_dim apart, so that the queries and keys of a
+ * packed projection are one call).  The first rot_dim values of a head are pairs, (2i, 2i + 1) if interleaved, else (i, i + rot_dim / 2):
+ *   (a, b) -> scale * (a cos - b sin, b cos + a sin),  angle = positions[token] * freqs[i];  the others stay as they are.
+ * positions: device, one per token, of any value (NULL: the token's index).  freqs: host memory, rot_dim / 2 values in radians a position, read before the
+ * call returns.  Angles are reduced in 64 bits.  y may be x (same stride); otherwise they do not overlap.  rot_dim even, 2 to 512 and at most head_dim;
+ * any alignment of an element; tokens below 2^31, tokens * heads * head_dim below 2^38; tokens == 0 is allowed and does nothing. */
+int monet_rope_fwd(void *stream, int dtype, const void *x, void *y, const int32_t *positions, const double *freqs, int64_t tokens, int heads, int head_dim,
+                   int rot_dim, int64_t x_ld, int64_t y_ld, int interleaved, float scale);
+/* The gradient: dx (may be dy, with the same stride, if nothing is added to) is dy turned back, times scale; accumulate != 0 adds to it. */
+int monet_rope_bwd(void *stream, int dtype, const void *dy, void *dx, const int32_t *positions, const double *freqs, int64_t tokens, int heads, int head_dim,
+                   int rot_dim, int64_t dy_ld, int64_t dx_ld, int interleaved, float scale, int accumulate);
+/* Host only: freqs[i] = base^(-2 i / rot_dim), for i < rot_dim / 2.  factor: a context so many times longer.  low = high = 0: every frequency is divided by
+ * it (1: none).  Otherwise a pair that turns more than `high` times over `original` positions is left as it is, one that turns less than
+ * `low` times is divided, and in between the two are blended in proportion. */
+int monet_rope_freqs(double *freqs, int rot_dim, double base, double factor, double original, double low, double high);
 
 /* An activation x [rows][cols] held in 8 bits until its backward operator: 32 neighbouring columns share a power of two 2^e, the
  * smallest from e = -126 up with max|x| / 2^e < 127.5, and a code is x / 2^e rounded to nearest, ties to even.  A group with an

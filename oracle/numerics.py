@@ -423,6 +423,79 @@ def linear_ce_bwd(x, w, labels):
     return dl @ w, dl.T @ x
 
 
+def linear_distill_fwd(x, w, index, target, temperature, target_lse=None):
+    """A linear layer against a teacher's top logits: rows' entries index [rows, top] (those outside 0 .. vocab - 1 do not count) with the
+    teacher's logits target.  z = x w^T / T, p = softmax of the entries' target / T (with target_lse: exp(target / T - target_lse)).
+    Returns T^2 times the mean over the rows with weight of sum p (log p + lse - z) (0 if there are none), lse of z, the rows' weight
+    sum p, and per entry the gradient of its row's sum by z there."""
+    z = x @ w.T / temperature
+    m = z.max(axis=1)
+    lse = m + np.log(np.exp(z - m[:, None]).sum(axis=1))
+    loss, mass, delta = np.zeros(len(x)), np.zeros(len(x)), np.zeros(index.shape)
+    for r in range(len(x)):
+        inside = np.flatnonzero((index[r] >= 0) & (index[r] < w.shape[0]))
+        has = inside[target[r, inside] != -np.inf]
+        if len(has) == 0:
+            continue
+        t = target[r, has] / temperature
+        logp = t - (np.log(np.exp(t - t.max()).sum()) + t.max() if target_lse is None else target_lse[r])
+        p = np.exp(logp)
+        at = index[r, has]
+        loss[r], mass[r] = (p * (logp + lse[r] - z[r, at])).sum(), p.sum()
+        for j in inside:
+            delta[r, j] = mass[r] * np.exp(z[r, index[r, j]] - lse[r]) - p[at == index[r, j]].sum()
+    return temperature ** 2 * loss.sum() / max(np.count_nonzero(mass), 1), lse, mass, delta
+
+
+def linear_distill_bwd(x, w, index, target, temperature, target_lse=None):
+    """Gradients of that loss: dx, dw."""
+    _, lse, mass, delta = linear_distill_fwd(x, w, index, target, temperature, target_lse)
+    d = mass[:, None] * np.exp(x @ w.T / temperature - lse[:, None])
+    for r, j in np.ndindex(index.shape):
+        if mass[r] != 0 and 0 <= index[r, j] < w.shape[0]:
+            d[r, index[r, j]] = delta[r, j]
+    d *= temperature / max(np.count_nonzero(mass), 1)
+    return d @ w, d.T @ x
+
+
+def layernorm_fwd(x, gamma, beta, eps):
+    """Rows of x [rows, cols] to mean 0 and variance 1 (biased, eps added), times gamma plus beta; and the rows' mean and 1 / deviation."""
+    mean = x.mean(axis=1)
+    rstd = 1.0 / np.sqrt(((x - mean[:, None]) ** 2).mean(axis=1) + eps)
+    return (x - mean[:, None]) * rstd[:, None] * gamma + beta, mean, rstd
+
+
+def layernorm_bwd(dy, x, gamma, eps):
+    """Gradients of sum(dy * y): dx, dgamma, dbeta."""
+    _, mean, rstd = layernorm_fwd(x, gamma, 0.0, eps)
+    xh = (x - mean[:, None]) * rstd[:, None]
+    g = dy * gamma
+    dx = rstd[:, None] * (g - g.mean(axis=1, keepdims=True) - xh * (g * xh).mean(axis=1, keepdims=True))
+    return dx, (dy * xh).sum(axis=0), dy.sum(axis=0)
+
+
+def rope_freqs(rot, base, factor=1.0, original=0.0, low=0.0, high=0.0):
+    """Radians a position for each pair of a head: base^(-2 i / rot), slower by `factor`; with low < high, pairs that turn more than `high` times over
+    `original` positions are left as they are, those that turn less than `low` times are not, in between a blend."""
+    f = base ** (-2.0 * np.arange(rot // 2) / rot)
+    keep = np.clip((original * f / (2 * np.pi) - low) / (high - low), 0.0, 1.0) if high > low else 0.0
+    return f * keep + f / factor * (1.0 - keep)
+
+
+def rope_fwd(x, positions, freqs, interleaved, scale=1.0):
+    """x [tokens, heads, dim]: the first 2 * len(freqs) of a head turned pair by pair by positions * freqs and scaled."""
+    y, half = x.astype(F64), len(freqs)
+    a, b = (np.arange(0, 2 * half, 2), np.arange(1, 2 * half, 2)) if interleaved else (np.arange(half), np.arange(half, 2 * half))
+    z = (x[..., a] + 1j * x[..., b]) * (scale * np.exp(1j * np.multiply.outer(positions, freqs)))[:, None, :]
+    y[..., a], y[..., b] = z.real, z.imag
+    return y
+
+
+def rope_bwd(dy, positions, freqs, interleaved, scale=1.0):
+    """The gradient: turned back."""
+    return rope_fwd(dy, positions, -np.asarray(freqs), interleaved, scale)
+
+
 ACT8_GROUP = 32
 
 

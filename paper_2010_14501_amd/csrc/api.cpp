@@ -1276,6 +1276,56 @@ extern "C" int monet_linear_ce_bwd(void *stream, int dtype, const void *x, const
 extern "C" int64_t monet_linear_ce_workspace_bytes(int grad, int dtype, int64_t rows, int width, int vocab) {
     return guarded_bytes([&] { return linear_ce_workspace_bytes(grad != 0, dtype, rows, width, vocab); });
 }
+extern "C" int monet_linear_distill_fwd(void *stream, int dtype, const void *x, const void *w, const int32_t *index, const float *target,
+                                        const float *target_lse, float *loss, float *lse, float *mass, float *delta, int64_t rows, int width, int vocab,
+                                        int top, float temperature, void *ws, size_t ws_bytes) {
+    return guarded([&] {
+        linear_distill_fwd((hipStream_t)stream, dtype, x, w, index, target, target_lse, loss, lse, mass, delta, rows, width, vocab, top, temperature, ws,
+                           ws_bytes);
+    });
+}
+extern "C" int monet_linear_distill_bwd(void *stream, int dtype, const void *x, const void *w, const int32_t *index, const float *lse, const float *mass,
+                                        const float *delta, void *dx, void *dw, int64_t rows, int width, int vocab, int top, float temperature,
+                                        int accumulate, void *ws, size_t ws_bytes) {
+    return guarded([&] {
+        linear_distill_bwd((hipStream_t)stream, dtype, x, w, index, lse, mass, delta, dx, dw, rows, width, vocab, top, temperature, accumulate != 0, ws,
+                           ws_bytes);
+    });
+}
+extern "C" int64_t monet_linear_distill_workspace_bytes(int grad, int dtype, int64_t rows, int width, int vocab, int top) {
+    return guarded_bytes([&] { return linear_distill_workspace_bytes(grad != 0, dtype, rows, width, vocab, top); });
+}
+extern "C" int monet_layernorm_fwd(void *stream, int dtype, int param_dtype, const void *x, const void *gamma, const void *beta, void *y, float *stats,
+                                   int64_t rows, int cols, int64_t x_ld, int64_t y_ld, float eps) {
+    return guarded([&] { layernorm_fwd((hipStream_t)stream, dtype, param_dtype, x, gamma, beta, y, stats, rows, cols, x_ld, y_ld, eps); });
+}
+extern "C" int monet_layernorm_bwd(void *stream, int dtype, int param_dtype, const void *dy, const void *x, const void *gamma, const float *stats, void *dx,
+                                   void *dgamma, void *dbeta, int64_t rows, int cols, int64_t dy_ld, int64_t x_ld, int64_t dx_ld, int accumulate, void *ws,
+                                   size_t ws_bytes) {
+    return guarded([&] {
+        layernorm_bwd((hipStream_t)stream, dtype, param_dtype, dy, x, gamma, stats, dx, dgamma, dbeta, rows, cols, dy_ld, x_ld, dx_ld, accumulate, ws,
+                      ws_bytes);
+    });
+}
+extern "C" int64_t monet_layernorm_bwd_workspace_bytes(int dtype, int64_t rows, int cols) {
+    return guarded_bytes([&] { return layernorm_bwd_workspace_bytes(dtype, rows, cols); });
+}
+extern "C" int monet_rope_freqs(double *freqs, int rot_dim, double base, double factor, double original, double low, double high) {
+    return guarded([&] { rope_freqs(freqs, rot_dim, base, factor, original, low, high); });
+}
+extern "C" int monet_rope_fwd(void *stream, int dtype, const void *x, void *y, const int32_t *positions, const double *freqs, int64_t tokens, int heads,
+                              int head_dim, int rot_dim, int64_t x_ld, int64_t y_ld, int interleaved, float scale) {
+    return guarded([&] {
+        rope((hipStream_t)stream, dtype, x, y, positions, freqs, tokens, heads, head_dim, rot_dim, x_ld, y_ld, interleaved != 0, scale, false, false);
+    });
+}
+extern "C" int monet_rope_bwd(void *stream, int dtype, const void *dy, void *dx, const int32_t *positions, const double *freqs, int64_t tokens, int heads,
+                              int head_dim, int rot_dim, int64_t dy_ld, int64_t dx_ld, int interleaved, float scale, int accumulate) {
+    return guarded([&] {
+        rope((hipStream_t)stream, dtype, dy, dx, positions, freqs, tokens, heads, head_dim, rot_dim, dy_ld, dx_ld, interleaved != 0, scale, true,
+             accumulate != 0);
+    });
+}
 extern "C" int64_t monet_act8_bytes(int64_t rows, int64_t cols) {
     return guarded_bytes([&] { return act8_bytes(rows, cols); });
 }

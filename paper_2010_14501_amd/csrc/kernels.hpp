@@ -238,6 +238,22 @@ void linear_ce_fwd(hipStream_t st, int dtype, const void *x, const void *w, cons
                    int width, int vocab, void *ws, size_t ws_bytes);
 void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *labels, const float *lse, void *dx, void *dw,
                    int64_t rows, int width, int vocab, bool accumulate, void *ws, size_t ws_bytes);
+size_t linear_distill_workspace_bytes(bool grad, int dtype, int64_t rows, int width, int vocab, int top);
+void linear_distill_fwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *index, const float *target, const float *target_lse,
+                        float *loss, float *lse, float *mass, float *delta, int64_t rows, int width, int vocab, int top, float heat, void *ws,
+                        size_t ws_bytes);
+void linear_distill_bwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *index, const float *lse, const float *mass,
+                        const float *delta, void *dx, void *dw, int64_t rows, int width, int vocab, int top, float heat, bool accumulate, void *ws,
+                        size_t ws_bytes);
+void layernorm_fwd(hipStream_t st, int dtype, int param_dtype, const void *x, const void *gamma, const void *beta, void *y, float *stats, int64_t rows,
+                   int cols, int64_t x_ld, int64_t y_ld, float eps);
+size_t layernorm_bwd_workspace_bytes(int dtype, int64_t rows, int cols);
+void layernorm_bwd(hipStream_t st, int dtype, int param_dtype, const void *dy, const void *x, const void *gamma, const float *stats, void *dx, void *dgamma,
+                   void *dbeta, int64_t rows, int cols, int64_t dy_ld, int64_t x_ld, int64_t dx_ld, int accumulate, void *ws, size_t ws_bytes);
+void rope_freqs(double *freqs, int rot_dim, double base, double factor, double original, double low, double high);      // host
+// inverse: turned back (the gradient); freqs: host memory, rot_dim / 2 values, read before the call returns
+void rope(hipStream_t st, int dtype, const void *x, void *y, const int32_t *positions, const double *freqs, int64_t tokens, int heads, int head_dim,
+          int rot_dim, int64_t x_ld, int64_t y_ld, bool interleaved, float scale, bool inverse, bool accumulate);
 size_t act8_bytes(int64_t rows, int64_t cols);
 void act8_check_values(int64_t rows, int64_t cols);      // refuses what pack and unpack refuse
 void act8_pack(hipStream_t st, int dtype, const void *x, int64_t ld, void *code, int64_t rows, int64_t cols);

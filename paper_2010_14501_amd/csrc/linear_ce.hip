@@ -8,6 +8,7 @@
 // products whose results are rounded to bf16 themselves; the rounding, at most 2^-8 of a value, averages out over the sums.  1 / count
 // comes in behind the products: the label's entries p - 1 are near -1 and would otherwise all be rounded the same way).  Sums are fp32.
 // fp32: the convolution kernels' products, a piece of logits in the workspace at a time; with few rows two of them on the vector units.
+#include <cmath>
 #include <initializer_list>
 #include <type_traits>
 #include <vector>
@@ -31,12 +32,15 @@ __device__ __forceinline__ Soft soft_join(Soft a, Soft b) {
     return {m, (a.m == -INFINITY ? a.s : a.s * exp_of(a.m - m)) + (b.m == -INFINITY ? b.s : b.s * exp_of(b.m - m))};
 }
 
-// rows of the result are vocabulary entries, columns tokens: a lane has 16 * MB logits of each of its NB tokens
-struct CeStatsEpilogue {
+// rows of the result are vocabulary entries, columns tokens: a lane has 16 * MB logits of each of its NB tokens.  LABELS: the label's logit
+// is kept as well; otherwise the logits are `by` times the product (1 / temperature).
+template <bool LABELS>
+struct StatsEpilogue {
     const int32_t *labels;
     float2 *part;           // [vocab / (32 MB)][rows]: a wave's rows together
     float *hit;             // the label's logit
     int rows, vocab;
+    float by;
     template <int MB, int NB>
     __device__ __forceinline__ void operator()(floatx16 (&acc)[MB][NB], int m0, int n0, int, int) const {
         static_assert(MB == 4 || MB == 2, "");
@@ -44,7 +48,7 @@ struct CeStatsEpilogue {
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const int t = n0 + 32 * j + (l & 31);
-            const int label = t < rows ? labels[t] : -1;
+            const int label = LABELS && t < rows ? labels[t] : -1;
             float top = -INFINITY, mine = 0.f;
             bool found = false;
 #pragma unroll
@@ -52,8 +56,9 @@ struct CeStatsEpilogue {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int v = m0 + 32 * i + result_row(r, l);
+                    if (!LABELS) acc[i][j][r] *= by;
                     if (v >= vocab) acc[i][j][r] = -INFINITY;
-                    if (v == label) { mine = acc[i][j][r]; found = true; }
+                    if (LABELS && v == label) { mine = acc[i][j][r]; found = true; }
                     top = fmaxf(top, acc[i][j][r]);
                 }
             if (found && label < vocab) hit[t] = mine;
@@ -100,6 +105,37 @@ struct CeGradEpilogue {
                         const float p = exp_of(acc[i][j][r + q] - ls);
                         d[q] = has && v < piece ? p - (v0 + v == label ? 1.f : 0.f) : 0.f;
                     }
+                    if (m0 + 32 * i + result_row(r, l) < ld)
+                        *(uint2 *)(row + 32 * i + result_row(r, l)) = make_uint2(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]));
+                }
+        }
+    }
+};
+
+// The same against a teacher: count / T dl = mass exp(l / T - lse), without the teacher's entries, which distill_entries_kernel puts in.
+struct DistillGradEpilogue {
+    const float *mass, *lse;
+    unsigned short *dl;
+    int64_t ld;
+    int rows, piece;
+    float by;           // 1 / T
+    template <int MB, int NB>
+    __device__ __forceinline__ void operator()(floatx16 (&acc)[MB][NB], int m0, int n0, int, int) const {
+        const int l = threadIdx.x & 63;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int t = n0 + 32 * j + (l & 31);
+            if (t >= rows) continue;
+            const float m = mass[t], ls = lse[t];
+            unsigned short *row = dl + t * ld + m0;
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    float d[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        d[q] = m != 0.f && m0 + 32 * i + result_row(r + q, l) < piece ? m * exp_of(acc[i][j][r + q] * by - ls) : 0.f;
                     if (m0 + 32 * i + result_row(r, l) < ld)
                         *(uint2 *)(row + 32 * i + result_row(r, l)) = make_uint2(pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3]));
                 }
@@ -168,8 +204,9 @@ struct RoundEpilogue {
     }
 };
 
-// 16 threads to a token: lse and the row's loss from the parts of its logits.  TOKENS = 64: the only workgroup, which takes the mean as well.
-template <int TOKENS>
+// 16 threads to a token: lse and the row's loss (LABELS false: lse alone) from the parts of its logits.  TOKENS = 64: the only workgroup, which
+// takes the mean as well.
+template <int TOKENS, bool LABELS = true>
 __global__ __launch_bounds__(TOKENS * 16) void ce_merge_kernel(const float2 *__restrict__ part, int parts, const float *__restrict__ hit,
                                                                const int32_t *__restrict__ labels, float *__restrict__ lse,
                                                                float *__restrict__ row_loss, float *__restrict__ loss, int rows, int vocab) {
@@ -194,15 +231,15 @@ __global__ __launch_bounds__(TOKENS * 16) void ce_merge_kernel(const float2 *__r
     __syncthreads();
     if (s) return;
     float mine = 0.f;
-    const bool has = t < rows && (unsigned)labels[t] < (unsigned)vocab;
+    const bool has = LABELS && t < rows && (unsigned)labels[t] < (unsigned)vocab;
     if (t < rows) {
         for (int b = 1; b < 16; ++b) a = soft_join(a, seg[b][l]);
         const float ls = a.m + logf(a.s);
         lse[t] = ls;
         mine = has ? ls - hit[t] : 0.f;
-        if (TOKENS < 64) row_loss[t] = mine;
+        if (TOKENS < 64 && LABELS) row_loss[t] = mine;
     }
-    if (TOKENS < 64) return;
+    if (TOKENS < 64 || !LABELS) return;
     double sum = mine;       // one wave by now
     for (int w = 32; w; w /= 2) sum += __shfl_xor(sum, w);
     const int count = __popcll(__ballot(has));
@@ -253,9 +290,11 @@ __global__ __launch_bounds__(256) void ce_round_kernel(const float *__restrict__
 
 // fp32: maximum and sum of CE_SEGMENT logits of a row's piece (grid y: which), and the label's logit.  The logits are read once, into registers; a
 // row's segments go to different workgroups, since there may be a single row (92544 logits of it: 4.6 us, with one workgroup to a row 122).
+// LABELS false: `by` times the logits, no label.
 constexpr int CE_SEGMENT = 4096;
+template <bool LABELS>
 __global__ __launch_bounds__(256) void ce_piece_stats_kernel(const float *__restrict__ logits, int piece, int v0, const int32_t *__restrict__ labels,
-                                                             float2 *__restrict__ part, float *__restrict__ hit) {
+                                                             float2 *__restrict__ part, float *__restrict__ hit, float by) {
     __shared__ Soft seg[256];
     const int64_t t = blockIdx.x;
     const float *row = logits + t * piece;
@@ -264,7 +303,7 @@ __global__ __launch_bounds__(256) void ce_piece_stats_kernel(const float *__rest
 #pragma unroll
     for (int i = 0; i < CE_SEGMENT / 256; ++i) {
         const int v = from + i * 256 + threadIdx.x;
-        x[i] = v < to ? row[v] : -INFINITY;
+        x[i] = v < to ? (LABELS ? row[v] : row[v] * by) : -INFINITY;
         top = fmaxf(top, x[i]);
     }
     const float base = top == -INFINITY ? 0.f : fminf(top, 3.4028235e38f);
@@ -279,6 +318,7 @@ __global__ __launch_bounds__(256) void ce_piece_stats_kernel(const float *__rest
     }
     if (threadIdx.x) return;
     part[blockIdx.y * (int64_t)gridDim.x + t] = make_float2(seg[0].m, seg[0].s);
+    if (!LABELS) return;
     const int label = labels[t] - v0;
     if (label >= from && label < to) hit[t] = row[label];
 }
@@ -303,6 +343,147 @@ __global__ __launch_bounds__(256) void ce_piece_grad_kernel(float *__restrict__ 
     const int label = labels[t];
     float *at = logits + t * piece + v;
     *at = (unsigned)label < (unsigned)vocab ? (exp_of(*at - lse[t]) - (v0 + v == label ? 1.f : 0.f)) * inv : 0.f;
+}
+
+// ---- against a teacher's top logits
+// Entry j of a row is vocabulary index i_j with the teacher's logit t_j; p_j = exp(t_j / T - its normaliser), 0 for an index outside the vocabulary.
+//   loss = sum_j p_j (log p_j + lse - z_j),   mass = sum_j p_j,   delta_j = mass exp(z_j - lse) - (sum of p at the same index)
+// with z_j = x . w[i_j] / T.  One workgroup to a row; z by a wave's sums over the columns, each in the same order, so that an index that comes
+// twice gets the same number twice.  Bound by reading rows * top rows of w.
+constexpr int DISTILL_TOP = 1024;      // entries of a row, at most
+template <class T>
+__device__ __forceinline__ float distill_dot(const T *x, const T *w, int width, int l);
+template <>
+__device__ __forceinline__ float distill_dot<float>(const float *x, const float *w, int width, int l) {
+    float s = 0.f;
+    for (int c = l; c < width; c += 64) s = fmaf(x[c], w[c], s);
+    return s;
+}
+template <>
+__device__ __forceinline__ float distill_dot<unsigned short>(const unsigned short *x, const unsigned short *w, int width, int l) {
+    float s = 0.f;
+    for (int c = 8 * l; c < width; c += 512) {
+        const uint4 a = *(const uint4 *)(x + c), b = *(const uint4 *)(w + c);
+        const unsigned aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            s = fmaf(__uint_as_float(aw[q] << 16), __uint_as_float(bw[q] << 16), s);
+            s = fmaf(__uint_as_float(aw[q] & 0xffff0000u), __uint_as_float(bw[q] & 0xffff0000u), s);
+        }
+    }
+    return s;
+}
+__device__ __forceinline__ float sum_of_256(float v, float *seg) {      // the same in every thread
+    for (int w = 32; w; w /= 2) v += __shfl_xor(v, w);
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) seg[threadIdx.x / 64] = v;
+    __syncthreads();
+    return (seg[0] + seg[1]) + (seg[2] + seg[3]);
+}
+__device__ __forceinline__ float max_of_256(float v, float *seg) {
+    for (int w = 32; w; w /= 2) v = fmaxf(v, __shfl_xor(v, w));
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) seg[threadIdx.x / 64] = v;
+    __syncthreads();
+    return fmaxf(fmaxf(seg[0], seg[1]), fmaxf(seg[2], seg[3]));
+}
+template <class T>
+__global__ __launch_bounds__(256) void distill_rows_kernel(const T *__restrict__ x, const T *__restrict__ w, const int32_t *__restrict__ index,
+                                                           const float *__restrict__ target, const float *__restrict__ target_lse,
+                                                           const float *__restrict__ lse, float *__restrict__ mass, float *__restrict__ delta,
+                                                           float *__restrict__ row_loss, int width, int vocab, int top, float heat) {
+    __shared__ float z[DISTILL_TOP], p[DISTILL_TOP], seg[4];
+    __shared__ int at[DISTILL_TOP];
+    const int64_t t = blockIdx.x;
+    const int wave = threadIdx.x / 64, l = threadIdx.x & 63;
+    index += t * top;
+    target += t * top;
+    for (int j = threadIdx.x; j < top; j += 256) at[j] = (unsigned)index[j] < (unsigned)vocab ? index[j] : -1;
+    __syncthreads();
+    for (int j = wave; j < top; j += 4) {
+        const int v = __builtin_amdgcn_readfirstlane(at[j]);
+        float s = v < 0 ? 0.f : distill_dot(x + t * width, w + (int64_t)v * width, width, l);
+        for (int k = 32; k; k /= 2) s += __shfl_xor(s, k);
+        if (l == 0) z[j] = s / heat;
+    }
+    float most = -INFINITY;
+    for (int j = threadIdx.x; j < top; j += 256)
+        if (at[j] >= 0) most = fmaxf(most, target[j] / heat);
+    float norm;
+    if (target_lse) norm = target_lse[t];
+    else {
+        most = max_of_256(most, seg);
+        float sum = 0.f;
+        for (int j = threadIdx.x; j < top; j += 256)
+            if (at[j] >= 0 && target[j] != -INFINITY) sum += expf(target[j] / heat - most);
+        norm = most + logf(sum_of_256(sum, seg));
+    }
+    __syncthreads();
+    const float ls = lse[t];
+    float loss = 0.f, m = 0.f;
+    for (int j = threadIdx.x; j < top; j += 256) {
+        // an entry of weight 0 adds nothing, whatever the row's logits are
+        const float logp = target[j] / heat - norm, pj = at[j] < 0 || target[j] == -INFINITY ? 0.f : expf(logp);
+        p[j] = pj;
+        m += pj;
+        if (pj != 0.f) loss += pj * (logp + (ls - z[j]));
+    }
+    loss = sum_of_256(loss, seg);
+    m = sum_of_256(m, seg);
+    for (int j = threadIdx.x; j < top; j += 256) {
+        float d = 0.f;
+        if (at[j] >= 0 && m != 0.f) {
+            float same = 0.f;
+            for (int i = 0; i < top; ++i) same += at[i] == at[j] ? p[i] : 0.f;
+            d = m * expf(z[j] - ls) - same;
+        }
+        delta[t * top + j] = d;
+    }
+    if (threadIdx.x) return;
+    mass[t] = m;
+    row_loss[t] = loss;
+}
+// T^2 times the mean of the losses of the rows with weight, and inv = T / their number (0 for none); sums in a fixed order
+__global__ __launch_bounds__(1024) void distill_mean_kernel(const float *__restrict__ row_loss, const float *__restrict__ mass, int rows, float heat,
+                                                            float *__restrict__ loss, float *__restrict__ inv) {
+    __shared__ double sums[1024];
+    __shared__ int counts[1024];
+    double sum = 0;
+    int count = 0;
+    for (int t = threadIdx.x; t < rows; t += 1024)
+        if (mass[t] != 0.f) { ++count; if (row_loss) sum += row_loss[t]; }
+    sums[threadIdx.x] = sum;
+    counts[threadIdx.x] = count;
+    for (int w = 512; w; w /= 2) {
+        __syncthreads();
+        if ((int)threadIdx.x < w) { sums[threadIdx.x] += sums[threadIdx.x + w]; counts[threadIdx.x] += counts[threadIdx.x + w]; }
+    }
+    if (threadIdx.x) return;
+    if (loss) *loss = counts[0] ? (float)((double)heat * heat * sums[0] / counts[0]) : 0.f;
+    if (inv) *inv = counts[0] ? heat / counts[0] : 0.f;
+}
+// bf16: the teacher's entries of a piece, over what the product's epilogue wrote there.  An index that comes twice has the same delta twice.
+__global__ __launch_bounds__(256) void distill_entries_kernel(const int32_t *__restrict__ index, const float *__restrict__ delta, int64_t n, int top, int v0,
+                                                              int piece, unsigned short *__restrict__ dl, int64_t ld) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    const int64_t v = (int64_t)index[i] - v0;
+    if (v >= 0 && v < piece) dl[i / top * ld + v] = float_bf16(delta[i]);
+}
+// fp32: dl in the place of a row's 256 logits, then the teacher's entries among them
+__global__ __launch_bounds__(256) void distill_piece_grad_kernel(float *__restrict__ logits, int piece, int v0, const float *__restrict__ mass,
+                                                                 const float *__restrict__ lse, const int32_t *__restrict__ index,
+                                                                 const float *__restrict__ delta, int top, const float *__restrict__ inv, float by) {
+    const int64_t t = blockIdx.x;
+    const int from = blockIdx.y * 256, to = min(piece, from + 256), v = from + threadIdx.x;
+    const float m = mass[t], f = *inv;
+    float *row = logits + t * piece;
+    if (v < to) row[v] = m != 0.f ? m * exp_of(row[v] * by - lse[t]) * f : 0.f;
+    __syncthreads();
+    for (int j = threadIdx.x; j < top; j += 256) {
+        const int64_t e = (int64_t)index[t * top + j] - v0;
+        if (e >= from && e < to) row[e] = delta[t * top + j] * f;
+    }
 }
 
 // fp32 and few rows: dx += dl W, which reads all of W for rows * 2 operations an entry.  A matrix tile would be mostly empty, and its few
@@ -561,59 +742,34 @@ GemmShape ce_logits_shape(const CePlan &p, const void *x, const void *w, int v0,
 }
 ConvShape ce_conv_shape(const CePlan &p, int piece) { return ConvShape{p.rows, 1, 1, p.width, piece, 1, 1, 1, 0, 1, 1}; }
 
-}  // namespace
-
-size_t linear_ce_workspace_bytes(bool grad, int dtype, int64_t rows, int width, int vocab) {
-    return (size_t)std::max(ce_plan(grad, dtype, rows, width, vocab).bytes(), ce_plan(false, dtype, rows, width, vocab).bytes());
-}
-
-void linear_ce_fwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *labels, float *loss, float *lse, int64_t rows,
-                   int width, int vocab, void *ws, size_t ws_bytes) {
-    const CePlan p = ce_plan(false, dtype, rows, width, vocab);
-    check_ws(p, ws, ws_bytes);
-    check_aligned(p, {x, w});
-    check_words({labels, loss, lse});
-    float *hit = (float *)ws, *row_loss = hit + up(rows, 64);
-    float2 *part = (float2 *)(row_loss + up(rows, 64));
+// the parts of lse (and the labels' logits) of all logits, which are `by` times the products where there are no labels
+template <bool LABELS>
+void vocab_stats(hipStream_t st, const CePlan &p, const void *x, const void *w, const int32_t *labels, float2 *part, float *hit, float by, void *ws) {
     if (p.bf16) {
-        gemm_bf16<false, false>(st, ce_logits_shape(p, x, w, 0, vocab), CeStatsEpilogue{labels, part, hit, p.rows, vocab}, "linear_ce logits launch");
-    } else {
-        float *logits = (float *)((char *)ws + p.fixed), *product = p.product ? (float *)((char *)logits - p.product) : nullptr;
-        const size_t product_bytes = (size_t)p.product;
-        const std::vector<int> at = p.pieces();
-        int64_t done = 0;      // parts
-        for (size_t i = 0; i + 1 < at.size(); ++i) {
-            const int piece = at[i + 1] - at[i], segments = (int)cut(piece, CE_SEGMENT);
-            const float *wp = (const float *)w + (int64_t)at[i] * width;
-            if (!ce_few_logits(st, (const float *)x, wp, width, p.rows, piece, logits)) conv_fwd(st, (const float *)x, wp, logits, ce_conv_shape(p, piece), 1, product, product_bytes);
-            hipLaunchKernelGGL(ce_piece_stats_kernel, dim3(p.rows, segments), dim3(256), 0, st, logits, piece, at[i], labels, part + done * rows, hit);
-            hip_check(hipGetLastError(), "linear_ce statistics launch");
-            done += segments;
-        }
-    }
-    if (rows <= 64 && rows * p.parts() <= 1 << 14) {      // few enough for one workgroup: a launch less
-        hipLaunchKernelGGL(ce_merge_kernel<64>, dim3(1), dim3(1024), 0, st, part, (int)p.parts(), hit, labels, lse, row_loss, loss, p.rows, vocab);
-        hip_check(hipGetLastError(), "linear_ce merge launch");
+        gemm_bf16<false, false>(st, ce_logits_shape(p, x, w, 0, p.vocab), StatsEpilogue<LABELS>{labels, part, hit, p.rows, p.vocab, by}, "linear_ce logits launch");
         return;
     }
-    hipLaunchKernelGGL(ce_merge_kernel<16>, dim3((unsigned)cut(rows, 16)), dim3(256), 0, st, part, (int)p.parts(), hit, labels, lse, row_loss, loss, p.rows, vocab);
-    hip_check(hipGetLastError(), "linear_ce merge launch");
-    hipLaunchKernelGGL(ce_mean_kernel, dim3(1), dim3(1024), 0, st, row_loss, labels, p.rows, vocab, loss, (float *)nullptr);
-    hip_check(hipGetLastError(), "linear_ce mean launch");
+    float *logits = (float *)((char *)ws + p.fixed), *product = p.product ? (float *)((char *)logits - p.product) : nullptr;
+    const std::vector<int> at = p.pieces();
+    int64_t done = 0;      // parts
+    for (size_t i = 0; i + 1 < at.size(); ++i) {
+        const int piece = at[i + 1] - at[i], segments = (int)cut(piece, CE_SEGMENT);
+        const float *wp = (const float *)w + (int64_t)at[i] * p.width;
+        if (!ce_few_logits(st, (const float *)x, wp, p.width, p.rows, piece, logits))
+            conv_fwd(st, (const float *)x, wp, logits, ce_conv_shape(p, piece), 1, product, (size_t)p.product);
+        hipLaunchKernelGGL(ce_piece_stats_kernel<LABELS>, dim3(p.rows, segments), dim3(256), 0, st, logits, piece, at[i], labels, part + done * p.rows, hit, by);
+        hip_check(hipGetLastError(), "linear_ce statistics launch");
+        done += segments;
+    }
 }
 
-void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *labels, const float *lse, void *dx, void *dw,
-                   int64_t rows, int width, int vocab, bool accumulate, void *ws, size_t ws_bytes) {
-    const CePlan p = ce_plan(true, dtype, rows, width, vocab);
-    check_ws(p, ws, ws_bytes);
-    check_aligned(p, {x, w, dx, dw});
-    check_words({labels, lse});
-    float *inv = (float *)ws;
-    const bool count = p.bf16 || rows > 1024;
-    if (count) {
-        hipLaunchKernelGGL(ce_mean_kernel, dim3(1), dim3(1024), 0, st, (const float *)nullptr, labels, p.rows, vocab, (float *)nullptr, inv);
-        hip_check(hipGetLastError(), "linear_ce count launch");
-    }
+// dx and dw, a piece of the logits' gradient dl at a time.  grad_bf16(g, d, ld, v0, piece) launches the product g with an epilogue that leaves dl / *inv
+// in d, rows ld apart; grad_f32(d, v0, piece) puts dl in the place of the logits d.
+template <class GradBf16, class GradF32>
+void vocab_gradients(hipStream_t st, const CePlan &p, const void *x, const void *w, void *dx, void *dw, bool accumulate, void *ws, const float *inv,
+                     GradBf16 &&grad_bf16, GradF32 &&grad_f32) {
+    const int64_t rows = p.rows;
+    const int width = p.width;
     const std::vector<int> at = p.pieces();
     char *dl = (char *)ws + p.fixed;
     float *parts = (float *)((char *)ws + 256);
@@ -622,8 +778,7 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
         if (p.bf16) {
             unsigned short *d = (unsigned short *)dl;
             const int64_t ld = up(piece, 8);
-            gemm_bf16<false, false>(st, ce_logits_shape(p, x, w, v0, piece),
-                                    CeGradEpilogue{labels, lse, d, ld, p.rows, piece, v0, vocab}, "linear_ce gradient launch");
+            grad_bf16(ce_logits_shape(p, x, w, v0, piece), d, ld, v0, piece);
             GemmShape g{};
             // dx[t][c] (+)= sum over v of w[v][c] dl[t][v]
             g.a = (const unsigned short *)w + (int64_t)v0 * width; g.lda = width;
@@ -652,9 +807,7 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
             float *product = p.product ? parts : nullptr;
             const size_t product_bytes = (size_t)p.product;
             if (!ce_few_logits(st, (const float *)x, wp, width, p.rows, piece, d)) conv_fwd(st, (const float *)x, wp, d, cs, 1, product, product_bytes);
-            hipLaunchKernelGGL((count ? ce_piece_grad_kernel<false> : ce_piece_grad_kernel<true>), dim3(p.rows, (unsigned)cut(piece, 256)), dim3(256), 0, st, d, piece, v0,
-                               labels, lse, inv, p.rows, vocab);
-            hip_check(hipGetLastError(), "linear_ce gradient launch");
+            grad_f32(d, v0, piece);
             if (p.few_rows(piece)) {
                 const int per = p.few_per(piece), ranges = (int)cut(piece, per), n = p.rows * width;
                 const dim3 grid((unsigned)cut(width, 256), ranges);
@@ -672,6 +825,123 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
             conv_wgrad(st, (const float *)x, d, (float *)dw + (int64_t)v0 * width, cs, splits, splits > 1 ? product : nullptr, splits > 1 ? product_bytes : 0);
         }
     }
+}
+
+}  // namespace
+
+size_t linear_ce_workspace_bytes(bool grad, int dtype, int64_t rows, int width, int vocab) {
+    return (size_t)std::max(ce_plan(grad, dtype, rows, width, vocab).bytes(), ce_plan(false, dtype, rows, width, vocab).bytes());
+}
+
+void linear_ce_fwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *labels, float *loss, float *lse, int64_t rows,
+                   int width, int vocab, void *ws, size_t ws_bytes) {
+    const CePlan p = ce_plan(false, dtype, rows, width, vocab);
+    check_ws(p, ws, ws_bytes);
+    check_aligned(p, {x, w});
+    check_words({labels, loss, lse});
+    float *hit = (float *)ws, *row_loss = hit + up(rows, 64);
+    float2 *part = (float2 *)(row_loss + up(rows, 64));
+    vocab_stats<true>(st, p, x, w, labels, part, hit, 1.f, ws);
+    if (rows <= 64 && rows * p.parts() <= 1 << 14) {      // few enough for one workgroup: a launch less
+        hipLaunchKernelGGL(ce_merge_kernel<64>, dim3(1), dim3(1024), 0, st, part, (int)p.parts(), hit, labels, lse, row_loss, loss, p.rows, vocab);
+        hip_check(hipGetLastError(), "linear_ce merge launch");
+        return;
+    }
+    hipLaunchKernelGGL(ce_merge_kernel<16>, dim3((unsigned)cut(rows, 16)), dim3(256), 0, st, part, (int)p.parts(), hit, labels, lse, row_loss, loss, p.rows, vocab);
+    hip_check(hipGetLastError(), "linear_ce merge launch");
+    hipLaunchKernelGGL(ce_mean_kernel, dim3(1), dim3(1024), 0, st, row_loss, labels, p.rows, vocab, loss, (float *)nullptr);
+    hip_check(hipGetLastError(), "linear_ce mean launch");
+}
+
+void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *labels, const float *lse, void *dx, void *dw,
+                   int64_t rows, int width, int vocab, bool accumulate, void *ws, size_t ws_bytes) {
+    const CePlan p = ce_plan(true, dtype, rows, width, vocab);
+    check_ws(p, ws, ws_bytes);
+    check_aligned(p, {x, w, dx, dw});
+    check_words({labels, lse});
+    float *inv = (float *)ws;
+    const bool count = p.bf16 || rows > 1024;
+    if (count) {
+        hipLaunchKernelGGL(ce_mean_kernel, dim3(1), dim3(1024), 0, st, (const float *)nullptr, labels, p.rows, vocab, (float *)nullptr, inv);
+        hip_check(hipGetLastError(), "linear_ce count launch");
+    }
+    vocab_gradients(st, p, x, w, dx, dw, accumulate, ws, inv,
+        [&](const GemmShape &g, unsigned short *d, int64_t ld, int v0, int piece) {
+            gemm_bf16<false, false>(st, g, CeGradEpilogue{labels, lse, d, ld, p.rows, piece, v0, vocab}, "linear_ce gradient launch");
+        },
+        [&](float *d, int v0, int piece) {
+            hipLaunchKernelGGL((count ? ce_piece_grad_kernel<false> : ce_piece_grad_kernel<true>), dim3(p.rows, (unsigned)cut(piece, 256)), dim3(256), 0, st, d, piece, v0,
+                               labels, lse, inv, p.rows, vocab);
+            hip_check(hipGetLastError(), "linear_ce gradient launch");
+        });
+}
+
+namespace {
+CePlan distill_plan(bool grad, int dtype, int64_t rows, int width, int vocab, int top) {
+    if (top < 1 || top > DISTILL_TOP) throw KernelError("linear_distill: 1 to " + std::to_string(DISTILL_TOP) + " entries a row");
+    return ce_plan(grad, dtype, rows, width, vocab);
+}
+void distill_check(float heat) {
+    if (!(heat > 0.f) || !std::isfinite(heat) || !std::isfinite(1.f / heat)) throw KernelError("linear_distill: the temperature must be positive and finite");
+}
+}  // namespace
+
+size_t linear_distill_workspace_bytes(bool grad, int dtype, int64_t rows, int width, int vocab, int top) {
+    distill_plan(grad, dtype, rows, width, vocab, top);
+    return linear_ce_workspace_bytes(grad, dtype, rows, width, vocab);
+}
+
+void linear_distill_fwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *index, const float *target, const float *target_lse,
+                        float *loss, float *lse, float *mass, float *delta, int64_t rows, int width, int vocab, int top, float heat, void *ws,
+                        size_t ws_bytes) {
+    const CePlan p = distill_plan(false, dtype, rows, width, vocab, top);
+    distill_check(heat);
+    check_ws(p, ws, ws_bytes);
+    check_aligned(p, {x, w});
+    check_words({index, target, loss, lse, mass, delta});
+    if ((uintptr_t)target_lse % 4) throw KernelError("linear_distill: target_lse must be 4-byte aligned");
+    float *row_loss = (float *)ws;
+    float2 *part = (float2 *)(row_loss + 2 * up(rows, 64));
+    vocab_stats<false>(st, p, x, w, nullptr, part, nullptr, 1.f / heat, ws);
+    if (rows <= 64 && rows * p.parts() <= 1 << 14)
+        hipLaunchKernelGGL((ce_merge_kernel<64, false>), dim3(1), dim3(1024), 0, st, part, (int)p.parts(), nullptr, nullptr, lse, nullptr, nullptr, p.rows, vocab);
+    else
+        hipLaunchKernelGGL((ce_merge_kernel<16, false>), dim3((unsigned)cut(rows, 16)), dim3(256), 0, st, part, (int)p.parts(), nullptr, nullptr, lse, nullptr, nullptr, p.rows, vocab);
+    hip_check(hipGetLastError(), "linear_distill merge launch");
+    if (p.bf16)
+        hipLaunchKernelGGL(distill_rows_kernel<unsigned short>, dim3(p.rows), dim3(256), 0, st, (const unsigned short *)x, (const unsigned short *)w, index, target,
+                           target_lse, lse, mass, delta, row_loss, width, vocab, top, heat);
+    else
+        hipLaunchKernelGGL(distill_rows_kernel<float>, dim3(p.rows), dim3(256), 0, st, (const float *)x, (const float *)w, index, target, target_lse, lse, mass,
+                           delta, row_loss, width, vocab, top, heat);
+    hip_check(hipGetLastError(), "linear_distill rows launch");
+    hipLaunchKernelGGL(distill_mean_kernel, dim3(1), dim3(1024), 0, st, row_loss, mass, p.rows, heat, loss, (float *)nullptr);
+    hip_check(hipGetLastError(), "linear_distill mean launch");
+}
+
+void linear_distill_bwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *index, const float *lse, const float *mass,
+                        const float *delta, void *dx, void *dw, int64_t rows, int width, int vocab, int top, float heat, bool accumulate, void *ws,
+                        size_t ws_bytes) {
+    const CePlan p = distill_plan(true, dtype, rows, width, vocab, top);
+    distill_check(heat);
+    check_ws(p, ws, ws_bytes);
+    check_aligned(p, {x, w, dx, dw});
+    check_words({index, lse, mass, delta});
+    float *inv = (float *)ws;
+    hipLaunchKernelGGL(distill_mean_kernel, dim3(1), dim3(1024), 0, st, (const float *)nullptr, mass, p.rows, heat, (float *)nullptr, inv);
+    hip_check(hipGetLastError(), "linear_distill count launch");
+    vocab_gradients(st, p, x, w, dx, dw, accumulate, ws, inv,
+        [&](const GemmShape &g, unsigned short *d, int64_t ld, int v0, int piece) {
+            gemm_bf16<false, false>(st, g, DistillGradEpilogue{mass, lse, d, ld, p.rows, piece, 1.f / heat}, "linear_distill gradient launch");
+            const int64_t n = rows * top;
+            hipLaunchKernelGGL(distill_entries_kernel, dim3((unsigned)cut(n, 256)), dim3(256), 0, st, index, delta, n, top, v0, piece, d, ld);
+            hip_check(hipGetLastError(), "linear_distill entries launch");
+        },
+        [&](float *d, int v0, int piece) {
+            hipLaunchKernelGGL(distill_piece_grad_kernel, dim3(p.rows, (unsigned)cut(piece, 256)), dim3(256), 0, st, d, piece, v0, mass, lse, index, delta, top,
+                               inv, 1.f / heat);
+            hip_check(hipGetLastError(), "linear_distill gradient launch");
+        });
 }
 
 }  // namespace monet

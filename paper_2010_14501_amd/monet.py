@@ -142,16 +142,28 @@ def load_library():
     lib.monet_linear_ce_fwd.argtypes = [vp, i32] + [vp] * 5 + [i64, i32, i32, vp, sz]
     lib.monet_linear_ce_bwd.argtypes = [vp, i32] + [vp] * 6 + [i64, i32, i32, i32, vp, sz]
     lib.monet_linear_ce_workspace_bytes.argtypes = [i32, i32, i64, i32, i32]
+    d = C.c_double
+    lib.monet_linear_distill_fwd.argtypes = [vp, i32] + [vp] * 9 + [i64, i32, i32, i32, f, vp, sz]
+    lib.monet_linear_distill_bwd.argtypes = [vp, i32] + [vp] * 8 + [i64, i32, i32, i32, f, i32, vp, sz]
+    lib.monet_linear_distill_workspace_bytes.argtypes = [i32, i32, i64, i32, i32, i32]
+    lib.monet_layernorm_fwd.argtypes = [vp, i32, i32] + [vp] * 5 + [i64, i32, i64, i64, f]
+    lib.monet_layernorm_bwd.argtypes = [vp, i32, i32] + [vp] * 7 + [i64, i32, i64, i64, i64, i32, vp, sz]
+    lib.monet_layernorm_bwd_workspace_bytes.argtypes = [i32, i64, i32]
+    lib.monet_rope_freqs.argtypes = [vp, i32, d, d, d, d, d]
+    lib.monet_rope_fwd.argtypes = [vp, i32] + [vp] * 4 + [i64, i32, i32, i32, i64, i64, i32, f]
+    lib.monet_rope_bwd.argtypes = [vp, i32] + [vp] * 4 + [i64, i32, i32, i32, i64, i64, i32, f, i32]
     lib.monet_act8_bytes.argtypes = [i64, i64]
     lib.monet_act8_pack.argtypes = [vp, i32, vp, i64, vp, i64, i64]
     lib.monet_act8_unpack.argtypes = [vp, i32, vp, vp, i64, i64, i64]
     lib.monet_act8_wgrad.argtypes = [vp, i32, vp, vp, vp, i64, i64, i64, vp, sz]
     lib.monet_act8_wgrad_workspace_bytes.argtypes = [i32, i64, i64, i64]
     for name in ("monet_attention_bwd_workspace_bytes", "monet_linear_ce_workspace_bytes", "monet_act8_bytes",
+                 "monet_linear_distill_workspace_bytes", "monet_layernorm_bwd_workspace_bytes",
                  "monet_act8_wgrad_workspace_bytes"):
         getattr(lib, name).restype = i64
     for name in ("monet_attention_fwd", "monet_attention_bwd", "monet_linear_ce_fwd", "monet_linear_ce_bwd", "monet_act8_pack",
-                 "monet_act8_unpack", "monet_act8_wgrad"):
+                 "monet_act8_unpack", "monet_act8_wgrad", "monet_linear_distill_fwd", "monet_linear_distill_bwd", "monet_layernorm_fwd",
+                 "monet_layernorm_bwd", "monet_rope_freqs", "monet_rope_fwd", "monet_rope_bwd"):
         getattr(lib, name).restype = i32
     for name in ("monet_conv_fwd", "monet_conv_dgrad", "monet_conv_wgrad", "monet_bn_stats", "monet_bn_stats_static", "monet_bn_apply", "monet_bn_bwd",
                  "monet_relu_fwd", "monet_relu_bwd", "monet_maxpool_fwd", "monet_maxpool_bwd", "monet_copy",
