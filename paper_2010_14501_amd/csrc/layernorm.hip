@@ -4,6 +4,7 @@
 //   dx = rstd (g - sum g / cols - xh sum(g xh) / cols),  dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy.
 // Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx.  All sums are fp32.
 #include <cmath>
+#include <type_traits>
 
 #include "../../include/monet_kernels.h"
 #include "kernels.hpp"
@@ -26,6 +27,286 @@ __device__ __forceinline__ float sum_of_256(float v, float *seg) {      // the s
     return (seg[0] + seg[1]) + (seg[2] + seg[3]);
 }
 
+// ---- rows that fit the registers: W waves to a row, a lane holds CH pieces of 16 bytes
+template <class T> constexpr int VEC = 16 / sizeof(T);
+template <class T, int W, int CH> constexpr int CAPACITY = W * 64 * VEC<T> * CH;
+
+// 16 bytes at any address of an element: rows of odd length begin anywhere, and one such load is what aligned ones cost
+typedef unsigned uintx4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned uintx4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ uintx4 load16(const float *p) { return *(const uintx4_at4 *)p; }
+__device__ __forceinline__ uintx4 load16(const unsigned short *p) { return *(const uintx4_at2 *)p; }
+__device__ __forceinline__ void store16(float *p, uintx4 v) { *(uintx4_at4 *)p = v; }
+__device__ __forceinline__ void store16(unsigned short *p, uintx4 v) { *(uintx4_at2 *)p = v; }
+__device__ __forceinline__ void unpack(uintx4 v, float (&f)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);
+}
+__device__ __forceinline__ void unpack(uintx4 v, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(v[i] << 16); f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ uintx4 pack(const float (&f)[4]) {
+    uintx4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(f[i]);
+    return v;
+}
+__device__ __forceinline__ uintx4 pack(const float (&f)[8]) {
+    uintx4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
+    return v;
+}
+// Where a lane's piece begins, and how many of its values belong to the piece before: in a row whose length is no multiple of a piece, the last
+// piece is moved back to the row's end (values that two lanes hold are added once, and stored twice alike).  A piece behind the end: nothing.
+template <class T, bool TAIL>
+struct Piece {
+    int c, skip;
+    bool has;
+    __device__ __forceinline__ Piece(int at, int cols) : c(at), skip(0), has(at < cols) {
+        if (TAIL && at + VEC<T> > cols) { c = cols - VEC<T>; skip = at - c; }
+    }
+    __device__ __forceinline__ uintx4 load(const T *row) const { return has ? load16(row + c) : uintx4{}; }
+    // v[e] where e counts, else 0
+    __device__ __forceinline__ float once(float v, int e) const { return !TAIL || e >= skip ? v : 0.f; }
+    __device__ __forceinline__ void store(T *row, const float (&f)[VEC<T>], bool add) const {
+        if (!has) return;
+        if (!add) { store16(row + c, pack(f)); return; }
+#pragma unroll
+        for (int e = 0; e < VEC<T>; ++e)
+            if (e >= skip) put(row + c + e, f[e], true);
+    }
+    __device__ __forceinline__ void params(const void *p, bool bf16, float missing, float (&f)[VEC<T>]) const {
+#pragma unroll
+        for (int e = 0; e < VEC<T>; ++e) f[e] = has ? missing : 0.f;
+        if (!p || !has) return;
+        if (bf16) {
+            typedef unsigned short half __attribute__((ext_vector_type(VEC<T>)));
+            half v;
+            __builtin_memcpy(&v, (const unsigned short *)p + c, sizeof v);
+#pragma unroll
+            for (int e = 0; e < VEC<T>; ++e) f[e] = bf16_float(v[e]);
+        } else
+            __builtin_memcpy(f, (const float *)p + c, sizeof f);
+    }
+};
+
+// the sum over a wave, in every lane: neighbours, fours, eights, 16 lanes, then the four rows of 16 through their last lanes
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_add(float v) {
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    v = dpp_add<0xb1, 0xf>(v);       // quad_perm 1 0 3 2
+    v = dpp_add<0x4e, 0xf>(v);       // quad_perm 2 3 0 1
+    v = dpp_add<0x141, 0xf>(v);      // row_half_mirror
+    v = dpp_add<0x140, 0xf>(v);      // row_mirror
+    v = dpp_add<0x142, 0xa>(v);      // row_bcast15
+    v = dpp_add<0x143, 0xc>(v);      // row_bcast31
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+// the sums of W waves; `at`: this group's and this sum's place in LDS, not used again before the next barrier but one
+template <int W>
+__device__ __forceinline__ float group_sum(float v, float *at, int wave) {
+    v = wave_sum(v);
+    if (W == 1) return v;
+    if ((threadIdx.x & 63) == 0) at[wave] = v;
+    __syncthreads();
+    v = at[0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) v += at[i];
+    return v;
+}
+
+template <int W> constexpr int FWD_THREADS = W <= 4 ? 256 : 64 * W;
+
+template <class T, int W, int CH, bool TAIL>
+__global__ __launch_bounds__(FWD_THREADS<W>) void layernorm_rows_kernel(const T *x, const void *__restrict__ gamma, const void *__restrict__ beta, bool params_bf16,
+                                                                        T *y, float2 *__restrict__ stats, int64_t rows, int cols, int64_t x_ld, int64_t y_ld,
+                                                                        float eps) {
+    constexpr int V = VEC<T>, GROUPS = FWD_THREADS<W> / 64 / W;
+    __shared__ float sums[2][GROUPS][W];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x & 63, group = wave / W, lot = wave % W;
+    const auto piece = [&](int k) { return Piece<T, TAIL>(((k * W + lot) * 64 + l) * V, cols); };
+    float g[CH][V], b[CH][V];
+    uintx4 raw[CH], next[CH];
+    const auto load = [&](int64_t row, uintx4 (&v)[CH]) {
+        const T *x_row = x + min(row, rows - 1) * x_ld;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) v[k] = piece(k).load(x_row);
+    };
+    load((int64_t)blockIdx.x * GROUPS + group, raw);
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        piece(k).params(gamma, params_bf16, 1.f, g[k]);
+        piece(k).params(beta, params_bf16, 0.f, b[k]);
+    }
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += step) {
+        const int64_t row = first + group;
+        if (first + step < rows) load(row + step, next);
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            float f[V];
+            unpack(raw[k], f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum += piece(k).once(f[e], e);
+        }
+        const float mean = group_sum<W>(sum, sums[0][group], lot) / cols;      // divided: the mean of equal values is that value
+        sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            float f[V];
+            unpack(raw[k], f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = piece(k).has ? piece(k).once(f[e] - mean, e) : 0.f;
+                sum = fmaf(d, d, sum);
+            }
+        }
+        const float rstd = 1.f / sqrtf(group_sum<W>(sum, sums[1][group], lot) / cols + eps);
+        if (row < rows) {
+            if (stats && lot == 0 && l == 0) stats[row] = make_float2(mean, rstd);
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                float f[V];
+                unpack(raw[k], f);
+#pragma unroll
+                for (int e = 0; e < V; ++e) f[e] = fmaf((f[e] - mean) * rstd, g[k][e], b[k][e]);
+                piece(k).store(y + row * y_ld, f, false);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < CH; ++k) raw[k] = next[k];
+    }
+}
+
+// dx, and this workgroup's rows' part of dgamma and dbeta: a lane's columns are the same in every row
+template <int W> constexpr int BWD_WAVES = W <= 8 ? 8 : W;
+template <class T, int W, int CH, bool TAIL>
+__global__ __launch_bounds__(64 * BWD_WAVES<W>) void layernorm_rows_bwd_kernel(const T *dy, const T *__restrict__ x, const void *__restrict__ gamma, bool params_bf16,
+                                                                            const float2 *__restrict__ stats, T *dx, float *__restrict__ part, int64_t rows,
+                                                                            int cols, int64_t dy_ld, int64_t x_ld, int64_t dx_ld, int add, void *dgamma, void *dbeta) {
+    constexpr int V = VEC<T>, GROUPS = BWD_WAVES<W> / W, N = CH * V, THREADS = 64 * BWD_WAVES<W>;
+    constexpr bool AHEAD = W <= 8;      // the next row's loads begin before this one is worked; 16 waves have registers for one row
+    __shared__ float sums[2][2][GROUPS][W];
+    __shared__ float joined[GROUPS > 1 ? THREADS * N : 1];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x & 63, group = wave / W, lot = wave % W;
+    const float by = 1.f / cols;
+    const auto piece = [&](int k) { return Piece<T, TAIL>(((k * W + lot) * 64 + l) * V, cols); };
+    float g[N], a[N] = {}, b[N] = {};
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        float f[V];
+        piece(k).params(gamma, params_bf16, 1.f, f);
+#pragma unroll
+        for (int e = 0; e < V; ++e) g[k * V + e] = f[e];
+    }
+    uintx4 rd[CH], rx[CH], nd[CH], nx[CH];
+    float2 st, nst;
+    const auto load = [&](int64_t row, uintx4 (&d)[CH], uintx4 (&v)[CH], float2 &s) {
+        if (row >= rows) {      // adds nothing: zeros of a row whose mean is 0
+#pragma unroll
+            for (int k = 0; k < CH; ++k) d[k] = v[k] = uintx4{};
+            s = make_float2(0.f, 0.f);
+            return;
+        }
+        s = stats[row];
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            d[k] = piece(k).load(dy + row * dy_ld);
+            v[k] = piece(k).load(x + row * x_ld);
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    load((int64_t)blockIdx.x * GROUPS + group, rd, rx, st);
+    int turn = 0;
+    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += step, turn ^= 1) {
+        const int64_t row = first + group;
+        if (AHEAD) load(row + step, nd, nx, nst);
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            float d[V], v[V];
+            unpack(rd[k], d);
+            unpack(rx[k], v);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const int i = k * V + e;
+                const float xh = (v[e] - st.x) * st.y, o = piece(k).once(d[e], e), t = o * g[i];
+                s1 += t;
+                s2 = fmaf(t, xh, s2);
+                a[i] = fmaf(o, xh, a[i]);
+                b[i] += o;
+            }
+        }
+        s1 = wave_sum(s1);
+        s2 = wave_sum(s2);
+        if (W > 1) {      // two places in turn: who still reads the other one has not passed this barrier
+            if (l == 0) { sums[turn][0][group][lot] = s1; sums[turn][1][group][lot] = s2; }
+            __syncthreads();
+            s1 = sums[turn][0][group][0];
+            s2 = sums[turn][1][group][0];
+#pragma unroll
+            for (int i = 1; i < W; ++i) { s1 += sums[turn][0][group][i]; s2 += sums[turn][1][group][i]; }
+        }
+        s1 *= by;
+        s2 *= by;
+        if (dx && row < rows) {
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                float d[V], v[V];
+                unpack(rd[k], d);
+                unpack(rx[k], v);
+#pragma unroll
+                for (int e = 0; e < V; ++e) d[e] = st.y * (d[e] * g[k * V + e] - s1 - (v[e] - st.x) * st.y * s2);
+                piece(k).store(dx + row * dx_ld, d, add & 1);
+            }
+        }
+        if (AHEAD) {
+#pragma unroll
+            for (int k = 0; k < CH; ++k) { rd[k] = nd[k]; rx[k] = nx[k]; }
+            st = nst;
+        } else
+            load(row + step, rd, rx, st);
+    }
+    if (!dgamma && !dbeta) return;
+    // the groups' sums, in their order; the only workgroup has the results, no part of them
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float(&s)[N] = which ? b : a;
+        if (GROUPS > 1) {
+            if (which) __syncthreads();
+#pragma unroll
+            for (int i = 0; i < N; ++i) joined[i * THREADS + threadIdx.x] = s[i];
+            __syncthreads();
+            if (group == 0) {
+#pragma unroll
+                for (int o = 1; o < GROUPS; ++o)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) s[i] += joined[i * THREADS + o * W * 64 + threadIdx.x];
+            }
+        }
+        void *out = which ? dbeta : dgamma;
+        if (group || !out) continue;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const Piece<T, TAIL> at = piece(k);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if (!at.has || e < at.skip) continue;
+                const int c = at.c + e;
+                if (gridDim.x > 1) part[((int64_t)blockIdx.x * 2 + which) * cols + c] = s[k * V + e];
+                else if (params_bf16) put((unsigned short *)out + c, s[k * V + e], add >> (1 + which) & 1);
+                else put((float *)out + c, s[k * V + e], add >> (1 + which) & 1);
+            }
+        }
+    }
+}
+
+// ---- longer rows
 // a workgroup to a row, which is read once for each of its sums and once more for the result
 template <class T, class P>
 __global__ __launch_bounds__(256) void layernorm_fwd_kernel(const T *x, const P *__restrict__ gamma, const P *__restrict__ beta, T *y,
@@ -92,27 +373,69 @@ __global__ __launch_bounds__(256) void layernorm_columns_kernel(const T *__restr
     part[((int64_t)blockIdx.y * 2 + wave) * cols + c] = (sums[wave][0][l] + sums[wave][1][l]) + (sums[wave][2][l] + sums[wave][3][l]);
 }
 
-// the parts' sums: grid y 0 dgamma, 1 dbeta (null: not wanted); four waves take a share of the ranges each, in a fixed order
+// the parts' sums: grid y 0 dgamma, 1 dbeta (null: not wanted); sixteen waves take a share of the ranges each, in a fixed order
 template <class P>
-__global__ __launch_bounds__(256) void layernorm_join_kernel(const float *__restrict__ part, int ranges, int cols, P *dgamma, P *dbeta, int add) {
-    __shared__ float sums[4][64];
+__global__ __launch_bounds__(1024) void layernorm_join_kernel(const float *__restrict__ part, int ranges, int cols, P *dgamma, P *dbeta, int add) {
+    __shared__ float sums[16][64];
     const int l = threadIdx.x & 63, wave = threadIdx.x / 64, c = blockIdx.x * 64 + l, which = blockIdx.y;
     P *out = which ? dbeta : dgamma;
     if (!out) return;
     float s = 0.f;
-    if (c < cols)
-        for (int r = wave; r < ranges; r += 4) s += part[((int64_t)r * 2 + which) * cols + c];
+    if (c < cols) {
+#pragma unroll 8
+        for (int r = wave; r < ranges; r += 16) s += part[((int64_t)r * 2 + which) * cols + c];
+    }
     sums[wave][l] = s;
     __syncthreads();
     if (wave || c >= cols) return;
-    put(out + c, (sums[0][l] + sums[1][l]) + (sums[2][l] + sums[3][l]), add >> which & 1);
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += sums[w][l];
+    put(out + c, s, add >> which & 1);
 }
 
 int64_t cut(int64_t n, int64_t by) { return (n + by - 1) / by; }
 
 constexpr int LAYERNORM_COLS = 1 << 20;
 
-int64_t layernorm_ranges(int64_t rows, int cols) {
+// Calls f(waves to a row, pieces of 16 bytes to a lane of it) with the smallest form that a row fits.  BACK: the backward pass.  false: the row does not
+// fit, or no piece of it does.
+template <class T, bool BACK, class F>
+bool layernorm_form(int cols, F &&f) {
+    constexpr int M = BACK ? 4 : 16 / VEC<T>;       // pieces to a lane of one wave or more
+    if (cols < VEC<T>) return false;
+    const auto fits = [&](auto w, auto ch) {
+        if (cols > CAPACITY<T, decltype(w)::value, decltype(ch)::value>) return false;
+        f(w, ch);
+        return true;
+    };
+    using std::integral_constant;
+    const integral_constant<int, M> m;
+    if (fits(integral_constant<int, 1>(), integral_constant<int, 1>()) || fits(integral_constant<int, 1>(), integral_constant<int, 2>()) ||
+        fits(integral_constant<int, 1>(), m) || fits(integral_constant<int, 2>(), m) || fits(integral_constant<int, 4>(), m) ||
+        fits(integral_constant<int, 8>(), m))
+        return true;
+    if constexpr (!BACK) return fits(integral_constant<int, 16>(), m);
+    else if constexpr (std::is_same<T, float>::value) return fits(integral_constant<int, 16>(), m);
+    else return false;
+}
+template <class F>
+void by_tail(bool tail, F &&f) {
+    if (tail) f(std::true_type());
+    else f(std::false_type());
+}
+// Parts of dgamma and dbeta: the workgroups that share the rows of a backward pass (as many as are on the card at once), or, of rows that do not fit
+// the registers, ranges of rows
+int64_t layernorm_ranges(int dtype, int64_t rows, int cols) {
+    int64_t rows_at_once = 0, groups = 0;
+    const auto form = [&](auto w, auto ch) {
+        constexpr int W = decltype(w)::value, CH = decltype(ch)::value;
+        rows_at_once = BWD_WAVES<W> / W;
+        groups = W <= 8 && CH * (dtype == MONET_F32 ? 4 : 8) <= 16 ? 512 : 256;
+    };
+    dtype == MONET_F32 ? layernorm_form<float, true>(cols, form) : layernorm_form<unsigned short, true>(cols, form);
+    // few values: one workgroup, which needs no second launch (37 rows of 203 in fp32, both passes: 24 us, with a join 27.5)
+    if (rows && rows_at_once && rows * cols <= 1 << 14 && rows <= 8 * rows_at_once) return 1;
+    if (rows_at_once) return std::min(groups, cut(rows, rows_at_once));
     return std::min<int64_t>(cut(rows, 32), std::max<int64_t>(1, 1024 / cut(cols, 64)));
 }
 void layernorm_shape(int dtype, int64_t rows, int cols) {
@@ -158,6 +481,14 @@ void layernorm_fwd(hipStream_t st, int dtype, int param_dtype, const void *x, co
     by_types(dtype, param_dtype, [&](auto t, auto p) {
         using T = decltype(t);
         using P = decltype(p);
+        const bool rows_fit = layernorm_form<T, false>(cols, [&](auto w, auto ch) {
+            constexpr int W = decltype(w)::value, CH = decltype(ch)::value, GROUPS = FWD_THREADS<W> / 64 / W;
+            by_tail(cols % VEC<T>, [&](auto tail) {
+                hipLaunchKernelGGL((layernorm_rows_kernel<T, W, CH, decltype(tail)::value>), dim3((unsigned)std::min<int64_t>(cut(rows, GROUPS), 256 * 1024 / FWD_THREADS<W>)),
+                                   dim3(FWD_THREADS<W>), 0, st, (const T *)x, gamma, beta, param_dtype == MONET_BF16, (T *)y, (float2 *)stats, rows, cols, x_ld, y_ld, eps);
+            });
+        });
+        if (rows_fit) return;
         hipLaunchKernelGGL((layernorm_fwd_kernel<T, P>), dim3((unsigned)rows), dim3(256), 0, st, (const T *)x, (const P *)gamma, (const P *)beta, (T *)y,
                            (float2 *)stats, cols, x_ld, y_ld, eps);
     });
@@ -166,7 +497,7 @@ void layernorm_fwd(hipStream_t st, int dtype, int param_dtype, const void *x, co
 
 size_t layernorm_bwd_workspace_bytes(int dtype, int64_t rows, int cols) {
     layernorm_shape(dtype, rows, cols);
-    return (size_t)(layernorm_ranges(rows, cols) * 2 * cols * 4);
+    return (size_t)(layernorm_ranges(dtype, rows, cols) * 2 * cols * 4);
 }
 
 void layernorm_bwd(hipStream_t st, int dtype, int param_dtype, const void *dy, const void *x, const void *gamma, const float *stats, void *dx, void *dgamma,
@@ -189,21 +520,40 @@ void layernorm_bwd(hipStream_t st, int dtype, int param_dtype, const void *dy, c
         if (!ws || ws_bytes < need) throw KernelError("layernorm: workspace of " + std::to_string(ws_bytes) + " bytes, " + std::to_string(need) + " needed");
         if ((uintptr_t)ws % 256) throw KernelError("layernorm: the workspace must be 256-byte aligned");
     }
-    const int64_t ranges = layernorm_ranges(rows, cols);
+    const int64_t ranges = layernorm_ranges(dtype, rows, cols);
     by_types(dtype, param_dtype, [&](auto t, auto p) {
         using T = decltype(t);
         using P = decltype(p);
-        if (columns) {
-            if (rows) {
-                hipLaunchKernelGGL(layernorm_columns_kernel<T>, dim3((unsigned)cut(cols, 64), (unsigned)ranges), dim3(256), 0, st, (const T *)dy, (const T *)x,
-                                   (const float2 *)stats, (float *)ws, rows, cut(rows, ranges), cols, dy_ld, x_ld);
-                hip_check(hipGetLastError(), "layernorm columns launch");
-            }
-            hipLaunchKernelGGL(layernorm_join_kernel<P>, dim3((unsigned)cut(cols, 64), 2), dim3(256), 0, st, (const float *)ws, (int)ranges, cols, (P *)dgamma,
+        const auto join = [&] {
+            hipLaunchKernelGGL(layernorm_join_kernel<P>, dim3((unsigned)cut(cols, 64), 2), dim3(1024), 0, st, (const float *)ws, (int)ranges, cols, (P *)dgamma,
                                (P *)dbeta, accumulate >> 1);
             hip_check(hipGetLastError(), "layernorm join launch");
+        };
+        if (!rows) {
+            if (columns) join();
+            return;
         }
-        if (dx && rows) {
+        if (!dx && !columns) return;
+        const bool rows_fit = layernorm_form<T, true>(cols, [&](auto w, auto ch) {
+            constexpr int W = decltype(w)::value, CH = decltype(ch)::value;
+            by_tail(cols % VEC<T>, [&](auto tail) {
+                hipLaunchKernelGGL((layernorm_rows_bwd_kernel<T, W, CH, decltype(tail)::value>), dim3((unsigned)ranges), dim3(64 * BWD_WAVES<W>), 0, st, (const T *)dy,
+                                   (const T *)x, gamma, param_dtype == MONET_BF16, (const float2 *)stats, (T *)dx, (float *)ws, rows, cols, dy_ld, x_ld,
+                                   dx_ld, accumulate, dgamma, dbeta);
+            });
+            hip_check(hipGetLastError(), "layernorm gradients launch");
+        });
+        if (rows_fit) {
+            if (columns && ranges > 1) join();
+            return;
+        }
+        if (columns) {
+            hipLaunchKernelGGL(layernorm_columns_kernel<T>, dim3((unsigned)cut(cols, 64), (unsigned)ranges), dim3(256), 0, st, (const T *)dy, (const T *)x,
+                               (const float2 *)stats, (float *)ws, rows, cut(rows, ranges), cols, dy_ld, x_ld);
+            hip_check(hipGetLastError(), "layernorm columns launch");
+            join();
+        }
+        if (dx) {
             hipLaunchKernelGGL((layernorm_dx_kernel<T, P>), dim3((unsigned)rows), dim3(256), 0, st, (const T *)dy, (const T *)x, (const P *)gamma,
                                (const float2 *)stats, (T *)dx, cols, dy_ld, x_ld, dx_ld, accumulate & 1);
             hip_check(hipGetLastError(), "layernorm gradient launch");
