@@ -310,45 +310,46 @@ __global__ __launch_bounds__(64 * BWD_WAVES<W>) void layernorm_rows_bwd_kernel(c
 // a workgroup to a row, which is read once for each of its sums and once more for the result
 template <class T, class P>
 __global__ __launch_bounds__(256) void layernorm_fwd_kernel(const T *x, const P *__restrict__ gamma, const P *__restrict__ beta, T *y,
-                                                            float2 *__restrict__ stats, int cols, int64_t x_ld, int64_t y_ld, float eps) {
+                                                            float2 *__restrict__ stats, int64_t rows, int cols, int64_t x_ld, int64_t y_ld, float eps) {
     __shared__ float seg[4];
-    const int64_t row = blockIdx.x;
-    x += row * x_ld;
-    y += row * y_ld;
-    float sum = 0.f;
-    for (int c = threadIdx.x; c < cols; c += 256) sum += value(x[c]);
-    const float mean = sum_of_256(sum, seg) / cols;
-    sum = 0.f;
-    for (int c = threadIdx.x; c < cols; c += 256) {
-        const float d = value(x[c]) - mean;
-        sum = fmaf(d, d, sum);
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const T *from = x + row * x_ld;
+        T *to = y + row * y_ld;
+        float sum = 0.f;
+        for (int c = threadIdx.x; c < cols; c += 256) sum += value(from[c]);
+        const float mean = sum_of_256(sum, seg) / cols;
+        sum = 0.f;
+        for (int c = threadIdx.x; c < cols; c += 256) {
+            const float d = value(from[c]) - mean;
+            sum = fmaf(d, d, sum);
+        }
+        const float rstd = 1.f / sqrtf(sum_of_256(sum, seg) / cols + eps);
+        for (int c = threadIdx.x; c < cols; c += 256)
+            put(to + c, fmaf((value(from[c]) - mean) * rstd, gamma ? value(gamma[c]) : 1.f, beta ? value(beta[c]) : 0.f), false);
+        if (stats && threadIdx.x == 0) stats[row] = make_float2(mean, rstd);
     }
-    const float rstd = 1.f / sqrtf(sum_of_256(sum, seg) / cols + eps);
-    for (int c = threadIdx.x; c < cols; c += 256)
-        put(y + c, fmaf((value(x[c]) - mean) * rstd, gamma ? value(gamma[c]) : 1.f, beta ? value(beta[c]) : 0.f), false);
-    if (stats && threadIdx.x == 0) stats[row] = make_float2(mean, rstd);
 }
 
 template <class T, class P>
 __global__ __launch_bounds__(256) void layernorm_dx_kernel(const T *dy, const T *__restrict__ x, const P *__restrict__ gamma, const float2 *__restrict__ stats,
-                                                           T *dx, int cols, int64_t dy_ld, int64_t x_ld, int64_t dx_ld, bool add) {
+                                                           T *dx, int64_t rows, int cols, int64_t dy_ld, int64_t x_ld, int64_t dx_ld, bool add) {
     __shared__ float seg[4];
-    const int64_t row = blockIdx.x;
-    dy += row * dy_ld;
-    x += row * x_ld;
-    dx += row * dx_ld;
-    const float mean = stats[row].x, rstd = stats[row].y;
-    float a = 0.f, b = 0.f;
-    for (int c = threadIdx.x; c < cols; c += 256) {
-        const float g = value(dy[c]) * (gamma ? value(gamma[c]) : 1.f);
-        a += g;
-        b = fmaf(g, (value(x[c]) - mean) * rstd, b);
-    }
-    a = sum_of_256(a, seg) / cols;
-    b = sum_of_256(b, seg) / cols;
-    for (int c = threadIdx.x; c < cols; c += 256) {
-        const float g = value(dy[c]) * (gamma ? value(gamma[c]) : 1.f);
-        put(dx + c, rstd * (g - a - (value(x[c]) - mean) * rstd * b), add);
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const T *go = dy + row * dy_ld, *from = x + row * x_ld;
+        T *to = dx + row * dx_ld;
+        const float mean = stats[row].x, rstd = stats[row].y;
+        float a = 0.f, b = 0.f;
+        for (int c = threadIdx.x; c < cols; c += 256) {
+            const float g = value(go[c]) * (gamma ? value(gamma[c]) : 1.f);
+            a += g;
+            b = fmaf(g, (value(from[c]) - mean) * rstd, b);
+        }
+        a = sum_of_256(a, seg) / cols;
+        b = sum_of_256(b, seg) / cols;
+        for (int c = threadIdx.x; c < cols; c += 256) {
+            const float g = value(go[c]) * (gamma ? value(gamma[c]) : 1.f);
+            put(to + c, rstd * (g - a - (value(from[c]) - mean) * rstd * b), add);
+        }
     }
 }
 
@@ -489,8 +490,8 @@ void layernorm_fwd(hipStream_t st, int dtype, int param_dtype, const void *x, co
             });
         });
         if (rows_fit) return;
-        hipLaunchKernelGGL((layernorm_fwd_kernel<T, P>), dim3((unsigned)rows), dim3(256), 0, st, (const T *)x, (const P *)gamma, (const P *)beta, (T *)y,
-                           (float2 *)stats, cols, x_ld, y_ld, eps);
+        hipLaunchKernelGGL((layernorm_fwd_kernel<T, P>), dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), dim3(256), 0, st, (const T *)x, (const P *)gamma, (const P *)beta, (T *)y,
+                           (float2 *)stats, rows, cols, x_ld, y_ld, eps);
     });
     hip_check(hipGetLastError(), "layernorm launch");
 }
@@ -554,8 +555,8 @@ void layernorm_bwd(hipStream_t st, int dtype, int param_dtype, const void *dy, c
             join();
         }
         if (dx) {
-            hipLaunchKernelGGL((layernorm_dx_kernel<T, P>), dim3((unsigned)rows), dim3(256), 0, st, (const T *)dy, (const T *)x, (const P *)gamma,
-                               (const float2 *)stats, (T *)dx, cols, dy_ld, x_ld, dx_ld, accumulate & 1);
+            hipLaunchKernelGGL((layernorm_dx_kernel<T, P>), dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), dim3(256), 0, st, (const T *)dy, (const T *)x, (const P *)gamma,
+                               (const float2 *)stats, (T *)dx, rows, cols, dy_ld, x_ld, dx_ld, accumulate & 1);
             hip_check(hipGetLastError(), "layernorm gradient launch");
         }
     });
