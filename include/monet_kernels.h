@@ -333,7 +333,8 @@ int64_t monet_layernorm_bwd_workspace_bytes(int dtype, int64_t rows, int cols);
  *   (a, b) -> scale * (a cos - b sin, b cos + a sin),  angle = positions[token] * freqs[i];  the others stay as they are.
  * positions: device, one per token, of any value (NULL: the token's index).  freqs: host memory, rot_dim / 2 values in radians a position, read before the
  * call returns.  Angles are reduced in 64 bits.  y may be x (same stride); otherwise they do not overlap.  rot_dim even, 2 to 512 and at most head_dim;
- * any alignment of an element; tokens below 2^24, heads * head_dim below 2^26, strides below 2^31; tokens == 0 is allowed and does nothing. */
+ * any alignment of an element; tokens and heads * head_dim below 2^24, head_dim at most 2^15, strides below
+ * 2^31; tokens == 0 is allowed and does nothing. */
 int monet_rope_fwd(void *stream, int dtype, const void *x, void *y, const int32_t *positions, const double *freqs, int64_t tokens, int heads, int head_dim,
                    int rot_dim, int64_t x_ld, int64_t y_ld, int interleaved, float scale);
 /* The gradient: dx (may be dy, with the same stride, if nothing is added to) is dy turned back, times scale; accumulate != 0 adds to it. */

@@ -33,90 +33,67 @@ __device__ __forceinline__ void turn(double turns, float &c, float &s) {
     if (n & 2) s = -s;
 }
 
-// A unit of a head: V pairs, two runs of V values (interleaved: one of 2 V), or V values that stay.  A workgroup takes `per_token` units of each of
-// `at_once` tokens, up to ROPE_UNITS to a thread: all of them are loaded before the angles of its tokens are computed, each once for all heads.
-constexpr int ROPE_UNITS = 4;
+// A unit of a head: V pairs, two runs of V values that lie `half` (interleaved: V) apart, or up to two neighbouring runs that stay.  A workgroup has
+// `at_once` tokens; a thread keeps its unit and its token, with their cosines and sines in registers, and takes every `lanes`-th head, the next
+// one's values loaded before this one's are turned.  The angles are computed together, each once for all heads.  Heads and units from two divisions a
+// unit instead of a thread, and the angles read from LDS for every unit: 165 us where this takes 124.
 template <class T, int V, bool INTERLEAVED>
-__global__ __launch_bounds__(256) void rope_kernel(const T *x, T *y, const int32_t *__restrict__ positions, const RopeFreqs f, int64_t tokens, unsigned at_once,
-                                                   unsigned units, unsigned per_token, unsigned per_head, unsigned dim, unsigned half, int64_t x_ld, int64_t y_ld,
-                                                   float scale, int inverse, int add) {
+__global__ __launch_bounds__(256) void rope_kernel(const T *x, T *y, const int32_t *__restrict__ positions, const RopeFreqs f, int64_t tokens, int at_once,
+                                                   int lanes, int units, int heads, int dim, int half, int64_t x_ld, int64_t y_ld, float scale, int inverse,
+                                                   int add) {
     extern __shared__ float2 table[];       // [token][pair]: cos, sin
     const int64_t t0 = (int64_t)blockIdx.x * at_once;
-    const unsigned here = (unsigned)min((int64_t)at_once, tokens - t0), first = blockIdx.y * per_token, count = min(per_token, units - first);
-    T va[ROPE_UNITS][V], vb[ROPE_UNITS][V];
-    const auto place = [&](unsigned i, unsigned &token, unsigned &u) {      // of unit i: the offset of its head
-        token = i / count;
-        const unsigned j = first + i - token * count, h = j / per_head;
-        u = j - h * per_head;
-        return (int64_t)h * dim;
+    const int here = (int)min((int64_t)at_once, tokens - t0), wide = min(256, units - (int)blockIdx.y * 256);
+    const unsigned slot = threadIdx.x / (unsigned)wide, token = slot / (unsigned)lanes;
+    const int u = blockIdx.y * 256 + threadIdx.x - slot * wide, lane = slot - token * lanes;
+    const bool mine = (int)token < here, turns = u * V < half;
+    const int at = turns && !INTERLEAVED ? V * u : 2 * V * u, other = turns && !INTERLEAVED ? half : V;
+    const bool both = turns || at + 2 * V <= dim;
+    const T *from = x + (t0 + token) * x_ld + at;
+    T *to = y + (t0 + token) * y_ld + at;
+    struct Run { T v[V]; };
+    Run a, b;
+    const auto load = [&](int h) {
+        __builtin_memcpy(&a, from + (int64_t)h * dim, sizeof a);
+        if (both) __builtin_memcpy(&b, from + (int64_t)h * dim + other, sizeof b);
     };
-#pragma unroll
-    for (int k = 0; k < ROPE_UNITS; ++k) {
-        const unsigned i = k * 256 + threadIdx.x;
-        if (i >= here * count) break;
-        unsigned token, u;
-        const int64_t head = place(i, token, u);
-        const T *p = x + (t0 + token) * x_ld + head;
-        if (u * V >= half) __builtin_memcpy(va[k], p + half + u * V, sizeof va[k]);
-        else if (INTERLEAVED) {
-            __builtin_memcpy(va[k], p + 2 * V * u, sizeof va[k]);
-            __builtin_memcpy(vb[k], p + 2 * V * u + V, sizeof vb[k]);
-        } else {
-            __builtin_memcpy(va[k], p + V * u, sizeof va[k]);
-            __builtin_memcpy(vb[k], p + half + V * u, sizeof vb[k]);
-        }
-    }
-    for (unsigned i = threadIdx.x; i < here * half; i += 256) {
-        const unsigned token = i / half, pair = i - token * half;
+    if (mine && lane < heads) load(lane);
+    for (unsigned i = threadIdx.x; i < (unsigned)(here * half); i += 256) {
+        const unsigned t = i / (unsigned)half, pair = i - t * half;
         float c, s;
-        turn((positions ? positions[t0 + token] : (int)(t0 + token)) * f.turns[pair], c, s);
+        turn((positions ? positions[t0 + t] : (int)(t0 + t)) * f.turns[pair], c, s);
         table[i] = make_float2(c * scale, s * (inverse ? -scale : scale));
     }
     __syncthreads();
+    if (!mine) return;
+    float2 cs[V];
 #pragma unroll
-    for (int k = 0; k < ROPE_UNITS; ++k) {
-        const unsigned i = k * 256 + threadIdx.x;
-        if (i >= here * count) break;
-        unsigned token, u;
-        const int64_t head = place(i, token, u);
-        T *p = y + (t0 + token) * y_ld + head;
-        const auto store = [&](T *at, const float (&f)[V]) {
-            T v[V];
-            if (add) __builtin_memcpy(v, at, sizeof v);
-#pragma unroll
-            for (int e = 0; e < V; ++e) put(v + e, f[e], add);
-            __builtin_memcpy(at, v, sizeof v);
-        };
-        if (u * V >= half) {
-            float stays[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) stays[e] = value(va[k][e]);
-            store(p + half + u * V, stays);
-            continue;
-        }
-        const float2 *cs = table + token * half + u * V;
-        float a[V], b[V];
+    for (int e = 0; e < V; ++e) cs[e] = turns ? table[token * half + u * V + e] : make_float2(1.f, 0.f);
+    for (int h = lane; h < heads; h += lanes) {
+        const Run oa = a, ob = b;
+        if (h + lanes < heads) load(h + lanes);
+        float m[V], n[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) {       // pair e: values 2 e and 2 e + 1 of the two runs, or e of each
-            const float m = value(INTERLEAVED ? (2 * e < V ? va[k][2 * e % V] : vb[k][2 * e % V]) : va[k][e]);
-            const float n = value(INTERLEAVED ? (2 * e + 1 < V ? va[k][(2 * e + 1) % V] : vb[k][(2 * e + 1) % V]) : vb[k][e]);
-            const float2 t = cs[e];
-            a[e] = m * t.x - n * t.y;
-            b[e] = n * t.x + m * t.y;
+            const float p = value(INTERLEAVED ? (2 * e < V ? oa.v[2 * e % V] : ob.v[2 * e % V]) : oa.v[e]);
+            const float q = value(INTERLEAVED ? (2 * e + 1 < V ? oa.v[(2 * e + 1) % V] : ob.v[(2 * e + 1) % V]) : ob.v[e]);
+            m[e] = p * cs[e].x - q * cs[e].y;
+            n[e] = p * cs[e].y + q * cs[e].x;
         }
-        if (INTERLEAVED) {
-            float low[V], high[V];
+        T *p = to + (int64_t)h * dim;
+        Run ra, rb;
+        if (add) {
+            __builtin_memcpy(&ra, p, sizeof ra);
+            if (both) __builtin_memcpy(&rb, p + other, sizeof rb);
+        }
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                low[e] = e % 2 ? b[e / 2] : a[e / 2];
-                high[e] = (e + V) % 2 ? b[(e + V) / 2] : a[(e + V) / 2];
-            }
-            store(p + 2 * V * u, low);
-            store(p + 2 * V * u + V, high);
-        } else {
-            store(p + V * u, a);
-            store(p + half + V * u, b);
+        for (int e = 0; e < V; ++e) {       // what stays is what it was, whatever lies beside it
+            const float lo = INTERLEAVED ? (e % 2 ? n[e / 2] : m[e / 2]) : m[e], hi = INTERLEAVED ? ((e + V) % 2 ? n[(e + V) / 2] : m[(e + V) / 2]) : n[e];
+            put(ra.v + e, turns ? lo : value(oa.v[e]), add);
+            put(rb.v + e, turns ? hi : value(ob.v[e]), add);
         }
+        __builtin_memcpy(p, &ra, sizeof ra);
+        if (both) __builtin_memcpy(p + other, &rb, sizeof rb);
     }
 }
 
@@ -144,7 +121,7 @@ void rope(hipStream_t st, int dtype, const void *x, void *y, const int32_t *posi
     if (rot_dim < 2 || rot_dim % 2 || rot_dim > ROPE_DIM || rot_dim > head_dim)
         throw KernelError("rope: rot_dim must be even, 2 to head_dim and at most " + std::to_string(ROPE_DIM));
     const int64_t width = (int64_t)heads * head_dim;
-    if (tokens >= 1 << 24 || width >= 1 << 26) throw KernelError("rope: shape too large");
+    if (tokens >= 1 << 24 || width >= 1 << 24 || head_dim > 1 << 15) throw KernelError("rope: shape too large");
     if (!std::isfinite(scale)) throw KernelError("rope: the scale must be finite");
     if (!freqs) throw KernelError("rope: null pointer");
     RopeFreqs f;
@@ -164,13 +141,13 @@ void rope(hipStream_t st, int dtype, const void *x, void *y, const int32_t *posi
         using T = decltype(t);
         constexpr int V = decltype(v)::value;
         if (half % V || rest % V) return false;
-        const unsigned per_head = (unsigned)((half + (x == y ? 0 : rest)) / V), units = per_head * (unsigned)heads, most = 256 * ROPE_UNITS;
-        const unsigned per_token = std::min(units, most);
-        // several tokens to a workgroup where there are enough of them to fill the card; 8 KB of angles at most
-        const unsigned at_once = (unsigned)std::max<int64_t>(1, std::min<int64_t>({most / per_token, tokens / 512, 1024 / half}));
-        const dim3 grid((unsigned)((tokens + at_once - 1) / at_once), (units + per_token - 1) / per_token);
+        const int units = half / V + (x == y ? 0 : (rest / V + 1) / 2), slots = 256 / std::min(units, 256);
+        // about two heads to a thread: 16384 tokens, 40 heads, both ways, 124 us in bf16 with 128 wide heads (5.4 TB/s; a plain copy reaches 5.6), 101 with 96
+        // wide ones of which 24 turn; three: 127 and 101; six: 134 and 113; fp32 of 96 wide ones, of which 24 turn: two 189, six 218
+        const int at_once = (int)std::max<int64_t>(1, std::min<int64_t>({slots, (int64_t)slots * 2 / heads, tokens / 512, 2048 / half}));
+        const dim3 grid((unsigned)((tokens + at_once - 1) / at_once), (units + 255) / 256);
         hipLaunchKernelGGL((rope_kernel<T, V, decltype(interleaved_)::value>), grid, dim3(256), at_once * half * sizeof(float2), st, (const T *)x, (T *)y, positions,
-                           f, tokens, at_once, units, per_token, per_head, (unsigned)head_dim, (unsigned)half, x_ld, y_ld, scale, inverse, accumulate);
+                           f, tokens, at_once, slots / at_once, units, heads, head_dim, half, x_ld, y_ld, scale, inverse, accumulate);
         return true;
     };
     using std::integral_constant;
