@@ -349,29 +349,41 @@ __global__ __launch_bounds__(256) void ce_piece_grad_kernel(float *__restrict__ 
 // Entry j of a row is vocabulary index i_j with the teacher's logit t_j; p_j = exp(t_j / T - its normaliser), 0 for an index outside the vocabulary.
 //   loss = sum_j p_j (log p_j + lse - z_j),   mass = sum_j p_j,   delta_j = mass exp(z_j - lse) - (sum of p at the same index)
 // with z_j = x . w[i_j] / T.  One workgroup to a row; z by a wave's sums over the columns, each in the same order, so that an index that comes
-// twice gets the same number twice.  Bound by reading rows * top rows of w.
+// twice gets the same number twice.  Bound by reading rows * top rows of w, most of them from the caches: 8192 rows, 64 entries, 4096 columns, bf16
+// (4.3 GB): 550 us, one entry at a time to a wave 640; 1000 rows, 64 entries, 1024 columns (131 MB): 24 us.
 constexpr int DISTILL_TOP = 1024;      // entries of a row, at most
-template <class T>
-__device__ __forceinline__ float distill_dot(const T *x, const T *w, int width, int l);
-template <>
-__device__ __forceinline__ float distill_dot<float>(const float *x, const float *w, int width, int l) {
-    float s = 0.f;
-    for (int c = l; c < width; c += 64) s = fmaf(x[c], w[c], s);
-    return s;
-}
-template <>
-__device__ __forceinline__ float distill_dot<unsigned short>(const unsigned short *x, const unsigned short *w, int width, int l) {
-    float s = 0.f;
-    for (int c = 8 * l; c < width; c += 512) {
-        const uint4 a = *(const uint4 *)(x + c), b = *(const uint4 *)(w + c);
-        const unsigned aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+// the lanes' shares of N dot products with one x: 16 bytes a lane and step, the rest of a row value by value
+template <int N>
+__device__ __forceinline__ void distill_dots(const float *x, const float *const (&w)[N], int width, int l, float (&s)[N]) {
+    typedef float any __attribute__((ext_vector_type(4), aligned(4)));
+    int c = 4 * l;
+    for (; c + 4 <= width; c += 256) {
+        const any f = *(const any *)(x + c);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            s = fmaf(__uint_as_float(aw[q] << 16), __uint_as_float(bw[q] << 16), s);
-            s = fmaf(__uint_as_float(aw[q] & 0xffff0000u), __uint_as_float(bw[q] & 0xffff0000u), s);
+        for (int j = 0; j < N; ++j) {
+            const any g = *(const any *)(w[j] + c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[j] = fmaf(f[e], g[e], s[j]);
         }
     }
-    return s;
+    for (int e = c; e < min(c + 4, width); ++e)
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[j] = fmaf(x[e], w[j][e], s[j]);
+}
+template <int N>
+__device__ __forceinline__ void distill_dots(const unsigned short *x, const unsigned short *const (&w)[N], int width, int l, float (&s)[N]) {
+    for (int c = 8 * l; c < width; c += 512) {
+        const uintx4 f = *(const uintx4 *)(x + c);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const uintx4 g = *(const uintx4 *)(w[j] + c);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                s[j] = fmaf(__uint_as_float(f[q] << 16), __uint_as_float(g[q] << 16), s[j]);
+                s[j] = fmaf(__uint_as_float(f[q] & 0xffff0000u), __uint_as_float(g[q] & 0xffff0000u), s[j]);
+            }
+        }
+    }
 }
 __device__ __forceinline__ float sum_of_256(float v, float *seg) {      // the same in every thread
     for (int w = 32; w; w /= 2) v += __shfl_xor(v, w);
@@ -390,22 +402,55 @@ __device__ __forceinline__ float max_of_256(float v, float *seg) {
 template <class T>
 __global__ __launch_bounds__(256) void distill_rows_kernel(const T *__restrict__ x, const T *__restrict__ w, const int32_t *__restrict__ index,
                                                            const float *__restrict__ target, const float *__restrict__ target_lse,
-                                                           const float *__restrict__ lse, float *__restrict__ mass, float *__restrict__ delta,
-                                                           float *__restrict__ row_loss, int width, int vocab, int top, float heat) {
+                                                           const float2 *__restrict__ part, int parts, int rows, float *__restrict__ lse,
+                                                           float *__restrict__ mass, float *__restrict__ delta, float *__restrict__ row_loss, int width,
+                                                           int vocab, int top, float heat) {
     __shared__ float z[DISTILL_TOP], p[DISTILL_TOP], seg[4];
     __shared__ int at[DISTILL_TOP];
+    __shared__ Soft joined[4];
     const int64_t t = blockIdx.x;
     const int wave = threadIdx.x / 64, l = threadIdx.x & 63;
     index += t * top;
     target += t * top;
     for (int j = threadIdx.x; j < top; j += 256) at[j] = (unsigned)index[j] < (unsigned)vocab ? index[j] : -1;
     __syncthreads();
-    for (int j = wave; j < top; j += 4) {
-        const int v = __builtin_amdgcn_readfirstlane(at[j]);
-        float s = v < 0 ? 0.f : distill_dot(x + t * width, w + (int64_t)v * width, width, l);
-        for (int k = 32; k; k /= 2) s += __shfl_xor(s, k);
-        if (l == 0) z[j] = s / heat;
+    // the row's lse from its parts, unless it is there already
+    float ls = 0.f;
+    if (part) {
+        Soft a{-INFINITY, 0.f};
+        for (int b = threadIdx.x; b < parts; b += 256) {
+            const float2 v = part[(int64_t)b * rows + t];
+            a = soft_join(a, Soft{v.x, v.y});
+        }
+        for (int k = 32; k; k /= 2) a = soft_join(a, Soft{__shfl_xor(a.m, k), __shfl_xor(a.s, k)});
+        if (l == 0) joined[wave] = a;
     }
+    const auto dots = [&](int j0, auto n) {      // entries j0 .. j0 + N - 1; one that is none repeats the first that is
+        constexpr int N = decltype(n)::value;
+        const T *row[N];
+        int some = -1;
+#pragma unroll
+        for (int j = N - 1; j >= 0; --j) {
+            const int v = __builtin_amdgcn_readfirstlane(j0 + j < top ? at[j0 + j] : -1);
+            if (v >= 0) some = v;
+            row[j] = w + (int64_t)v * width;
+        }
+        if (some < 0) return;
+        float s[N] = {};
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (row[j] < w) row[j] = w + (int64_t)some * width;
+        distill_dots(x + t * width, row, width, l, s);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            for (int k = 32; k; k /= 2) s[j] += __shfl_xor(s[j], k);
+            if (l == 0 && j0 + j < top) z[j0 + j] = s[j] / heat;
+        }
+    };
+    if (top >= 16)
+        for (int j = 4 * wave; j < top; j += 16) dots(j, std::integral_constant<int, 4>());
+    else
+        for (int j = wave; j < top; j += 4) dots(j, std::integral_constant<int, 1>());
     float most = -INFINITY;
     for (int j = threadIdx.x; j < top; j += 256)
         if (at[j] >= 0) most = fmaxf(most, target[j] / heat);
@@ -419,7 +464,12 @@ __global__ __launch_bounds__(256) void distill_rows_kernel(const T *__restrict__
         norm = most + logf(sum_of_256(sum, seg));
     }
     __syncthreads();
-    const float ls = lse[t];
+    if (part) {
+        const Soft a = soft_join(soft_join(joined[0], joined[1]), soft_join(joined[2], joined[3]));
+        ls = a.m + logf(a.s);
+        if (threadIdx.x == 0) lse[t] = ls;
+    } else
+        ls = lse[t];
     float loss = 0.f, m = 0.f;
     for (int j = threadIdx.x; j < top; j += 256) {
         // an entry of weight 0 adds nothing, whatever the row's logits are
@@ -443,24 +493,34 @@ __global__ __launch_bounds__(256) void distill_rows_kernel(const T *__restrict__
     mass[t] = m;
     row_loss[t] = loss;
 }
-// T^2 times the mean of the losses of the rows with weight, and inv = T / their number (0 for none); sums in a fixed order
-__global__ __launch_bounds__(1024) void distill_mean_kernel(const float *__restrict__ row_loss, const float *__restrict__ mass, int rows, float heat,
-                                                            float *__restrict__ loss, float *__restrict__ inv) {
-    __shared__ double sums[1024];
-    __shared__ int counts[1024];
-    double sum = 0;
+// the rows with weight, and the sum of their losses (row_loss may be null), in the first thread of a workgroup of 64 * WAVES; in a fixed order
+template <int WAVES>
+__device__ __forceinline__ int distill_count(const float *row_loss, const float *mass, int rows, double &sum) {
+    __shared__ double sums[WAVES];
+    __shared__ int counts[WAVES];
     int count = 0;
-    for (int t = threadIdx.x; t < rows; t += 1024)
+    sum = 0;
+    for (int t = threadIdx.x; t < rows; t += 64 * WAVES)
         if (mass[t] != 0.f) { ++count; if (row_loss) sum += row_loss[t]; }
-    sums[threadIdx.x] = sum;
-    counts[threadIdx.x] = count;
-    for (int w = 512; w; w /= 2) {
-        __syncthreads();
-        if ((int)threadIdx.x < w) { sums[threadIdx.x] += sums[threadIdx.x + w]; counts[threadIdx.x] += counts[threadIdx.x + w]; }
-    }
-    if (threadIdx.x) return;
-    if (loss) *loss = counts[0] ? (float)((double)heat * heat * sums[0] / counts[0]) : 0.f;
-    if (inv) *inv = counts[0] ? heat / counts[0] : 0.f;
+    for (int k = 32; k; k /= 2) { sum += __shfl_xor(sum, k); count += __shfl_xor(count, k); }
+    if (threadIdx.x % 64 == 0) { sums[threadIdx.x / 64] = sum; counts[threadIdx.x / 64] = count; }
+    __syncthreads();
+    sum = 0;
+    count = 0;
+    for (int i = 0; i < WAVES; ++i) { sum += sums[i]; count += counts[i]; }
+    return count;
+}
+// T^2 times the mean of the losses of the rows with weight
+__global__ __launch_bounds__(1024) void distill_mean_kernel(const float *__restrict__ row_loss, const float *__restrict__ mass, int rows, float heat,
+                                                            float *__restrict__ loss) {
+    double sum;
+    const int count = distill_count<16>(row_loss, mass, rows, sum);
+    if (threadIdx.x == 0) *loss = count ? (float)((double)heat * heat * sum / count) : 0.f;
+}
+__global__ __launch_bounds__(1024) void distill_inv_kernel(const float *__restrict__ mass, int rows, float heat, float *__restrict__ inv) {
+    double sum;
+    const int count = distill_count<16>(nullptr, mass, rows, sum);
+    if (threadIdx.x == 0) *inv = count ? heat / count : 0.f;
 }
 // bf16: the teacher's entries of a piece, over what the product's epilogue wrote there.  An index that comes twice has the same delta twice.
 __global__ __launch_bounds__(256) void distill_entries_kernel(const int32_t *__restrict__ index, const float *__restrict__ delta, int64_t n, int top, int v0,
@@ -470,15 +530,25 @@ __global__ __launch_bounds__(256) void distill_entries_kernel(const int32_t *__r
     const int64_t v = (int64_t)index[i] - v0;
     if (v >= 0 && v < piece) dl[i / top * ld + v] = float_bf16(delta[i]);
 }
-// fp32: dl in the place of a row's 256 logits, then the teacher's entries among them
+// fp32: dl in the place of a row's 256 logits, then the teacher's entries among them.  COUNT: with up to 64 rows every workgroup counts those with
+// weight itself, a launch less (777 rows, 16000 entries: 52 us so, 26 without).
+template <bool COUNT>
 __global__ __launch_bounds__(256) void distill_piece_grad_kernel(float *__restrict__ logits, int piece, int v0, const float *__restrict__ mass,
                                                                  const float *__restrict__ lse, const int32_t *__restrict__ index,
-                                                                 const float *__restrict__ delta, int top, const float *__restrict__ inv, float by) {
+                                                                 const float *__restrict__ delta, int top, const float *__restrict__ inv, int rows, float heat) {
     const int64_t t = blockIdx.x;
     const int from = blockIdx.y * 256, to = min(piece, from + 256), v = from + threadIdx.x;
-    const float m = mass[t], f = *inv;
+    const float m = mass[t], by = 1.f / heat;
     float *row = logits + t * piece;
-    if (v < to) row[v] = m != 0.f ? m * exp_of(row[v] * by - lse[t]) * f : 0.f;
+    const float x = v < to ? row[v] : 0.f;
+    float f;
+    if (COUNT) {
+        double sum;
+        const int count = distill_count<4>(nullptr, mass, rows, sum);
+        f = count ? heat / count : 0.f;
+    } else
+        f = *inv;
+    if (v < to) row[v] = m != 0.f ? m * exp_of(x * by - lse[t]) * f : 0.f;
     __syncthreads();
     for (int j = threadIdx.x; j < top; j += 256) {
         const int64_t e = (int64_t)index[t * top + j] - v0;
@@ -903,19 +973,22 @@ void linear_distill_fwd(hipStream_t st, int dtype, const void *x, const void *w,
     float *row_loss = (float *)ws;
     float2 *part = (float2 *)(row_loss + 2 * up(rows, 64));
     vocab_stats<false>(st, p, x, w, nullptr, part, nullptr, 1.f / heat, ws);
-    if (rows <= 64 && rows * p.parts() <= 1 << 14)
-        hipLaunchKernelGGL((ce_merge_kernel<64, false>), dim3(1), dim3(1024), 0, st, part, (int)p.parts(), nullptr, nullptr, lse, nullptr, nullptr, p.rows, vocab);
-    else
-        hipLaunchKernelGGL((ce_merge_kernel<16, false>), dim3((unsigned)cut(rows, 16)), dim3(256), 0, st, part, (int)p.parts(), nullptr, nullptr, lse, nullptr, nullptr, p.rows, vocab);
-    hip_check(hipGetLastError(), "linear_distill merge launch");
-    if (p.bf16)
-        hipLaunchKernelGGL(distill_rows_kernel<unsigned short>, dim3(p.rows), dim3(256), 0, st, (const unsigned short *)x, (const unsigned short *)w, index, target,
-                           target_lse, lse, mass, delta, row_loss, width, vocab, top, heat);
-    else
-        hipLaunchKernelGGL(distill_rows_kernel<float>, dim3(p.rows), dim3(256), 0, st, (const float *)x, (const float *)w, index, target, target_lse, lse, mass,
-                           delta, row_loss, width, vocab, top, heat);
-    hip_check(hipGetLastError(), "linear_distill rows launch");
-    hipLaunchKernelGGL(distill_mean_kernel, dim3(1), dim3(1024), 0, st, row_loss, mass, p.rows, heat, loss, (float *)nullptr);
+    // a row's workgroup joins its parts itself, a launch less, where reading 8 bytes from each of as many lines costs little
+    const int parts = (int)p.parts();
+    const bool merged = rows * parts > 1 << 19;
+    if (merged) {
+        hipLaunchKernelGGL((ce_merge_kernel<16, false>), dim3((unsigned)cut(rows, 16)), dim3(256), 0, st, part, parts, nullptr, nullptr, lse, nullptr, nullptr, p.rows, vocab);
+        hip_check(hipGetLastError(), "linear_distill merge launch");
+    }
+    const auto rows_kernel = [&](auto t) {
+        using T = decltype(t);
+        hipLaunchKernelGGL(distill_rows_kernel<T>, dim3(p.rows), dim3(256), 0, st, (const T *)x, (const T *)w, index, target, target_lse,
+                           merged ? nullptr : part, parts, p.rows, lse, mass, delta, row_loss, width, vocab, top, heat);
+        hip_check(hipGetLastError(), "linear_distill rows launch");
+    };
+    if (p.bf16) rows_kernel((unsigned short)0);
+    else rows_kernel(0.f);
+    hipLaunchKernelGGL(distill_mean_kernel, dim3(1), dim3(1024), 0, st, row_loss, mass, p.rows, heat, loss);
     hip_check(hipGetLastError(), "linear_distill mean launch");
 }
 
@@ -928,8 +1001,11 @@ void linear_distill_bwd(hipStream_t st, int dtype, const void *x, const void *w,
     check_aligned(p, {x, w, dx, dw});
     check_words({index, lse, mass, delta});
     float *inv = (float *)ws;
-    hipLaunchKernelGGL(distill_mean_kernel, dim3(1), dim3(1024), 0, st, (const float *)nullptr, mass, p.rows, heat, (float *)nullptr, inv);
-    hip_check(hipGetLastError(), "linear_distill count launch");
+    const bool count = p.bf16 || rows > 64;
+    if (count) {
+        hipLaunchKernelGGL(distill_inv_kernel, dim3(1), dim3(1024), 0, st, mass, p.rows, heat, inv);
+        hip_check(hipGetLastError(), "linear_distill count launch");
+    }
     vocab_gradients(st, p, x, w, dx, dw, accumulate, ws, inv,
         [&](const GemmShape &g, unsigned short *d, int64_t ld, int v0, int piece) {
             gemm_bf16<false, false>(st, g, DistillGradEpilogue{mass, lse, d, ld, p.rows, piece, 1.f / heat}, "linear_distill gradient launch");
@@ -938,8 +1014,8 @@ void linear_distill_bwd(hipStream_t st, int dtype, const void *x, const void *w,
             hip_check(hipGetLastError(), "linear_distill entries launch");
         },
         [&](float *d, int v0, int piece) {
-            hipLaunchKernelGGL(distill_piece_grad_kernel, dim3(p.rows, (unsigned)cut(piece, 256)), dim3(256), 0, st, d, piece, v0, mass, lse, index, delta, top,
-                               inv, 1.f / heat);
+            hipLaunchKernelGGL((count ? distill_piece_grad_kernel<false> : distill_piece_grad_kernel<true>), dim3(p.rows, (unsigned)cut(piece, 256)), dim3(256), 0, st,
+                               d, piece, v0, mass, lse, index, delta, top, inv, p.rows, heat);
             hip_check(hipGetLastError(), "linear_distill gradient launch");
         });
 }

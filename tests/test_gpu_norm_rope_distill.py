@@ -525,7 +525,8 @@ def test_linear_distill_of_one_entry_is_the_cross_entropy(dtype):
     monet.call("monet_linear_ce_fwd", stream(), dtype, x.data_ptr(), w.data_ptr(), lab.data_ptr(), loss.data_ptr(), lse.data_ptr(), rows, width, vocab, ws.data_ptr(), need)
     monet.call("monet_linear_ce_bwd", stream(), dtype, x.data_ptr(), w.data_ptr(), lab.data_ptr(), lse.data_ptr(), dx.data_ptr(), dw.data_ptr(), rows, width, vocab, 0,
                ws.data_ptr(), need)
-    assert torch.equal(got[1], lse) and torch.allclose(got[0], loss, rtol=1e-6)
+    # the same parts of 64 logits or more, joined in another order: sums of vocab / 64 positive terms at most and a logarithm, each off by its own
+    assert ((got[1] - lse).abs() <= 2 * ((vocab // 64 + 16) * U + 4 * U * lse.abs())).all() and torch.allclose(got[0], loss, rtol=1e-6)
     # the same sums of dl, whose entries may be a rounding apart; the bounds of two results, each off by its own
     dl = torch.softmax(x.double() @ w.double().t(), 1)
     dl.scatter_add_(1, lab.clamp(min=0).long()[:, None], torch.full((rows, 1), -1.0, dtype=torch.float64, device="cuda"))
