@@ -42,7 +42,7 @@ class ONode:
 
     @property
     def is_aux(self):
-        return self.op in ("mask", "poolidx", "lse", "act8")
+        return self.op in ("mask", "poolidx", "lse", "act8", "normstats")
 
     @property
     def persist(self):

@@ -71,6 +71,14 @@ def forward_op(g: OGraph, n, get, params, stats, recompute=False):
     elif n.op == "linearce":
         loss, stats[n.id] = nm.linear_ce_fwd(x, params[n.pars[0]], get(n.ins[1]))
         y = np.array([loss])
+    elif n.op == "lineardistill":
+        loss, *stats[n.id] = nm.linear_distill_fwd(x, params[n.pars[0]], *_teacher(n, get))
+        y = np.array([loss])
+    elif n.op == "layernorm":
+        y, mean, rstd = nm.layernorm_fwd(x, params[n.pars[0]], params[n.pars[1]], float(a["eps"]))
+        aux["normstats"] = lambda: np.stack([mean, rstd], axis=1)
+    elif n.op == "rope":
+        y = _rope(n, x, get(n.ins[1]), nm.rope_fwd)
     elif n.op == "softmaxce":
         y = np.array([nm.softmaxce_fwd(x, get(n.ins[1]))])
     elif n.op == "sumloss":
@@ -84,6 +92,19 @@ def _attention_operands(n, get):
     """q, k, v as [tokens, heads, dim] and the sequences' offsets."""
     dim = int(n.attrs["dim"])
     return tuple(get(r).reshape(get(r).shape[0], -1, dim) for r in n.ins[:3]) + (get(n.ins[3]),)
+
+
+def _rope(n, x, positions, turn):
+    a = n.attrs
+    freqs = nm.rope_freqs(int(a["rot"]), *(float(a[k]) for k in ("base", "factor", "original", "low", "high")))
+    y = turn(x.reshape(x.shape[0], int(a["heads"]), int(a["dim"])), positions, freqs, a["interleaved"] == "1", float(a["scale"]))
+    return y.reshape(x.shape)
+
+
+def _teacher(n, get):
+    """The entries' indices and logits, rows x top, and the temperature."""
+    top = int(n.attrs["top"])
+    return get(n.ins[1]).reshape(-1, top), get(n.ins[2]).reshape(-1, top), float(n.attrs["temperature"])
 
 
 def backward_op(g: OGraph, bop, algo, gy, get, params, stats):
@@ -163,6 +184,14 @@ def backward_op(g: OGraph, bop, algo, gy, get, params, stats):
     if kind == "linearce_bwd":
         dx, dw = nm.linear_ce_bwd(get(n.ins[0]), params[n.pars[0]], get(n.ins[1]))
         return {0: dx}, {n.pars[0]: dw}
+    if kind == "lineardistill_bwd":
+        dx, dw = nm.linear_distill_bwd(get(n.ins[0]), params[n.pars[0]], *_teacher(n, get))
+        return {0: dx}, {n.pars[0]: dw}
+    if kind == "layernorm_bwd":
+        dx, dgamma, dbeta = nm.layernorm_bwd(gy, get(n.ins[0]), params[n.pars[0]], float(a["eps"]))
+        return {0: dx}, {n.pars[0]: dgamma, n.pars[1]: dbeta}
+    if kind == "rope_bwd":
+        return {0: _rope(n, gy, get(n.ins[1]), nm.rope_bwd)}, {}
     if kind == "softmaxce_bwd":
         return {0: nm.softmaxce_bwd(get(n.ins[0]), get(n.ins[1]))}, {}
     if kind == "sumloss_bwd":

@@ -168,6 +168,8 @@ struct StepCtx {
     float *scratch() const { return (float *)(mp->base + mp->plan.scratch_off); }
     size_t scratch_bytes() const { return (size_t)mp->plan.scratch_bytes; }
     float *ce_lse(int node) const { return (float *)(mp->base + mp->plan.ce_lse_off.at(node)); }
+    float *distill_mass(int node) const { return (float *)(mp->base + mp->plan.distill_off.at(node).first); }
+    float *distill_delta(int node) const { return (float *)(mp->base + mp->plan.distill_off.at(node).second); }
     float *bn_stats(int node) const { return (float *)(mp->base + mp->plan.bn_stats_off.at(node)); }
     size_t index_of(const Launch &L) const { return (size_t)(&L - mp->plan.launches.data()); }
     bool feeds_stats(const Launch &L) const { return mp->feeds_stats[index_of(L)] != 0; }
@@ -298,6 +300,17 @@ void run_forward(const StepCtx &c, const Launch &L, const BnAffine *affine = nul
         const auto &is = g.shape_of(n.ins[0]);
         linear_ce_fwd(c.st, MONET_F32, in0, c.weights[n.pars[0]], (const int32_t *)c.ptr(L.in[1]), out, c.ce_lse(L.id), is[0], (int)is[1],
                       (int)g.params[n.pars[0]].shape[0], c.ptr(L.a[4]), (size_t)align_up(n.fimpls[L.impl].ws));
+    } else if (op == "lineardistill") {
+        const auto &is = g.shape_of(n.ins[0]);
+        linear_distill_fwd(c.st, MONET_F32, in0, c.weights[n.pars[0]], (const int32_t *)c.ptr(L.in[1]), (const float *)c.ptr(L.in[2]), nullptr, out,
+                           c.ce_lse(L.id), c.distill_mass(L.id), c.distill_delta(L.id), is[0], (int)is[1], (int)g.params[n.pars[0]].shape[0],
+                           n.attr_int("top"), (float)n.attr_f("temperature", 1.0), c.ptr(L.a[4]), (size_t)align_up(n.fimpls[L.impl].ws));
+    } else if (op == "layernorm") {
+        layernorm_fwd(c.st, MONET_F32, MONET_F32, in0, c.weights[n.pars[0]], c.weights[n.pars[1]], out, (L.flags & 2) ? (float *)c.ptr(L.a[3]) : nullptr,
+                      n.shape[0], (int)n.shape[1], n.shape[1], n.shape[1], (float)n.attr_f("eps", 1e-5));
+    } else if (op == "rope") {
+        rope(c.st, MONET_F32, in0, out, (const int32_t *)c.ptr(L.in[1]), c.mp->plan.rope_freqs.at(L.id).data(), n.shape[0], n.attr_int("heads"),
+             n.attr_int("dim"), n.attr_int("rot"), n.shape[1], n.shape[1], n.attr_int("interleaved") == 1, (float)n.attr_f("scale", 1.0), false, false);
     } else if (op == "softmaxce") {
         const auto &is = g.shape_of(n.ins[0]);
         const int classes = (int)is.back();
@@ -399,6 +412,20 @@ void run_backward(const StepCtx &c, const Launch &L) {
         Ref lab; lab.region = R_EXT; lab.off = -n.ins[1];
         linear_ce_bwd(c.st, MONET_F32, dep, c.weights[n.pars[0]], (const int32_t *)c.ptr(lab), c.ce_lse(b.node), d0, c.grads[n.pars[0]], is[0],
                       (int)is[1], (int)g.params[n.pars[0]].shape[0], acc0, c.ptr(L.a[4]), (size_t)align_up(im.ws));
+    } else if (kd == "lineardistill_bwd") {
+        const auto &is = g.shape_of(n.ins[0]);
+        Ref index; index.region = R_EXT; index.off = -n.ins[1];
+        linear_distill_bwd(c.st, MONET_F32, dep, c.weights[n.pars[0]], (const int32_t *)c.ptr(index), c.ce_lse(b.node), c.distill_mass(b.node),
+                           c.distill_delta(b.node), d0, c.grads[n.pars[0]], is[0], (int)is[1], (int)g.params[n.pars[0]].shape[0], n.attr_int("top"),
+                           (float)n.attr_f("temperature", 1.0), acc0, c.ptr(L.a[4]), (size_t)align_up(im.ws));
+    } else if (kd == "layernorm_bwd") {
+        layernorm_bwd(c.st, MONET_F32, MONET_F32, gy, c.ptr(L.dep[0]), c.weights[n.pars[0]], (const float *)c.ptr(L.dep[1]), d0, c.grads[n.pars[0]],
+                      c.grads[n.pars[1]], n.shape[0], (int)n.shape[1], n.shape[1], n.shape[1], n.shape[1], acc0 ? 1 : 0, c.ptr(L.a[4]),
+                      (size_t)(im.ws > 0 ? align_up(im.ws) : 0));
+    } else if (kd == "rope_bwd") {
+        Ref at; at.region = R_EXT; at.off = -n.ins[1];
+        rope(c.st, MONET_F32, gy, d0, (const int32_t *)c.ptr(at), c.mp->plan.rope_freqs.at(b.node).data(), n.shape[0], n.attr_int("heads"), n.attr_int("dim"),
+             n.attr_int("rot"), n.shape[1], n.shape[1], n.attr_int("interleaved") == 1, (float)n.attr_f("scale", 1.0), true, acc0);
     } else if (kd == "linear_dgrad") {
         const auto &is = g.shape_of(n.ins[0]);
         linear_dgrad(c.st, gy, c.weights[n.pars[0]], d0, (int)is[0], (int)(numel_of(is) / is[0]), (int)n.shape[1], acc0, c.scratch(),
@@ -916,12 +943,14 @@ extern "C" int monet_plan_launch_info(const monet_plan *p, size_t index, monet_l
             flops = 2.5 * attention_flops(n);
             issued = 3.5 * attention_flops(n);
             bytes = 2.0 * e + 4.0 * e + 4.0 * (numel_of(g.shape_of(n.ins[1])) + numel_of(g.shape_of(n.ins[2])));
-        } else if (b.kind == "linearce_bwd") {
+        } else if (b.kind == "linearce_bwd" || b.kind == "lineardistill_bwd") {
             const double rows = g.shape_of(n.ins[0])[0], w = numel_of(g.params[n.pars[0]].shape);
             flops = 4.0 * rows * w;
             issued = 6.0 * rows * w;
             bytes = 8.0 * (numel_of(g.shape_of(n.ins[0])) + w);
         }
+        else if (b.kind == "layernorm_bwd") bytes = 3 * e + ((L.flags & 1) ? e : 0);
+        else if (b.kind == "rope_bwd") bytes = 2 * e + ((L.flags & 1) ? e : 0);
         else if (b.kind == "linear_dgrad") conv_cost(linear_shape(g, n), "linear_dgrad");
         else if (b.kind == "bn_bwd") bytes = 5 * e;                      // reduce pass reads dy,t; apply pass reads dy,t, writes dx
         else if (b.kind == "relu_bwd" || b.kind == "relu6_bwd")
@@ -950,7 +979,7 @@ extern "C" int monet_plan_launch_info(const monet_plan *p, size_t index, monet_l
         } else if (n.op == "attention") {
             flops = attention_flops(n);
             bytes = 2.0 * e + 4.0 * (numel_of(g.shape_of(n.ins[1])) + numel_of(g.shape_of(n.ins[2])));
-        } else if (n.op == "linearce") {
+        } else if (n.op == "linearce" || n.op == "lineardistill") {
             const double rows = g.shape_of(n.ins[0])[0], w = numel_of(g.params[n.pars[0]].shape);
             flops = 2.0 * rows * w;
             bytes = 4.0 * (numel_of(g.shape_of(n.ins[0])) + w);

@@ -251,6 +251,7 @@ size_t layernorm_bwd_workspace_bytes(int dtype, int64_t rows, int cols);
 void layernorm_bwd(hipStream_t st, int dtype, int param_dtype, const void *dy, const void *x, const void *gamma, const float *stats, void *dx, void *dgamma,
                    void *dbeta, int64_t rows, int cols, int64_t dy_ld, int64_t x_ld, int64_t dx_ld, int accumulate, void *ws, size_t ws_bytes);
 void rope_freqs(double *freqs, int rot_dim, double base, double factor, double original, double low, double high);      // host
+void rope_check(int64_t tokens, int heads, int head_dim, int rot_dim, float scale);      // refuses what rope refuses of these
 // inverse: turned back (the gradient); freqs: host memory, rot_dim / 2 values, read before the call returns
 void rope(hipStream_t st, int dtype, const void *x, void *y, const int32_t *positions, const double *freqs, int64_t tokens, int heads, int head_dim,
           int rot_dim, int64_t x_ld, int64_t y_ld, bool interleaved, float scale, bool inverse, bool accumulate);

@@ -113,7 +113,7 @@ void Graph::parse(const std::string &text) {
                 n.pars = parse_refs(take(a, "par"));
                 n.shape = parse_dims(take(a, "shape"));
                 n.attrs = a;
-                n.aux = (n.op == "mask" || n.op == "poolidx" || n.op == "lse" || n.op == "act8");
+                n.aux = (n.op == "mask" || n.op == "poolidx" || n.op == "lse" || n.op == "act8" || n.op == "normstats");
                 n.persist = n.attr_int("persist") == 1;
                 int64_t esz = n.op == "mask" ? 8 : (n.op == "poolidx" || n.op == "act8" ? 1 : 4);
                 n.bytes = n.persist ? 0 : align_up(numel(n.shape) * esz);
@@ -272,7 +272,9 @@ static void check_declared_deps(const Graph &g) {
                 want = {n.ins[0], n.ins[1], n.ins[2], n.id};
                 aux0();
             }
-            else if (b.kind == "linearce_bwd") { known = algo == "pieces"; input0(); }
+            else if (b.kind == "linearce_bwd" || b.kind == "lineardistill_bwd") { known = algo == "pieces"; input0(); }
+            else if (b.kind == "layernorm_bwd") { known = algo == "from_input"; input0(); aux0(); }
+            else if (b.kind == "rope_bwd") { known = algo == "direct"; }
             else if (b.kind == "linear_dgrad") { known = algo == "gemm"; }
             else if (b.kind == "bn_bwd") {
                 if (algo == "from_input") input0(); else if (algo == "from_output") want.push_back(n.id); else known = false;
@@ -291,6 +293,12 @@ static void check_declared_deps(const Graph &g) {
                 throw PlanError(MONET_BAD_GRAPH, "backward operator " + std::to_string(k) + " (" + algo + "): declared dependencies differ from what the kernel reads");
         }
     }
+}
+
+static std::vector<double> rope_node_freqs(const Node &n) {
+    std::vector<double> f(std::max(0, n.attr_int("rot") / 2));
+    rope_freqs(f.data(), n.attr_int("rot"), n.attr_f("base", 10000.0), n.attr_f("factor", 1.0), n.attr_f("original", 0.0), n.attr_f("low", 0.0), n.attr_f("high", 0.0));
+    return f;
 }
 
 // What the kernels of a transformer's operators take from the graph text: shapes within their limits, workspaces that are large enough, backward
@@ -348,6 +356,40 @@ static void check_transformer_nodes(const Graph &g) {
             const auto bytes = [&](bool grad) { return workspace([&] { return linear_ce_workspace_bytes(grad, MONET_F32, x[0], (int)x[1], (int)w[0]); }); };
             for (const FwdImpl &im : n.fimpls) enough(im.ws, bytes(false));
             each_impl("linearce_bwd", "pieces", bytes(true));
+        } else if (n.op == "lineardistill") {
+            need(n.persist && n.ins.size() == 3 && n.ins[0] > 0 && n.pars.size() == 1, "is a persistent node with an input, the entries' indices and logits and a parameter");
+            const auto &x = g.shape_of(n.ins[0]), &w = g.params[n.pars[0]].shape;
+            need(x.size() == 2 && w.size() == 2 && x[1] == w[1], "input rows x width and parameter vocab x width do not fit");
+            need(x[1] <= INT32_MAX && w[0] <= INT32_MAX, "width or vocabulary too large");
+            const int64_t top = n.attr_int("top");
+            need(offsets(n.ins[1], x[0] * top), "indices must be an external i32 tensor of rows x top values");
+            need(n.ins[2] <= 0 && g.exts[-n.ins[2]].dtype == "f32" && numel(g.exts[-n.ins[2]].shape) == x[0] * top, "logits must be an external f32 tensor of rows x top values");
+            const float heat = (float)n.attr_f("temperature", 1.0);
+            need(heat >= 1e-30f && heat <= 1e30f, "temperature must be positive and finite");
+            const auto bytes = [&](bool grad) {
+                return workspace([&] { return linear_distill_workspace_bytes(grad, MONET_F32, x[0], (int)x[1], (int)w[0], (int)top); });
+            };
+            for (const FwdImpl &im : n.fimpls) enough(im.ws, bytes(false));
+            each_impl("lineardistill_bwd", "pieces", bytes(true));
+        } else if (n.op == "layernorm") {
+            need(n.ins.size() == 1 && n.ins[0] > 0 && n.pars.size() == 2, "has one input that a node computes, a weight and a bias");
+            need(n.shape.size() == 2 && g.shape_of(n.ins[0]) == n.shape && n.shape[1] <= INT32_MAX, "input and output must be the same rows x columns");
+            for (int p : n.pars) need(numel(g.params[p].shape) == n.shape[1], "weight and bias must have a value for each column");
+            const float eps = (float)n.attr_f("eps", 1e-5);
+            need(eps > 0.f && eps <= 1e30f, "eps must be positive and finite");
+            need(aux && aux->op == "normstats" && numel(aux->shape) == 2 * n.shape[0], "needs an intermediate normstats of rows x 2");
+            for (const FwdImpl &im : n.fimpls) need(!im.inplace, "cannot run in place: its backward operator reads the input");
+            each_impl("layernorm_bwd", "from_input", workspace([&] { return layernorm_bwd_workspace_bytes(MONET_F32, n.shape[0], (int)n.shape[1]); }));
+        } else if (n.op == "rope") {
+            const int64_t heads = n.attr_int("heads"), dim = n.attr_int("dim"), rot = n.attr_int("rot");
+            need(n.ins.size() == 2 && n.ins[0] > 0, "inputs are a node and the positions");
+            need(n.shape.size() == 2 && g.shape_of(n.ins[0]) == n.shape && n.shape[1] == heads * dim, "input and output must be tokens x (heads * dim)");
+            need(offsets(n.ins[1], n.shape[0]), "positions must be an external i32 tensor of one value per token");
+            workspace([&] {
+                rope_check(n.shape[0], (int)heads, (int)dim, (int)rot, (float)n.attr_f("scale", 1.0));
+                rope_node_freqs(n);
+                return 0;
+            });
         } else if (n.op == "linear" && aux) {
             need(n.ins.size() == 1 && n.pars.size() == 2, "has one input, a weight and a bias");
             const auto &x = g.shape_of(n.ins[0]);
@@ -357,7 +399,7 @@ static void check_transformer_nodes(const Graph &g) {
                 act8_check_values(x[0], x[1]);
                 return act8_wgrad_workspace_bytes(MONET_F32, x[0], x[1], n.shape[1]);
             }));
-        } else if (aux && (aux->op == "lse" || aux->op == "act8"))
+        } else if (aux && (aux->op == "lse" || aux->op == "act8" || aux->op == "normstats"))
             need(false, "does not write such an intermediate");
     }
     for (const Bop &b : g.bops) {
@@ -367,6 +409,9 @@ static void check_transformer_nodes(const Graph &g) {
         };
         if (b.kind == "attention_bwd") belongs(n.op == "attention");
         if (b.kind == "linearce_bwd") belongs(n.op == "linearce");
+        if (b.kind == "lineardistill_bwd") belongs(n.op == "lineardistill");
+        if (b.kind == "layernorm_bwd") belongs(n.op == "layernorm");
+        if (b.kind == "rope_bwd") belongs(n.op == "rope");
         for (const BwdImpl &im : b.impls)
             if (im.algo == "from_code") belongs(b.kind == "linear_wgrad" && n.op == "linear");
     }
@@ -850,17 +895,23 @@ void Plan::build(const std::string &graph_text, const std::string &schedule_text
     check_declared_deps(g);
     sch.parse(schedule_text, g);
     validate();
-    // constant region: loss scalar, BatchNorm statistics, a vocabulary loss's lse, reduction scratch
+    // constant region: loss scalar, BatchNorm statistics, what a vocabulary loss keeps of its rows, reduction scratch
     int64_t off = 0;
     loss_off = off; off += kAlign;
     for (int i = 1; i <= g.N(); ++i)
         if (g.nodes[i].op == "bn") {
             bn_stats_off[i] = off;
             off += align_up(2 * g.nodes[i].shape.back() * 4);
-        } else if (g.nodes[i].op == "linearce") {
+        } else if (g.nodes[i].op == "linearce" || g.nodes[i].op == "lineardistill") {
+            const int64_t rows = g.shape_of(g.nodes[i].ins[0])[0];
             ce_lse_off[i] = off;
-            off += align_up(g.shape_of(g.nodes[i].ins[0])[0] * 4);
-        }
+            off += align_up(rows * 4);
+            if (g.nodes[i].op == "lineardistill") {
+                distill_off[i] = {off, off + align_up(rows * 4)};
+                off += align_up(rows * 4) + align_up(rows * g.nodes[i].attr_int("top") * 4);
+            }
+        } else if (g.nodes[i].op == "rope")
+            rope_freqs[i] = rope_node_freqs(g.nodes[i]);
     scratch_off = off;
     // holds the partial results of the two-level reductions; the largest user is BatchNorm's forward statistics
     // in groups of 64 rows (2 floats per group and channel: 72 MB for VGG-16's first layers at batch 176)

@@ -125,6 +125,8 @@ struct Plan {
     std::vector<std::map<std::pair<int, int>, int64_t>> where;   // per launch: live tensor offsets
     std::map<int, int64_t> bn_stats_off;   // node -> offset in the persistent region
     std::map<int, int64_t> ce_lse_off;     // the same for the lse of a vocabulary loss's rows
+    std::map<int, std::pair<int64_t, int64_t>> distill_off;    // and for the weight and the entries' gradients of a loss against a teacher
+    std::map<int, std::vector<double>> rope_freqs;             // node -> radians a position of its pairs
     int64_t loss_off = 0;
     int64_t scratch_off = 0, scratch_bytes = 0;
     int64_t persistent_bytes = 0;

@@ -114,15 +114,18 @@ void rope_freqs(double *freqs, int rot_dim, double base, double factor, double o
     }
 }
 
-void rope(hipStream_t st, int dtype, const void *x, void *y, const int32_t *positions, const double *freqs, int64_t tokens, int heads, int head_dim,
-          int rot_dim, int64_t x_ld, int64_t y_ld, bool interleaved, float scale, bool inverse, bool accumulate) {
-    if (dtype != MONET_F32 && dtype != MONET_BF16) throw KernelError("rope: dtype must be MONET_F32 or MONET_BF16");
+void rope_check(int64_t tokens, int heads, int head_dim, int rot_dim, float scale) {
     if (tokens < 0 || heads < 1 || head_dim < 1) throw KernelError("rope: bad shape");
     if (rot_dim < 2 || rot_dim % 2 || rot_dim > ROPE_DIM || rot_dim > head_dim)
         throw KernelError("rope: rot_dim must be even, 2 to head_dim and at most " + std::to_string(ROPE_DIM));
-    const int64_t width = (int64_t)heads * head_dim;
-    if (tokens >= 1 << 24 || width >= 1 << 24 || head_dim > 1 << 15) throw KernelError("rope: shape too large");
+    if (tokens >= 1 << 24 || (int64_t)heads * head_dim >= 1 << 24 || head_dim > 1 << 15) throw KernelError("rope: shape too large");
     if (!std::isfinite(scale)) throw KernelError("rope: the scale must be finite");
+}
+
+void rope(hipStream_t st, int dtype, const void *x, void *y, const int32_t *positions, const double *freqs, int64_t tokens, int heads, int head_dim,
+          int rot_dim, int64_t x_ld, int64_t y_ld, bool interleaved, float scale, bool inverse, bool accumulate) {
+    if (dtype != MONET_F32 && dtype != MONET_BF16) throw KernelError("rope: dtype must be MONET_F32 or MONET_BF16");
+    rope_check(tokens, heads, head_dim, rot_dim, scale);
     if (!freqs) throw KernelError("rope: null pointer");
     RopeFreqs f;
     for (int i = 0; i < ROPE_DIM / 2; ++i) {
@@ -130,6 +133,7 @@ void rope(hipStream_t st, int dtype, const void *x, void *y, const int32_t *posi
         if (!std::isfinite(f.turns[i])) throw KernelError("rope: frequencies must be finite");
     }
     if (!tokens) return;
+    const int64_t width = (int64_t)heads * head_dim;
     if (!x || !y) throw KernelError("rope: null pointer");
     if (((uintptr_t)x | (uintptr_t)y) % (dtype == MONET_BF16 ? 2 : 4) || (uintptr_t)positions % 4) throw KernelError("rope: pointer not aligned");
     if (x_ld < width || y_ld < width) throw KernelError("rope: token stride below heads * head_dim");

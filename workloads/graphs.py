@@ -54,7 +54,7 @@ class Node:
 
 
 class Graph:
-    AUX_OPS = ("mask", "poolidx", "lse", "act8")
+    AUX_OPS = ("mask", "poolidx", "lse", "act8", "normstats")
 
     def __init__(self):
         self.exts = []      # (ref, name, dtype, shape)
@@ -362,6 +362,43 @@ class Graph:
         self.fimpls[i] = [dict(algo="pieces", ws=_library_bytes("monet_linear_ce_workspace_bytes", 0, 0, rows, width, vocab), cost=flop)]
         ws = _library_bytes("monet_linear_ce_workspace_bytes", 1, 0, rows, width, vocab)
         self._pending_bops(i, [("linearce_bwd", [dict(algo="pieces", deps=[x], ws=ws, cost=3 * flop)])])
+        return i
+
+    def lineardistill(self, x, index, target, vocab, temperature=1.0, name="head"):
+        """Loss: divergence of a linear layer's softmax over `vocab` classes from a teacher's top logits: `index` (i32) and `target` (f32) are
+        external tensors [rows, top].  The logits are never held."""
+        rows, width = self.shape_of(x)
+        top = self.shape_of(index)[1]
+        w = self.param(name + ".w", (vocab, width))
+        i = self._add("lineardistill", [x, index, target], [w], (1,), persist=1, top=top, temperature=float(temperature))
+        flop = 2.0 * rows * width * vocab
+        self.fimpls[i] = [dict(algo="pieces", ws=_library_bytes("monet_linear_distill_workspace_bytes", 0, 0, rows, width, vocab, top), cost=flop)]
+        ws = _library_bytes("monet_linear_distill_workspace_bytes", 1, 0, rows, width, vocab, top)
+        self._pending_bops(i, [("lineardistill_bwd", [dict(algo="pieces", deps=[x], ws=ws, cost=3 * flop)])])
+        return i
+
+    def layernorm(self, x, name="norm", eps=1e-5):
+        """Layer norm over the columns of x [rows, cols].  The forward pass leaves mean and 1 / deviation of the rows as an intermediate node."""
+        rows, cols = self.shape_of(x)
+        gamma, beta = self.param(name + ".gamma", (cols,)), self.param(name + ".beta", (cols,))
+        i = self._add("layernorm", [x], [gamma, beta], (rows, cols), eps=eps)
+        stats = self._add("normstats", [i], [], (rows, 2))
+        by, c = self._bytes(x), RIDGE_FLOP_PER_BYTE
+        self.fimpls[i] = [dict(algo="direct", ws=0, cost=2 * by * c)]
+        ws = _library_bytes("monet_layernorm_bwd_workspace_bytes", 0, rows, cols)
+        self._pending_bops(i, [("layernorm_bwd", [dict(algo="from_input", deps=[x, stats], ws=ws, cost=3 * by * c)])])
+        return i
+
+    def rope(self, x, positions, heads, rot=None, base=10000.0, factor=1.0, original=0.0, low=0.0, high=0.0, interleaved=False, scale=1.0):
+        """Rotary positions of x [tokens, heads * dim]; positions: an external i32 tensor, one per token.  The backward pass reads nothing but the
+        gradient, so the operator may run in place."""
+        tokens, width = self.shape_of(x)
+        dim = width // heads
+        i = self._add("rope", [x, positions], [], (tokens, width), heads=heads, dim=dim, rot=dim if rot is None else rot, base=float(base),
+                      factor=float(factor), original=float(original), low=float(low), high=float(high), interleaved=int(interleaved), scale=float(scale))
+        by, c = self._bytes(x), RIDGE_FLOP_PER_BYTE
+        self.fimpls[i] = [dict(algo="direct", ws=0, cost=2 * by * c), dict(algo="inplace", ws=0, cost=2 * by * c, inplace=1)]
+        self._pending_bops(i, [("rope_bwd", [dict(algo="direct", deps=[], ws=0, cost=2 * by * c)])])
         return i
 
     def softmaxce(self, x, labels):
@@ -742,28 +779,43 @@ def googlenet(batch=320, hw=224, classes=1000, stem=(64, 64, 192), inceptions=GO
     return g
 
 
-def transformer(lens=(40, 1, 23), width=64, heads=4, kv_heads=2, hidden=128, layers=2, vocab=300, code=True):
+def transformer(lens=(40, 1, 23), width=64, heads=4, kv_heads=2, hidden=128, layers=2, vocab=300, code=True, norm=False, rotary=False, teacher=0):
     """Decoder-shaped network over packed sequences of the given lengths: per layer attention between linear layers and two linear layers
-    around a ReLU, each behind a residual add, and the vocabulary loss.  The input is the embedded tokens; no normalisation.  With `code`
-    every linear layer offers its input in 8 bits."""
+    around a ReLU, each behind a residual add, and the vocabulary loss.  The input is the embedded tokens.  With `code`
+    every linear layer offers its input in 8 bits.  With `norm` a layer norm lies before attention, before the linear layers and before the loss;
+    with `rotary` queries and keys carry their positions in the sequence; with `teacher` the loss is against that many of a teacher's logits a token."""
     g = Graph()
     tokens, dim = sum(lens), width // heads
     x = g.ext("embedded", "f32", (tokens, width))
     labels = g.ext("labels", "i32", (tokens,))
     cu = g.ext("cu_seqlens", "i32", (len(lens) + 1,))
     g.ext_values[cu] = [sum(lens[:i]) for i in range(len(lens) + 1)]
+    if rotary:
+        positions = g.ext("positions", "i32", (tokens,))
+        g.ext_values[positions] = [t for n in lens for t in range(n)]
+    if teacher:
+        index, target = g.ext("teacher_index", "i32", (tokens, teacher)), g.ext("teacher_logits", "f32", (tokens, teacher))
     for layer in range(layers):
         g.begin_block(f"layer{layer}")
         name = f"l{layer}."
         if layer == 0:
             x = g.linear(x, width, name="in", code=code)
-        q = g.linear(x, heads * dim, name=name + "q", code=code)
-        k = g.linear(x, kv_heads * dim, name=name + "k", code=code)
-        v = g.linear(x, kv_heads * dim, name=name + "v", code=code)
+        a = g.layernorm(x, name=name + "norm1") if norm else x
+        q = g.linear(a, heads * dim, name=name + "q", code=code)
+        k = g.linear(a, kv_heads * dim, name=name + "k", code=code)
+        v = g.linear(a, kv_heads * dim, name=name + "v", code=code)
+        if rotary:
+            q, k = g.rope(q, positions, heads), g.rope(k, positions, kv_heads)
         o = g.linear(g.attention(q, k, v, cu, heads, kv_heads), width, name=name + "o", code=code)
         x = g.add(x, o)
-        h = g.linear(g.relu(g.linear(x, hidden, name=name + "up", code=code)), width, name=name + "down", code=code)
+        a = g.layernorm(x, name=name + "norm2") if norm else x
+        h = g.linear(g.relu(g.linear(a, hidden, name=name + "up", code=code)), width, name=name + "down", code=code)
         x = g.add(x, h)
         g.end_block()
-    g.linearce(x, labels, vocab)
+    if norm:
+        x = g.layernorm(x, name="norm")
+    if teacher:
+        g.lineardistill(x, index, target, vocab, temperature=2.0)
+    else:
+        g.linearce(x, labels, vocab)
     return g

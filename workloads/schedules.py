@@ -373,12 +373,12 @@ def googlenet_alternate_schedule(g: Graph, variants=None):
 
 def code_set(g: Graph):
     """What a transformer holds when every linear layer's weight gradient reads its input in 8 bits: the 8-bit inputs, sign masks,
-    block outputs, and attention's output and row statistics.  Queries, keys and values are computed again from the block's input."""
+    block outputs, layer norms' and attention's row statistics, and attention's output.  Queries, keys and values are computed again from the block's input."""
     F = block_output_set(g)
     for n in g.nodes:
         if n.op == "attention":
             F |= {n.id, g.aux_of(n.id)}
-        elif n.op in ("act8", "mask"):
+        elif n.op in ("act8", "mask", "normstats"):
             F.add(n.id)
     return F
 

@@ -22,7 +22,7 @@ def make_inputs(g: Graph, seed=0, gamma_beta="unit"):
     for n in g.nodes:
         if n.op == "softmaxce":
             classes = g.shape_of(n.ins[0])[-1]
-        elif n.op == "linearce":
+        elif n.op in ("linearce", "lineardistill"):
             classes = g.params[n.pars[0]][2][0]
     for ref, name, dt, shp in g.exts:
         if ref in g.ext_values:
