@@ -9,6 +9,7 @@
 #include "../../include/monet_kernels.h"
 #include "kernels.hpp"
 #include "tile_bf16.hpp"
+#include "wave_sum.hpp"
 
 namespace monet {
 
@@ -92,20 +93,6 @@ struct Piece {
     }
 };
 
-// the sum over a wave, in every lane: neighbours, fours, eights, 16 lanes, then the four rows of 16 through their last lanes
-template <int CTRL, int ROWS>
-__device__ __forceinline__ float dpp_add(float v) {
-    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
-}
-__device__ __forceinline__ float wave_sum(float v) {
-    v = dpp_add<0xb1, 0xf>(v);       // quad_perm 1 0 3 2
-    v = dpp_add<0x4e, 0xf>(v);       // quad_perm 2 3 0 1
-    v = dpp_add<0x141, 0xf>(v);      // row_half_mirror
-    v = dpp_add<0x140, 0xf>(v);      // row_mirror
-    v = dpp_add<0x142, 0xa>(v);      // row_bcast15
-    v = dpp_add<0x143, 0xc>(v);      // row_bcast31
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
-}
 // the sums of W waves; `at`: this group's and this sum's place in LDS, not used again before the next barrier but one
 template <int W>
 __device__ __forceinline__ float group_sum(float v, float *at, int wave) {

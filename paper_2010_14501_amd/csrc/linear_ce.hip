@@ -16,6 +16,7 @@
 #include "../../include/monet_kernels.h"
 #include "gemm_bf16.hpp"
 #include "kernels.hpp"
+#include "wave_sum.hpp"
 
 namespace monet {
 
@@ -385,111 +386,116 @@ __device__ __forceinline__ void distill_dots(const unsigned short *x, const unsi
         }
     }
 }
-__device__ __forceinline__ float sum_of_256(float v, float *seg) {      // the same in every thread
-    for (int w = 32; w; w /= 2) v += __shfl_xor(v, w);
-    __syncthreads();
-    if (threadIdx.x % 64 == 0) seg[threadIdx.x / 64] = v;
-    __syncthreads();
-    return (seg[0] + seg[1]) + (seg[2] + seg[3]);
-}
-__device__ __forceinline__ float max_of_256(float v, float *seg) {
-    for (int w = 32; w; w /= 2) v = fmaxf(v, __shfl_xor(v, w));
-    __syncthreads();
-    if (threadIdx.x % 64 == 0) seg[threadIdx.x / 64] = v;
-    __syncthreads();
-    return fmaxf(fmaxf(seg[0], seg[1]), fmaxf(seg[2], seg[3]));
-}
+constexpr int DISTILL_WAVES = 8;
 template <class T>
-__global__ __launch_bounds__(256) void distill_rows_kernel(const T *__restrict__ x, const T *__restrict__ w, const int32_t *__restrict__ index,
-                                                           const float *__restrict__ target, const float *__restrict__ target_lse,
-                                                           const float2 *__restrict__ part, int parts, int rows, float *__restrict__ lse,
-                                                           float *__restrict__ mass, float *__restrict__ delta, float *__restrict__ row_loss, int width,
-                                                           int vocab, int top, float heat) {
-    __shared__ float z[DISTILL_TOP], p[DISTILL_TOP], seg[4];
+__global__ __launch_bounds__(64 * DISTILL_WAVES) void distill_rows_kernel(const T *__restrict__ x, const T *__restrict__ w, const int32_t *__restrict__ index,
+                                                                          const float *__restrict__ target, const float *__restrict__ target_lse,
+                                                                          const float2 *__restrict__ part, int parts, int rows, float *__restrict__ lse,
+                                                                          float *__restrict__ mass, float *__restrict__ delta, float *__restrict__ row_loss,
+                                                                          int width, int vocab, int top, float heat) {
+    __shared__ float z[DISTILL_TOP], p[DISTILL_TOP];
     __shared__ int at[DISTILL_TOP];
-    __shared__ Soft joined[4];
+    __shared__ unsigned seen[DISTILL_TOP];      // a bit for each value of an index's lowest 15 bits
+    __shared__ Soft joined[DISTILL_WAVES];
+    __shared__ int twice;                       // an index may come more than once
+    constexpr int THREADS = 64 * DISTILL_WAVES;
     const int64_t t = blockIdx.x;
     const int wave = threadIdx.x / 64, l = threadIdx.x & 63;
     index += t * top;
     target += t * top;
-    for (int j = threadIdx.x; j < top; j += 256) at[j] = (unsigned)index[j] < (unsigned)vocab ? index[j] : -1;
-    __syncthreads();
+    if (threadIdx.x == 0) twice = 0;
+    for (int j = threadIdx.x; j < DISTILL_TOP; j += THREADS) seen[j] = 0;
     // the row's lse from its parts, unless it is there already
-    float ls = 0.f;
+    Soft a{-INFINITY, 0.f};
     if (part) {
-        Soft a{-INFINITY, 0.f};
-        for (int b = threadIdx.x; b < parts; b += 256) {
+        for (int b = threadIdx.x; b < parts; b += THREADS) {
             const float2 v = part[(int64_t)b * rows + t];
             a = soft_join(a, Soft{v.x, v.y});
         }
-        for (int k = 32; k; k /= 2) a = soft_join(a, Soft{__shfl_xor(a.m, k), __shfl_xor(a.s, k)});
-        if (l == 0) joined[wave] = a;
     }
-    const auto dots = [&](int j0, auto n) {      // entries j0 .. j0 + N - 1; one that is none repeats the first that is
+    for (int j = threadIdx.x; j < top; j += THREADS) at[j] = (unsigned)index[j] < (unsigned)vocab ? index[j] : -1;
+    __syncthreads();
+    for (int j = threadIdx.x; j < top; j += THREADS) {
+        const unsigned v = at[j] & 0x7fff, bit = 1u << (v & 31);
+        if (at[j] >= 0 && (atomicOr(&seen[v / 32], bit) & bit)) twice = 1;
+    }
+    const auto dots = [&](int j0, auto n) {      // entries j0 .. j0 + N - 1; one that is none repeats another
         constexpr int N = decltype(n)::value;
         const T *row[N];
-        int some = -1;
+        int v[N], some = -1;
 #pragma unroll
-        for (int j = N - 1; j >= 0; --j) {
-            const int v = __builtin_amdgcn_readfirstlane(j0 + j < top ? at[j0 + j] : -1);
-            if (v >= 0) some = v;
-            row[j] = w + (int64_t)v * width;
+        for (int j = 0; j < N; ++j) {
+            v[j] = __builtin_amdgcn_readfirstlane(j0 + j < top ? at[j0 + j] : -1);
+            some = max(some, v[j]);
         }
         if (some < 0) return;
         float s[N] = {};
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (row[j] < w) row[j] = w + (int64_t)some * width;
+        for (int j = 0; j < N; ++j) row[j] = w + (int64_t)(v[j] < 0 ? some : v[j]) * width;
         distill_dots(x + t * width, row, width, l, s);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            for (int k = 32; k; k /= 2) s[j] += __shfl_xor(s[j], k);
+            s[j] = wave_sum(s[j]);
             if (l == 0 && j0 + j < top) z[j0 + j] = s[j] / heat;
         }
     };
     if (top >= 16)
-        for (int j = 4 * wave; j < top; j += 16) dots(j, std::integral_constant<int, 4>());
+        for (int j = 4 * wave; j < top; j += 4 * DISTILL_WAVES) dots(j, std::integral_constant<int, 4>());
     else
-        for (int j = wave; j < top; j += 4) dots(j, std::integral_constant<int, 1>());
-    float most = -INFINITY;
-    for (int j = threadIdx.x; j < top; j += 256)
-        if (at[j] >= 0) most = fmaxf(most, target[j] / heat);
+        for (int j = wave; j < top; j += DISTILL_WAVES) dots(j, std::integral_constant<int, 1>());
+    if (part) {
+        const float m = wave_max(a.m);
+        a = Soft{m, wave_sum(a.m == -INFINITY ? a.s : a.s * exp_of(a.m - m))};
+        if (l == 0) joined[wave] = a;
+    }
+    __syncthreads();
+    if (wave) return;
+    // the rest is one wave's
+    float ls;
+    if (part) {
+        a = joined[0];
+#pragma unroll
+        for (int i = 1; i < DISTILL_WAVES; ++i) a = soft_join(a, joined[i]);
+        ls = a.m + logf(a.s);
+        if (l == 0) lse[t] = ls;
+    } else
+        ls = lse[t];
     float norm;
     if (target_lse) norm = target_lse[t];
     else {
-        most = max_of_256(most, seg);
-        float sum = 0.f;
-        for (int j = threadIdx.x; j < top; j += 256)
+        float most = -INFINITY, sum = 0.f;
+        for (int j = l; j < top; j += 64)
+            if (at[j] >= 0) most = fmaxf(most, target[j] / heat);
+        most = wave_max(most);
+        for (int j = l; j < top; j += 64)
             if (at[j] >= 0 && target[j] != -INFINITY) sum += expf(target[j] / heat - most);
-        norm = most + logf(sum_of_256(sum, seg));
+        norm = most + logf(wave_sum(sum));
     }
-    __syncthreads();
-    if (part) {
-        const Soft a = soft_join(soft_join(joined[0], joined[1]), soft_join(joined[2], joined[3]));
-        ls = a.m + logf(a.s);
-        if (threadIdx.x == 0) lse[t] = ls;
-    } else
-        ls = lse[t];
     float loss = 0.f, m = 0.f;
-    for (int j = threadIdx.x; j < top; j += 256) {
+    for (int j = l; j < top; j += 64) {
         // an entry of weight 0 adds nothing, whatever the row's logits are
         const float logp = target[j] / heat - norm, pj = at[j] < 0 || target[j] == -INFINITY ? 0.f : expf(logp);
         p[j] = pj;
         m += pj;
         if (pj != 0.f) loss += pj * (logp + (ls - z[j]));
     }
-    loss = sum_of_256(loss, seg);
-    m = sum_of_256(m, seg);
-    for (int j = threadIdx.x; j < top; j += 256) {
+    loss = wave_sum(loss);
+    m = wave_sum(m);
+    __builtin_amdgcn_wave_barrier();       // p is read by other lanes than wrote it
+    const bool search = __builtin_amdgcn_readfirstlane(twice);
+    for (int j = l; j < top; j += 64) {
         float d = 0.f;
         if (at[j] >= 0 && m != 0.f) {
-            float same = 0.f;
-            for (int i = 0; i < top; ++i) same += at[i] == at[j] ? p[i] : 0.f;
+            float same = p[j];
+            if (search) {
+                same = 0.f;
+                for (int i = 0; i < top; ++i) same += at[i] == at[j] ? p[i] : 0.f;
+            }
             d = m * expf(z[j] - ls) - same;
         }
         delta[t * top + j] = d;
     }
-    if (threadIdx.x) return;
+    if (l) return;
     mass[t] = m;
     row_loss[t] = loss;
 }
@@ -525,10 +531,10 @@ __global__ __launch_bounds__(1024) void distill_inv_kernel(const float *__restri
 // bf16: the teacher's entries of a piece, over what the product's epilogue wrote there.  An index that comes twice has the same delta twice.
 __global__ __launch_bounds__(256) void distill_entries_kernel(const int32_t *__restrict__ index, const float *__restrict__ delta, int64_t n, int top, int v0,
                                                               int piece, unsigned short *__restrict__ dl, int64_t ld) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    const int64_t v = (int64_t)index[i] - v0;
-    if (v >= 0 && v < piece) dl[i / top * ld + v] = float_bf16(delta[i]);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t v = (int64_t)index[i] - v0;
+        if (v >= 0 && v < piece) dl[i / top * ld + v] = float_bf16(delta[i]);
+    }
 }
 // fp32: dl in the place of a row's 256 logits, then the teacher's entries among them.  COUNT: with up to 64 rows every workgroup counts those with
 // weight itself, a launch less (777 rows, 16000 entries: 52 us so, 26 without).
@@ -982,7 +988,7 @@ void linear_distill_fwd(hipStream_t st, int dtype, const void *x, const void *w,
     }
     const auto rows_kernel = [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL(distill_rows_kernel<T>, dim3(p.rows), dim3(256), 0, st, (const T *)x, (const T *)w, index, target, target_lse,
+        hipLaunchKernelGGL(distill_rows_kernel<T>, dim3(p.rows), dim3(64 * DISTILL_WAVES), 0, st, (const T *)x, (const T *)w, index, target, target_lse,
                            merged ? nullptr : part, parts, p.rows, lse, mass, delta, row_loss, width, vocab, top, heat);
         hip_check(hipGetLastError(), "linear_distill rows launch");
     };
@@ -1010,7 +1016,7 @@ void linear_distill_bwd(hipStream_t st, int dtype, const void *x, const void *w,
         [&](const GemmShape &g, unsigned short *d, int64_t ld, int v0, int piece) {
             gemm_bf16<false, false>(st, g, DistillGradEpilogue{mass, lse, d, ld, p.rows, piece, 1.f / heat}, "linear_distill gradient launch");
             const int64_t n = rows * top;
-            hipLaunchKernelGGL(distill_entries_kernel, dim3((unsigned)cut(n, 256)), dim3(256), 0, st, index, delta, n, top, v0, piece, d, ld);
+            hipLaunchKernelGGL(distill_entries_kernel, dim3((unsigned)std::min<int64_t>(cut(n, 256), 1 << 16)), dim3(256), 0, st, index, delta, n, top, v0, piece, d, ld);
             hip_check(hipGetLastError(), "linear_distill entries launch");
         },
         [&](float *d, int v0, int piece) {
