@@ -353,6 +353,7 @@ __global__ __launch_bounds__(256) void ce_piece_grad_kernel(float *__restrict__ 
 // twice gets the same number twice.  Bound by reading rows * top rows of w, most of them from the caches: 8192 rows, 64 entries, 4096 columns, bf16
 // (4.3 GB): 550 us, one entry at a time to a wave 640; 1000 rows, 64 entries, 1024 columns (131 MB): 24 us.
 constexpr int DISTILL_TOP = 1024;      // entries of a row, at most
+constexpr int DISTILL_TAIL = 16;       // fp32: more than a large vocabulary has over a multiple of 16, below
 // the lanes' shares of N dot products with one x: 16 bytes a lane and step, the rest of a row value by value
 template <int N>
 __device__ __forceinline__ void distill_dots(const float *x, const float *const (&w)[N], int width, int l, float (&s)[N]) {
@@ -392,8 +393,8 @@ __global__ __launch_bounds__(64 * DISTILL_WAVES) void distill_rows_kernel(const 
                                                                           const float *__restrict__ target, const float *__restrict__ target_lse,
                                                                           const float2 *__restrict__ part, int parts, int rows, float *__restrict__ lse,
                                                                           float *__restrict__ mass, float *__restrict__ delta, float *__restrict__ row_loss,
-                                                                          int width, int vocab, int top, float heat) {
-    __shared__ float z[DISTILL_TOP], p[DISTILL_TOP];
+                                                                          int width, int vocab, int tail, int top, float heat) {
+    __shared__ float z[DISTILL_TOP], p[DISTILL_TOP], last[DISTILL_TAIL];
     __shared__ int at[DISTILL_TOP];
     __shared__ unsigned seen[DISTILL_TOP];      // a bit for each value of an index's lowest 15 bits
     __shared__ Soft joined[DISTILL_WAVES];
@@ -419,13 +420,14 @@ __global__ __launch_bounds__(64 * DISTILL_WAVES) void distill_rows_kernel(const 
         const unsigned v = at[j] & 0x7fff, bit = 1u << (v & 31);
         if (at[j] >= 0 && (atomicOr(&seen[v / 32], bit) & bit)) twice = 1;
     }
-    const auto dots = [&](int j0, auto n) {      // entries j0 .. j0 + N - 1; one that is none repeats another
+    // entries j0 .. j0 + N - 1 of `n`, whose vocabulary indices are which(j); one that is none repeats another
+    const auto dots = [&](int j0, int end, auto n, auto which, float *out) {
         constexpr int N = decltype(n)::value;
         const T *row[N];
         int v[N], some = -1;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            v[j] = __builtin_amdgcn_readfirstlane(j0 + j < top ? at[j0 + j] : -1);
+            v[j] = __builtin_amdgcn_readfirstlane(j0 + j < end ? which(j0 + j) : -1);
             some = max(some, v[j]);
         }
         if (some < 0) return;
@@ -436,13 +438,16 @@ __global__ __launch_bounds__(64 * DISTILL_WAVES) void distill_rows_kernel(const 
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             s[j] = wave_sum(s[j]);
-            if (l == 0 && j0 + j < top) z[j0 + j] = s[j] / heat;
+            if (l == 0 && j0 + j < end) out[j0 + j] = s[j] / heat;
         }
     };
+    const auto entry = [&](int j) { return at[j]; };
     if (top >= 16)
-        for (int j = 4 * wave; j < top; j += 4 * DISTILL_WAVES) dots(j, std::integral_constant<int, 4>());
+        for (int j = 4 * wave; j < top; j += 4 * DISTILL_WAVES) dots(j, top, std::integral_constant<int, 4>(), entry, z);
     else
-        for (int j = wave; j < top; j += DISTILL_WAVES) dots(j, std::integral_constant<int, 1>());
+        for (int j = wave; j < top; j += DISTILL_WAVES) dots(j, top, std::integral_constant<int, 1>(), entry, z);
+    for (int j = 2 * wave; j < tail; j += 2 * DISTILL_WAVES)
+        dots(j, tail, std::integral_constant<int, 2>(), [&](int i) { return vocab - tail + i; }, last);
     if (part) {
         const float m = wave_max(a.m);
         a = Soft{m, wave_sum(a.m == -INFINITY ? a.s : a.s * exp_of(a.m - m))};
@@ -456,10 +461,15 @@ __global__ __launch_bounds__(64 * DISTILL_WAVES) void distill_rows_kernel(const 
         a = joined[0];
 #pragma unroll
         for (int i = 1; i < DISTILL_WAVES; ++i) a = soft_join(a, joined[i]);
+    } else {
+        ls = lse[t];
+        a = ls == INFINITY ? Soft{3.4028235e38f, INFINITY} : Soft{ls, ls == -INFINITY ? 0.f : 1.f};
+    }
+    if (part || tail) {
+        for (int j = 0; j < tail; ++j) a = soft_join(a, last[j] == INFINITY ? Soft{3.4028235e38f, INFINITY} : Soft{last[j], 1.f});
         ls = a.m + logf(a.s);
         if (l == 0) lse[t] = ls;
-    } else
-        ls = lse[t];
+    }
     float norm;
     if (target_lse) norm = target_lse[t];
     else {
@@ -560,6 +570,66 @@ __global__ __launch_bounds__(256) void distill_piece_grad_kernel(float *__restri
         const int64_t e = (int64_t)index[t * top + j] - v0;
         if (e >= from && e < to) row[e] = delta[t * top + j] * f;
     }
+}
+
+// fp32: the `tail` entries that a large vocabulary has over a multiple of 16, from v0 on.  As a piece of their own they took six launches of the matrix
+// products, mostly empty tiles: both passes of 100 rows, 512 columns, 5003 entries 149 us, with
+// these kernels 101; 777 rows, 1000 columns, 16001 entries 819 and 775.  A workgroup to a row: their
+// logits, dl (kept for dw), and their share of dx, which is there already.
+__global__ __launch_bounds__(256) void distill_tail_kernel(const float *__restrict__ x, const float *__restrict__ w, const int32_t *__restrict__ index,
+                                                           const float *__restrict__ lse, const float *__restrict__ mass, const float *__restrict__ delta,
+                                                           const float *__restrict__ inv, float *__restrict__ dl, float *__restrict__ dx, int rows, int width,
+                                                           int v0, int tail, int top, float heat) {
+    __shared__ float d[DISTILL_TAIL];
+    const int64_t t = blockIdx.x;
+    const int wave = threadIdx.x / 64, l = threadIdx.x & 63;
+    const float m = mass[t], f = *inv;
+    x += t * width;
+    w += (int64_t)v0 * width;
+    if (threadIdx.x < DISTILL_TAIL) d[threadIdx.x] = 0.f;
+    const float *row[4];
+    float s[4] = {};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) row[j] = w + (int64_t)min(4 * wave + j, tail - 1) * width;
+    if (m != 0.f && 4 * wave < tail) distill_dots(x, row, width, l, s);
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        s[j] = wave_sum(s[j]);
+        if (l == 0 && m != 0.f && 4 * wave + j < tail) d[4 * wave + j] = m * expf(s[j] / heat - lse[t]) * f;
+    }
+    __syncthreads();
+    for (int j = threadIdx.x; j < top; j += 256) {
+        const int64_t e = (int64_t)index[t * top + j] - v0;
+        if (e >= 0 && e < tail) d[e] = delta[t * top + j] * f;
+    }
+    __syncthreads();
+    if (threadIdx.x < DISTILL_TAIL) dl[t * DISTILL_TAIL + threadIdx.x] = d[threadIdx.x];
+    for (int c = threadIdx.x; c < width; c += 256) {
+        float sum = dx[t * width + c];
+        for (int j = 0; j < tail; ++j) sum = fmaf(d[j], w[(int64_t)j * width + c], sum);
+        dx[t * width + c] = sum;
+    }
+}
+// 64 columns of dw's last rows over a range of rows (grid y), or, of the only range, the result
+__global__ __launch_bounds__(256) void distill_tail_wgrad_kernel(const float *__restrict__ x, const float *__restrict__ dl, int64_t rows, int64_t per, int width, int tail,
+                                                                 float *__restrict__ part) {
+    __shared__ float sums[4][DISTILL_TAIL][64];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x & 63, c = blockIdx.x * 64 + l;
+    const int64_t from = blockIdx.y * per, to = min(rows, from + per);
+    float acc[DISTILL_TAIL] = {};
+#pragma unroll 4
+    for (int64_t t = from + wave; t < to; t += 4) {
+        const float v = x[t * width + min(c, width - 1)];
+#pragma unroll
+        for (int j = 0; j < DISTILL_TAIL; ++j) acc[j] = fmaf(dl[t * DISTILL_TAIL + j], v, acc[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < DISTILL_TAIL; ++j) sums[wave][j][l] = acc[j];
+    __syncthreads();
+    if (c >= width) return;
+    for (int j = wave; j < tail; j += 4)
+        part[((int64_t)blockIdx.y * tail + j) * width + c] = (sums[0][j][l] + sums[1][j][l]) + (sums[2][j][l] + sums[3][j][l]);
 }
 
 // fp32 and few rows: dx += dl W, which reads all of W for rows * 2 operations an entry.  A matrix tile would be mostly empty, and its few
@@ -790,8 +860,9 @@ CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab) {
     return p;
 }
 
-void check_ws(const CePlan &p, const void *ws, size_t ws_bytes) {
-    if (!ws || (int64_t)ws_bytes < p.bytes()) throw KernelError("linear_ce: workspace of " + std::to_string(ws_bytes) + " bytes, " + std::to_string(p.bytes()) + " needed");
+void check_ws(const CePlan &p, const void *ws, size_t ws_bytes, int64_t front = 0) {
+    if (!ws || (int64_t)ws_bytes < front + p.bytes())
+        throw KernelError("linear_ce: workspace of " + std::to_string(ws_bytes) + " bytes, " + std::to_string(front + p.bytes()) + " needed");
     if ((uintptr_t)ws % 256) throw KernelError("linear_ce: the workspace must be 256-byte aligned");
 }
 void check_aligned(const CePlan &p, std::initializer_list<const void *> ptrs) {
@@ -953,9 +1024,18 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
 }
 
 namespace {
+// the vocabulary without its tail, which has kernels of its own
+int distill_tail(int dtype, int vocab) { return dtype == MONET_F32 && vocab > 4096 ? vocab % DISTILL_TAIL : 0; }
 CePlan distill_plan(bool grad, int dtype, int64_t rows, int width, int vocab, int top) {
     if (top < 1 || top > DISTILL_TOP) throw KernelError("linear_distill: 1 to " + std::to_string(DISTILL_TOP) + " entries a row");
-    return ce_plan(grad, dtype, rows, width, vocab);
+    return ce_plan(grad, dtype, rows, width, vocab - distill_tail(dtype, vocab));
+}
+int64_t distill_tail_ranges(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(64, rows / 64)); }
+// bytes in front of the plan's: dl of the tail, and dw's parts if there are several
+int64_t distill_tail_bytes(bool grad, int dtype, int64_t rows, int width, int vocab) {
+    const int64_t tail = distill_tail(dtype, vocab), ranges = distill_tail_ranges(rows);
+    if (!grad || !tail) return 0;
+    return up(rows * DISTILL_TAIL * 4, 256) + (ranges > 1 ? up(ranges * tail * width * 4, 256) : 0);
 }
 void distill_check(float heat) {
     if (!(heat > 0.f) || !std::isfinite(heat) || !std::isfinite(1.f / heat)) throw KernelError("linear_distill: the temperature must be positive and finite");
@@ -963,8 +1043,8 @@ void distill_check(float heat) {
 }  // namespace
 
 size_t linear_distill_workspace_bytes(bool grad, int dtype, int64_t rows, int width, int vocab, int top) {
-    distill_plan(grad, dtype, rows, width, vocab, top);
-    return linear_ce_workspace_bytes(grad, dtype, rows, width, vocab);
+    const int64_t forward = distill_plan(false, dtype, rows, width, vocab, top).bytes();
+    return (size_t)std::max(forward, distill_plan(grad, dtype, rows, width, vocab, top).bytes() + distill_tail_bytes(grad, dtype, rows, width, vocab));
 }
 
 void linear_distill_fwd(hipStream_t st, int dtype, const void *x, const void *w, const int32_t *index, const float *target, const float *target_lse,
@@ -989,7 +1069,7 @@ void linear_distill_fwd(hipStream_t st, int dtype, const void *x, const void *w,
     const auto rows_kernel = [&](auto t) {
         using T = decltype(t);
         hipLaunchKernelGGL(distill_rows_kernel<T>, dim3(p.rows), dim3(64 * DISTILL_WAVES), 0, st, (const T *)x, (const T *)w, index, target, target_lse,
-                           merged ? nullptr : part, parts, p.rows, lse, mass, delta, row_loss, width, vocab, top, heat);
+                           merged ? nullptr : part, parts, p.rows, lse, mass, delta, row_loss, width, vocab, distill_tail(dtype, vocab), top, heat);
         hip_check(hipGetLastError(), "linear_distill rows launch");
     };
     if (p.bf16) rows_kernel((unsigned short)0);
@@ -1002,12 +1082,16 @@ void linear_distill_bwd(hipStream_t st, int dtype, const void *x, const void *w,
                         const float *delta, void *dx, void *dw, int64_t rows, int width, int vocab, int top, float heat, bool accumulate, void *ws,
                         size_t ws_bytes) {
     const CePlan p = distill_plan(true, dtype, rows, width, vocab, top);
+    const int64_t front = distill_tail_bytes(true, dtype, rows, width, vocab);
+    const int tail = distill_tail(dtype, vocab);
     distill_check(heat);
-    check_ws(p, ws, ws_bytes);
+    check_ws(p, ws, ws_bytes, front);
     check_aligned(p, {x, w, dx, dw});
     check_words({index, lse, mass, delta});
+    float *dl = (float *)ws;
+    ws = (char *)ws + front;
     float *inv = (float *)ws;
-    const bool count = p.bf16 || rows > 64;
+    const bool count = p.bf16 || rows > 64 || tail;
     if (count) {
         hipLaunchKernelGGL(distill_inv_kernel, dim3(1), dim3(1024), 0, st, mass, p.rows, heat, inv);
         hip_check(hipGetLastError(), "linear_distill count launch");
@@ -1024,6 +1108,19 @@ void linear_distill_bwd(hipStream_t st, int dtype, const void *x, const void *w,
                                d, piece, v0, mass, lse, index, delta, top, inv, p.rows, heat);
             hip_check(hipGetLastError(), "linear_distill gradient launch");
         });
+    if (!tail) return;
+    hipLaunchKernelGGL(distill_tail_kernel, dim3(p.rows), dim3(256), 0, st, (const float *)x, (const float *)w, index, lse, mass, delta, inv, dl, (float *)dx, p.rows,
+                       width, vocab - tail, tail, top, heat);
+    hip_check(hipGetLastError(), "linear_distill tail launch");
+    const int64_t ranges = distill_tail_ranges(rows);
+    float *out = (float *)dw + (int64_t)(vocab - tail) * width, *part = ranges > 1 ? dl + up(rows * DISTILL_TAIL, 64) : out;
+    hipLaunchKernelGGL(distill_tail_wgrad_kernel, dim3((unsigned)cut(width, 64), (unsigned)ranges), dim3(256), 0, st, (const float *)x, dl, rows, cut(rows, ranges), width,
+                       tail, part);
+    hip_check(hipGetLastError(), "linear_distill tail launch");
+    if (ranges == 1) return;
+    hipLaunchKernelGGL(ce_few_rows_join_kernel, dim3((unsigned)cut((int64_t)tail * width, 64)), dim3(1024), 0, st, part, (int)ranges, tail * width, out, 0);
+    hip_check(hipGetLastError(), "linear_distill tail launch");
 }
+
 
 }  // namespace monet

@@ -159,6 +159,35 @@ def test_layernorm_matches_64_bits(case, dtype, pdtype):
 
 
 @BOTH
+@pytest.mark.parametrize("rows,cols", [((1 << 20) + 77, 3), (40000, 64), (5000, 1028), (1300, 4100)])
+def test_layernorm_of_many_rows(dtype, rows, cols):
+    """Rows in several turns of every workgroup, against the formulas in 64 bits on the GPU."""
+    torch = torch_mod()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    normal = lambda *shape: torch.randn(*shape, generator=g, device="cuda")   # noqa: E731
+    x, dy, gamma, beta = (normal(rows, cols) + 0.5).to(tdtype(dtype)), normal(rows, cols).to(tdtype(dtype)), 1 + 0.1 * normal(cols), normal(cols)
+    y, stats, dx, dg, db = layernorm_call(dtype, monet.F32, x, gamma, beta, dy)
+    x, dy, gamma, beta = x.double(), dy.double(), gamma.double(), beta.double()
+    c = x - x.mean(1, keepdim=True)
+    rstd = ((c * c).mean(1, keepdim=True) + EPS).rsqrt()
+    xh, gr = c * rstd, dy * gamma
+    a, b = gr.mean(1, keepdim=True), (gr * xh).mean(1, keepdim=True)
+    # first-order bounds as in layernorm_bounds, with each row's largest values in the place of its own
+    n, r = -(-cols // 64) + 16, R if dtype == monet.BF16 else 0.0
+    top = lambda t: t.abs().amax(1, keepdim=True)   # noqa: E731
+    exh = rstd * 2 * (n + 4) * U * top(x) + top(xh) * ((n + 6) * U + (n + 4) * U * top(x) * rstd * 2 * (n + 4) * U * top(x) * rstd + 8 * U)
+    assert ((y.double() - (xh * gamma + beta)).abs() <= 1.1 * (gamma.abs() * exh + 3 * U * ((xh * gamma).abs() + beta.abs()) + r * (xh * gamma + beta).abs())).all()
+    want = rstd * (gr - a - xh * b)
+    edx = rstd * ((n + 4) * U * top(gr) + exh * b.abs() + xh.abs() * (top(gr) * exh + (n + 6) * U * top(gr) * top(xh)) + 4 * U * (gr.abs() + a.abs() + (xh * b).abs()))
+    assert ((dx.double() - want).abs() <= 1.1 * (edx + want.abs() * (r + 2 * (n + 8) * U))).all()
+    # a column's sum: a workgroup's rows one after another, 512 workgroups at most in 16 shares; no longer a chain than rows / 8 + 64 (few columns: rows / 4)
+    chain = rows / 4 + 64
+    assert ((dg.double() - (dy * xh).sum(0)).abs() <= 1.1 * ((dy.abs() * exh).sum(0) + chain * U * (dy * xh).abs().sum(0))).all()
+    assert ((db.double() - dy.sum(0)).abs() <= 1.1 * chain * U * dy.abs().sum(0)).all()
+
+
+@BOTH
 @pytest.mark.parametrize("cols", [48, 203, 4096, 20000, 40000])
 def test_layernorm_parts(dtype, cols):
     """No weights, no statistics; single results of the backward pass; in place."""
@@ -325,6 +354,21 @@ def test_rope_in_place_and_without_positions(dtype, dim, rot, interleaved):
     assert torch.equal(back, rope_call(dtype, want, at, freqs, heads, dim, interleaved, 1.0, True))
 
 
+@BOTH
+@pytest.mark.parametrize("n,heads,dim,rot,interleaved", [(70001, 1, 16, 16, False), (9001, 3, 96, 40, True), (4100, 10, 128, 128, False), (1500, 2, 80, 80, False)])
+def test_rope_of_many_tokens(dtype, n, heads, dim, rot, interleaved):
+    """Several tokens to a workgroup, the last one with fewer."""
+    torch = torch_mod()
+    rng = np.random.default_rng(n)
+    x, tx = rounded(rng.standard_normal((n, heads, dim)), dtype)
+    at = rng.integers(0, 1 << 20, n).astype(np.int32)
+    freqs = nm.rope_freqs(rot, 10000.0)
+    got = rope_call(dtype, tx, torch.from_numpy(at).cuda(), freqs, heads, dim, interleaved, 1.0, False, 0, 8)
+    want = nm.rope_fwd(x, at.astype(np.int64), freqs, interleaved)
+    within(host(got), want, rope_bounds(x, want, at.astype(np.int64), freqs, interleaved, 1.0, dtype), "y")
+    assert torch.equal(got[..., rot:], tx[..., rot:])
+
+
 def test_rope_of_no_tokens_and_special_values():
     torch = torch_mod()
     freqs = nm.rope_freqs(64, 10000.0)
@@ -441,7 +485,7 @@ DISTILL_CASES = [
     # rows, width, vocab, top, temperature
     (1, 8, 1, 1, 1.0), (1, 64, 2, 3, 2.0), (24, 128, 1009, 8, 2.0), (130, 72, 257, 64, 1.0), (5, 200, 5003, 33, 0.7), (300, 64, 700, 5, 3.5),
     (257, 264, 4111, 16, 1.0), (64, 8, 9000, 257, 4.0), (33, 1032, 300, 1024, 1.0), (9, 520, 2000, 2, 1.0), (1, 144, 8209, 20, 1.0), (7, 328, 8215, 65, 2.0),
-    (17, 520, 4097, 9, 2.0),
+    (17, 520, 4097, 9, 2.0), (1100, 24, 4110, 3, 1.0), (140, 33 * 8, 4127, 40, 2.0),
 ]
 
 
@@ -487,12 +531,13 @@ def test_linear_distill_without_an_entry(dtype):
 
 
 @BOTH
-def test_linear_distill_special_values_stay_in_their_row(dtype):
+@pytest.mark.parametrize("vocab", [1000, 4113])
+def test_linear_distill_special_values_stay_in_their_row(dtype, vocab):
     """Logits in the thousands, an infinity and a NaN in rows' inputs, a teacher's logit that is infinite: other rows do not change, but for their
     rounding in fp32, whose products take another form in a tile with such a value.  Both results are within a bound of the exact one, so they are
     within twice the bound of each other."""
     torch = torch_mod()
-    (x64, x), (w64, w), index, target = distill_inputs(40, 64, 1000, 6, dtype, 4)
+    (x64, x), (w64, w), index, target = distill_inputs(40, 64, vocab, 6, dtype, 4)
     index[:8] = np.arange(48).reshape(8, 6)
     index[6] = -1                                       # a row without an entry, with a NaN
     target[:8] = 1.0
