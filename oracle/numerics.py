@@ -438,7 +438,8 @@ def linear_distill_fwd(x, w, index, target, temperature, target_lse=None):
         if len(has) == 0:
             continue
         t = target[r, has] / temperature
-        logp = t - (np.log(np.exp(t - t.max()).sum()) + t.max() if target_lse is None else target_lse[r])
+        d = t - t.max()                # first: the logarithm would be lost beside logits of 1e38
+        logp = d - np.log(np.exp(d).sum()) if target_lse is None else t - target_lse[r]
         p = np.exp(logp)
         at = index[r, has]
         loss[r], mass[r] = (p * (logp + lse[r] - z[r, at])).sum(), p.sum()

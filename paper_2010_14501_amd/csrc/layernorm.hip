@@ -423,7 +423,9 @@ int64_t layernorm_ranges(int dtype, int64_t rows, int cols) {
     dtype == MONET_F32 ? layernorm_form<float, true>(cols, form) : layernorm_form<unsigned short, true>(cols, form);
     // few values: one workgroup, which needs no second launch (37 rows of 203 in fp32, both passes: 24 us, with a join 27.5)
     if (rows && rows_at_once && rows * cols <= 1 << 14 && rows <= 8 * rows_at_once) return 1;
-    if (rows_at_once) return std::min(groups, cut(rows, rows_at_once));
+    // three turns or more to a workgroup, since a part costs as much as four rows of bf16 (1000 x 8192: backward pass 24 us with two turns, 18.5 with three), unless fewer than
+    // 128 workgroups are left
+    if (rows_at_once) return std::min({groups, cut(rows, rows_at_once), std::max<int64_t>(128, cut(rows, 3 * rows_at_once))});
     return std::min<int64_t>(cut(rows, 32), std::max<int64_t>(1, 1024 / cut(cols, 64)));
 }
 void layernorm_shape(int dtype, int64_t rows, int cols) {

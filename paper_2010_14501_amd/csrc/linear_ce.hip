@@ -470,21 +470,23 @@ __global__ __launch_bounds__(64 * DISTILL_WAVES) void distill_rows_kernel(const 
         ls = a.m + logf(a.s);
         if (l == 0) lse[t] = ls;
     }
-    float norm;
+    // log p = (target - most) / T - norm; the difference first, so that the lowest numbers of all do not become infinite
+    float most = 0.f, norm;
     if (target_lse) norm = target_lse[t];
     else {
-        float most = -INFINITY, sum = 0.f;
+        most = -INFINITY;
         for (int j = l; j < top; j += 64)
-            if (at[j] >= 0) most = fmaxf(most, target[j] / heat);
+            if (at[j] >= 0) most = fmaxf(most, target[j]);
         most = wave_max(most);
+        float sum = 0.f;
         for (int j = l; j < top; j += 64)
-            if (at[j] >= 0 && target[j] != -INFINITY) sum += expf(target[j] / heat - most);
-        norm = most + logf(wave_sum(sum));
+            if (at[j] >= 0 && target[j] != -INFINITY) sum += expf((target[j] - most) / heat);
+        norm = logf(wave_sum(sum));
     }
     float loss = 0.f, m = 0.f;
     for (int j = l; j < top; j += 64) {
         // an entry of weight 0 adds nothing, whatever the row's logits are
-        const float logp = target[j] / heat - norm, pj = at[j] < 0 || target[j] == -INFINITY ? 0.f : expf(logp);
+        const float logp = (target[j] - most) / heat - norm, pj = at[j] < 0 || target[j] == -INFINITY ? 0.f : expf(logp);
         p[j] = pj;
         m += pj;
         if (pj != 0.f) loss += pj * (logp + (ls - z[j]));

@@ -558,6 +558,29 @@ def test_linear_distill_special_values_stay_in_their_row(dtype, vocab):
 
 
 @BOTH
+@pytest.mark.parametrize("heat", [0.5, 1.0, 4.0])
+def test_linear_distill_masked_with_the_lowest_number(dtype, heat):
+    """Entries at fp32's lowest number have no weight beside others; a row of nothing else is uniform."""
+    torch = torch_mod()
+    (x, tx), (w, tw), index, target = distill_inputs(12, 64, 500, 9, dtype, 6)
+    index[:] = np.arange(12 * 9).reshape(12, 9)
+    target[np.isinf(target)] = 0.0
+    lowest = np.finfo(np.float32).min
+    target[::2, 3:] = lowest
+    target[5] = lowest
+    target[7] = -target[5]                       # and at the largest one
+    got = distill_call(dtype, tx, tw, torch.from_numpy(index).cuda(), torch.from_numpy(target).cuda(), heat)
+    target = target.astype(np.float64)
+    fwd = nm.linear_distill_fwd(x, w, index, target, heat)
+    want = [np.array([fwd[0]]), *fwd[1:], *nm.linear_distill_bwd(x, w, index, target, heat)]
+    # the bounds of the same weights from ordinary numbers: 100 T below the row's largest is 0 in fp32 and nearly so in 64 bits (e^-100)
+    plain = np.where(np.abs(target) > 1e38, np.where(np.abs(target).min(axis=1, keepdims=True) > 1e38, 0.0, target.max(axis=1, keepdims=True) - 100 * heat), target)
+    for name, g, v, b in zip(("loss", "lse", "mass", "delta", "dx", "dw"), got, want, distill_bounds(x, w, index, plain, heat, None, dtype)):
+        within(host(g), v, b, name)
+    assert abs(host(got[2]) - 1).max() < 16 * U
+
+
+@BOTH
 def test_linear_distill_of_one_entry_is_the_cross_entropy(dtype):
     torch = torch_mod()
     rows, width, vocab = 300, 136, 2003
