@@ -354,38 +354,48 @@ __global__ __launch_bounds__(256) void ce_piece_grad_kernel(float *__restrict__ 
 // (4.3 GB): 550 us, one entry at a time to a wave 640; 1000 rows, 64 entries, 1024 columns (131 MB): 24 us.
 constexpr int DISTILL_TOP = 1024;      // entries of a row, at most
 constexpr int DISTILL_TAIL = 16;       // fp32: more than a large vocabulary has over a multiple of 16, below
-// the lanes' shares of N dot products with one x: 16 bytes a lane and step, the rest of a row value by value
-template <int N>
-__device__ __forceinline__ void distill_dots(const float *x, const float *const (&w)[N], int width, int l, float (&s)[N]) {
+// N dot products with one x by G lanes, of which this is lane g: 16 bytes at a time, and of a row of floats that is no multiple of four the rest value by
+// value.  The sums are in all of the lanes.
+template <int G>
+__device__ __forceinline__ float distill_lanes_sum(float v) {
+    static_assert(G == 16 || G == 64, "");
+    return G == 64 ? wave_sum(v) : row_sum(v);
+}
+template <int G, int N>
+__device__ __forceinline__ void distill_dots(const float *x, const float *const (&w)[N], int width, int g, float (&s)[N]) {
     typedef float any __attribute__((ext_vector_type(4), aligned(4)));
-    int c = 4 * l;
-    for (; c + 4 <= width; c += 256) {
+    int c = 4 * g;
+    for (; c + 4 <= width; c += 4 * G) {
         const any f = *(const any *)(x + c);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const any g = *(const any *)(w[j] + c);
+            const any v = *(const any *)(w[j] + c);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[j] = fmaf(f[e], g[e], s[j]);
+            for (int e = 0; e < 4; ++e) s[j] = fmaf(f[e], v[e], s[j]);
         }
     }
     for (int e = c; e < min(c + 4, width); ++e)
 #pragma unroll
         for (int j = 0; j < N; ++j) s[j] = fmaf(x[e], w[j][e], s[j]);
+#pragma unroll
+    for (int j = 0; j < N; ++j) s[j] = distill_lanes_sum<G>(s[j]);
 }
-template <int N>
-__device__ __forceinline__ void distill_dots(const unsigned short *x, const unsigned short *const (&w)[N], int width, int l, float (&s)[N]) {
-    for (int c = 8 * l; c < width; c += 512) {
+template <int G, int N>
+__device__ __forceinline__ void distill_dots(const unsigned short *x, const unsigned short *const (&w)[N], int width, int g, float (&s)[N]) {
+    for (int c = 8 * g; c < width; c += 8 * G) {
         const uintx4 f = *(const uintx4 *)(x + c);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const uintx4 g = *(const uintx4 *)(w[j] + c);
+            const uintx4 v = *(const uintx4 *)(w[j] + c);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                s[j] = fmaf(__uint_as_float(f[q] << 16), __uint_as_float(g[q] << 16), s[j]);
-                s[j] = fmaf(__uint_as_float(f[q] & 0xffff0000u), __uint_as_float(g[q] & 0xffff0000u), s[j]);
+                s[j] = fmaf(__uint_as_float(f[q] << 16), __uint_as_float(v[q] << 16), s[j]);
+                s[j] = fmaf(__uint_as_float(f[q] & 0xffff0000u), __uint_as_float(v[q] & 0xffff0000u), s[j]);
             }
         }
     }
+#pragma unroll
+    for (int j = 0; j < N; ++j) s[j] = distill_lanes_sum<G>(s[j]);
 }
 constexpr int DISTILL_WAVES = 8;
 template <class T>
@@ -394,8 +404,9 @@ __global__ __launch_bounds__(64 * DISTILL_WAVES) void distill_rows_kernel(const 
                                                                           const float2 *__restrict__ part, int parts, int rows, float *__restrict__ lse,
                                                                           float *__restrict__ mass, float *__restrict__ delta, float *__restrict__ row_loss,
                                                                           int width, int vocab, int tail, int top, float heat) {
-    __shared__ float z[DISTILL_TOP], p[DISTILL_TOP], last[DISTILL_TAIL];
-    __shared__ int at[DISTILL_TOP];
+    __shared__ float z[DISTILL_TOP], last[DISTILL_TAIL];
+    __shared__ alignas(16) float p[DISTILL_TOP];
+    __shared__ alignas(16) int at[DISTILL_TOP];
     __shared__ unsigned seen[DISTILL_TOP];      // a bit for each value of an index's lowest 15 bits
     __shared__ Soft joined[DISTILL_WAVES];
     __shared__ int twice;                       // an index may come more than once
@@ -414,40 +425,51 @@ __global__ __launch_bounds__(64 * DISTILL_WAVES) void distill_rows_kernel(const 
             a = soft_join(a, Soft{v.x, v.y});
         }
     }
-    for (int j = threadIdx.x; j < top; j += THREADS) at[j] = (unsigned)index[j] < (unsigned)vocab ? index[j] : -1;
+    const int whole = (top + 3) & ~3;       // entries behind the last one have no index and no weight
+    for (int j = threadIdx.x; j < whole; j += THREADS) {
+        const int v = j < top ? index[j] : -1;
+        at[j] = (unsigned)v < (unsigned)vocab ? v : -1;
+        if (j >= top) p[j] = 0.f;
+    }
     __syncthreads();
     for (int j = threadIdx.x; j < top; j += THREADS) {
         const unsigned v = at[j] & 0x7fff, bit = 1u << (v & 31);
         if (at[j] >= 0 && (atomicOr(&seen[v / 32], bit) & bit)) twice = 1;
     }
-    // entries j0 .. j0 + N - 1 of `n`, whose vocabulary indices are which(j); one that is none repeats another
-    const auto dots = [&](int j0, int end, auto n, auto which, float *out) {
-        constexpr int N = decltype(n)::value;
-        const T *row[N];
-        int v[N], some = -1;
+    // G lanes to an entry of `end`, N entries at a time; their vocabulary indices are which(j), below 0 for one that is none
+    const auto dots = [&](int end, auto lanes, auto n, auto which, float *out) {
+        constexpr int G = decltype(lanes)::value, N = decltype(n)::value;
+        for (int j0 = N * (threadIdx.x / G); j0 < end; j0 += N * (THREADS / G)) {
+            const T *row[N];
+            float s[N] = {};
+            int some = -1, v[N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            v[j] = __builtin_amdgcn_readfirstlane(j0 + j < end ? which(j0 + j) : -1);
-            some = max(some, v[j]);
-        }
-        if (some < 0) return;
-        float s[N] = {};
+            for (int j = 0; j < N; ++j) {
+                v[j] = j0 + j < end ? which(j0 + j) : -1;
+                if (G == 64) v[j] = __builtin_amdgcn_readfirstlane(v[j]);
+                some = max(some, v[j]);
+            }
 #pragma unroll
-        for (int j = 0; j < N; ++j) row[j] = w + (int64_t)(v[j] < 0 ? some : v[j]) * width;
-        distill_dots(x + t * width, row, width, l, s);
+            for (int j = 0; j < N; ++j) row[j] = w + (int64_t)max(v[j] < 0 ? some : v[j], 0) * width;      // one that is none repeats another, or the first
+            distill_dots<G>(x + t * width, row, some < 0 ? 0 : width, threadIdx.x % G, s);
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            s[j] = wave_sum(s[j]);
-            if (l == 0 && j0 + j < end) out[j0 + j] = s[j] / heat;
+            for (int j = 0; j < N; ++j)
+                if (threadIdx.x % G == 0 && j0 + j < end) out[j0 + j] = s[j] / heat;
         }
     };
+    // a wave to an entry where the row has its 16 bytes for every lane, else a quarter of one: 64 rows, 99 entries, 160 columns, bf16 13.5 us, with waves 22.6;
+    // 1320 rows, 69 entries, 4000 columns 70 and 50
     const auto entry = [&](int j) { return at[j]; };
-    if (top >= 16)
-        for (int j = 4 * wave; j < top; j += 4 * DISTILL_WAVES) dots(j, top, std::integral_constant<int, 4>(), entry, z);
-    else
-        for (int j = wave; j < top; j += DISTILL_WAVES) dots(j, top, std::integral_constant<int, 1>(), entry, z);
-    for (int j = 2 * wave; j < tail; j += 2 * DISTILL_WAVES)
-        dots(j, tail, std::integral_constant<int, 2>(), [&](int i) { return vocab - tail + i; }, last);
+    using std::integral_constant;
+    const integral_constant<int, 16> quarter;
+    const integral_constant<int, 64> whole_wave;
+    if (width * (int64_t)sizeof(T) >= 1024) {
+        if (top >= 32) dots(top, whole_wave, integral_constant<int, 4>(), entry, z);
+        else if (top >= 16) dots(top, whole_wave, integral_constant<int, 2>(), entry, z);
+        else dots(top, whole_wave, integral_constant<int, 1>(), entry, z);
+    } else if (top >= 48) dots(top, quarter, integral_constant<int, 2>(), entry, z);
+    else dots(top, quarter, integral_constant<int, 1>(), entry, z);
+    if (tail) dots(tail, quarter, integral_constant<int, 1>(), [&](int i) { return vocab - tail + i; }, last);
     if (part) {
         const float m = wave_max(a.m);
         a = Soft{m, wave_sum(a.m == -INFINITY ? a.s : a.s * exp_of(a.m - m))};
@@ -501,7 +523,14 @@ __global__ __launch_bounds__(64 * DISTILL_WAVES) void distill_rows_kernel(const 
             float same = p[j];
             if (search) {
                 same = 0.f;
-                for (int i = 0; i < top; ++i) same += at[i] == at[j] ? p[i] : 0.f;
+                for (int i = 0; i < whole; i += 4) {
+                    const int4 v = *(const int4 *)(at + i);
+                    const float4 q = *(const float4 *)(p + i);
+                    same += v.x == at[j] ? q.x : 0.f;
+                    same += v.y == at[j] ? q.y : 0.f;
+                    same += v.z == at[j] ? q.z : 0.f;
+                    same += v.w == at[j] ? q.w : 0.f;
+                }
             }
             d = m * expf(z[j] - ls) - same;
         }
@@ -583,23 +612,17 @@ __global__ __launch_bounds__(256) void distill_tail_kernel(const float *__restri
                                                            const float *__restrict__ inv, float *__restrict__ dl, float *__restrict__ dx, int rows, int width,
                                                            int v0, int tail, int top, float heat) {
     __shared__ float d[DISTILL_TAIL];
+    static_assert(DISTILL_TAIL == 256 / 16, "");
     const int64_t t = blockIdx.x;
-    const int wave = threadIdx.x / 64, l = threadIdx.x & 63;
     const float m = mass[t], f = *inv;
     x += t * width;
     w += (int64_t)v0 * width;
-    if (threadIdx.x < DISTILL_TAIL) d[threadIdx.x] = 0.f;
-    const float *row[4];
-    float s[4] = {};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) row[j] = w + (int64_t)min(4 * wave + j, tail - 1) * width;
-    if (m != 0.f && 4 * wave < tail) distill_dots(x, row, width, l, s);
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        s[j] = wave_sum(s[j]);
-        if (l == 0 && m != 0.f && 4 * wave + j < tail) d[4 * wave + j] = m * expf(s[j] / heat - lse[t]) * f;
-    }
+    // 16 lanes to an entry
+    const int j = threadIdx.x / 16;
+    const float *row[1] = {w + (int64_t)min(j, tail - 1) * width};
+    float s[1] = {};
+    if (m != 0.f) distill_dots<16>(x, row, width, threadIdx.x & 15, s);
+    if (threadIdx.x % 16 == 0) d[j] = m != 0.f && j < tail ? m * expf(s[0] / heat - lse[t]) * f : 0.f;
     __syncthreads();
     for (int j = threadIdx.x; j < top; j += 256) {
         const int64_t e = (int64_t)index[t * top + j] - v0;
@@ -743,8 +766,9 @@ bool ce_few_logits(hipStream_t st, const float *x, const float *w, int width, in
     return true;
 }
 
-// out (+)= the sum over the ranges of part, in a fixed order: sixteen waves take a share of the ranges each
-__global__ __launch_bounds__(1024) void ce_few_rows_join_kernel(const float *__restrict__ part, int ranges, int n, float *__restrict__ out, int add) {
+// out (+)= the sum over the ranges of part, in a fixed order: sixteen waves take a share of the ranges each.  T bf16: times *by, rounded.
+template <class T = float>
+__global__ __launch_bounds__(1024) void ce_few_rows_join_kernel(const float *__restrict__ part, int ranges, int n, T *__restrict__ out, int add, const float *by = nullptr) {
     __shared__ float sums[16][64];
     const int wave = threadIdx.x / 64, l = threadIdx.x & 63, i = blockIdx.x * 64 + l;
     float sum = 0.f;
@@ -757,7 +781,8 @@ __global__ __launch_bounds__(1024) void ce_few_rows_join_kernel(const float *__r
     if (wave || i >= n) return;
 #pragma unroll
     for (int w = 1; w < 16; ++w) sum += sums[w][l];
-    out[i] = add ? out[i] + sum : sum;
+    if constexpr (std::is_same<T, float>::value) out[i] = add ? out[i] + sum : sum;
+    else out[i] = float_bf16((add ? bf16_float(out[i]) : 0.f) + sum * *by);
 }
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -766,18 +791,18 @@ int64_t cut(int64_t n, int64_t by) { return (n + by - 1) / by; }
 constexpr int64_t CE_PIECE_BYTES = 256ll << 20;      // a piece of logits or of their gradient
 
 // Results of few tiles leave CUs idle while their reduction is long: as many ranges as fill the card, of at least `least` indices.
-int ce_splits(int64_t tiles, int64_t red, int64_t least) {
-    return (int)std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), red / least, 16}));
+int ce_splits(int64_t tiles, int64_t red, int64_t least, int64_t most = 16) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>({256 / std::max<int64_t>(tiles, 1), red / least, most}));
 }
 
 // Ranges of the reduction over a piece in dx = dl W.  Large tiles (gemm_tile) where ranges of 4096 entries or more make whole rounds of one to a CU
 // (a range's fp32 sums cost 8 bytes of traffic for each result) and few of their entries lie outside the result: backward pass of 512 rows,
 // 2048 columns, 100000 entries 830 us, with small tiles 997; 4096 rows, 2048 columns, 50176 entries 2459 and 2542.  Small ones otherwise:
 // 4000 rows, 1600 columns, 50257 entries (112 large tiles; three ranges are 1.3 rounds) 2126 us, with large ones 2248.
-int ce_input_ranges(int64_t rows, int64_t width, int piece) {
+int ce_input_ranges(int64_t rows, int64_t width, int piece, int64_t most) {
     const int64_t large = cut(width, 256) * cut(rows, 256), ranges = cut(256, large);
     if (ranges <= 16 && piece / ranges >= 4096 && 5 * rows * width * ranges >= 4 * 65536 * up(large * ranges, 256)) return (int)ranges;
-    return ce_splits(cut(width, 128) * cut(rows, 128), piece, 512);
+    return ce_splits(cut(width, 128) * cut(rows, 128), piece, 512, most);
 }
 
 // How a call goes through the vocabulary, and its workspace: forward [hit][row_loss][part][product][logits (fp32)], backward
@@ -787,12 +812,19 @@ struct CePlan {
     bool bf16;
     int unit = 0;                   // bf16 forward: logits to a part
     int piece = 0;                  // logits of a piece
-    int ranges = 1, chunk = 0;      // bf16 backward: of the reduction over a piece in dx
+    int64_t most = 16;              // ranges of the reduction over a piece in dx, at most
+    int ranges = 1, chunk = 0;      // bf16 backward: those ranges
     int64_t product = 0;            // fp32: bytes for the products' partial results
     int64_t fixed = 0, per_col = 0;              // bytes without the pieces, and for each logit of a piece
 
     int64_t bytes() const { return fixed + per_col * piece; }
     int wgrad_splits(int piece) const { return ce_splits(cut(width, 128) * cut(piece, 128), rows, 64); }
+    // fp32: ranges in dx where its tiles are so few that `most` of them do not fill the card; 1: what the product chooses by itself, 16 at most.  205 rows, 80
+    // columns, 82288 entries: the product 49 us, in 16 ranges 163
+    int dgrad_splits(int piece) const {
+        const int64_t tiles = cut(rows, 128) * (width <= 64 ? 1 : cut(width, 128));
+        return most > 16 && 16 * tiles < 256 && !few_rows(piece) ? ce_splits(tiles, piece, 512, most) : 1;
+    }
     bool few_rows(int piece) const { return rows <= CE_FEW_ROWS || (rows <= 2 * CE_FEW_ROWS && (int64_t)piece * width <= 1 << 20); }      // twice: where W stays in L2
     int few_per(int piece) const {      // entries of W for a workgroup: four workgroups to a CU
         return (int)up(cut(piece, std::max<int64_t>(1, std::min<int64_t>(1024 / cut(width, 256), cut(piece, 64)))), 16);
@@ -816,13 +848,14 @@ struct CePlan {
     }
 };
 
-CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab) {
+CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab, int64_t most = 16) {
     if (dtype != MONET_F32 && dtype != MONET_BF16) throw KernelError("linear_ce: dtype must be MONET_F32 or MONET_BF16");
     if (rows < 1 || width < 1 || vocab < 1) throw KernelError("linear_ce: bad shape");
     const bool bf16 = dtype == MONET_BF16;
     if (bf16 && width % 8) throw KernelError("linear_ce: bf16 needs a width that is a multiple of 8");
     if (rows >= (1 << 24) || width > (1 << 20) || vocab > (1 << 28)) throw KernelError("linear_ce: shape too large");
     CePlan p{(int)rows, width, vocab, bf16};
+    p.most = most;
     if (bf16 && !grad) {
         if (!gemm_fits(vocab, rows, 1, width, width)) throw KernelError("linear_ce: rows * vocab too large");
         p.unit = gemm_tile(vocab, rows) / 2;
@@ -841,7 +874,7 @@ CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab) {
     }
     p.fixed = 256;
     if (bf16) {
-        p.ranges = ce_input_ranges(rows, width, p.piece);
+        p.ranges = ce_input_ranges(rows, width, p.piece, most);
         const int64_t ld = up(p.piece, 8);
         if (!gemm_fits(p.piece, rows, 1, width, width) || !gemm_fits(width, rows, p.ranges, width, ld) || !gemm_fits(width, p.piece, 1, width, ld))
             throw KernelError("linear_ce: rows * width too large");      // before anything is launched
@@ -854,6 +887,7 @@ CePlan ce_plan(bool grad, int dtype, int64_t rows, int width, int vocab) {
         for (size_t i = 0; i + 1 < at.size(); ++i) {
             const int64_t piece = at[i + 1] - at[i], splits = p.wgrad_splits((int)piece);
             if (splits > 1) p.product = std::max(p.product, splits * piece * width * 4);
+            if (p.dgrad_splits((int)piece) > 1) p.product = std::max(p.product, p.dgrad_splits((int)piece) * rows * width * 4);
             if (p.few_rows((int)piece)) p.product = std::max(p.product, cut(piece, p.few_per((int)piece)) * rows * width * 4);
         }
         p.product = up(p.product, 256);
@@ -940,7 +974,11 @@ void vocab_gradients(hipStream_t st, const CePlan &p, const void *x, const void 
                 gemm_bf16<true, false>(st, g, SumEpilogue{parts, width, rows * width, i > 0}, "linear_ce input gradient launch");
                 if (i + 2 == at.size()) {
                     const int64_t n = rows * width;
-                    hipLaunchKernelGGL(ce_round_kernel, dim3((unsigned)cut(n, 2048)), dim3(256), 0, st, parts, p.ranges, n, inv, (unsigned short *)dx, accumulate);
+                    if (p.ranges > 16)      // few results: 64 rows, 160 columns in 64 ranges 20 us with a thread to eight of them
+                        hipLaunchKernelGGL(ce_few_rows_join_kernel<unsigned short>, dim3((unsigned)cut(n, 64)), dim3(1024), 0, st, parts, p.ranges, (int)n,
+                                           (unsigned short *)dx, accumulate, (const float *)inv);
+                    else
+                        hipLaunchKernelGGL(ce_round_kernel, dim3((unsigned)cut(n, 2048)), dim3(256), 0, st, parts, p.ranges, n, inv, (unsigned short *)dx, accumulate);
                     hip_check(hipGetLastError(), "linear_ce round launch");
                 }
             }
@@ -965,10 +1003,10 @@ void vocab_gradients(hipStream_t st, const CePlan &p, const void *x, const void 
                 else
                     hipLaunchKernelGGL(ce_few_rows_kernel<CE_FEW_ROWS>, dim3(grid.x, grid.y, (unsigned)cut(rows, CE_FEW_ROWS)), dim3(256), 0, st, d, piece, wp, width, p.rows, per, product);
                 hip_check(hipGetLastError(), "linear_ce input gradient launch");
-                hipLaunchKernelGGL(ce_few_rows_join_kernel, dim3((unsigned)cut(n, 64)), dim3(1024), 0, st, product, ranges, n, (float *)dx, accumulate || i > 0);
+                hipLaunchKernelGGL(ce_few_rows_join_kernel<float>, dim3((unsigned)cut(n, 64)), dim3(1024), 0, st, product, ranges, n, (float *)dx, accumulate || i > 0, (const float *)nullptr);
                 hip_check(hipGetLastError(), "linear_ce input gradient sum launch");
             } else {
-                conv_dgrad(st, d, wp, (float *)dx, cs, accumulate || i > 0, 1, product, product_bytes);
+                conv_dgrad(st, d, wp, (float *)dx, cs, accumulate || i > 0, p.dgrad_splits(piece), product, product_bytes);
             }
             const int splits = p.wgrad_splits(piece);
             conv_wgrad(st, (const float *)x, d, (float *)dw + (int64_t)v0 * width, cs, splits, splits > 1 ? product : nullptr, splits > 1 ? product_bytes : 0);
@@ -1026,16 +1064,22 @@ void linear_ce_bwd(hipStream_t st, int dtype, const void *x, const void *w, cons
 }
 
 namespace {
-// the vocabulary without its tail, which has kernels of its own
-int distill_tail(int dtype, int vocab) { return dtype == MONET_F32 && vocab > 4096 ? vocab % DISTILL_TAIL : 0; }
+// The entries that the matrix products do not take: with a piece that is no multiple of 16 they read value by value.  Both passes, us, those entries among
+// the others and in kernels of their own: 24 rows, 128 columns, 1009 entries 49 and 56; 64, 256 and 1009 59 and 58; 300, 512 and 1001 88 and 80; 690,
+// 3856 and 539 244 and 208; 2000, 2000 and 4001 1477 and 928.
+int distill_tail(int dtype, int64_t rows, int width, int vocab) {
+    const bool large = vocab > 4096 || (vocab >= 64 && rows * width * vocab >= 1 << 24);
+    return dtype == MONET_F32 && large ? vocab % DISTILL_TAIL : 0;
+}
 CePlan distill_plan(bool grad, int dtype, int64_t rows, int width, int vocab, int top) {
     if (top < 1 || top > DISTILL_TOP) throw KernelError("linear_distill: 1 to " + std::to_string(DISTILL_TOP) + " entries a row");
-    return ce_plan(grad, dtype, rows, width, vocab - distill_tail(dtype, vocab));
+    if (rows < 1 || width < 1 || vocab < 1) throw KernelError("linear_distill: bad shape");
+    return ce_plan(grad, dtype, rows, width, vocab - distill_tail(dtype, rows, width, vocab), 64);
 }
 int64_t distill_tail_ranges(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(64, rows / 64)); }
 // bytes in front of the plan's: dl of the tail, and dw's parts if there are several
 int64_t distill_tail_bytes(bool grad, int dtype, int64_t rows, int width, int vocab) {
-    const int64_t tail = distill_tail(dtype, vocab), ranges = distill_tail_ranges(rows);
+    const int64_t tail = distill_tail(dtype, rows, width, vocab), ranges = distill_tail_ranges(rows);
     if (!grad || !tail) return 0;
     return up(rows * DISTILL_TAIL * 4, 256) + (ranges > 1 ? up(ranges * tail * width * 4, 256) : 0);
 }
@@ -1071,7 +1115,7 @@ void linear_distill_fwd(hipStream_t st, int dtype, const void *x, const void *w,
     const auto rows_kernel = [&](auto t) {
         using T = decltype(t);
         hipLaunchKernelGGL(distill_rows_kernel<T>, dim3(p.rows), dim3(64 * DISTILL_WAVES), 0, st, (const T *)x, (const T *)w, index, target, target_lse,
-                           merged ? nullptr : part, parts, p.rows, lse, mass, delta, row_loss, width, vocab, distill_tail(dtype, vocab), top, heat);
+                           merged ? nullptr : part, parts, p.rows, lse, mass, delta, row_loss, width, vocab, distill_tail(dtype, rows, width, vocab), top, heat);
         hip_check(hipGetLastError(), "linear_distill rows launch");
     };
     if (p.bf16) rows_kernel((unsigned short)0);
@@ -1085,7 +1129,7 @@ void linear_distill_bwd(hipStream_t st, int dtype, const void *x, const void *w,
                         size_t ws_bytes) {
     const CePlan p = distill_plan(true, dtype, rows, width, vocab, top);
     const int64_t front = distill_tail_bytes(true, dtype, rows, width, vocab);
-    const int tail = distill_tail(dtype, vocab);
+    const int tail = distill_tail(dtype, rows, width, vocab);
     distill_check(heat);
     check_ws(p, ws, ws_bytes, front);
     check_aligned(p, {x, w, dx, dw});
@@ -1120,7 +1164,7 @@ void linear_distill_bwd(hipStream_t st, int dtype, const void *x, const void *w,
                        tail, part);
     hip_check(hipGetLastError(), "linear_distill tail launch");
     if (ranges == 1) return;
-    hipLaunchKernelGGL(ce_few_rows_join_kernel, dim3((unsigned)cut((int64_t)tail * width, 64)), dim3(1024), 0, st, part, (int)ranges, tail * width, out, 0);
+    hipLaunchKernelGGL(ce_few_rows_join_kernel<float>, dim3((unsigned)cut((int64_t)tail * width, 64)), dim3(1024), 0, st, part, (int)ranges, tail * width, out, 0, (const float *)nullptr);
     hip_check(hipGetLastError(), "linear_distill tail launch");
 }
 
