@@ -547,8 +547,19 @@ __device__ __forceinline__ int distill_count(const float *row_loss, const float 
     __shared__ int counts[WAVES];
     int count = 0;
     sum = 0;
-    for (int t = threadIdx.x; t < rows; t += 64 * WAVES)
-        if (mass[t] != 0.f) { ++count; if (row_loss) sum += row_loss[t]; }
+    constexpr int AHEAD = 8;       // rows of a thread whose loads are under way together
+    for (int t0 = threadIdx.x; t0 < rows; t0 += 64 * WAVES * AHEAD) {
+        float m[AHEAD], v[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int t = t0 + 64 * WAVES * i;
+            m[i] = t < rows ? mass[t] : 0.f;
+            v[i] = row_loss && t < rows ? row_loss[t] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (m[i] != 0.f) { ++count; sum += v[i]; }
+    }
     for (int k = 32; k; k /= 2) { sum += __shfl_xor(sum, k); count += __shfl_xor(count, k); }
     if (threadIdx.x % 64 == 0) { sums[threadIdx.x / 64] = sum; counts[threadIdx.x / 64] = count; }
     __syncthreads();
@@ -617,12 +628,20 @@ __global__ __launch_bounds__(256) void distill_tail_kernel(const float *__restri
     const float m = mass[t], f = *inv;
     x += t * width;
     w += (int64_t)v0 * width;
-    // 16 lanes to an entry
-    const int j = threadIdx.x / 16;
-    const float *row[1] = {w + (int64_t)min(j, tail - 1) * width};
-    float s[1] = {};
-    if (m != 0.f) distill_dots<16>(x, row, width, threadIdx.x & 15, s);
-    if (threadIdx.x % 16 == 0) d[j] = m != 0.f && j < tail ? m * expf(s[0] / heat - lse[t]) * f : 0.f;
+    // 16 lanes to an entry, or, of up to four, a wave
+    const auto entry = [&](auto lanes) {
+        constexpr int G = decltype(lanes)::value;
+        const int j = threadIdx.x / G;
+        const float *row[1] = {w + (int64_t)min(j, tail - 1) * width};
+        float s[1] = {};
+        if (m != 0.f) distill_dots<G>(x, row, width, threadIdx.x % G, s);
+        if (threadIdx.x % G == 0) d[j] = m != 0.f && j < tail ? m * expf(s[0] / heat - lse[t]) * f : 0.f;
+    };
+    if (tail > 4) entry(std::integral_constant<int, 16>());
+    else {
+        if (threadIdx.x >= 4 && threadIdx.x < DISTILL_TAIL) d[threadIdx.x] = 0.f;
+        entry(std::integral_constant<int, 64>());
+    }
     __syncthreads();
     for (int j = threadIdx.x; j < top; j += 256) {
         const int64_t e = (int64_t)index[t * top + j] - v0;
