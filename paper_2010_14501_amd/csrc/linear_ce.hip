@@ -351,7 +351,7 @@ __global__ __launch_bounds__(256) void ce_piece_grad_kernel(float *__restrict__ 
 //   loss = sum_j p_j (log p_j + lse - z_j),   mass = sum_j p_j,   delta_j = mass exp(z_j - lse) - (sum of p at the same index)
 // with z_j = x . w[i_j] / T.  One workgroup to a row; z by a wave's sums over the columns, each in the same order, so that an index that comes
 // twice gets the same number twice.  Bound by reading rows * top rows of w, most of them from the caches: 8192 rows, 64 entries, 4096 columns, bf16
-// (4.3 GB): 550 us, one entry at a time to a wave 640; 1000 rows, 64 entries, 1024 columns (131 MB): 24 us.
+// (4.3 GB): 530 us, one entry at a time to each of four waves 640; 1000 rows, 64 entries, 1024 columns (131 MB): 22 us, so 30.
 constexpr int DISTILL_TOP = 1024;      // entries of a row, at most
 constexpr int DISTILL_TAIL = 16;       // fp32: more than a large vocabulary has over a multiple of 16, below
 // N dot products with one x by G lanes, of which this is lane g: 16 bytes at a time, and of a row of floats that is no multiple of four the rest value by
@@ -615,9 +615,8 @@ __global__ __launch_bounds__(256) void distill_piece_grad_kernel(float *__restri
 }
 
 // fp32: the `tail` entries that a large vocabulary has over a multiple of 16, from v0 on.  As a piece of their own they took six launches of the matrix
-// products, mostly empty tiles: both passes of 100 rows, 512 columns, 5003 entries 149 us, with
-// these kernels 101; 777 rows, 1000 columns, 16001 entries 819 and 775.  A workgroup to a row: their
-// logits, dl (kept for dw), and their share of dx, which is there already.
+// products, mostly empty tiles: both passes of 100 rows, 512 columns, 5003 entries 149 us, with these kernels 101; 777 rows, 1000 columns, 16001 entries
+// 819 and 767.  A workgroup to a row: their logits, dl (kept for dw), and their share of dx, which is there already.
 __global__ __launch_bounds__(256) void distill_tail_kernel(const float *__restrict__ x, const float *__restrict__ w, const int32_t *__restrict__ index,
                                                            const float *__restrict__ lse, const float *__restrict__ mass, const float *__restrict__ delta,
                                                            const float *__restrict__ inv, float *__restrict__ dl, float *__restrict__ dx, int rows, int width,

@@ -306,6 +306,7 @@ ROPE_CASES = [
     (33, 8, 40, 10, True, 0, 8, 8), (9, 6, 64, 64, True, 0, 0, 0), (64, 4, 64, 32, False, 16, 0, 0), (130, 10, 80, 80, False, 1, 0, 0), (37, 12, 96, 48, True, 0, 0, 4),
     (5, 4, 96, 24, False, 32, 32, 2), (70, 5, 128, 128, False, 256, 0, 0), (29, 3, 128, 64, True, 0, 24, 0), (11, 9, 256, 256, False, 0, 0, 0), (6, 2, 600, 512, False, 0, 0, 0),
     (4, 1, 640, 2, True, 0, 0, 0), (1000, 1, 24, 12, False, 0, 0, 0), (2, 300, 16, 16, False, 0, 0, 0), (3, 2, 44, 44, False, 4, 4, 0), (3, 2, 44, 20, True, 2, 2, 2),
+    (3, 2, 701, 2, True, 0, 1, 0), (2, 3, 1031, 510, False, 1, 0, 1), (5, 1, 2050, 512, False, 0, 0, 2),
 ]
 
 
@@ -367,6 +368,19 @@ def test_rope_of_many_tokens(dtype, n, heads, dim, rot, interleaved):
     want = nm.rope_fwd(x, at.astype(np.int64), freqs, interleaved)
     within(host(got), want, rope_bounds(x, want, at.astype(np.int64), freqs, interleaved, 1.0, dtype), "y")
     assert torch.equal(got[..., rot:], tx[..., rot:])
+
+
+def test_rope_of_the_most_tokens():
+    torch = torch_mod()
+    n = (1 << 24) - 1
+    x = torch.randn(n, 2, device="cuda").bfloat16()
+    y = x.clone()
+    freqs = np.array([0.37])
+    monet.call("monet_rope_fwd", stream(), monet.BF16, y.data_ptr(), y.data_ptr(), None, freqs.ctypes.data, n, 1, 2, 2, 2, 2, 0, 1.0)
+    at = torch.cat([torch.arange(0, n, 99991, device="cuda"), torch.tensor([n - 2, n - 1], device="cuda")])
+    ref = host(x[at]).reshape(-1, 1, 2)
+    want = nm.rope_fwd(ref, at.cpu().numpy(), freqs, False)
+    within(host(y[at]).reshape(-1, 1, 2), want, rope_bounds(ref, want, at.cpu().numpy(), freqs, False, 1.0, monet.BF16), "y")
 
 
 def test_rope_of_no_tokens_and_special_values():

@@ -132,3 +132,18 @@ def test_declared_workspaces_are_checked(kind):
     for less in (0, -5, (ws + 255) // 256 * 256 - 256):
         with pytest.raises(M.MonetError, match="are needed"):
             M.Plan(g.text().replace(at, at.replace(f" ws={ws}", f" ws={less}"), 1), sch)
+
+
+def test_integer_program_schedules_the_operators():
+    """A budget below what storing everything takes: the program recomputes some of them, within the budget by the oracle's model and the executor's."""
+    from test_ilp_host import check
+    from workloads import ilp
+    g = graphs.transformer(lens=(40, 60), layers=1, vocab=40, code=False, **ALL)
+    store = M.Plan(g.text(), schedules.store_everything_schedule(g).text()).predicted_peak
+    costs = []
+    for frac in (1.0, 0.8):
+        sch, obj, status = ilp.solve(g, int(frac * store), time_limit=60)
+        assert sch is not None, (frac, status)
+        check(g, sch, int(frac * store), obj)
+        costs.append(obj)
+    assert costs[0] < costs[1]
