@@ -28,9 +28,9 @@ __device__ __forceinline__ float sum_of_256(float v, float *seg) {      // the s
     return (seg[0] + seg[1]) + (seg[2] + seg[3]);
 }
 
-// ---- rows that fit the registers: W waves to a row, a lane holds CH pieces of 16 bytes
+// ---- rows that fit the registers: L lanes to a row (4, 16 or whole waves), each with CH pieces of 16 bytes
 template <class T> constexpr int VEC = 16 / sizeof(T);
-template <class T, int W, int CH> constexpr int CAPACITY = W * 64 * VEC<T> * CH;
+template <class T, int L, int CH> constexpr int CAPACITY = L * VEC<T> * CH;
 
 // 16 bytes at any address of an element: rows of odd length begin anywhere, and one such load is what aligned ones cost
 typedef unsigned uintx4_at2 __attribute__((ext_vector_type(4), aligned(2)));
@@ -93,32 +93,40 @@ struct Piece {
     }
 };
 
-// the sums of W waves; `at`: this group's and this sum's place in LDS, not used again before the next barrier but one
-template <int W>
+// the sum of the L lanes of a row; `at`: this group's and this sum's place in LDS, not used again before the next barrier but one
+template <int L>
 __device__ __forceinline__ float group_sum(float v, float *at, int wave) {
+    if (L == 4) return quad_sum(v);
+    if (L == 16) return row_sum(v);
     v = wave_sum(v);
-    if (W == 1) return v;
+    if (L == 64) return v;
     if ((threadIdx.x & 63) == 0) at[wave] = v;
     __syncthreads();
     v = at[0];
 #pragma unroll
-    for (int i = 1; i < W; ++i) v += at[i];
+    for (int i = 1; i < L / 64; ++i) v += at[i];
     return v;
 }
+// which of a workgroup's rows a thread works on: the same for a wave where it has a wave or more
+template <int L>
+__device__ __forceinline__ int group_of() {
+    return L >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) / (L / 64) : threadIdx.x / L;
+}
+template <int L> constexpr int WAVES_OF = L < 64 ? 1 : L / 64;      // of a row
 
 // A workgroup walks over rows with gamma and beta in registers, the next row's loads under way while this one's mean, deviations from it and results are
 // computed: two passes over registers, one over memory.  16384 x 4096, bf16: 47 us (5.7 TB/s); with gamma and beta loaded value by value for every row 147;
 // a row read three times (layernorm_fwd_kernel) 128.  1023 x 12289, fp32: 20 us (4.9 TB/s).
-template <int W> constexpr int FWD_THREADS = W <= 4 ? 256 : 64 * W;
+template <int L> constexpr int FWD_THREADS = L <= 256 ? 256 : L;
 
-template <class T, int W, int CH, bool TAIL>
-__global__ __launch_bounds__(FWD_THREADS<W>) void layernorm_rows_kernel(const T *x, const void *__restrict__ gamma, const void *__restrict__ beta, bool params_bf16,
+template <class T, int L, int CH, bool TAIL>
+__global__ __launch_bounds__(FWD_THREADS<L>) void layernorm_rows_kernel(const T *x, const void *__restrict__ gamma, const void *__restrict__ beta, bool params_bf16,
                                                                         T *y, float2 *__restrict__ stats, int64_t rows, int cols, int64_t x_ld, int64_t y_ld,
                                                                         float eps) {
-    constexpr int V = VEC<T>, GROUPS = FWD_THREADS<W> / 64 / W;
-    __shared__ float sums[2][GROUPS][W];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x & 63, group = wave / W, lot = wave % W;
-    const auto piece = [&](int k) { return Piece<T, TAIL>(((k * W + lot) * 64 + l) * V, cols); };
+    constexpr int V = VEC<T>, GROUPS = FWD_THREADS<L> / L;
+    __shared__ float sums[2][GROUPS][WAVES_OF<L>];
+    const int group = group_of<L>(), l = threadIdx.x % L, lot = threadIdx.x / 64 % WAVES_OF<L>;
+    const auto piece = [&](int k) { return Piece<T, TAIL>((k * L + l) * V, cols); };
     float g[CH][V], b[CH][V];
     uintx4 raw[CH], next[CH];
     const auto load = [&](int64_t row, uintx4 (&v)[CH]) {
@@ -144,7 +152,7 @@ __global__ __launch_bounds__(FWD_THREADS<W>) void layernorm_rows_kernel(const T 
 #pragma unroll
             for (int e = 0; e < V; ++e) sum += piece(k).once(f[e], e);
         }
-        const float mean = group_sum<W>(sum, sums[0][group], lot) / cols;      // divided: the mean of equal values is that value
+        const float mean = group_sum<L>(sum, sums[0][group], lot) / cols;      // divided: the mean of equal values is that value
         sum = 0.f;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
@@ -156,9 +164,9 @@ __global__ __launch_bounds__(FWD_THREADS<W>) void layernorm_rows_kernel(const T 
                 sum = fmaf(d, d, sum);
             }
         }
-        const float rstd = 1.f / sqrtf(group_sum<W>(sum, sums[1][group], lot) / cols + eps);
+        const float rstd = 1.f / sqrtf(group_sum<L>(sum, sums[1][group], lot) / cols + eps);
         if (row < rows) {
-            if (stats && lot == 0 && l == 0) stats[row] = make_float2(mean, rstd);
+            if (stats && l == 0) stats[row] = make_float2(mean, rstd);
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
                 float f[V];
@@ -177,18 +185,18 @@ __global__ __launch_bounds__(FWD_THREADS<W>) void layernorm_rows_kernel(const T 
 // read once for all three results.  Eight waves with up to 32 values of a row to a lane (160 registers of sums, gamma and two rows under way; with 16 waves
 // and 128 registers it spilled); as many workgroups as are on the card at once, since each leaves a part of 8 bytes a column.  16384 x 4096, bf16: 84 us
 // (4.9 TB/s) and 4.5 for the join of 256 parts; in three kernels that read dy and x twice 430.  1023 x 12289, fp32: 42 us, 25 MB of its 175 parts.
-template <int W> constexpr int BWD_WAVES = W <= 8 ? 8 : W;
-template <class T, int W, int CH, bool TAIL>
-__global__ __launch_bounds__(64 * BWD_WAVES<W>) void layernorm_rows_bwd_kernel(const T *dy, const T *__restrict__ x, const void *__restrict__ gamma, bool params_bf16,
+template <int L> constexpr int BWD_THREADS = L <= 512 ? 512 : L;
+template <class T, int L, int CH, bool TAIL>
+__global__ __launch_bounds__(BWD_THREADS<L>) void layernorm_rows_bwd_kernel(const T *dy, const T *__restrict__ x, const void *__restrict__ gamma, bool params_bf16,
                                                                             const float2 *__restrict__ stats, T *dx, float *__restrict__ part, int64_t rows,
                                                                             int cols, int64_t dy_ld, int64_t x_ld, int64_t dx_ld, int add, void *dgamma, void *dbeta) {
-    constexpr int V = VEC<T>, GROUPS = BWD_WAVES<W> / W, N = CH * V, THREADS = 64 * BWD_WAVES<W>;
-    constexpr bool AHEAD = W <= 8;      // the next row's loads begin before this one is worked; 16 waves have registers for one row
+    constexpr int V = VEC<T>, THREADS = BWD_THREADS<L>, GROUPS = THREADS / L, N = CH * V, W = WAVES_OF<L>;
+    constexpr bool AHEAD = L <= 512;      // the next row's loads begin before this one is worked; 16 waves have registers for one row
     __shared__ float sums[2][2][GROUPS][W];
     __shared__ float joined[GROUPS > 1 ? THREADS * N : 1];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x & 63, group = wave / W, lot = wave % W;
+    const int group = group_of<L>(), l = threadIdx.x % L, lot = threadIdx.x / 64 % W;
     const float by = 1.f / cols;
-    const auto piece = [&](int k) { return Piece<T, TAIL>(((k * W + lot) * 64 + l) * V, cols); };
+    const auto piece = [&](int k) { return Piece<T, TAIL>((k * L + l) * V, cols); };
     float g[N], a[N] = {}, b[N] = {};
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
@@ -235,10 +243,13 @@ __global__ __launch_bounds__(64 * BWD_WAVES<W>) void layernorm_rows_bwd_kernel(c
                 b[i] += o;
             }
         }
-        s1 = wave_sum(s1);
-        s2 = wave_sum(s2);
-        if (W > 1) {      // two places in turn: who still reads the other one has not passed this barrier
-            if (l == 0) { sums[turn][0][group][lot] = s1; sums[turn][1][group][lot] = s2; }
+        if (W == 1) {
+            s1 = group_sum<L>(s1, nullptr, 0);
+            s2 = group_sum<L>(s2, nullptr, 0);
+        } else {      // two places in turn: who still reads the other one has not passed this barrier
+            s1 = wave_sum(s1);
+            s2 = wave_sum(s2);
+            if (threadIdx.x % 64 == 0) { sums[turn][0][group][lot] = s1; sums[turn][1][group][lot] = s2; }
             __syncthreads();
             s1 = sums[turn][0][group][0];
             s2 = sums[turn][1][group][0];
@@ -270,16 +281,23 @@ __global__ __launch_bounds__(64 * BWD_WAVES<W>) void layernorm_rows_bwd_kernel(c
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         float(&s)[N] = which ? b : a;
+        if (L < 64) {      // a wave's rows
+#pragma unroll
+            for (int k = 32; k >= L; k /= 2)
+#pragma unroll
+                for (int i = 0; i < N; ++i) s[i] += __shfl_xor(s[i], k);
+        }
         if (GROUPS > 1) {
+            constexpr int APART = L < 64 ? 64 : L;      // threads from one sum to the next
             if (which) __syncthreads();
 #pragma unroll
             for (int i = 0; i < N; ++i) joined[i * THREADS + threadIdx.x] = s[i];
             __syncthreads();
             if (group == 0) {
 #pragma unroll
-                for (int o = 1; o < GROUPS; ++o)
+                for (int o = 1; o < THREADS / APART; ++o)
 #pragma unroll
-                    for (int i = 0; i < N; ++i) s[i] += joined[i * THREADS + o * W * 64 + threadIdx.x];
+                    for (int i = 0; i < N; ++i) s[i] += joined[i * THREADS + o * APART + threadIdx.x];
             }
         }
         void *out = which ? dbeta : dgamma;
@@ -392,25 +410,27 @@ int64_t cut(int64_t n, int64_t by) { return (n + by - 1) / by; }
 
 constexpr int LAYERNORM_COLS = 1 << 20;
 
-// Calls f(waves to a row, pieces of 16 bytes to a lane of it) with the smallest form that a row fits.  BACK: the backward pass.  false: the row does not
+// Calls f(lanes to a row, pieces of 16 bytes to a lane of it) with the smallest form that a row fits.  BACK: the backward pass.  false: the row does not
 // fit, or no piece of it does.
 template <class T, bool BACK, class F>
 bool layernorm_form(int cols, F &&f) {
-    constexpr int M = BACK ? 4 : 16 / VEC<T>;       // pieces to a lane of one wave or more
+    constexpr int M = BACK ? 4 : 16 / VEC<T>;       // pieces to a lane of a wave or more
     if (cols < VEC<T>) return false;
-    const auto fits = [&](auto w, auto ch) {
-        if (cols > CAPACITY<T, decltype(w)::value, decltype(ch)::value>) return false;
-        f(w, ch);
+    const auto fits = [&](auto l, auto ch) {
+        if (cols > CAPACITY<T, decltype(l)::value, decltype(ch)::value>) return false;
+        f(l, ch);
         return true;
     };
     using std::integral_constant;
+    const integral_constant<int, 1> one;
+    const integral_constant<int, 2> two;
+    const integral_constant<int, 16> quarter;
+    const integral_constant<int, 64> wave;
     const integral_constant<int, M> m;
-    if (fits(integral_constant<int, 1>(), integral_constant<int, 1>()) || fits(integral_constant<int, 1>(), integral_constant<int, 2>()) ||
-        fits(integral_constant<int, 1>(), m) || fits(integral_constant<int, 2>(), m) || fits(integral_constant<int, 4>(), m) ||
-        fits(integral_constant<int, 8>(), m))
+    if (fits(integral_constant<int, 4>(), one) || fits(quarter, one) || fits(quarter, two) || fits(wave, one) || fits(wave, two) || fits(wave, m) ||
+        fits(integral_constant<int, 128>(), m) || fits(integral_constant<int, 256>(), m) || fits(integral_constant<int, 512>(), m))
         return true;
-    if constexpr (!BACK) return fits(integral_constant<int, 16>(), m);
-    else if constexpr (std::is_same<T, float>::value) return fits(integral_constant<int, 16>(), m);
+    if constexpr (!BACK || std::is_same<T, float>::value) return fits(integral_constant<int, 1024>(), m);
     else return false;
 }
 template <class F>
@@ -422,10 +442,10 @@ void by_tail(bool tail, F &&f) {
 // the registers, ranges of rows
 int64_t layernorm_ranges(int dtype, int64_t rows, int cols) {
     int64_t rows_at_once = 0, groups = 0;
-    const auto form = [&](auto w, auto ch) {
-        constexpr int W = decltype(w)::value, CH = decltype(ch)::value;
-        rows_at_once = BWD_WAVES<W> / W;
-        groups = W <= 8 && CH * (dtype == MONET_F32 ? 4 : 8) <= 16 ? 512 : 256;
+    const auto form = [&](auto l, auto ch) {
+        constexpr int L = decltype(l)::value, CH = decltype(ch)::value;
+        rows_at_once = BWD_THREADS<L> / L;
+        groups = L <= 512 && CH * (dtype == MONET_F32 ? 4 : 8) <= 16 ? 512 : 256;
     };
     dtype == MONET_F32 ? layernorm_form<float, true>(cols, form) : layernorm_form<unsigned short, true>(cols, form);
     // few values: one workgroup, which needs no second launch (37 rows of 203 in fp32, both passes: 24 us, with a join 27.5)
@@ -478,11 +498,11 @@ void layernorm_fwd(hipStream_t st, int dtype, int param_dtype, const void *x, co
     by_types(dtype, param_dtype, [&](auto t, auto p) {
         using T = decltype(t);
         using P = decltype(p);
-        const bool rows_fit = layernorm_form<T, false>(cols, [&](auto w, auto ch) {
-            constexpr int W = decltype(w)::value, CH = decltype(ch)::value, GROUPS = FWD_THREADS<W> / 64 / W;
+        const bool rows_fit = layernorm_form<T, false>(cols, [&](auto l, auto ch) {
+            constexpr int L = decltype(l)::value, CH = decltype(ch)::value, GROUPS = FWD_THREADS<L> / L;
             by_tail(cols % VEC<T>, [&](auto tail) {
-                hipLaunchKernelGGL((layernorm_rows_kernel<T, W, CH, decltype(tail)::value>), dim3((unsigned)std::min<int64_t>(cut(rows, GROUPS), 256 * 1024 / FWD_THREADS<W>)),
-                                   dim3(FWD_THREADS<W>), 0, st, (const T *)x, gamma, beta, param_dtype == MONET_BF16, (T *)y, (float2 *)stats, rows, cols, x_ld, y_ld, eps);
+                hipLaunchKernelGGL((layernorm_rows_kernel<T, L, CH, decltype(tail)::value>), dim3((unsigned)std::min<int64_t>(cut(rows, GROUPS), 256 * 1024 / FWD_THREADS<L>)),
+                                   dim3(FWD_THREADS<L>), 0, st, (const T *)x, gamma, beta, param_dtype == MONET_BF16, (T *)y, (float2 *)stats, rows, cols, x_ld, y_ld, eps);
             });
         });
         if (rows_fit) return;
@@ -531,10 +551,10 @@ void layernorm_bwd(hipStream_t st, int dtype, int param_dtype, const void *dy, c
             return;
         }
         if (!dx && !columns) return;
-        const bool rows_fit = layernorm_form<T, true>(cols, [&](auto w, auto ch) {
-            constexpr int W = decltype(w)::value, CH = decltype(ch)::value;
+        const bool rows_fit = layernorm_form<T, true>(cols, [&](auto l, auto ch) {
+            constexpr int L = decltype(l)::value, CH = decltype(ch)::value;
             by_tail(cols % VEC<T>, [&](auto tail) {
-                hipLaunchKernelGGL((layernorm_rows_bwd_kernel<T, W, CH, decltype(tail)::value>), dim3((unsigned)ranges), dim3(64 * BWD_WAVES<W>), 0, st, (const T *)dy,
+                hipLaunchKernelGGL((layernorm_rows_bwd_kernel<T, L, CH, decltype(tail)::value>), dim3((unsigned)ranges), dim3(BWD_THREADS<L>), 0, st, (const T *)dy,
                                    (const T *)x, gamma, param_dtype == MONET_BF16, (const float2 *)stats, (T *)dx, (float *)ws, rows, cols, dy_ld, x_ld,
                                    dx_ld, accumulate, dgamma, dbeta);
             });

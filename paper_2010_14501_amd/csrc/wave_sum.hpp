@@ -22,12 +22,15 @@ __device__ __forceinline__ float wave_join(float v, float none, F &&f) {
 __device__ __forceinline__ float wave_sum(float v) {
     return wave_join(v, 0.f, [](float a, float b) { return a + b; });
 }
-// over 16 neighbouring lanes, in all of them
-__device__ __forceinline__ float row_sum(float v) {
+// over four and over 16 neighbouring lanes, in all of them
+__device__ __forceinline__ float quad_sum(float v) {
     const auto add = [](float a, float b) { return a + b; };
     v = dpp_join<0xb1, 0xf>(v, 0.f, add);
-    v = dpp_join<0x4e, 0xf>(v, 0.f, add);
-    v = dpp_join<0x141, 0xf>(v, 0.f, add);
+    return dpp_join<0x4e, 0xf>(v, 0.f, add);
+}
+__device__ __forceinline__ float row_sum(float v) {
+    const auto add = [](float a, float b) { return a + b; };
+    v = dpp_join<0x141, 0xf>(quad_sum(v), 0.f, add);
     return dpp_join<0x140, 0xf>(v, 0.f, add);
 }
 __device__ __forceinline__ float wave_max(float v) {
