@@ -59,30 +59,43 @@ __device__ __forceinline__ uintx4 pack(const float (&f)[8]) {
     for (int i = 0; i < 4; ++i) v[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
     return v;
 }
-// Where a lane's piece begins, and how many of its values belong to the piece before: in a row whose length is no multiple of a piece, the last
-// piece is moved back to the row's end (values that two lanes hold are added once, and stored twice alike).  A piece behind the end: nothing.
-template <class T, bool TAIL>
+// A lane's piece of a row.  WHOLE: rows are whole pieces.  MOVED: the last piece is moved back to the row's end (values that two lanes hold are added once,
+// and stored twice alike).  SHORT: the row is shorter than a piece and goes value by value.  A piece behind the end: nothing.
+enum { WHOLE, MOVED, SHORT };
+template <class T, int ROWS>
 struct Piece {
-    int c, skip;
+    int c, from, to;        // values from .. to - 1 count
     bool has;
-    __device__ __forceinline__ Piece(int at, int cols) : c(at), skip(0), has(at < cols) {
-        if (TAIL && at + VEC<T> > cols) { c = cols - VEC<T>; skip = at - c; }
+    __device__ __forceinline__ Piece(int at, int cols) : c(at), from(0), to(VEC<T>), has(at < cols) {
+        if (ROWS == MOVED && at + VEC<T> > cols) { c = cols - VEC<T>; from = at - c; }
+        if (ROWS == SHORT) to = cols - at;
     }
-    __device__ __forceinline__ uintx4 load(const T *row) const { return has ? load16(row + c) : uintx4{}; }
-    // v[e] where e counts, else 0
-    __device__ __forceinline__ float once(float v, int e) const { return !TAIL || e >= skip ? v : 0.f; }
-    __device__ __forceinline__ void store(T *row, const float (&f)[VEC<T>], bool add) const {
-        if (!has) return;
-        if (!add) { store16(row + c, pack(f)); return; }
+    __device__ __forceinline__ bool counts(int e) const { return (ROWS != MOVED || e >= from) && (ROWS != SHORT || e < to); }
+    __device__ __forceinline__ uintx4 load(const T *row) const {
+        if (ROWS != SHORT) return has ? load16(row + c) : uintx4{};
+        T v[VEC<T>] = {};
 #pragma unroll
         for (int e = 0; e < VEC<T>; ++e)
-            if (e >= skip) put(row + c + e, f[e], true);
+            if (e < to) v[e] = row[c + e];
+        return __builtin_bit_cast(uintx4, v);
+    }
+    __device__ __forceinline__ float once(float v, int e) const { return counts(e) ? v : 0.f; }
+    __device__ __forceinline__ void store(T *row, const float (&f)[VEC<T>], bool add) const {
+        if (!has) return;
+        if (ROWS != SHORT && !add) { store16(row + c, pack(f)); return; }
+#pragma unroll
+        for (int e = 0; e < VEC<T>; ++e)
+            if (counts(e)) put(row + c + e, f[e], add);
     }
     __device__ __forceinline__ void params(const void *p, bool bf16, float missing, float (&f)[VEC<T>]) const {
 #pragma unroll
         for (int e = 0; e < VEC<T>; ++e) f[e] = has ? missing : 0.f;
         if (!p || !has) return;
-        if (bf16) {
+        if (ROWS == SHORT) {
+#pragma unroll
+            for (int e = 0; e < VEC<T>; ++e)
+                if (e < to) f[e] = bf16 ? bf16_float(((const unsigned short *)p)[c + e]) : ((const float *)p)[c + e];
+        } else if (bf16) {
             typedef unsigned short half __attribute__((ext_vector_type(VEC<T>)));
             half v;
             __builtin_memcpy(&v, (const unsigned short *)p + c, sizeof v);
@@ -116,17 +129,18 @@ template <int L> constexpr int WAVES_OF = L < 64 ? 1 : L / 64;      // of a row
 
 // A workgroup walks over rows with gamma and beta in registers, the next row's loads under way while this one's mean, deviations from it and results are
 // computed: two passes over registers, one over memory.  16384 x 4096, bf16: 47 us (5.7 TB/s); with gamma and beta loaded value by value for every row 147;
-// a row read three times (layernorm_fwd_kernel) 128.  1023 x 12289, fp32: 20 us (4.9 TB/s).
+// a row read three times (layernorm_fwd_kernel) 128.  1023 x 12289, fp32: 20 us (4.9 TB/s).  Short rows share a wave: 327680 x 128, bf16, 16 lanes each 26 us,
+// a wave each 82.
 template <int L> constexpr int FWD_THREADS = L <= 256 ? 256 : L;
 
-template <class T, int L, int CH, bool TAIL>
+template <class T, int L, int CH, int ROWS>
 __global__ __launch_bounds__(FWD_THREADS<L>) void layernorm_rows_kernel(const T *x, const void *__restrict__ gamma, const void *__restrict__ beta, bool params_bf16,
                                                                         T *y, float2 *__restrict__ stats, int64_t rows, int cols, int64_t x_ld, int64_t y_ld,
                                                                         float eps) {
     constexpr int V = VEC<T>, GROUPS = FWD_THREADS<L> / L;
     __shared__ float sums[2][GROUPS][WAVES_OF<L>];
     const int group = group_of<L>(), l = threadIdx.x % L, lot = threadIdx.x / 64 % WAVES_OF<L>;
-    const auto piece = [&](int k) { return Piece<T, TAIL>((k * L + l) * V, cols); };
+    const auto piece = [&](int k) { return Piece<T, ROWS>((k * L + l) * V, cols); };
     float g[CH][V], b[CH][V];
     uintx4 raw[CH], next[CH];
     const auto load = [&](int64_t row, uintx4 (&v)[CH]) {
@@ -186,7 +200,7 @@ __global__ __launch_bounds__(FWD_THREADS<L>) void layernorm_rows_kernel(const T 
 // and 128 registers it spilled); as many workgroups as are on the card at once, since each leaves a part of 8 bytes a column.  16384 x 4096, bf16: 84 us
 // (4.9 TB/s) and 4.5 for the join of 256 parts; in three kernels that read dy and x twice 430.  1023 x 12289, fp32: 42 us, 25 MB of its 175 parts.
 template <int L> constexpr int BWD_THREADS = L <= 512 ? 512 : L;
-template <class T, int L, int CH, bool TAIL>
+template <class T, int L, int CH, int ROWS>
 __global__ __launch_bounds__(BWD_THREADS<L>) void layernorm_rows_bwd_kernel(const T *dy, const T *__restrict__ x, const void *__restrict__ gamma, bool params_bf16,
                                                                             const float2 *__restrict__ stats, T *dx, float *__restrict__ part, int64_t rows,
                                                                             int cols, int64_t dy_ld, int64_t x_ld, int64_t dx_ld, int add, void *dgamma, void *dbeta) {
@@ -196,7 +210,7 @@ __global__ __launch_bounds__(BWD_THREADS<L>) void layernorm_rows_bwd_kernel(cons
     __shared__ float joined[GROUPS > 1 ? THREADS * N : 1];
     const int group = group_of<L>(), l = threadIdx.x % L, lot = threadIdx.x / 64 % W;
     const float by = 1.f / cols;
-    const auto piece = [&](int k) { return Piece<T, TAIL>((k * L + l) * V, cols); };
+    const auto piece = [&](int k) { return Piece<T, ROWS>((k * L + l) * V, cols); };
     float g[N], a[N] = {}, b[N] = {};
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
@@ -304,10 +318,10 @@ __global__ __launch_bounds__(BWD_THREADS<L>) void layernorm_rows_bwd_kernel(cons
         if (group || !out) continue;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const Piece<T, TAIL> at = piece(k);
+            const Piece<T, ROWS> at = piece(k);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                if (!at.has || e < at.skip) continue;
+                if (!at.has || !at.counts(e)) continue;
                 const int c = at.c + e;
                 if (gridDim.x > 1) part[((int64_t)blockIdx.x * 2 + which) * cols + c] = s[k * V + e];
                 else if (params_bf16) put((unsigned short *)out + c, s[k * V + e], add >> (1 + which) & 1);
@@ -317,9 +331,8 @@ __global__ __launch_bounds__(BWD_THREADS<L>) void layernorm_rows_bwd_kernel(cons
     }
 }
 
-// ---- longer rows (more than 16384 columns), and ones of less than 16 bytes: 1000 x 30000 in bf16 both passes 260 us where 1000 x 16384 take 60; 32768 x 3
-// 65 us.  A row is read again for each of its sums.
-// a workgroup to a row, which is read once for each of its sums and once more for the result
+// ---- longer rows (more than 16384 columns), which are read again for each of their sums: 1000 x 30000 in bf16 both passes 260 us where 1000 x 16384 take 60.
+// A workgroup to a row, which is read once for each of its sums and once more for the result
 template <class T, class P>
 __global__ __launch_bounds__(256) void layernorm_fwd_kernel(const T *x, const P *__restrict__ gamma, const P *__restrict__ beta, T *y,
                                                             float2 *__restrict__ stats, int64_t rows, int cols, int64_t x_ld, int64_t y_ld, float eps) {
@@ -410,12 +423,11 @@ int64_t cut(int64_t n, int64_t by) { return (n + by - 1) / by; }
 
 constexpr int LAYERNORM_COLS = 1 << 20;
 
-// Calls f(lanes to a row, pieces of 16 bytes to a lane of it) with the smallest form that a row fits.  BACK: the backward pass.  false: the row does not
-// fit, or no piece of it does.
+// Calls f(lanes to a row, pieces of 16 bytes to a lane of it) with the smallest form that a row of a piece or more fits.  BACK: the backward pass.  false: the
+// row does not fit.
 template <class T, bool BACK, class F>
 bool layernorm_form(int cols, F &&f) {
     constexpr int M = BACK ? 4 : 16 / VEC<T>;       // pieces to a lane of a wave or more
-    if (cols < VEC<T>) return false;
     const auto fits = [&](auto l, auto ch) {
         if (cols > CAPACITY<T, decltype(l)::value, decltype(ch)::value>) return false;
         f(l, ch);
@@ -433,21 +445,29 @@ bool layernorm_form(int cols, F &&f) {
     if constexpr (!BACK || std::is_same<T, float>::value) return fits(integral_constant<int, 1024>(), m);
     else return false;
 }
-template <class F>
-void by_tail(bool tail, F &&f) {
-    if (tail) f(std::true_type());
-    else f(std::false_type());
+// Calls f(lanes, pieces, WHOLE, MOVED or SHORT) with the form of a row; false: it does not fit the registers
+template <class T, bool BACK, class F>
+bool layernorm_rows_form(int cols, F &&f) {
+    using std::integral_constant;
+    if (cols < VEC<T>) {
+        f(integral_constant<int, 4>(), integral_constant<int, 1>(), integral_constant<int, SHORT>());
+        return true;
+    }
+    return layernorm_form<T, BACK>(cols, [&](auto l, auto ch) {
+        if (cols % VEC<T>) f(l, ch, integral_constant<int, MOVED>());
+        else f(l, ch, integral_constant<int, WHOLE>());
+    });
 }
 // Parts of dgamma and dbeta: the workgroups that share the rows of a backward pass (as many as are on the card at once), or, of rows that do not fit
 // the registers, ranges of rows
 int64_t layernorm_ranges(int dtype, int64_t rows, int cols) {
     int64_t rows_at_once = 0, groups = 0;
-    const auto form = [&](auto l, auto ch) {
+    const auto form = [&](auto l, auto ch, auto) {
         constexpr int L = decltype(l)::value, CH = decltype(ch)::value;
         rows_at_once = BWD_THREADS<L> / L;
         groups = L <= 512 && CH * (dtype == MONET_F32 ? 4 : 8) <= 16 ? 512 : 256;
     };
-    dtype == MONET_F32 ? layernorm_form<float, true>(cols, form) : layernorm_form<unsigned short, true>(cols, form);
+    dtype == MONET_F32 ? layernorm_rows_form<float, true>(cols, form) : layernorm_rows_form<unsigned short, true>(cols, form);
     // few values: one workgroup, which needs no second launch (37 rows of 203 in fp32, both passes: 24 us, with a join 27.5)
     if (rows && rows_at_once && rows * cols <= 1 << 14 && rows <= 8 * rows_at_once) return 1;
     // three turns or more to a workgroup, since a part costs as much as four rows of bf16 (1000 x 8192: backward pass 24 us with two turns, 18.5 with three), unless fewer than
@@ -498,12 +518,11 @@ void layernorm_fwd(hipStream_t st, int dtype, int param_dtype, const void *x, co
     by_types(dtype, param_dtype, [&](auto t, auto p) {
         using T = decltype(t);
         using P = decltype(p);
-        const bool rows_fit = layernorm_form<T, false>(cols, [&](auto l, auto ch) {
+        const bool rows_fit = layernorm_rows_form<T, false>(cols, [&](auto l, auto ch, auto form) {
             constexpr int L = decltype(l)::value, CH = decltype(ch)::value, GROUPS = FWD_THREADS<L> / L;
-            by_tail(cols % VEC<T>, [&](auto tail) {
-                hipLaunchKernelGGL((layernorm_rows_kernel<T, L, CH, decltype(tail)::value>), dim3((unsigned)std::min<int64_t>(cut(rows, GROUPS), 256 * 1024 / FWD_THREADS<L>)),
-                                   dim3(FWD_THREADS<L>), 0, st, (const T *)x, gamma, beta, param_dtype == MONET_BF16, (T *)y, (float2 *)stats, rows, cols, x_ld, y_ld, eps);
-            });
+            hipLaunchKernelGGL((layernorm_rows_kernel<T, L, CH, decltype(form)::value>), dim3((unsigned)std::min<int64_t>(cut(rows, GROUPS), 256 * 1024 / FWD_THREADS<L>)),
+                               dim3(FWD_THREADS<L>), 0, st, (const T *)x, gamma, beta, param_dtype == MONET_BF16, (T *)y, (float2 *)stats, rows, cols, x_ld, y_ld,
+                               eps);
         });
         if (rows_fit) return;
         hipLaunchKernelGGL((layernorm_fwd_kernel<T, P>), dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), dim3(256), 0, st, (const T *)x, (const P *)gamma, (const P *)beta, (T *)y,
@@ -551,13 +570,11 @@ void layernorm_bwd(hipStream_t st, int dtype, int param_dtype, const void *dy, c
             return;
         }
         if (!dx && !columns) return;
-        const bool rows_fit = layernorm_form<T, true>(cols, [&](auto l, auto ch) {
+        const bool rows_fit = layernorm_rows_form<T, true>(cols, [&](auto l, auto ch, auto form) {
             constexpr int L = decltype(l)::value, CH = decltype(ch)::value;
-            by_tail(cols % VEC<T>, [&](auto tail) {
-                hipLaunchKernelGGL((layernorm_rows_bwd_kernel<T, L, CH, decltype(tail)::value>), dim3((unsigned)ranges), dim3(BWD_THREADS<L>), 0, st, (const T *)dy,
-                                   (const T *)x, gamma, param_dtype == MONET_BF16, (const float2 *)stats, (T *)dx, (float *)ws, rows, cols, dy_ld, x_ld,
-                                   dx_ld, accumulate, dgamma, dbeta);
-            });
+            hipLaunchKernelGGL((layernorm_rows_bwd_kernel<T, L, CH, decltype(form)::value>), dim3((unsigned)ranges), dim3(BWD_THREADS<L>), 0, st, (const T *)dy,
+                               (const T *)x, gamma, param_dtype == MONET_BF16, (const float2 *)stats, (T *)dx, (float *)ws, rows, cols, dy_ld, x_ld, dx_ld,
+                               accumulate, dgamma, dbeta);
             hip_check(hipGetLastError(), "layernorm gradients launch");
         });
         if (rows_fit) {

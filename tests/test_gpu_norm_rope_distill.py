@@ -1,8 +1,9 @@
 """Layer norm, rotary positions and the loss against a teacher's top logits on the GPU, through the C ABI, against the oracle in 64 bits.
 
 Bounds are element by element and follow from the arithmetic: U = 2^-24 a rounding in fp32, R = 2^-8 a rounding to bf16 (half a step relative to
-the value).  A sum of n products in fp32 is off by at most (n + 2) U times the sum of their magnitudes; sums over the columns of a row are taken by
-64 lanes or more, so that n there is a lane's share and the 16 steps that join them at most.  Exponentials, logarithms and sines are taken as 4 U."""
+the value).  A sum of n products in fp32 is off by at most (n + 2) U times the sum of their magnitudes.  Layer norm's sums over a row are taken by many
+lanes, so that n there is cols / 64 + 16 at most: a lane's share and up to 16 steps that join them, or, in rows of up to 256, up to 16 values and four
+steps.  Exponentials, logarithms and sines are taken as 4 U."""
 import numpy as np
 import pytest
 
