@@ -20,14 +20,6 @@ __device__ __forceinline__ float value(unsigned short v) { return bf16_float(v);
 __device__ __forceinline__ void put(float *p, float v, bool add) { *p = add ? *p + v : v; }
 __device__ __forceinline__ void put(unsigned short *p, float v, bool add) { *p = float_bf16(add ? bf16_float(*p) + v : v); }
 
-__device__ __forceinline__ float sum_of_256(float v, float *seg) {      // the same in every thread
-    for (int w = 32; w; w /= 2) v += __shfl_xor(v, w);
-    __syncthreads();
-    if (threadIdx.x % 64 == 0) seg[threadIdx.x / 64] = v;
-    __syncthreads();
-    return (seg[0] + seg[1]) + (seg[2] + seg[3]);
-}
-
 // ---- rows that fit the registers: L lanes to a row (4, 16 or whole waves), each with CH pieces of 16 bytes
 template <class T> constexpr int VEC = 16 / sizeof(T);
 template <class T, int L, int CH> constexpr int CAPACITY = L * VEC<T> * CH;
@@ -129,7 +121,7 @@ template <int L> constexpr int WAVES_OF = L < 64 ? 1 : L / 64;      // of a row
 
 // A workgroup walks over rows with gamma and beta in registers, the next row's loads under way while this one's mean, deviations from it and results are
 // computed: two passes over registers, one over memory.  16384 x 4096, bf16: 47 us (5.7 TB/s); with gamma and beta loaded value by value for every row 147;
-// a row read three times (layernorm_fwd_kernel) 128.  1023 x 12289, fp32: 20 us (4.9 TB/s).  Short rows share a wave: 327680 x 128, bf16, 16 lanes each 26 us,
+// a row read three times, value by value, 128.  1023 x 12289, fp32: 20 us (4.9 TB/s).  Short rows share a wave: 327680 x 128, bf16, 16 lanes each 26 us,
 // a wave each 82.
 template <int L> constexpr int FWD_THREADS = L <= 256 ? 256 : L;
 
@@ -198,7 +190,7 @@ __global__ __launch_bounds__(FWD_THREADS<L>) void layernorm_rows_kernel(const T 
 // dx, and this workgroup's rows' part of dgamma and dbeta: a lane's columns are the same in every row, so their sums stay in its registers and dy and x are
 // read once for all three results.  Eight waves with up to 32 values of a row to a lane (160 registers of sums, gamma and two rows under way; with 16 waves
 // and 128 registers it spilled); as many workgroups as are on the card at once, since each leaves a part of 8 bytes a column.  16384 x 4096, bf16: 84 us
-// (4.9 TB/s) and 4.5 for the join of 256 parts; in three kernels that read dy and x twice 430.  1023 x 12289, fp32: 42 us, 25 MB of its 175 parts.
+// (4.9 TB/s) and 4.5 for the join of 256 parts; in three kernels that read dy and x twice, value by value, 430.  1023 x 12289, fp32: 42 us, 25 MB of its 175 parts.
 template <int L> constexpr int BWD_THREADS = L <= 512 ? 512 : L;
 template <class T, int L, int CH, int ROWS>
 __global__ __launch_bounds__(BWD_THREADS<L>) void layernorm_rows_bwd_kernel(const T *dy, const T *__restrict__ x, const void *__restrict__ gamma, bool params_bf16,
@@ -331,72 +323,139 @@ __global__ __launch_bounds__(BWD_THREADS<L>) void layernorm_rows_bwd_kernel(cons
     }
 }
 
-// ---- longer rows (more than 16384 columns), which are read again for each of their sums: 1000 x 30000 in bf16 both passes 260 us where 1000 x 16384 take 60.
-// A workgroup to a row, which is read once for each of its sums and once more for the result
-template <class T, class P>
-__global__ __launch_bounds__(256) void layernorm_fwd_kernel(const T *x, const P *__restrict__ gamma, const P *__restrict__ beta, T *y,
-                                                            float2 *__restrict__ stats, int64_t rows, int cols, int64_t x_ld, int64_t y_ld, float eps) {
-    __shared__ float seg[4];
+// ---- longer rows (more than 16384 columns), which are read again, mostly from L2, for each of their sums; pieces as above: 1000 x 30000 in bf16 forward 25 us,
+// backward 70 (5 and 2.6 TB/s)
+constexpr int LONG_THREADS = 1024;
+__device__ __forceinline__ float long_sum(float v, float *seg) {      // the same in every thread
+    v = wave_sum(v);
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) seg[threadIdx.x / 64] = v;
+    __syncthreads();
+    v = seg[0];
+#pragma unroll
+    for (int i = 1; i < LONG_THREADS / 64; ++i) v += seg[i];
+    return v;
+}
+template <class T>
+__global__ __launch_bounds__(LONG_THREADS) void layernorm_fwd_kernel(const T *x, const void *__restrict__ gamma, const void *__restrict__ beta, bool params_bf16,
+                                                                     T *y, float2 *__restrict__ stats, int64_t rows, int cols, int64_t x_ld, int64_t y_ld,
+                                                                     float eps) {
+    constexpr int V = VEC<T>;
+    __shared__ float seg[LONG_THREADS / 64];
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const T *from = x + row * x_ld;
         T *to = y + row * y_ld;
-        float sum = 0.f;
-        for (int c = threadIdx.x; c < cols; c += 256) sum += value(from[c]);
-        const float mean = sum_of_256(sum, seg) / cols;
-        sum = 0.f;
-        for (int c = threadIdx.x; c < cols; c += 256) {
-            const float d = value(from[c]) - mean;
-            sum = fmaf(d, d, sum);
+        const auto sum = [&](auto of) {
+            float s = 0.f;
+            for (int c = threadIdx.x * V; c < cols; c += LONG_THREADS * V) {
+                const Piece<T, MOVED> at(c, cols);
+                float f[V];
+                unpack(at.load(from), f);
+#pragma unroll
+                for (int e = 0; e < V; ++e) s += at.once(of(f[e]), e);
+            }
+            return long_sum(s, seg);
+        };
+        const float mean = sum([](float v) { return v; }) / cols;
+        const float rstd = 1.f / sqrtf(sum([&](float v) { return (v - mean) * (v - mean); }) / cols + eps);
+        // in place, a moved piece would read what the piece before it has stored: its values come in before anybody stores
+        const int last = (cols - 1) / V * V;
+        const bool mine = last / V % LONG_THREADS == (int)threadIdx.x;
+        uintx4 end{};
+        if (mine) end = Piece<T, MOVED>(last, cols).load(from);
+        copies_arrived();
+        for (int c = threadIdx.x * V; c < cols; c += LONG_THREADS * V) {
+            const Piece<T, MOVED> at(c, cols);
+            float f[V], g[V], b[V];
+            unpack(c == last ? end : at.load(from), f);
+            at.params(gamma, params_bf16, 1.f, g);
+            at.params(beta, params_bf16, 0.f, b);
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] = fmaf((f[e] - mean) * rstd, g[e], b[e]);
+            at.store(to, f, false);
         }
-        const float rstd = 1.f / sqrtf(sum_of_256(sum, seg) / cols + eps);
-        for (int c = threadIdx.x; c < cols; c += 256)
-            put(to + c, fmaf((value(from[c]) - mean) * rstd, gamma ? value(gamma[c]) : 1.f, beta ? value(beta[c]) : 0.f), false);
         if (stats && threadIdx.x == 0) stats[row] = make_float2(mean, rstd);
     }
 }
 
-template <class T, class P>
-__global__ __launch_bounds__(256) void layernorm_dx_kernel(const T *dy, const T *__restrict__ x, const P *__restrict__ gamma, const float2 *__restrict__ stats,
-                                                           T *dx, int64_t rows, int cols, int64_t dy_ld, int64_t x_ld, int64_t dx_ld, bool add) {
-    __shared__ float seg[4];
+template <class T>
+__global__ __launch_bounds__(LONG_THREADS) void layernorm_dx_kernel(const T *dy, const T *__restrict__ x, const void *__restrict__ gamma, bool params_bf16,
+                                                                    const float2 *__restrict__ stats, T *dx, int64_t rows, int cols, int64_t dy_ld, int64_t x_ld,
+                                                                    int64_t dx_ld, bool add) {
+    constexpr int V = VEC<T>;
+    __shared__ float seg[LONG_THREADS / 64];
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const T *go = dy + row * dy_ld, *from = x + row * x_ld;
         T *to = dx + row * dx_ld;
         const float mean = stats[row].x, rstd = stats[row].y;
         float a = 0.f, b = 0.f;
-        for (int c = threadIdx.x; c < cols; c += 256) {
-            const float g = value(go[c]) * (gamma ? value(gamma[c]) : 1.f);
-            a += g;
-            b = fmaf(g, (value(from[c]) - mean) * rstd, b);
+        for (int c = threadIdx.x * V; c < cols; c += LONG_THREADS * V) {
+            const Piece<T, MOVED> at(c, cols);
+            float d[V], v[V], g[V];
+            unpack(at.load(go), d);
+            unpack(at.load(from), v);
+            at.params(gamma, params_bf16, 1.f, g);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float t = at.once(d[e], e) * g[e];
+                a += t;
+                b = fmaf(t, (v[e] - mean) * rstd, b);
+            }
         }
-        a = sum_of_256(a, seg) / cols;
-        b = sum_of_256(b, seg) / cols;
-        for (int c = threadIdx.x; c < cols; c += 256) {
-            const float g = value(go[c]) * (gamma ? value(gamma[c]) : 1.f);
-            put(to + c, rstd * (g - a - (value(from[c]) - mean) * rstd * b), add);
+        a = long_sum(a, seg) / cols;
+        b = long_sum(b, seg) / cols;
+        const int last = (cols - 1) / V * V;      // as in the forward pass
+        const bool mine = last / V % LONG_THREADS == (int)threadIdx.x;
+        uintx4 end{};
+        if (mine) end = Piece<T, MOVED>(last, cols).load(go);
+        copies_arrived();
+        for (int c = threadIdx.x * V; c < cols; c += LONG_THREADS * V) {
+            const Piece<T, MOVED> at(c, cols);
+            float d[V], v[V], g[V];
+            unpack(c == last ? end : at.load(go), d);
+            unpack(at.load(from), v);
+            at.params(gamma, params_bf16, 1.f, g);
+#pragma unroll
+            for (int e = 0; e < V; ++e) d[e] = rstd * (d[e] * g[e] - a - (v[e] - mean) * rstd * b);
+            at.store(to, d, add);
         }
     }
 }
 
-// 64 columns of a range of rows: part[range][0: dgamma, 1: dbeta][cols]
+// 64 pieces of a range of rows: part[range][0: dgamma, 1: dbeta][cols]
 template <class T>
 __global__ __launch_bounds__(256) void layernorm_columns_kernel(const T *__restrict__ dy, const T *__restrict__ x, const float2 *__restrict__ stats,
                                                                 float *__restrict__ part, int64_t rows, int64_t per, int cols, int64_t dy_ld, int64_t x_ld) {
-    __shared__ float sums[2][4][64];
-    const int l = threadIdx.x & 63, wave = threadIdx.x / 64, c = blockIdx.x * 64 + l;
+    constexpr int V = VEC<T>;
+    __shared__ float sums[2][4][V][64];
+    const int l = threadIdx.x & 63, wave = threadIdx.x / 64;
+    const Piece<T, MOVED> at((blockIdx.x * 64 + l) * V, cols);
     const int64_t from = blockIdx.y * per, to = min(rows, from + per);
-    float a = 0.f, b = 0.f;
-    if (c < cols)
-        for (int64_t r = from + wave; r < to; r += 4) {
-            const float d = value(dy[r * dy_ld + c]);
-            a = fmaf(d, (value(x[r * x_ld + c]) - stats[r].x) * stats[r].y, a);
-            b += d;
+    float a[V] = {}, b[V] = {};
+#pragma unroll 2
+    for (int64_t r = from + wave; r < to; r += 4) {
+        const float2 st = stats[r];
+        float d[V], v[V];
+        unpack(at.load(dy + r * dy_ld), d);
+        unpack(at.load(x + r * x_ld), v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            a[e] = fmaf(d[e], (v[e] - st.x) * st.y, a[e]);
+            b[e] += d[e];
         }
-    sums[0][wave][l] = a;
-    sums[1][wave][l] = b;
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        sums[0][wave][e][l] = a[e];
+        sums[1][wave][e][l] = b[e];
+    }
     __syncthreads();
-    if (wave >= 2 || c >= cols) return;
-    part[((int64_t)blockIdx.y * 2 + wave) * cols + c] = (sums[wave][0][l] + sums[wave][1][l]) + (sums[wave][2][l] + sums[wave][3][l]);
+    if (wave >= 2 || !at.has) return;
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        if (at.counts(e))
+            part[((int64_t)blockIdx.y * 2 + wave) * cols + at.c + e] =
+                (sums[wave][0][e][l] + sums[wave][1][e][l]) + (sums[wave][2][e][l] + sums[wave][3][e][l]);
 }
 
 // the parts' sums: grid y 0 dgamma, 1 dbeta (null: not wanted); sixteen waves take a share of the ranges each, in a fixed order
@@ -473,7 +532,7 @@ int64_t layernorm_ranges(int dtype, int64_t rows, int cols) {
     // three turns or more to a workgroup, since a part costs as much as four rows of bf16 (1000 x 8192: backward pass 24 us with two turns, 18.5 with three), unless fewer than
     // 128 workgroups are left
     if (rows_at_once) return std::min({groups, cut(rows, rows_at_once), std::max<int64_t>(128, cut(rows, 3 * rows_at_once))});
-    return std::min<int64_t>(cut(rows, 32), std::max<int64_t>(1, 1024 / cut(cols, 64)));
+    return std::min<int64_t>(cut(rows, 32), std::max<int64_t>(1, 2048 / cut(cols, 64 * (dtype == MONET_F32 ? 4 : 8))));
 }
 void layernorm_shape(int dtype, int64_t rows, int cols) {
     if (dtype != MONET_F32 && dtype != MONET_BF16) throw KernelError("layernorm: dtype must be MONET_F32 or MONET_BF16");
@@ -525,8 +584,8 @@ void layernorm_fwd(hipStream_t st, int dtype, int param_dtype, const void *x, co
                                eps);
         });
         if (rows_fit) return;
-        hipLaunchKernelGGL((layernorm_fwd_kernel<T, P>), dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), dim3(256), 0, st, (const T *)x, (const P *)gamma, (const P *)beta, (T *)y,
-                           (float2 *)stats, rows, cols, x_ld, y_ld, eps);
+        hipLaunchKernelGGL(layernorm_fwd_kernel<T>, dim3((unsigned)std::min<int64_t>(rows, 1 << 16)), dim3(LONG_THREADS), 0, st, (const T *)x, gamma, beta,
+                           param_dtype == MONET_BF16, (T *)y, (float2 *)stats, rows, cols, x_ld, y_ld, eps);
     });
     hip_check(hipGetLastError(), "layernorm launch");
 }
@@ -582,14 +641,14 @@ void layernorm_bwd(hipStream_t st, int dtype, int param_dtype, const void *dy, c
             return;
         }
         if (columns) {
-            hipLaunchKernelGGL(layernorm_columns_kernel<T>, dim3((unsigned)cut(cols, 64), (unsigned)ranges), dim3(256), 0, st, (const T *)dy, (const T *)x,
+            hipLaunchKernelGGL(layernorm_columns_kernel<T>, dim3((unsigned)cut(cols, 64 * VEC<T>), (unsigned)ranges), dim3(256), 0, st, (const T *)dy, (const T *)x,
                                (const float2 *)stats, (float *)ws, rows, cut(rows, ranges), cols, dy_ld, x_ld);
             hip_check(hipGetLastError(), "layernorm columns launch");
             join();
         }
         if (dx) {
-            hipLaunchKernelGGL((layernorm_dx_kernel<T, P>), dim3((unsigned)std::min<int64_t>(rows, 1 << 20)), dim3(256), 0, st, (const T *)dy, (const T *)x, (const P *)gamma,
-                               (const float2 *)stats, (T *)dx, rows, cols, dy_ld, x_ld, dx_ld, accumulate & 1);
+            hipLaunchKernelGGL(layernorm_dx_kernel<T>, dim3((unsigned)std::min<int64_t>(rows, 1 << 16)), dim3(LONG_THREADS), 0, st, (const T *)dy, (const T *)x, gamma,
+                               param_dtype == MONET_BF16, (const float2 *)stats, (T *)dx, rows, cols, dy_ld, x_ld, dx_ld, accumulate & 1);
             hip_check(hipGetLastError(), "layernorm gradient launch");
         }
     });

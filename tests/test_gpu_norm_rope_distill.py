@@ -189,7 +189,7 @@ def test_layernorm_of_many_rows(dtype, rows, cols):
 
 
 @BOTH
-@pytest.mark.parametrize("cols", [48, 203, 4096, 20000, 40000])
+@pytest.mark.parametrize("cols", [5, 30, 48, 203, 259, 4096, 4099, 12289, 20000, 40000, 40001, 70003])
 def test_layernorm_parts(dtype, cols):
     """No weights, no statistics; single results of the backward pass; in place."""
     torch = torch_mod()
