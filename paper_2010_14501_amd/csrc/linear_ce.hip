@@ -8,6 +8,8 @@
 // products whose results are rounded to bf16 themselves; the rounding, at most 2^-8 of a value, averages out over the sums.  1 / count
 // comes in behind the products: the label's entries p - 1 are near -1 and would otherwise all be rounded the same way).  Sums are fp32.
 // fp32: the convolution kernels' products, a piece of logits in the workspace at a time; with few rows two of them on the vector units.
+// The same layer against a teacher's top logits (linear_distill): l / T for l, mass exp(l / T - lse) - (the teacher's probabilities) for dl, T / count for
+// 1 / count; the products and the pieces are the same, the teacher's few entries of a row go through kernels of their own.
 #include <cmath>
 #include <initializer_list>
 #include <type_traits>

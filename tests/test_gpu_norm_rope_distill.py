@@ -648,6 +648,26 @@ def test_linear_distill_in_several_pieces():
         assert ((got.float() - ref).abs() <= 1.1 * (R * mag + R * ref.abs()) + 1e-12).all()
 
 
+@BOTH
+def test_linear_distill_beyond_32_bits(dtype):
+    """Rows that begin behind 2^31 elements of x (2^32 bytes, 2^33 in fp32): the last ones as in a call of their own, whose mean is over fewer rows.  The same
+    products in another tile; bounds as of any two results, each off by its own."""
+    torch = torch_mod()
+    rows, width, vocab, top, few = 263000, 8192, 72, 3, 65
+    x = torch.randn(rows, width, device="cuda", dtype=tdtype(dtype))
+    w = (torch.randn(vocab, width, device="cuda") / 64).to(tdtype(dtype))
+    index = torch.randint(0, vocab, (rows, top), device="cuda", dtype=torch.int32)
+    target = torch.randn(rows, top, device="cuda")
+    big = distill_call(dtype, x, w, index, target, 2.0)
+    own = distill_call(dtype, x[-few:].clone(), w, index[-few:].clone(), target[-few:].clone(), 2.0)
+    x, w, at, target = host(x[-few:]), host(w), index[-few:].cpu().numpy(), host(target[-few:])
+    bounds = distill_bounds(x, w, at, target, 2.0, None, dtype)
+    for i in (1, 2, 3):
+        within(host(big[i])[-few:], host(own[i]), 2 * bounds[i], i)
+    within(host(big[4])[-few:] * rows / few, host(own[4]), 2 * bounds[4] + 4 * U * np.abs(host(own[4])), "dx")
+    assert torch.isfinite(big[5]).all() and torch.isfinite(big[0]).all()
+
+
 # ---------------------------------------------------------------------- a step of all of them
 def block(dtype, t, n, lens, call=monet.call):
     """Layer norm -> rotary positions (in place, q and k of a packed tensor) -> attention -> layer norm -> loss against a teacher, and back, through
