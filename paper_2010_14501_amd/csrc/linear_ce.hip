@@ -431,7 +431,8 @@ constexpr int DISTILL_WAVES = 8;
 template <class T>
 __global__ __launch_bounds__(64 * DISTILL_WAVES) void distill_rows_kernel(const T *__restrict__ x, const T *__restrict__ w, const int32_t *__restrict__ index,
                                                                           const float *__restrict__ target, const float *__restrict__ target_lse,
-                                                                          const float2 *__restrict__ part, int parts, int rows, float *__restrict__ lse,
+                                                                          const float2 *__restrict__ part, int parts, const float *__restrict__ logits,
+                                                                          int piece, int rows, float *__restrict__ lse,
                                                                           float *__restrict__ mass, float *__restrict__ delta, float *__restrict__ row_loss,
                                                                           int width, int vocab, int tail, int top, float heat) {
     __shared__ float z[DISTILL_TOP], last[DISTILL_TAIL];
@@ -447,8 +448,26 @@ __global__ __launch_bounds__(64 * DISTILL_WAVES) void distill_rows_kernel(const 
     target += t * top;
     if (threadIdx.x == 0) twice = 0;
     for (int j = threadIdx.x; j < 1024; j += THREADS) seen[j] = make_uint4(0, 0, 0, 0);
-    // the row's lse from its parts, unless it is there already
+    // the row's lse from its parts or its logits, unless it is there already
     Soft a{-INFINITY, 0.f};
+    const bool joins = part || logits;
+    if (logits) {
+        constexpr int AHEAD = 8;
+        const float *row = logits + t * piece, by = 1.f / heat;
+        for (int v0 = threadIdx.x; v0 - (int)threadIdx.x < piece; v0 += AHEAD * THREADS) {
+            float f[AHEAD], m = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                f[i] = v0 + i * THREADS < piece ? row[v0 + i * THREADS] * by : -INFINITY;
+                m = fmaxf(m, f[i]);
+            }
+            const float base = m == -INFINITY ? 0.f : fminf(m, 3.4028235e38f);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) sum += exp_of(f[i] - base);
+            if (m == INFINITY) { m = 3.4028235e38f; sum = INFINITY; }
+            a = soft_join(a, Soft{m, sum});
+        }
+    }
     if (part) {
         for (int b = threadIdx.x; b < parts; b += THREADS) {
             const float2 v = part[(int64_t)b * rows + t];
@@ -500,7 +519,7 @@ __global__ __launch_bounds__(64 * DISTILL_WAVES) void distill_rows_kernel(const 
     } else if (top >= 48) dots(top, quarter, integral_constant<int, 2>(), entry, z);
     else dots(top, quarter, integral_constant<int, 1>(), entry, z);
     if (tail) dots(tail, quarter, integral_constant<int, 1>(), [&](int i) { return vocab - tail + i; }, last);
-    if (part) {
+    if (joins) {
         const float m = wave_max(a.m);
         a = Soft{m, wave_sum(a.m == -INFINITY ? a.s : a.s * exp_of(a.m - m))};
         if (l == 0) joined[wave] = a;
@@ -509,7 +528,7 @@ __global__ __launch_bounds__(64 * DISTILL_WAVES) void distill_rows_kernel(const 
     if (wave) return;
     // the rest is one wave's
     float ls;
-    if (part) {
+    if (joins) {
         a = joined[0];
 #pragma unroll
         for (int i = 1; i < DISTILL_WAVES; ++i) a = soft_join(a, joined[i]);
@@ -517,7 +536,7 @@ __global__ __launch_bounds__(64 * DISTILL_WAVES) void distill_rows_kernel(const 
         ls = lse[t];
         a = ls == INFINITY ? Soft{3.4028235e38f, INFINITY} : Soft{ls, ls == -INFINITY ? 0.f : 1.f};
     }
-    if (part || tail) {
+    if (joins || tail) {
         for (int j = 0; j < tail; ++j) a = soft_join(a, last[j] == INFINITY ? Soft{3.4028235e38f, INFINITY} : Soft{last[j], 1.f});
         ls = a.m + logf(a.s);
         if (l == 0) lse[t] = ls;
@@ -974,6 +993,7 @@ GemmShape ce_logits_shape(const CePlan &p, const void *x, const void *w, int v0,
 ConvShape ce_conv_shape(const CePlan &p, int piece) { return ConvShape{p.rows, 1, 1, p.width, piece, 1, 1, 1, 0, 1, 1}; }
 
 // the parts of lse (and the labels' logits) of all logits, which are `by` times the products where there are no labels
+// (part null: the logits alone, of the only piece)
 template <bool LABELS>
 void vocab_stats(hipStream_t st, const CePlan &p, const void *x, const void *w, const int32_t *labels, float2 *part, float *hit, float by, void *ws) {
     if (p.bf16) {
@@ -988,6 +1008,7 @@ void vocab_stats(hipStream_t st, const CePlan &p, const void *x, const void *w, 
         const float *wp = (const float *)w + (int64_t)at[i] * p.width;
         if (!ce_few_logits(st, (const float *)x, wp, p.width, p.rows, piece, logits))
             conv_fwd(st, (const float *)x, wp, logits, ce_conv_shape(p, piece), 1, product, (size_t)p.product);
+        if (!LABELS && !part) continue;
         hipLaunchKernelGGL(ce_piece_stats_kernel<LABELS>, dim3(p.rows, segments), dim3(256), 0, st, logits, piece, at[i], labels, part + done * p.rows, hit, by);
         hip_check(hipGetLastError(), "linear_ce statistics launch");
         done += segments;
@@ -1152,10 +1173,14 @@ void linear_distill_fwd(hipStream_t st, int dtype, const void *x, const void *w,
     if ((uintptr_t)target_lse % 4) throw KernelError("linear_distill: target_lse must be 4-byte aligned");
     float *row_loss = (float *)ws;
     float2 *part = (float2 *)(row_loss + 2 * up(rows, 64));
+    // fp32: logits that a row's workgroup takes in one step of its loads need no launch for their statistics (24 rows, 128 columns, 1009 entries, both passes 47 us,
+    // with one 50); of more, that launch has them from more workgroups (348 rows, 63168: 113 us together, the rows alone 128)
+    const bool direct = !p.bf16 && p.pieces().size() == 2 && p.piece <= 4096;
+    if (direct) part = nullptr;
     vocab_stats<false>(st, p, x, w, nullptr, part, nullptr, 1.f / heat, ws);
     // a row's workgroup joins its parts itself, a launch less, where reading 8 bytes from each of as many lines costs little
     const int parts = (int)p.parts();
-    const bool merged = rows * parts > 1 << 19;
+    const bool merged = !direct && rows * parts > 1 << 19;
     if (merged) {
         hipLaunchKernelGGL((ce_merge_kernel<16, false>), dim3((unsigned)cut(rows, 16)), dim3(256), 0, st, part, parts, nullptr, nullptr, lse, nullptr, nullptr, p.rows, vocab);
         hip_check(hipGetLastError(), "linear_distill merge launch");
@@ -1163,7 +1188,7 @@ void linear_distill_fwd(hipStream_t st, int dtype, const void *x, const void *w,
     const auto rows_kernel = [&](auto t) {
         using T = decltype(t);
         hipLaunchKernelGGL(distill_rows_kernel<T>, dim3(p.rows), dim3(64 * DISTILL_WAVES), 0, st, (const T *)x, (const T *)w, index, target, target_lse,
-                           merged ? nullptr : part, parts, p.rows, lse, mass, delta, row_loss, width, vocab, distill_tail(dtype, rows, width, vocab), top, heat);
+                           merged ? nullptr : part, parts, direct ? (const float *)((char *)ws + p.fixed) : nullptr, p.piece, p.rows, lse, mass, delta, row_loss, width, vocab, distill_tail(dtype, rows, width, vocab), top, heat);
         hip_check(hipGetLastError(), "linear_distill rows launch");
     };
     if (p.bf16) rows_kernel((unsigned short)0);
