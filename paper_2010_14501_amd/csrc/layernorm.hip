@@ -52,7 +52,8 @@ __device__ __forceinline__ uintx4 pack(const float (&f)[8]) {
     return v;
 }
 // A lane's piece of a row.  WHOLE: rows are whole pieces.  MOVED: the last piece is moved back to the row's end (values that two lanes hold are added once,
-// and stored twice alike).  SHORT: the row is shorter than a piece and goes value by value.  A piece behind the end: nothing.
+// and stored twice alike, where a row is in registers before any of it is stored).  SHORT: the row is shorter than a piece and goes value by value.  A piece
+// behind the end: nothing.
 enum { WHOLE, MOVED, SHORT };
 template <class T, int ROWS>
 struct Piece {
@@ -72,9 +73,10 @@ struct Piece {
         return __builtin_bit_cast(uintx4, v);
     }
     __device__ __forceinline__ float once(float v, int e) const { return counts(e) ? v : 0.f; }
-    __device__ __forceinline__ void store(T *row, const float (&f)[VEC<T>], bool add) const {
+    // alone: a moved piece stores only the values that count, which nobody else reads or stores
+    __device__ __forceinline__ void store(T *row, const float (&f)[VEC<T>], bool add, bool alone = false) const {
         if (!has) return;
-        if (ROWS != SHORT && !add) { store16(row + c, pack(f)); return; }
+        if (ROWS != SHORT && !add && !(alone && from)) { store16(row + c, pack(f)); return; }
 #pragma unroll
         for (int e = 0; e < VEC<T>; ++e)
             if (counts(e)) put(row + c + e, f[e], add);
@@ -358,21 +360,16 @@ __global__ __launch_bounds__(LONG_THREADS) void layernorm_fwd_kernel(const T *x,
         };
         const float mean = sum([](float v) { return v; }) / cols;
         const float rstd = 1.f / sqrtf(sum([&](float v) { return (v - mean) * (v - mean); }) / cols + eps);
-        // in place, a moved piece would read what the piece before it has stored: its values come in before anybody stores
-        const int last = (cols - 1) / V * V;
-        const bool mine = last / V % LONG_THREADS == (int)threadIdx.x;
-        uintx4 end{};
-        if (mine) end = Piece<T, MOVED>(last, cols).load(from);
-        copies_arrived();
+        // in place, others read and store their values meanwhile: everybody stores those that nobody else reads for a result
         for (int c = threadIdx.x * V; c < cols; c += LONG_THREADS * V) {
             const Piece<T, MOVED> at(c, cols);
             float f[V], g[V], b[V];
-            unpack(c == last ? end : at.load(from), f);
+            unpack(at.load(from), f);
             at.params(gamma, params_bf16, 1.f, g);
             at.params(beta, params_bf16, 0.f, b);
 #pragma unroll
             for (int e = 0; e < V; ++e) f[e] = fmaf((f[e] - mean) * rstd, g[e], b[e]);
-            at.store(to, f, false);
+            at.store(to, f, false, true);
         }
         if (stats && threadIdx.x == 0) stats[row] = make_float2(mean, rstd);
     }
@@ -404,20 +401,15 @@ __global__ __launch_bounds__(LONG_THREADS) void layernorm_dx_kernel(const T *dy,
         }
         a = long_sum(a, seg) / cols;
         b = long_sum(b, seg) / cols;
-        const int last = (cols - 1) / V * V;      // as in the forward pass
-        const bool mine = last / V % LONG_THREADS == (int)threadIdx.x;
-        uintx4 end{};
-        if (mine) end = Piece<T, MOVED>(last, cols).load(go);
-        copies_arrived();
         for (int c = threadIdx.x * V; c < cols; c += LONG_THREADS * V) {
             const Piece<T, MOVED> at(c, cols);
             float d[V], v[V], g[V];
-            unpack(c == last ? end : at.load(go), d);
+            unpack(at.load(go), d);
             unpack(at.load(from), v);
             at.params(gamma, params_bf16, 1.f, g);
 #pragma unroll
             for (int e = 0; e < V; ++e) d[e] = rstd * (d[e] * g[e] - a - (v[e] - mean) * rstd * b);
-            at.store(to, d, add);
+            at.store(to, d, add, true);      // as in the forward pass
         }
     }
 }
