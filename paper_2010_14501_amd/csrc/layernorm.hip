@@ -2,6 +2,9 @@
 //   mean = sum x / cols,  rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps),  xh = (x - mean) rstd,  y = xh gamma + beta.
 // Backward, with g = dy gamma:
 //   dx = rstd (g - sum g / cols - xh sum(g xh) / cols),  dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy.
+// A mean m from an fp32 sum is off by the sum's rounding, a few 2^-24 of it, which matters where the deviation is much smaller.  Rows with m^2 >= 16 var take a
+// third sum over d = x - m, mean = m + sum d / cols and var = sum d^2 / cols - (sum d / cols)^2: equal values are their own mean (48 of 1000.1 with eps 1e-5:
+// xh 0, without it 0.02).  The comparison costs 2 % of 4096 x 16384 in bf16; the third sum in all rows cost 9 %.
 // Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx.  All sums are fp32; a result is rounded once.
 #include <cmath>
 #include <type_traits>
@@ -114,6 +117,12 @@ __device__ __forceinline__ float group_sum(float v, float *at, int wave) {
     for (int i = 1; i < L / 64; ++i) v += at[i];
     return v;
 }
+__device__ __forceinline__ bool far_from_zero(float mean, float var) { return mean * mean >= 16.f * var; }
+// the mean and the variance with the mean deviation that was left; a variance beyond fp32 stays
+__device__ __forceinline__ void shift(float &mean, float &var, float off) {
+    mean += off;
+    if (var < INFINITY) var = fmaxf(var - off * off, 0.f);
+}
 // which of a workgroup's rows a thread works on: the same for a wave where it has a wave or more
 template <int L>
 __device__ __forceinline__ int group_of() {
@@ -125,14 +134,14 @@ template <int L> constexpr int WAVES_OF = L < 64 ? 1 : L / 64;      // of a row
 // computed: two passes over registers, one over memory.  16384 x 4096, bf16: 47 us (5.7 TB/s); with gamma and beta loaded value by value for every row 147;
 // a row read three times, value by value, 128.  1023 x 12289, fp32: 20 us (4.9 TB/s).  Short rows share a wave: 327680 x 128, bf16, 16 lanes each 26 us,
 // a wave each 82.
-template <int L> constexpr int FWD_THREADS = L <= 256 ? 256 : L;
+template <int L> constexpr int FWD_THREADS = L <= 64 ? 256 : L;
 
 template <class T, int L, int CH, int ROWS>
 __global__ __launch_bounds__(FWD_THREADS<L>) void layernorm_rows_kernel(const T *x, const void *__restrict__ gamma, const void *__restrict__ beta, bool params_bf16,
                                                                         T *y, float2 *__restrict__ stats, int64_t rows, int cols, int64_t x_ld, int64_t y_ld,
                                                                         float eps) {
     constexpr int V = VEC<T>, GROUPS = FWD_THREADS<L> / L;
-    __shared__ float sums[2][GROUPS][WAVES_OF<L>];
+    __shared__ float sums[3][GROUPS][WAVES_OF<L>];
     const int group = group_of<L>(), l = threadIdx.x % L, lot = threadIdx.x / 64 % WAVES_OF<L>;
     const auto piece = [&](int k) { return Piece<T, ROWS>((k * L + l) * V, cols); };
     float g[CH][V], b[CH][V];
@@ -160,7 +169,7 @@ __global__ __launch_bounds__(FWD_THREADS<L>) void layernorm_rows_kernel(const T 
 #pragma unroll
             for (int e = 0; e < V; ++e) sum += piece(k).once(f[e], e);
         }
-        const float mean = group_sum<L>(sum, sums[0][group], lot) / cols;      // divided: the mean of equal values is that value
+        float mean = group_sum<L>(sum, sums[0][group], lot) / cols;
         sum = 0.f;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
@@ -172,7 +181,20 @@ __global__ __launch_bounds__(FWD_THREADS<L>) void layernorm_rows_kernel(const T 
                 sum = fmaf(d, d, sum);
             }
         }
-        const float rstd = 1.f / sqrtf(group_sum<L>(sum, sums[1][group], lot) / cols + eps);
+        float var = group_sum<L>(sum, sums[1][group], lot) / cols;
+        static_assert(L < 128 || GROUPS == 1, "the rows of a workgroup would part at a barrier");
+        if (far_from_zero(mean, var)) {
+            sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                float f[V];
+                unpack(raw[k], f);
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum += piece(k).has ? piece(k).once(f[e] - mean, e) : 0.f;
+            }
+            shift(mean, var, group_sum<L>(sum, sums[2][group], lot) / cols);
+        }
+        const float rstd = 1.f / sqrtf(var + eps);
         if (row < rows) {
             if (stats && l == 0) stats[row] = make_float2(mean, rstd);
 #pragma unroll
@@ -338,6 +360,19 @@ __device__ __forceinline__ float long_sum(float v, float *seg) {      // the sam
     for (int i = 1; i < LONG_THREADS / 64; ++i) v += seg[i];
     return v;
 }
+// calls of(value) with a thread's values of a row
+template <class T, class F>
+__device__ __forceinline__ void long_values(const T *row, int cols, F &&of) {
+    constexpr int V = VEC<T>;
+    for (int c = threadIdx.x * V; c < cols; c += LONG_THREADS * V) {
+        const Piece<T, MOVED> at(c, cols);
+        float f[V];
+        unpack(at.load(row), f);
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (at.counts(e)) of(f[e]);
+    }
+}
 template <class T>
 __global__ __launch_bounds__(LONG_THREADS) void layernorm_fwd_kernel(const T *x, const void *__restrict__ gamma, const void *__restrict__ beta, bool params_bf16,
                                                                      T *y, float2 *__restrict__ stats, int64_t rows, int cols, int64_t x_ld, int64_t y_ld,
@@ -347,19 +382,18 @@ __global__ __launch_bounds__(LONG_THREADS) void layernorm_fwd_kernel(const T *x,
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const T *from = x + row * x_ld;
         T *to = y + row * y_ld;
-        const auto sum = [&](auto of) {
-            float s = 0.f;
-            for (int c = threadIdx.x * V; c < cols; c += LONG_THREADS * V) {
-                const Piece<T, MOVED> at(c, cols);
-                float f[V];
-                unpack(at.load(from), f);
-#pragma unroll
-                for (int e = 0; e < V; ++e) s += at.once(of(f[e]), e);
-            }
-            return long_sum(s, seg);
-        };
-        const float mean = sum([](float v) { return v; }) / cols;
-        const float rstd = 1.f / sqrtf(sum([&](float v) { return (v - mean) * (v - mean); }) / cols + eps);
+        float sum = 0.f;
+        long_values(from, cols, [&](float v) { sum += v; });
+        float mean = long_sum(sum, seg) / cols;
+        sum = 0.f;
+        long_values(from, cols, [&](float v) { sum = fmaf(v - mean, v - mean, sum); });
+        float var = long_sum(sum, seg) / cols;
+        if (far_from_zero(mean, var)) {
+            sum = 0.f;
+            long_values(from, cols, [&](float v) { sum += v - mean; });
+            shift(mean, var, long_sum(sum, seg) / cols);
+        }
+        const float rstd = 1.f / sqrtf(var + eps);
         // in place, others read and store their values meanwhile: everybody stores those that nobody else reads for a result
         for (int c = threadIdx.x * V; c < cols; c += LONG_THREADS * V) {
             const Piece<T, MOVED> at(c, cols);

@@ -1,8 +1,9 @@
 """Layer norm and the loss against a teacher in forms that only some sizes take, on the GPU; bounds as in test_gpu_norm_rope_distill.py."""
+import numpy as np
 import pytest
 
 from paper_2010_14501_amd import monet
-from test_gpu_norm_rope_distill import EPS, layernorm_call, layernorm_inputs, stream, torch_mod
+from test_gpu_norm_rope_distill import EPS, R, U, host, layernorm_call, layernorm_inputs, stream, tdtype, torch_mod
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +29,27 @@ def test_layernorm_of_long_ragged_rows_in_place(dtype, cols):
         monet.call("monet_layernorm_bwd", stream(), dtype, monet.F32, got.data_ptr(), tx.data_ptr(), tg.data_ptr(), stats.data_ptr(), got.data_ptr(), dg2.data_ptr(),
                    db2.data_ptr(), rows, cols, cols, cols, cols, 0, ws.data_ptr(), need)
         assert torch.equal(got, dx) and torch.equal(dg2, dg) and torch.equal(db2, db)
+
+
+@BOTH
+@pytest.mark.parametrize("cols", [3, 48, 200, 1000, 5003, 12289, 20000, 40003])
+def test_layernorm_of_constant_rows(dtype, cols):
+    """A row of equal values v, of any mantissa, is its own mean: y is beta, bit by bit, and nothing reaches dgamma.  A sum in fp32 is off by (n + 1) U of v, U = 2^-24, n
+    its longest chain (at most cols / 64 + 16, as in the other tests), so that d = v - mean, which is exact, is (n + 1) U v at most; the mean of these d is off by
+    (n + 1) U of that, (n + 1)^2 U^2 v < U v / 4, and the mean with it is v itself.  The variance is what is left of d^2 - d^2, each off by (n + 4) U of itself."""
+    torch = torch_mod()
+    values = [1000.1, 3.14159, -0.1, 12345.678, 7.0e-5, -65504.7, 1.0, 0.0]
+    (_, _), (_, tg), (_, tb), (_, tdy) = layernorm_inputs(len(values), cols, dtype, monet.F32, 11)
+    x = torch.tensor(values, device="cuda")[:, None].to(tdtype(dtype)).expand(-1, cols).contiguous()
+    y, stats, dx, dg, db = layernorm_call(dtype, monet.F32, x, tg, tb, tdy)
+    assert torch.equal(stats[:, 0], x[:, 0].float())
+    assert torch.equal(y, tb.to(x.dtype)[None].expand_as(y))
+    n = -(-cols // 64) + 16
+    d = (n + 1) * U * np.abs(host(x[:, 0]))
+    assert (np.abs(host(stats[:, 1]) * EPS ** 0.5 - 1) <= 1.1 * ((n + 4) * U * d * d / EPS + 4 * U)).all()
+    assert not dg.any()
+    # dx = rstd (g - mean g) alone
+    g = host(tdy) * host(tg)
+    want = (g - g.mean(axis=1, keepdims=True)) * host(stats[:, 1:])
+    size = np.abs(g).max(axis=1, keepdims=True) * host(stats[:, 1:])
+    assert (np.abs(host(dx) - want) <= 1.1 * ((n + 8) * U * size + (R if dtype == monet.BF16 else 0.0) * np.abs(want))).all()
