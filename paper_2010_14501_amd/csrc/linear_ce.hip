@@ -887,10 +887,12 @@ struct CePlan {
     int64_t bytes() const { return fixed + per_col * piece; }
     int wgrad_splits(int piece) const { return ce_splits(cut(width, 128) * cut(piece, 128), rows, 64); }
     // fp32: ranges in dx where its tiles are so few that `most` of them do not fill the card; 1: what the product chooses by itself, 16 at most.  205 rows, 80
-    // columns, 82288 entries: the product 49 us, in 16 ranges 163
+    // columns, 82288 entries: the product 49 us, in 16 ranges 163.  Not where that is fewer: 100 rows, 128 columns, 2000 entries backward 29 us, in 3 ranges
+    // of 512 entries or more 45
     int dgrad_splits(int piece) const {
         const int64_t tiles = cut(rows, 128) * (width <= 64 ? 1 : cut(width, 128));
-        return most > 16 && 16 * tiles < 256 && !few_rows(piece) ? ce_splits(tiles, piece, 512, most) : 1;
+        const int splits = most > 16 && !few_rows(piece) ? ce_splits(tiles, piece, 512, most) : 1;
+        return splits > 16 ? splits : 1;
     }
     bool few_rows(int piece) const { return rows <= CE_FEW_ROWS || (rows <= 2 * CE_FEW_ROWS && (int64_t)piece * width <= 1 << 20); }      // twice: where W stays in L2
     int few_per(int piece) const {      // entries of W for a workgroup: four workgroups to a CU

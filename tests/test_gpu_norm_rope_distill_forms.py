@@ -2,8 +2,10 @@
 import numpy as np
 import pytest
 
+from oracle import numerics as nm
 from paper_2010_14501_amd import monet
-from test_gpu_norm_rope_distill import EPS, R, U, host, layernorm_call, layernorm_inputs, stream, tdtype, torch_mod
+from test_gpu_norm_rope_distill import (EPS, R, U, distill_bounds, distill_call, distill_inputs, host, layernorm_call, layernorm_inputs, stream, tdtype, torch_mod,
+                                        within)
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +55,16 @@ def test_layernorm_of_constant_rows(dtype, cols):
     want = (g - g.mean(axis=1, keepdims=True)) * host(stats[:, 1:])
     size = np.abs(g).max(axis=1, keepdims=True) * host(stats[:, 1:])
     assert (np.abs(host(dx) - want) <= 1.1 * ((n + 8) * U * size + (R if dtype == monet.BF16 else 0.0) * np.abs(want))).all()
+
+
+@pytest.mark.parametrize("rows,width,vocab,top", [(100, 128, 2000, 8), (64, 160, 4000, 3), (300, 200, 2000, 5), (205, 80, 16387, 4), (40, 24, 9232, 2)])
+def test_linear_distill_input_gradient_of_few_tiles(rows, width, vocab, top):
+    """fp32, more than the few rows that have kernels of their own: dx over as many ranges of the vocabulary as the product takes by itself, or over more."""
+    torch = torch_mod()
+    (x, tx), (w, tw), index, target = distill_inputs(rows, width, vocab, top, monet.F32, 21)
+    got = distill_call(monet.F32, tx, tw, torch.from_numpy(index).cuda(), torch.from_numpy(target).cuda(), 2.0)
+    target = target.astype(np.float64)
+    fwd = nm.linear_distill_fwd(x, w, index, target, 2.0)
+    want = [np.array([fwd[0]]), *fwd[1:], *nm.linear_distill_bwd(x, w, index, target, 2.0)]
+    for name, g, v, b in zip(("loss", "lse", "mass", "delta", "dx", "dw"), got, want, distill_bounds(x, w, index, target, 2.0, None, monet.F32)):
+        within(host(g), v, b, name)
