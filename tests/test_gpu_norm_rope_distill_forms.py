@@ -68,3 +68,49 @@ def test_linear_distill_input_gradient_of_few_tiles(rows, width, vocab, top):
     want = [np.array([fwd[0]]), *fwd[1:], *nm.linear_distill_bwd(x, w, index, target, 2.0)]
     for name, g, v, b in zip(("loss", "lse", "mass", "delta", "dx", "dw"), got, want, distill_bounds(x, w, index, target, 2.0, None, monet.F32)):
         within(host(g), v, b, name)
+
+
+@pytest.mark.parametrize("rows,width,vocab,top", [(3000, 24, 29984, 5), (3000, 40, 30001, 3), (140000, 16, 1025, 4)])
+def test_linear_distill_in_several_pieces_in_fp32(rows, width, vocab, top):
+    """Logits beyond the workspace, against the formulas and the bounds of distill_bounds in 64 bits on the GPU: two pieces, two and what the vocabulary has over a
+    multiple of 16, and four with so many rows (560000 parts of their logits) that a kernel of its own joins the parts before that one entry more is added."""
+    torch = torch_mod()
+    heat = 2.0
+    assert monet.call("monet_linear_distill_workspace_bytes", 1, monet.F32, rows, width, vocab, top) < rows * vocab * 4
+    g = torch.Generator(device="cuda")
+    g.manual_seed(31)
+    normal = lambda *shape: torch.randn(*shape, generator=g, device="cuda")   # noqa: E731
+    x, w, target = normal(rows, width), normal(vocab, width) * 2 / width ** 0.5, 3 * normal(rows, top)
+    index = torch.randint(0, vocab, (rows, top), generator=g, device="cuda", dtype=torch.int32)
+    index[::7], index[1::5, -1], index[2::11, 1] = -1, vocab - 1, vocab
+    got = distill_call(monet.F32, x, w, index, target, heat)
+    x, w, t, at = x.double(), w.double(), target.double() / heat, index.clamp(0, vocab - 1).long()
+    has = (index >= 0) & (index < vocab)
+    mass = has.any(1).double()
+    logp = torch.log_softmax(t.masked_fill(~has, -np.inf), 1).masked_fill(~has, 0.0)
+    p = logp.exp() * has
+    z = x @ w.t() / heat
+    lse, top_z = z.logsumexp(1), z.abs().amax(1)
+    zj = z.gather(1, at)
+    ez = (width + 4) * U * (x.abs() @ w.abs().t()).amax(1) / heat
+    el = ez + 4 * U * top_z + (vocab + 16) * U + 4 * U * lse.abs()
+    elogp = (top + 24) * U + 8 * U * t.abs().amax(1)
+    ep = p * (elogp + 8 * U)[:, None]
+    term = (logp + lse[:, None] - zj).abs()
+    eterm = (elogp + el + ez)[:, None] + 4 * U * (logp.abs() + lse.abs()[:, None] + zj.abs())
+    loss = heat ** 2 * (p * (logp + lse[:, None] - zj)).sum() / mass.sum()
+    eloss = heat ** 2 * ((p * eterm + ep * term).sum() + (top + 8) * U * (p * term).sum()) / mass.sum() + 4 * U * loss.abs()
+    emass = ep.sum(1) + (top + 8) * U * mass
+    d = z.sub_(lse[:, None]).exp_().mul_(mass[:, None])
+    ed = d * (ez + el + 4 * U * top_z + 8 * U + 4 * U + emass)[:, None]     # of mass q, q <= mass q in rows with weight
+    d.scatter_add_(1, at, -p)
+    ed.scatter_add_(1, at, ep + (top + 12) * U * p)
+    delta, edelta = d.gather(1, at) * has, ed.gather(1, at)
+    f = heat / mass.sum()
+    d.mul_(f)
+    ed = ed.mul_(f).add_(d.abs(), alpha=6 * U)
+    size = d.abs()
+    for name, value, want, bound in (("loss", got[0], loss[None], eloss), ("lse", got[1], lse, el), ("mass", got[2], mass, emass), ("delta", got[3], delta, edelta),
+                                     ("dx", got[4], d @ w, (ed + (vocab + 8) * U * size) @ w.abs()),
+                                     ("dw", got[5], d.t() @ x, (ed + (rows + 8) * U * size).t() @ x.abs())):
+        assert ((value.double() - want).abs() <= 1.1 * bound + 1e-30).all(), name
