@@ -18,8 +18,6 @@ namespace monet {
 
 namespace {
 
-__device__ __forceinline__ float value(float v) { return v; }
-__device__ __forceinline__ float value(unsigned short v) { return bf16_float(v); }
 __device__ __forceinline__ void put(float *p, float v, bool add) { *p = add ? *p + v : v; }
 __device__ __forceinline__ void put(unsigned short *p, float v, bool add) { *p = float_bf16(add ? bf16_float(*p) + v : v); }
 
@@ -214,7 +212,7 @@ __global__ __launch_bounds__(FWD_THREADS<L>) void layernorm_rows_kernel(const T 
 // dx, and this workgroup's rows' part of dgamma and dbeta: a lane's columns are the same in every row, so their sums stay in its registers and dy and x are
 // read once for all three results.  Eight waves with up to 32 values of a row to a lane (160 registers of sums, gamma and two rows under way; with 16 waves
 // and 128 registers it spilled); as many workgroups as are on the card at once, since each leaves a part of 8 bytes a column.  16384 x 4096, bf16: 84 us
-// (4.9 TB/s) and 4.5 for the join of 256 parts; in three kernels that read dy and x twice, value by value, 430.  1023 x 12289, fp32: 42 us, 25 MB of its 175 parts.
+// (4.9 TB/s) and 4.5 for the join of 256 parts; in three kernels that read dy and x twice, value by value, 430.  1023 x 12289, fp32: 42 us, 25 MB of its 256 parts.
 template <int L> constexpr int BWD_THREADS = L <= 512 ? 512 : L;
 template <class T, int L, int CH, int ROWS>
 __global__ __launch_bounds__(BWD_THREADS<L>) void layernorm_rows_bwd_kernel(const T *dy, const T *__restrict__ x, const void *__restrict__ gamma, bool params_bf16,
@@ -578,12 +576,11 @@ void layernorm_param(const void *p, int param_dtype) {      // may be null
     if ((uintptr_t)p % (param_dtype == MONET_BF16 ? 2 : 4)) throw KernelError("layernorm: pointer not aligned");
 }
 
+// calls f with a value of the type
 template <class F>
-void by_types(int dtype, int param_dtype, F &&f) {
-    if (dtype == MONET_F32 && param_dtype == MONET_F32) f(0.f, 0.f);
-    else if (dtype == MONET_F32) f(0.f, (unsigned short)0);
-    else if (param_dtype == MONET_F32) f((unsigned short)0, 0.f);
-    else f((unsigned short)0, (unsigned short)0);
+void by_type(int dtype, F &&f) {
+    if (dtype == MONET_F32) f(0.f);
+    else f((unsigned short)0);
 }
 
 }  // namespace
@@ -600,9 +597,8 @@ void layernorm_fwd(hipStream_t st, int dtype, int param_dtype, const void *x, co
     layernorm_param(gamma, param_dtype);
     layernorm_param(beta, param_dtype);
     if ((uintptr_t)stats % 8) throw KernelError("layernorm: stats must be 8-byte aligned");
-    by_types(dtype, param_dtype, [&](auto t, auto p) {
+    by_type(dtype, [&](auto t) {
         using T = decltype(t);
-        using P = decltype(p);
         const bool rows_fit = layernorm_rows_form<T, false>(cols, [&](auto l, auto ch, auto form) {
             constexpr int L = decltype(l)::value, CH = decltype(ch)::value, GROUPS = FWD_THREADS<L> / L;
             hipLaunchKernelGGL((layernorm_rows_kernel<T, L, CH, decltype(form)::value>), dim3((unsigned)std::min<int64_t>(cut(rows, GROUPS), 256 * 1024 / FWD_THREADS<L>)),
@@ -642,14 +638,16 @@ void layernorm_bwd(hipStream_t st, int dtype, int param_dtype, const void *dy, c
         if ((uintptr_t)ws % 256) throw KernelError("layernorm: the workspace must be 256-byte aligned");
     }
     const int64_t ranges = layernorm_ranges(dtype, rows, cols);
-    by_types(dtype, param_dtype, [&](auto t, auto p) {
-        using T = decltype(t);
-        using P = decltype(p);
-        const auto join = [&] {
+    const auto join = [&] {
+        by_type(param_dtype, [&](auto p) {
+            using P = decltype(p);
             hipLaunchKernelGGL(layernorm_join_kernel<P>, dim3((unsigned)cut(cols, 64), 2), dim3(1024), 0, st, (const float *)ws, (int)ranges, cols, (P *)dgamma,
                                (P *)dbeta, accumulate >> 1);
-            hip_check(hipGetLastError(), "layernorm join launch");
-        };
+        });
+        hip_check(hipGetLastError(), "layernorm join launch");
+    };
+    by_type(dtype, [&](auto t) {
+        using T = decltype(t);
         if (!rows) {
             if (columns) join();
             return;
