@@ -375,6 +375,7 @@ static void check_transformer_nodes(const Graph &g) {
             need(n.ins.size() == 1 && n.ins[0] > 0 && n.pars.size() == 2, "has one input that a node computes, a weight and a bias");
             need(n.shape.size() == 2 && g.shape_of(n.ins[0]) == n.shape && n.shape[1] <= INT32_MAX, "input and output must be the same rows x columns");
             for (int p : n.pars) need(numel(g.params[p].shape) == n.shape[1], "weight and bias must have a value for each column");
+            need(n.pars[0] != n.pars[1], "weight and bias must be two parameters");
             const float eps = (float)n.attr_f("eps", 1e-5);
             need(eps > 0.f && eps <= 1e30f, "eps must be positive and finite");
             need(aux && aux->op == "normstats" && numel(aux->shape) == 2 * n.shape[0], "needs an intermediate normstats of rows x 2");
