@@ -305,7 +305,7 @@ int64_t monet_linear_ce_workspace_bytes(int grad, int dtype, int64_t rows, int w
  * An index may come more than once in a row.  x, w, loss, lse, sizes and workspaces as for linear_ce (dw is a sum over all rows: x has to be
  * finite in all of them); mass [rows], delta [rows][top] fp32, both needed by the backward call; top 1 to 1024; fp32 tensors, index and numbers 4-byte aligned.
  * As for linear_ce, bf16: a piece of the logits' gradient is rounded to bf16; a row's entries, large and few, do not average that out: dx and dw are off by 2.3e-3
- * (Frobenius norm; their own rounding alone 1.7e-3).  ws_bytes >= monet_linear_distill_workspace_bytes(grad = 0, ...). */
+ * (Frobenius norm; their own rounding alone 1.7e-3; in fp32 3e-7).  ws_bytes >= monet_linear_distill_workspace_bytes(grad = 0, ...). */
 int monet_linear_distill_fwd(void *stream, int dtype, const void *x, const void *w, const int32_t *index, const float *target, const float *target_lse,
                              float *loss, float *lse, float *mass, float *delta, int64_t rows, int width, int vocab, int top, float temperature, void *ws,
                              size_t ws_bytes);

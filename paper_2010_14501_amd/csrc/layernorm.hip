@@ -130,7 +130,7 @@ template <int L> constexpr int WAVES_OF = L < 64 ? 1 : L / 64;      // of a row
 
 // A workgroup walks over rows with gamma and beta in registers, the next row's loads under way while this one's mean, deviations from it and results are
 // computed: two passes over registers, one over memory.  16384 x 4096, bf16: 47 us (5.7 TB/s); with gamma and beta loaded value by value for every row 147;
-// a row read three times, value by value, 128.  1023 x 12289, fp32: 20 us (4.9 TB/s).  Short rows share a wave: 327680 x 128, bf16, 16 lanes each 26 us,
+// a row read three times, value by value, 128.  1023 x 12289, fp32: 21 us (4.7 TB/s).  Short rows share a wave: 327680 x 128, bf16, 16 lanes each 29 us,
 // a wave each 82.
 template <int L> constexpr int FWD_THREADS = L <= 64 ? 256 : L;
 
@@ -212,7 +212,7 @@ __global__ __launch_bounds__(FWD_THREADS<L>) void layernorm_rows_kernel(const T 
 // dx, and this workgroup's rows' part of dgamma and dbeta: a lane's columns are the same in every row, so their sums stay in its registers and dy and x are
 // read once for all three results.  Eight waves with up to 32 values of a row to a lane (160 registers of sums, gamma and two rows under way; with 16 waves
 // and 128 registers it spilled); as many workgroups as are on the card at once, since each leaves a part of 8 bytes a column.  16384 x 4096, bf16: 84 us
-// (4.9 TB/s) and 4.5 for the join of 256 parts; in three kernels that read dy and x twice, value by value, 430.  1023 x 12289, fp32: 42 us, 25 MB of its 256 parts.
+// (4.9 TB/s) and 4.5 for the join of 256 parts; in three kernels that read dy and x twice, value by value, 430.  1023 x 12289, fp32: 45 us, 25 MB of its 256 parts.
 template <int L> constexpr int BWD_THREADS = L <= 512 ? 512 : L;
 template <class T, int L, int CH, int ROWS>
 __global__ __launch_bounds__(BWD_THREADS<L>) void layernorm_rows_bwd_kernel(const T *dy, const T *__restrict__ x, const void *__restrict__ gamma, bool params_bf16,
@@ -345,8 +345,8 @@ __global__ __launch_bounds__(BWD_THREADS<L>) void layernorm_rows_bwd_kernel(cons
     }
 }
 
-// ---- longer rows (more than 16384 columns), which are read again, mostly from L2, for each of their sums; pieces as above: 1000 x 30000 in bf16 forward 25 us,
-// backward 70 (5 and 2.6 TB/s)
+// ---- longer rows (more than 16384 columns), which are read again, mostly from L2, for each of their sums; pieces as above: 1000 x 30000 in bf16 forward 37 us,
+// backward 77 (3.2 and 2.3 TB/s), where the caches hold the rows from an earlier launch 33 and 68
 constexpr int LONG_THREADS = 1024;
 __device__ __forceinline__ float long_sum(float v, float *seg) {      // the same in every thread
     v = wave_sum(v);
