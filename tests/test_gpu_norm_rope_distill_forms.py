@@ -4,8 +4,8 @@ import pytest
 
 from oracle import numerics as nm
 from paper_2010_14501_amd import monet
-from test_gpu_norm_rope_distill import (EPS, R, U, distill_bounds, distill_call, distill_inputs, host, layernorm_call, layernorm_inputs, stream, tdtype, torch_mod,
-                                        within)
+from test_gpu_norm_rope_distill import (EPS, R, U, distill_bounds, distill_call, distill_inputs, host, layernorm_bounds, layernorm_call, layernorm_inputs, rounded, stream,
+                                        tdtype, torch_mod, within)
 
 pytestmark = pytest.mark.gpu
 
@@ -55,6 +55,25 @@ def test_layernorm_of_constant_rows(dtype, cols):
     want = (g - g.mean(axis=1, keepdims=True)) * host(stats[:, 1:])
     size = np.abs(g).max(axis=1, keepdims=True) * host(stats[:, 1:])
     assert (np.abs(host(dx) - want) <= 1.1 * ((n + 8) * U * size + (R if dtype == monet.BF16 else 0.0) * np.abs(want))).all()
+
+
+@BOTH
+@pytest.mark.parametrize("cols", [2, 12, 31, 48, 100, 203, 700, 1500, 2040, 4100, 20001])
+def test_layernorm_of_rows_near_and_far_from_zero(dtype, cols):
+    """Rows whose mean is corrected beside rows whose mean is not, in one wave where several share it: the bounds of either, and the others' rows change no bit."""
+    torch = torch_mod()
+    (x, tx), (gamma, tg), (beta, tb), (dy, tdy) = layernorm_inputs(37, cols, dtype, monet.F32, 13)
+    clean = layernorm_call(dtype, monet.F32, tx, tg, tb, tdy)
+    x[1::3] = 3000.0 + np.random.default_rng(14).integers(-2, 3, x[1::3].shape) * (16 if dtype == monet.BF16 else 0.37)
+    x[2::3, :] = x[2::3, :1]
+    x, tx = rounded(x, dtype)
+    got = layernorm_call(dtype, monet.F32, tx, tg, tb, tdy)
+    for a, b in zip(got[:3], clean[:3]):
+        assert torch.equal(a[::3], b[::3])
+    want = [*nm.layernorm_fwd(x, gamma, beta, EPS), *nm.layernorm_bwd(dy, x, gamma, EPS)]
+    flat = (got[0], got[1][:, 0], got[1][:, 1], *got[2:])
+    for name, g, w, b in zip(("y", "mean", "rstd", "dx", "dgamma", "dbeta"), flat, want, layernorm_bounds(x, gamma, beta, dy, dtype, monet.F32)):
+        within(host(g), w, b, name)
 
 
 @pytest.mark.parametrize("rows,width,vocab,top", [(100, 128, 2000, 8), (64, 160, 4000, 3), (300, 200, 2000, 5), (205, 80, 16387, 4), (40, 24, 9232, 2)])
@@ -114,3 +133,18 @@ def test_linear_distill_in_several_pieces_in_fp32(rows, width, vocab, top):
                                      ("dx", got[4], d @ w, (ed + (vocab + 8) * U * size) @ w.abs()),
                                      ("dw", got[5], d.t() @ x, (ed + (rows + 8) * U * size).t() @ x.abs())):
         assert ((value.double() - want).abs() <= 1.1 * bound + 1e-30).all(), name
+
+
+@BOTH
+@pytest.mark.parametrize("cols", [3, 203, 4099, 16385, 16903, 20000])
+def test_layernorm_gradient_added_to_dy_in_place(dtype, cols):
+    """dx may be dy also where it is added to: the sum of both, as beside it."""
+    torch = torch_mod()
+    rows = 300
+    (_, tx), (_, tg), (_, tb), (_, tdy) = layernorm_inputs(rows, cols, dtype, monet.F32, 15)
+    _, stats, want, dg, db = layernorm_call(dtype, monet.F32, tx, tg, tb, tdy, accumulate=1, start=(tdy, torch.zeros_like(tg), torch.zeros_like(tg)))
+    need = monet.call("monet_layernorm_bwd_workspace_bytes", dtype, rows, cols)
+    ws, dg2, db2, got = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.empty_like(dg), torch.empty_like(db), tdy.clone()
+    monet.call("monet_layernorm_bwd", stream(), dtype, monet.F32, got.data_ptr(), tx.data_ptr(), tg.data_ptr(), stats.data_ptr(), got.data_ptr(), dg2.data_ptr(),
+               db2.data_ptr(), rows, cols, cols, cols, cols, 1, ws.data_ptr(), need)
+    assert torch.equal(got, want) and torch.equal(dg2, dg) and torch.equal(db2, db)
