@@ -4,7 +4,8 @@
 //   dx = rstd (g - sum g / cols - xh sum(g xh) / cols),  dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy.
 // A mean m from an fp32 sum is off by the sum's rounding, a few 2^-24 of it, which matters where the deviation is much smaller.  Rows with m^2 >= 16 var take a
 // third sum over d = x - m, mean = m + sum d / cols and var = sum d^2 / cols - (sum d / cols)^2: equal values are their own mean (48 of 1000.1 with eps 1e-5:
-// xh 0, without it 0.02).  The comparison costs 2 % of 4096 x 16384 in bf16; the third sum in all rows cost 9 %.
+// xh 0, without it 0.02).  In the other rows the mean's error is at most that of five values of a deviation's size.  The comparison costs 2 % of 4096 x 16384
+// in bf16; the third sum in all rows cost 9 %.
 // Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx.  All sums are fp32; a result is rounded once.
 #include <cmath>
 #include <type_traits>
@@ -131,7 +132,8 @@ template <int L> constexpr int WAVES_OF = L < 64 ? 1 : L / 64;      // of a row
 // A workgroup walks over rows with gamma and beta in registers, the next row's loads under way while this one's mean, deviations from it and results are
 // computed: two passes over registers, one over memory.  16384 x 4096, bf16: 47 us (5.7 TB/s); with gamma and beta loaded value by value for every row 147;
 // a row read three times, value by value, 128.  1023 x 12289, fp32: 21 us (4.7 TB/s).  Short rows share a wave: 327680 x 128, bf16, 16 lanes each 29 us,
-// a wave each 82.
+// a wave each 82.  Rows of two waves have a workgroup of their own, since only some rows take a third sum behind its barrier: 16384 x 2048, bf16: 24.4 us, two rows to
+// a workgroup and no third sum 24.1.
 template <int L> constexpr int FWD_THREADS = L <= 64 ? 256 : L;
 
 template <class T, int L, int CH, int ROWS>
